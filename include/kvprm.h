@@ -20,7 +20,9 @@
  *  - bf16 = IEEE bfloat16 bit patterns (uint16 storage).
  *  - A context is used by one host thread at a time.  Work is enqueued on the
  *    caller's CUDA stream (NULL = legacy default stream).
- *  - The library never writes the caller's weights or key/value pages.
+ *  - The library never writes the caller's weights, and writes key/value pages
+ *    only where that is the call's purpose (kvprm_steer, kvprm_cache_write,
+ *    kvprm_cache_expand).
  */
 #ifndef KVPRM_H
 #define KVPRM_H
@@ -555,6 +557,159 @@ KVPRM_API int kvprm_get_trace(kvprm_ctx* ctx, int32_t max_records, int32_t* cls,
 KVPRM_API int kvprm_get_trace_events(kvprm_ctx* ctx, int32_t max_records, int32_t* cls, double* start_us,
                                      double* end_us, double* events_us);
 KVPRM_API int kvprm_get_profile(kvprm_ctx* ctx, int64_t* launches, double* total_ms);
+
+/* ---------------------------------------------------------------------------
+ * Operators around the cache: rotary positions, the cache's pages written from
+ * (rotated) keys and values -- in bf16 or quantised to 8 bits -- and made
+ * readable to the scorer again, and the attention of a tree of drafted tokens
+ * over those pages (the test-time search of Sec. 2 extends its candidates by
+ * drafted steps before they are scored).  They need no context: all state is
+ * the caller's.  Calls are stream-ordered, allocate nothing and may be captured
+ * into a graph; tables (positions, slots, block tables, lengths, masks) are
+ * DEVICE arrays, so what the host cannot check is checked by the kernels, as
+ * each entry point says.  A failed call returns its code with nothing enqueued;
+ * kvprm_operator_error() describes the calling thread's last one.
+ *
+ * Element types of the tensors that these entry points take: */
+enum { KVPRM_F32 = 0, KVPRM_BF16 = 1, KVPRM_F16 = 2 };
+KVPRM_API const char* kvprm_operator_error(void);
+
+/* Rotary positions.  The first rotary_dim elements of a head are rotated in
+ * pairs, pair i = 0 .. rotary_dim / 2 - 1 by the angle p f_i at position p, and
+ * multiplied by `magnitude`; the others pass unchanged.
+ *  rotary_dim   even, 2 .. 256
+ *  interleaved  0: pairs (i, i + rotary_dim / 2); 1: pairs (2 i, 2 i + 1)
+ *  base         f_i = base^(-2 i / rotary_dim), > 1
+ *  scaling      how the f_i are stretched for contexts longer than the model's
+ *               original_len by `factor` (>= 1):
+ *    NONE    not;  LINEAR  f_i / factor;
+ *    BASE    base * factor^(rotary_dim / (rotary_dim - 2)) as the base;
+ *    SMOOTH  w f_i + (1 - w) f_i / factor, w = (n_i - low) / (high - low)
+ *            clamped to [0, 1], n_i = original_len f_i / 2 pi the turns of pair
+ *            i within the original context;
+ *    RAMP    the same with w falling linearly in i between floor(i(high)) and
+ *            ceil(i(low)), i(n) = rotary_dim ln(original_len / (2 pi n)) /
+ *            (2 ln base) the pair that turns n times (clamped to 0 and
+ *            rotary_dim - 1; 0 < low < high).
+ *  magnitude    finite; 1 unless the stretching asks for another.
+ * The handle holds the f_i as 64-bit fractions of a turn, on the host: a
+ * position's angle is their product in whole numbers modulo one turn, exact at
+ * every int32 position, before a sine and cosine in 32 bits. */
+enum { KVPRM_ROPE_NONE = 0, KVPRM_ROPE_LINEAR = 1, KVPRM_ROPE_BASE = 2, KVPRM_ROPE_RAMP = 3, KVPRM_ROPE_SMOOTH = 4 };
+typedef struct {
+  int32_t rotary_dim, interleaved, scaling, original_len;
+  double base, factor, low, high, magnitude;
+} kvprm_rope_config;
+typedef struct kvprm_rope kvprm_rope;
+/* Errors: KVPRM_EINVAL, KVPRM_ENOMEM (*out is then NULL).  No device is touched. */
+KVPRM_API int kvprm_rope_create(const kvprm_rope_config* cfg, kvprm_rope** out);
+KVPRM_API void kvprm_rope_destroy(kvprm_rope* rope);
+/* The host table: turns[i] = f_i / 2 pi in units of 2^-64, i < rotary_dim / 2. */
+KVPRM_API int kvprm_rope_turns(const kvprm_rope* rope, uint64_t* turns);
+
+/* One tensor of heads to rotate: device [n_tokens][n_heads][head_dim], rows of
+ * head_dim consecutive elements, strides in elements.  out may be in with the
+ * same strides (in place); other overlaps are undefined.  16-byte aligned rows
+ * (and rotary_dim a multiple of 16 bytes' elements, twice that when not
+ * interleaved) take 16-byte accesses, any others single elements. */
+typedef struct {
+  const void* in;
+  void* out;
+  int32_t n_heads;
+  int64_t in_token, in_head, out_token, out_head;
+} kvprm_heads;
+/* Rotates up to 4 tensors (queries and keys) of the same tokens in one launch.
+ *  dtype      of every tensor; arithmetic in 32 bits, one rounding at the end
+ *  head_dim   rotary_dim .. 512; at most 1024 heads in all
+ *  positions  device int32 [n_tokens], any value
+ *  inverse    0: x' = R(p) x.  1: the transpose, the angles negated (the gradient
+ *             with respect to x from that with respect to x')
+ * Errors: KVPRM_EINVAL, KVPRM_ECUDA. */
+KVPRM_API int kvprm_rope_rotate(const kvprm_rope* rope, int32_t dtype, int32_t head_dim, const int32_t* positions,
+                                int64_t n_tokens, int32_t inverse, const kvprm_heads* x, int32_t n_x, void* stream);
+
+/* One layer of a paged cache: pages [n_pages][2][n_kv_heads][16][head_dim] (keys,
+ * then values; head_dim 64 or 128), 16-byte aligned, of bf16 -- what the scoring
+ * calls read -- or of 8-bit floating point (4 exponent and 3 mantissa bits,
+ * largest value 448, no infinities) with a power of two for each row of head_dim
+ * elements: exponents, uint8 [n_pages][2][n_kv_heads][16] (16-byte aligned), a
+ * row's values being code * 2^(exponent - 127), NaN where the exponent is 255.  A power of two costs an 8-bit
+ * float nothing in precision, never rounds, and a byte per row. */
+enum { KVPRM_CACHE_BF16 = 0, KVPRM_CACHE_E4M3 = 1 };
+typedef struct {
+  void* pages;
+  void* exponents;   /* KVPRM_CACHE_E4M3 only, else NULL */
+  int64_t n_pages;
+  int32_t n_kv_heads, head_dim, format;
+} kvprm_cache;
+/* Writes tokens into their slots: token t's keys and values of every head go to
+ * slot slots[t] = 16 * page + place in the page (device int64).  A token whose
+ * slot is outside [0, 16 n_pages) is not written (padding, rejected drafts); of
+ * several tokens with one slot any may win.
+ *  k, v       device [n_tokens][n_kv_heads][head_dim] of `dtype`, with strides
+ *  rope, positions  keys are rotated on the way (both NULL: k is rotated already)
+ * The values are rounded once, from 32 bits: to bf16, or scaled by the smallest
+ * 2^e (e >= -127) that brings the row's largest finite magnitude to 448 or less
+ * and rounded to 8 bits, to nearest even; infinities become +-448 2^e, and a row
+ * with a NaN gets the exponent 255, which makes all of it read as NaN.
+ * Errors: KVPRM_EINVAL, KVPRM_ECUDA. */
+KVPRM_API int kvprm_cache_write(const kvprm_cache* cache, int32_t dtype, const void* k, int64_t k_token, int64_t k_head,
+                                const void* v, int64_t v_token, int64_t v_head, const int64_t* slots,
+                                int64_t n_tokens, const kvprm_rope* rope, const int32_t* positions, void* stream);
+/* Quantised pages into bf16 pages (that the scoring calls read): page src[i] of
+ * `cache` (KVPRM_CACHE_E4M3) becomes page dst[i] of out, a bf16 layer of
+ * out_pages pages with the same heads; src, dst device int32 [n].  A pair with a
+ * page outside its layer is left out.  Exact, but for magnitudes below bf16's
+ * least normal number.
+ * Errors: KVPRM_EINVAL, KVPRM_ECUDA. */
+KVPRM_API int kvprm_cache_expand(const kvprm_cache* cache, const int32_t* src, const int32_t* dst, int64_t n, void* out,
+                                 int64_t out_pages, void* stream);
+
+/* Attention of drafted tokens over the cache and over each other.  Sequence s
+ * has lens[s] cached tokens, in the pages block_table[s][0 ..], and the drafted
+ * tokens start[s] .. start[s + 1] - 1, whose keys and values are not in the
+ * cache.  A drafted token attends to every cached token of its sequence and to
+ * the drafted tokens j that its mask names (a tree: its ancestors and itself);
+ * query head h reads kv head floor(h / (n_q_heads / n_kv_heads)).
+ *   o = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q . k_j)
+ * A token that sees nothing gets zeros.
+ *  q            device bf16 [n_tokens][n_q_heads][head_dim], rotated
+ *  k, v         device bf16 [n_tokens][n_kv_heads][head_dim], k rotated
+ *  out          device bf16 [n_tokens][n_q_heads][head_dim]
+ *               each with token and head strides in elements, all rows 16-byte
+ *               aligned
+ *  block_table  device int32 [n_seqs][max_blocks]
+ *  lens         device int32 [n_seqs], start device int32 [n_seqs + 1]
+ *  mask         device uint32 [n_tokens][mask_words]: bit j % 32 of word j / 32 of
+ *               a token's row: it sees drafted token start[s] + j;
+ *               mask_words >= ceil(max_drafts / 32).  NULL: every drafted token
+ *               sees itself and those before it (a chain)
+ *  max_drafts   no sequence has more drafted tokens, 1 .. 1024
+ *  max_len      about the longest cached length; it sizes the launch, and results
+ *               do not depend on it beyond the order of sums
+ * Scores, weights' sums and accumulators are fp32; the weights that multiply the
+ * values are rounded to bf16, as the output is.
+ * What the host cannot see: a sequence whose length is negative or beyond its
+ * block table, or that has a page outside the cache, gets NaN in every output; one whose
+ * drafted tokens are not within [0, n_tokens), or more than max_drafts, is left
+ * out.  Slots past a length and drafts that no row sees may hold anything; a draft
+ * whose value row is not finite makes NaN of the rows that see it, and of no others.
+ *  workspace    device, kvprm_tree_workspace() bytes for the same arguments, 256-byte
+ *               aligned; its first 8192 bytes zero before its first use.  Every
+ *               call leaves them zero; calls that share it must be ordered.
+ * Errors: KVPRM_EINVAL, KVPRM_ECAPACITY (workspace too small), KVPRM_ECUDA. */
+typedef struct {
+  const void *q, *k, *v;
+  void* out;
+  int64_t q_token, q_head, k_token, k_head, v_token, v_head, out_token, out_head;
+  const int32_t *block_table, *lens, *start;
+  const uint32_t* mask;
+  int32_t max_blocks, n_seqs, n_tokens, n_q_heads, max_drafts, max_len, mask_words;
+  float scale;
+} kvprm_tree;
+KVPRM_API int kvprm_tree_workspace(const kvprm_cache* cache, const kvprm_tree* t, int64_t* bytes);
+KVPRM_API int kvprm_tree_attention(const kvprm_cache* cache, const kvprm_tree* t, void* workspace,
+                                   int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }
