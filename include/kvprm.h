@@ -628,7 +628,7 @@ typedef struct {
 KVPRM_API int kvprm_rope_rotate(const kvprm_rope* rope, int32_t dtype, int32_t head_dim, const int32_t* positions,
                                 int64_t n_tokens, int32_t inverse, const kvprm_heads* x, int32_t n_x, void* stream);
 
-/* One layer of a paged cache: pages [n_pages][2][n_kv_heads][16][head_dim] (keys,
+/* One layer of a paged cache (at most 2^30 pages): pages [n_pages][2][n_kv_heads][16][head_dim] (keys,
  * then values; head_dim 64 or 128), 16-byte aligned, of bf16 -- what the scoring
  * calls read -- or of 8-bit floating point (4 exponent and 3 mantissa bits,
  * largest value 448, no infinities) with a power of two for each row of head_dim
@@ -696,7 +696,9 @@ KVPRM_API int kvprm_cache_expand(const kvprm_cache* cache, const int32_t* src, c
  * whose value row is not finite makes NaN of the rows that see it, and of no others.
  *  workspace    device, kvprm_tree_workspace() bytes for the same arguments, 256-byte
  *               aligned; its first 8192 bytes zero before its first use.  Every
- *               call leaves them zero; calls that share it must be ordered.
+ *               call leaves them zero; calls that share it must be ordered.  Should
+ *               a wait inside the kernel give up (after 2 s), the rows that it
+ *               concerns get NaN and the int32 at byte 8188 is set.
  * Errors: KVPRM_EINVAL, KVPRM_ECAPACITY (workspace too small), KVPRM_ECUDA. */
 typedef struct {
   const void *q, *k, *v;

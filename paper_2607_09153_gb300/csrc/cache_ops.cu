@@ -450,7 +450,7 @@ int check_cache(const kvprm_cache* c, const char* who) {
     return operator_fail(KVPRM_EINVAL, "%s: cache format %d", who, c->format);
   if (c->head_dim != 64 && c->head_dim != 128)
     return operator_fail(KVPRM_EINVAL, "%s: head_dim %d is not 64 or 128", who, c->head_dim);
-  if (c->n_kv_heads < 1 || c->n_kv_heads > 1024 || c->n_pages < 0 || c->n_pages > (int64_t{1} << 31) - 1)
+  if (c->n_kv_heads < 1 || c->n_kv_heads > 1024 || c->n_pages < 0 || c->n_pages > (int64_t{1} << 30))
     return operator_fail(KVPRM_EINVAL, "%s: n_kv_heads %d, n_pages %lld", who, c->n_kv_heads,
                          static_cast<long long>(c->n_pages));
   if ((c->n_pages > 0 && !c->pages) || !aligned16(c->pages))

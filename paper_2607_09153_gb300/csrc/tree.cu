@@ -60,7 +60,7 @@ struct Frag {
 };
 
 template <int HD, bool E4M3>
-__global__ void __launch_bounds__(kThreads, 3) tree_rows16_kernel(const __grid_constant__ TreeLaunch a) {
+__global__ void __launch_bounds__(kThreads, kTreeRows16PerSm) tree_rows16_kernel(const __grid_constant__ TreeLaunch a) {
   using F = Frag<HD, E4M3>;
   constexpr int KS = HD / 16;   // 16-dim steps of q . k
   constexpr int NT = HD / 8;    // 8-dim tiles of the output
@@ -485,8 +485,6 @@ cudaError_t launch(const TreeLaunch& a, int ctas, cudaStream_t stream) {
 }
 
 }  // namespace
-
-int tree_rows16_ctas(int sms, const kvprm_cache&) { return 3 * sms; }
 
 cudaError_t launch_tree_rows16(const TreeLaunch& a, const kvprm_cache& c, int ctas, cudaStream_t stream) {
   if (c.head_dim == 128)

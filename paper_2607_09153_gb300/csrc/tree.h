@@ -9,7 +9,7 @@
 namespace kvprm {
 
 constexpr int kTreeSeqs = 1024;        // sequences of a launch (longer batches take several)
-constexpr int kTreeTickets = 2048;     // CTAs of a launch at most; the workspace's first words
+constexpr int kTreeTickets = 2048;     // the workspace's first words: a counter per CTA, and the last for waits that gave up
 constexpr int kTreePage = 16;
 
 struct TreeLaunch {
@@ -55,7 +55,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeLaunch& a, int s) {
 // off[s] = the first block of sequence s on the line, off[n_seqs] = W.  All threads of the CTA.
 template <int ROWS, int BLOCK, int THREADS>
 __device__ __forceinline__ void tree_line(const TreeLaunch& a, int64_t* off, int64_t* warp_sum) {
-  constexpr int kPer = kTreeSeqs / THREADS;
+  constexpr int kPer = (kTreeSeqs + THREADS - 1) / THREADS;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (a.n_seqs + THREADS - 1) / THREADS;   // <= kPer
   int64_t mine[kPer], sum = 0;
@@ -119,8 +119,10 @@ __device__ __forceinline__ uint32_t tree_sees16(const TreeLaunch& a, const TreeS
 
 #endif  // __CUDACC__
 
-// tree.cu: any number of rows, in tiles of 16.  CTAs of the launch, at most; bytes of partial results per CTA.
-int tree_rows16_ctas(int sms, const kvprm_cache& c);
+// tree.cu: query rows in tiles of 16; CTAs that run at once on an SM.
+constexpr int kTreeRows16PerSm = 3;
 cudaError_t launch_tree_rows16(const TreeLaunch& a, const kvprm_cache& c, int ctas, cudaStream_t stream);
+// tree_tc.cu: in pairs of tiles of 128, on the tensor cores; one CTA on an SM.  The cache has a page at least.
+cudaError_t launch_tree_tc(const TreeLaunch& a, const kvprm_cache& c, int ctas, cudaStream_t stream);
 
 }  // namespace kvprm

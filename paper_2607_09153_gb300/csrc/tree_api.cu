@@ -17,7 +17,8 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct TreePlan {
-  int ctas = 0, rows = 16;
+  bool tc = false;
+  int ctas = 0, rows = 16;   // rows: of a partial result
 };
 
 int check(const kvprm_cache* c, const kvprm_tree* t, const char* who) {
@@ -43,17 +44,19 @@ int sm_count(int* sms) {
   return KVPRM_OK;
 }
 
-// CTAs: as many as run at once, but no more than one per pair while pairs are short (a pair in one CTA needs no
-// joining), and 16 blocks for each where they are long.
+// More than 16 rows of a kv head go to the tensor cores.  CTAs: as many as run at once, but no more than one per pair
+// while pairs are short (a pair in one CTA needs no joining), and a few blocks for each where they are long.
 TreePlan plan(const kvprm_cache& c, const kvprm_tree& t, int sms) {
   TreePlan p;
-  const int group = t.n_q_heads / c.n_kv_heads;
-  const int64_t seqs = std::min<int64_t>(t.n_seqs, kTreeSeqs);
+  const int64_t rows = int64_t{t.max_drafts} * (t.n_q_heads / c.n_kv_heads);
+  p.tc = rows > 16 && c.n_pages > 0;
+  p.rows = p.tc ? 256 : 16;
+  const int64_t block = p.tc ? 128 : kTreePage, least = p.tc ? 4 : 16;
   const int64_t len = std::min<int64_t>(t.max_len, int64_t{kTreePage} * t.max_blocks);
-  const int64_t pairs = seqs * c.n_kv_heads * ceil_div(int64_t{t.max_drafts} * group, p.rows);
-  const int64_t blocks = ceil_div(len, kTreePage) + ceil_div(t.max_drafts, kTreePage);
-  const int64_t most = std::min(tree_rows16_ctas(sms, c), kTreeTickets);
-  p.ctas = static_cast<int>(std::max<int64_t>(1, std::min(most, std::max(pairs, pairs * blocks / 16))));
+  const int64_t pairs = std::min<int64_t>(t.n_seqs, kTreeSeqs) * c.n_kv_heads * ceil_div(rows, p.rows);
+  const int64_t blocks = ceil_div(len, block) + ceil_div(t.max_drafts, block);
+  const int64_t most = std::min<int64_t>(int64_t{sms} * (p.tc ? 1 : kTreeRows16PerSm), kTreeTickets - 1);
+  p.ctas = static_cast<int>(std::max<int64_t>(1, std::min(most, std::max(pairs, pairs * blocks / least))));
   return p;
 }
 
@@ -106,7 +109,8 @@ int kvprm_tree_attention(const kvprm_cache* cache, const kvprm_tree* t, void* wo
   a.part_ml = reinterpret_cast<float2*>(a.part_o + int64_t{2} * p.ctas * p.rows * cache->head_dim);
   for (a.seq0 = 0; a.seq0 < t->n_seqs; a.seq0 += kTreeSeqs) {
     a.n_seqs = std::min(kTreeSeqs, t->n_seqs - a.seq0);
-    const cudaError_t e = launch_tree_rows16(a, *cache, p.ctas, static_cast<cudaStream_t>(stream));
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const cudaError_t e = p.tc ? launch_tree_tc(a, *cache, p.ctas, st) : launch_tree_rows16(a, *cache, p.ctas, st);
     if (e != cudaSuccess) return operator_fail(KVPRM_ECUDA, "%s: %s", who, cudaGetErrorString(e));
   }
   return KVPRM_OK;

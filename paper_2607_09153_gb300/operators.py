@@ -4,13 +4,17 @@ or quantised to 8 bits, quantised pages expanded for the scorer, and the attenti
 Like kvprm.py this module only marshals arguments: shapes, types and devices are checked here, everything else by the
 library, and every step runs in its CUDA kernels.  Calls are enqueued on `stream` (default: torch's current one); a
 tensor that belongs to another stream has to be ordered by the caller, as for any torch operation.
+
+A decoding step's calls take a few microseconds on the GPU, so what is spent here counts: arguments are read once, and
+the C structs are packed as bytes (a ctypes structure takes about 0.2 us a field).
 """
 from __future__ import annotations
 
 import ctypes
 import math
+import struct
 
-from .kvprm import KVPRM_OK, KvprmError
+from .kvprm import KVPRM_ECAPACITY, KVPRM_OK, KvprmError
 from .kvprm import lib as _base_lib
 
 KVPRM_F32, KVPRM_BF16, KVPRM_F16 = range(3)
@@ -73,47 +77,73 @@ def _check(rc: int) -> None:
         raise KvprmError(rc, lib().kvprm_operator_error().decode())
 
 
-def _dtype(t) -> int:
-    import torch
-    code = {torch.float32: KVPRM_F32, torch.bfloat16: KVPRM_BF16, torch.float16: KVPRM_F16}.get(t.dtype)
-    if code is None:
-        raise TypeError(f"expected float32, bfloat16 or float16, got {t.dtype}")
-    return code
+class _Torch:
+    """What the calls need of torch, looked up once (the package imports without it)."""
 
-
-def _heads(name: str, t, device, dtype=None) -> None:
-    """[tokens][heads][head_dim] on `device`, the elements of a head side by side."""
-    if t.dim() != 3 or (t.stride(2) != 1 and t.shape[2] > 1):
-        raise ValueError(f"{name} is [tokens][heads][head_dim] with consecutive elements in a head, got "
-                         f"{tuple(t.shape)} with strides {tuple(t.stride())}")
-    if t.device != device or t.device.type != "cuda":
-        raise ValueError(f"{name} is on {t.device}, expected {device} (a CUDA device)")
-    if dtype is not None and t.dtype != dtype:
-        raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
-
-
-def _ints(name: str, t, dtype, shape, device) -> None:
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous() or t.device != device:
-        raise ValueError(f"{name} is a contiguous {dtype} tensor of shape {tuple(shape)} on {device}, got {t.dtype} "
-                         f"{tuple(t.shape)} on {t.device}")
-
-
-class _on:
-    """Makes the tensors' device current for the call (a no-op where it is) and gives the stream's handle."""
-
-    def __init__(self, device, stream):
+    def __init__(self):
         import torch
-        self.guard = torch.cuda.device(device) if device.index != torch.cuda.current_device() else None
-        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
+        self.torch = torch
+        self.codes = {torch.float32: KVPRM_F32, torch.bfloat16: KVPRM_BF16, torch.float16: KVPRM_F16}
+        self.bf16, self.i32, self.i64 = torch.bfloat16, torch.int32, torch.int64
+        self.e4m3, self.bytes = torch.float8_e4m3fn, (torch.uint8, torch.float8_e8m0fnu)
+        self.raw_stream = torch._C._cuda_getCurrentRawStream   # the handle alone: 0.1 us against 2 us for the object
+        self.device = torch._C._cuda_getDevice                  # the calls' tensors have initialised CUDA
+        self.capturing = torch.cuda.is_current_stream_capturing
+        self.empty = torch.empty   # 1.8 us; Tensor.new_empty takes 3.3
 
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.stream.cuda_stream
 
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+_t = None
+
+
+def _torch() -> _Torch:
+    global _t
+    if _t is None:
+        _t = _Torch()
+    return _t
+
+
+# struct layouts of the C ABI (the trailing 0q pads to the alignment, as C does)
+_HEADS = struct.Struct("@PPiqqqq")
+_CACHE = struct.Struct("@PPqiii0q")
+_TREE = struct.Struct("@PPPPqqqqqqqqPPPPiiiiiiif0q")
+assert _HEADS.size == ctypes.sizeof(KvprmHeads) and _CACHE.size == ctypes.sizeof(KvprmCache)
+assert _TREE.size == ctypes.sizeof(KvprmTree)
+
+
+def _heads(name: str, t, shape, dtype, device: int) -> tuple:
+    """Strides (token, head) of a tensor [tokens][heads][head_dim] whose heads' elements are side by side."""
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != device:
+        if t.dtype is not dtype:
+            raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
+        raise ValueError(f"{name} is {tuple(t.shape)} on {t.device}, expected {tuple(shape)} on CUDA device {device}")
+    st = t.stride()
+    if st[2] != 1 and shape[2] > 1:
+        raise ValueError(f"the elements of a head of {name} are not side by side: strides {st}")
+    return st
+
+
+def _rows(name: str, t) -> tuple:
+    """(shape, device index) of the tensor that the others of a call are compared with."""
+    shape, device = t.shape, t.get_device()
+    if len(shape) != 3 or device < 0:
+        raise ValueError(f"{name} is a CUDA tensor [tokens][heads][head_dim], got {tuple(shape)} on {t.device}")
+    return shape, device
+
+
+def _ints(name: str, t, dtype, shape: tuple, device: int) -> int:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name} is a contiguous {dtype} tensor of shape {tuple(shape)} on CUDA device {device}, got "
+                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _call(T, device: int, stream, function, *args) -> int:
+    """function(*args, stream handle) with the tensors' device current; the status."""
+    handle = T.raw_stream(device) if stream is None else stream.cuda_stream
+    if T.device() == device:
+        return function(*args, handle)
+    with T.torch.cuda.device(device):
+        return function(*args, handle)
 
 
 class Rope:
@@ -129,7 +159,9 @@ class Rope:
         self.rotary_dim = int(rotary_dim)
         cfg = KvprmRopeConfig(self.rotary_dim, int(interleaved), ROPE_SCALINGS.index(scaling), int(original_len),
                               float(base), float(factor), float(low), float(high), float(magnitude))
-        _check(lib().kvprm_rope_create(ctypes.byref(cfg), ctypes.byref(self.handle)))
+        L = lib()
+        self._rotate = L.kvprm_rope_rotate
+        _check(L.kvprm_rope_create(ctypes.byref(cfg), ctypes.byref(self.handle)))
 
     def turns(self) -> list:
         """Per pair, the turns that one position adds, in units of 2^-64."""
@@ -147,29 +179,36 @@ class Rope:
         return self._run(positions, grads, out, 1, stream)
 
     def _run(self, positions, tensors, out, inverse, stream):
-        import torch
+        T = _t or _torch()
         if not 1 <= len(tensors) <= 4:
             raise ValueError(f"1 to 4 tensors, got {len(tensors)}")
         x0 = tensors[0]
-        if out is None:
-            # the dense layout of the shape, also where the input is a slice of wider rows
-            out = tuple(torch.empty(t.shape, dtype=t.dtype, device=t.device) for t in tensors)
-        elif len(out) != len(tensors):
+        (n, _, hd), dev = _rows("a tensor", x0)
+        dtype = x0.dtype
+        code = T.codes.get(dtype)
+        if code is None:
+            raise TypeError(f"expected float32, bfloat16 or float16, got {dtype}")
+        if out is not None and len(out) != len(tensors):
             raise ValueError(f"{len(tensors)} tensors and {len(out)} outputs")
-        _ints("positions", positions, torch.int32, x0.shape[:1], x0.device)
-        rows = (KvprmHeads * len(tensors))()
-        for r, t, o in zip(rows, tensors, out):
-            _heads("a tensor", t, x0.device, x0.dtype)
-            _heads("an output", o, x0.device, x0.dtype)
-            if t.shape[0] != x0.shape[0] or t.shape[2] != x0.shape[2] or o.shape != t.shape:
-                raise ValueError("the tensors have different tokens or head_dim, or an output another shape")
-            r.in_, r.out, r.n_heads = t.data_ptr(), o.data_ptr(), t.shape[1]
-            r.in_token, r.in_head, _ = t.stride()
-            r.out_token, r.out_head, _ = o.stride()
-        with _on(x0.device, stream) as st:
-            _check(lib().kvprm_rope_rotate(self.handle, _dtype(x0), x0.shape[2], positions.data_ptr(), x0.shape[0],
-                                           inverse, rows, len(tensors), st))
-        return tuple(out)
+        result, packed = [], b""
+        for i, x in enumerate(tensors):
+            shape = x.shape
+            if len(shape) != 3 or shape[0] != n or shape[2] != hd:
+                raise ValueError(f"a tensor is {tuple(shape)}, expected [{n}][heads][{hd}]")
+            st = _heads("a tensor", x, shape, dtype, dev)
+            if out is None:
+                o = T.empty(shape, dtype=dtype, device=x.device)   # dense, also where x is a slice of wider rows
+                so = (shape[1] * hd, hd)
+            else:
+                o = out[i]
+                so = _heads("an output", o, shape, dtype, dev)
+            result.append(o)
+            packed += _HEADS.pack(x.data_ptr(), o.data_ptr(), shape[1], st[0], st[1], so[0], so[1])
+        at = _ints("positions", positions, T.i32, (n,), dev)
+        rc = _call(T, dev, stream, self._rotate, self.handle, code, hd, at, n, inverse, packed, len(result))
+        if rc != KVPRM_OK:
+            _check(rc)
+        return tuple(result)
 
     def __del__(self):
         try:
@@ -180,64 +219,65 @@ class Rope:
             pass
 
 
-def _cache(pages, exponents) -> KvprmCache:
-    """One layer's pages [n_pages][2][n_kv_heads][16][head_dim]: bfloat16, or float8_e4m3fn with exponents
-    [n_pages][2][n_kv_heads][16] (uint8 or float8_e8m0fnu)."""
-    import torch
-    if pages.dim() != 5 or pages.shape[1] != 2 or pages.shape[3] != PAGE or not pages.is_contiguous() or \
-            pages.device.type != "cuda":
+def _cache(T, pages, exponents) -> tuple:
+    """(C struct, kv heads, head_dim, device index) of one layer's pages [n_pages][2][n_kv_heads][16][head_dim]:
+    bfloat16, or float8_e4m3fn with exponents [n_pages][2][n_kv_heads][16] (uint8 or float8_e8m0fnu)."""
+    shape, device = pages.shape, pages.get_device()
+    if len(shape) != 5 or shape[1] != 2 or shape[3] != PAGE or device < 0 or not pages.is_contiguous():
         raise ValueError(f"pages are a contiguous CUDA tensor [n_pages][2][n_kv_heads][16][head_dim], got "
-                         f"{tuple(pages.shape)} on {pages.device}")
-    if pages.dtype == torch.bfloat16:
+                         f"{tuple(shape)} on {pages.device}")
+    if pages.dtype is T.bf16:
         if exponents is not None:
             raise ValueError("bfloat16 pages have no exponents")
-        return KvprmCache(pages.data_ptr(), None, pages.shape[0], pages.shape[2], pages.shape[4], KVPRM_CACHE_BF16)
-    if pages.dtype != torch.float8_e4m3fn:
+        return _CACHE.pack(pages.data_ptr(), 0, shape[0], shape[2], shape[4], KVPRM_CACHE_BF16), shape[2], shape[4], device
+    if pages.dtype is not T.e4m3:
         raise TypeError(f"pages are bfloat16 or float8_e4m3fn, got {pages.dtype}")
-    if exponents is None or exponents.dtype not in (torch.uint8, torch.float8_e8m0fnu) or \
-            exponents.shape != pages.shape[:4] or not exponents.is_contiguous() or exponents.device != pages.device:
+    if exponents is None or exponents.dtype not in T.bytes or exponents.shape != shape[:4] or \
+            exponents.get_device() != device or not exponents.is_contiguous():
         raise ValueError("float8_e4m3fn pages need contiguous uint8 or float8_e8m0fnu exponents "
                          "[n_pages][2][n_kv_heads][16]")
-    return KvprmCache(pages.data_ptr(), exponents.data_ptr(), pages.shape[0], pages.shape[2], pages.shape[4],
-                      KVPRM_CACHE_E4M3)
+    return (_CACHE.pack(pages.data_ptr(), exponents.data_ptr(), shape[0], shape[2], shape[4], KVPRM_CACHE_E4M3),
+            shape[2], shape[4], device)
 
 
 def cache_write(pages, slots, k, v, exponents=None, rope: Rope | None = None, positions=None, stream=None) -> None:
     """Writes tokens' keys and values [tokens][n_kv_heads][head_dim] into their slots (int64: 16 * page + place; below
     zero: not written), quantised where the pages are, the keys rotated on the way with `rope` and int32 `positions`."""
-    import torch
-    c = _cache(pages, exponents)
-    for name, t in (("k", k), ("v", v)):
-        _heads(name, t, pages.device, k.dtype)
-        if tuple(t.shape[1:]) != (c.n_kv_heads, c.head_dim) or t.shape[0] != k.shape[0]:
-            raise ValueError(f"{name} is {tuple(t.shape)}, expected [tokens][{c.n_kv_heads}][{c.head_dim}]")
-    _ints("slots", slots, torch.int64, k.shape[:1], pages.device)
+    T = _t or _torch()
+    c, heads, hd, dev = _cache(T, pages, exponents)
+    n, dtype = k.shape[0], k.dtype
+    code = T.codes.get(dtype)
+    if code is None:
+        raise TypeError(f"k is {dtype}, expected float32, bfloat16 or float16")
+    sk, sv = _heads("k", k, (n, heads, hd), dtype, dev), _heads("v", v, (n, heads, hd), dtype, dev)
     if (rope is None) != (positions is None):
         raise ValueError("rope and positions come together")
-    if positions is not None:
-        _ints("positions", positions, torch.int32, k.shape[:1], pages.device)
-    with _on(pages.device, stream) as st:
-        _check(lib().kvprm_cache_write(ctypes.byref(c), _dtype(k), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
-                                       v.stride(0), v.stride(1), slots.data_ptr(), k.shape[0],
-                                       rope.handle if rope is not None else None,
-                                       positions.data_ptr() if positions is not None else None, st))
+    handle = at = None
+    if rope is not None:
+        handle, at = rope.handle, _ints("positions", positions, T.i32, (n,), dev)
+    rc = _call(T, dev, stream, lib().kvprm_cache_write, c, code, k.data_ptr(), sk[0], sk[1], v.data_ptr(), sv[0], sv[1],
+               _ints("slots", slots, T.i64, (n,), dev), n, handle, at)
+    if rc != KVPRM_OK:
+        _check(rc)
 
 
 def cache_expand(pages, exponents, src, out, dst=None, stream=None):
-    """Quantised pages src[i] as bf16 pages dst[i] (default: i) of `out`, a layer that the scoring calls read; returns
-    `out`."""
-    import torch
-    c = _cache(pages, exponents)
-    if out.dtype != torch.bfloat16 or out.dim() != 5 or out.shape[1:] != pages.shape[1:] or not out.is_contiguous() or \
-            out.device != pages.device:
+    """Quantised pages src[i] (int32) as bf16 pages dst[i] (int32; default: i) of `out`, a layer that the scoring calls
+    read; returns `out`."""
+    T = _t or _torch()
+    c, _, _, dev = _cache(T, pages, exponents)
+    shape = out.shape
+    if out.dtype is not T.bf16 or len(shape) != 5 or shape[1:] != pages.shape[1:] or out.get_device() != dev or \
+            not out.is_contiguous():
         raise ValueError(f"out is a contiguous bfloat16 tensor [pages]{list(pages.shape[1:])} on {pages.device}")
+    n = src.shape[0]
     if dst is None:
-        dst = torch.arange(src.shape[0], dtype=torch.int32, device=pages.device)
-    _ints("src", src, torch.int32, src.shape[:1], pages.device)
-    _ints("dst", dst, torch.int32, src.shape[:1], pages.device)
-    with _on(pages.device, stream) as st:
-        _check(lib().kvprm_cache_expand(ctypes.byref(c), src.data_ptr(), dst.data_ptr(), src.shape[0], out.data_ptr(),
-                                        out.shape[0], st))
+        with T.torch.cuda.stream(stream):
+            dst = T.torch.arange(n, dtype=T.i32, device=out.device)
+    rc = _call(T, dev, stream, lib().kvprm_cache_expand, c, _ints("src", src, T.i32, (n,), dev),
+               _ints("dst", dst, T.i32, (n,), dev), n, out.data_ptr(), shape[0])
+    if rc != KVPRM_OK:
+        _check(rc)
     return out
 
 
@@ -266,20 +306,15 @@ def tree_mask(parents, start):
 _workspaces: dict = {}
 
 
-def _workspace(need: int, device, stream):
-    """Scratch of tree_attention, kept per device and stream: calls on one stream follow one another, so they can
-    share it, and each leaves its counters at zero.  A call that is being captured gets scratch of its own (the
-    graph's, zeroed by it): the graph may be replayed on any stream."""
-    import torch
-    if torch.cuda.is_current_stream_capturing():
-        with torch.cuda.stream(stream):
-            return torch.zeros(need, dtype=torch.uint8, device=device)
-    key = (device, stream.cuda_stream)
-    w = _workspaces.get(key)
-    if w is None or w.numel() < need:
-        with torch.cuda.stream(stream):
-            w = _workspaces[key] = torch.zeros(need, dtype=torch.uint8, device=device)
-    return w
+def _zeros(T, need: int, device: int, stream):
+    with T.torch.cuda.stream(stream):   # (None: the current one)
+        return T.torch.zeros(need, dtype=T.torch.uint8, device=T.torch.device("cuda", device))
+
+
+def _workspace_bytes(c: bytes, t: bytes) -> int:
+    need = ctypes.c_int64()
+    _check(lib().kvprm_tree_workspace(c, t, ctypes.byref(need)))
+    return need.value
 
 
 def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, max_len: int | None = None,
@@ -291,41 +326,48 @@ def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, ma
     cached ones in pages block_table[s][0 ..] (int32).  mask: int32 [tokens][words], bit j of a token's row: it sees
     drafted token j of its sequence (tree_mask); None: those up to itself.  max_len sizes the launch (default: the
     block table's width).  Returns [tokens][n_q_heads][head_dim]."""
-    import torch
-    c = _cache(pages, exponents)
-    dev = pages.device
-    for name, t, heads in (("q", q, q.shape[1]), ("k", k, c.n_kv_heads), ("v", v, c.n_kv_heads)):
-        _heads(name, t, dev, torch.bfloat16)
-        if t.shape[0] != q.shape[0] or t.shape[1] != heads or t.shape[2] != c.head_dim:
-            raise ValueError(f"{name} is {tuple(t.shape)}, expected [{q.shape[0]}][{heads}][{c.head_dim}]")
+    T = _t or _torch()
+    c, heads, hd, dev = _cache(T, pages, exponents)
+    shape, _ = _rows("q", q)
+    tokens, nq, _ = shape
+    bf16, i32 = T.bf16, T.i32
+    sq = _heads("q", q, (tokens, nq, hd), bf16, dev)
+    sk, sv = _heads("k", k, (tokens, heads, hd), bf16, dev), _heads("v", v, (tokens, heads, hd), bf16, dev)
     n = lens.shape[0]
     if block_table.dim() != 2:
         raise ValueError("block_table is [n_seqs][max_blocks]")
-    _ints("block_table", block_table, torch.int32, (n, block_table.shape[1]), dev)
-    _ints("lens", lens, torch.int32, (n,), dev)
-    _ints("start", start, torch.int32, (n + 1,), dev)
+    width = block_table.shape[1]
+    bits, words = 0, 0
     if mask is not None:
         if mask.dim() != 2:
             raise ValueError("mask is [tokens][words]")
-        _ints("mask", mask, torch.int32, (q.shape[0], mask.shape[1]), dev)
+        words = mask.shape[1]
+        bits = _ints("mask", mask, i32, (tokens, words), dev)
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        out = T.empty(shape, dtype=bf16, device=q.device)
+        so = (nq * hd, hd)
     else:
-        _heads("out", out, dev, torch.bfloat16)
-        if out.shape != q.shape:
-            raise ValueError(f"out is {tuple(out.shape)}, expected {tuple(q.shape)}")
-    t = KvprmTree(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), q.stride(0), q.stride(1), k.stride(0),
-                  k.stride(1), v.stride(0), v.stride(1), out.stride(0), out.stride(1), block_table.data_ptr(),
-                  lens.data_ptr(), start.data_ptr(), mask.data_ptr() if mask is not None else None,
-                  block_table.shape[1], n, q.shape[0], q.shape[1], int(max_drafts),
-                  PAGE * block_table.shape[1] if max_len is None else int(max_len),
-                  mask.shape[1] if mask is not None else 0,
-                  1.0 / math.sqrt(c.head_dim) if scale is None else float(scale))
-    on = _on(dev, stream)
-    with on as st:
-        if workspace is None:
-            need = ctypes.c_int64()
-            _check(lib().kvprm_tree_workspace(ctypes.byref(c), ctypes.byref(t), ctypes.byref(need)))
-            workspace = _workspace(need.value, dev, on.stream)
-        _check(lib().kvprm_tree_attention(ctypes.byref(c), ctypes.byref(t), workspace.data_ptr(), workspace.numel(), st))
+        so = _heads("out", out, shape, bf16, dev)
+    t = _TREE.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), sq[0], sq[1], sk[0], sk[1], sv[0], sv[1],
+                   so[0], so[1], _ints("block_table", block_table, i32, (n, width), dev),
+                   _ints("lens", lens, i32, (n,), dev), _ints("start", start, i32, (n + 1,), dev), bits, width, n,
+                   tokens, nq, max_drafts, PAGE * width if max_len is None else max_len, words,
+                   1.0 / math.sqrt(hd) if scale is None else scale)
+    go = lib().kvprm_tree_attention
+    if workspace is not None:
+        rc = _call(T, dev, stream, go, c, t, workspace.data_ptr(), workspace.numel())
+    else:
+        # Scratch is kept per device and stream: calls on one stream follow one another, so they can share it, and each
+        # leaves its counters at zero.  A call that is being captured gets scratch of its own (the graph's, zeroed by
+        # it): the graph may be replayed on any stream.
+        key = (dev, T.raw_stream(dev) if stream is None else stream.cuda_stream)
+        w = _workspaces.get(key)
+        if T.capturing():
+            w = _zeros(T, _workspace_bytes(c, t), dev, stream)
+        rc = KVPRM_ECAPACITY if w is None else _call(T, dev, stream, go, c, t, w.data_ptr(), w.numel())
+        if rc == KVPRM_ECAPACITY:
+            w = _workspaces[key] = _zeros(T, _workspace_bytes(c, t), dev, stream)
+            rc = _call(T, dev, stream, go, c, t, w.data_ptr(), w.numel())
+    if rc != KVPRM_OK:
+        _check(rc)
     return out

@@ -412,7 +412,8 @@ def test_tree_wide(nq, nkv, hd, mask, e4m3):
 
 @pytest.mark.parametrize("e4m3", [False, True])
 @pytest.mark.parametrize("lens,drafts", [([20011], [1]), ([20011], [9]), ([5000, 3, 7777], [40, 2, 33]),
-                                         ([12345], [64]), ([0] * 3 + [9000] + [0] * 3, [1] * 7)])
+                                         ([12345], [64]), ([0] * 3 + [9000] + [0] * 3, [1] * 7),
+                                         ([14000, 9999] * 3, [9, 200, 6, 12, 40, 5])])
 def test_tree_long(lens, drafts, e4m3):
     """Long caches, whose parts many CTAs score and one joins."""
     torch, _ = _kp()
@@ -440,14 +441,16 @@ def test_tree_peaked(e4m3):
     t.check(t.run(scale=-0.05), scale=-0.05)
 
 
-def test_tree_small_codes_count():
-    """Rows whose weight is all in e4m3's subnormal codes beside one large one that the query does not meet."""
+@pytest.mark.parametrize("drafts", [1, 20])
+@pytest.mark.parametrize("exponent", [6, 8, 30, -40])
+def test_tree_small_codes_count(drafts, exponent):
+    """Rows of e4m3's subnormal codes alone (0 .. 7/8 2^-6), at scales on both sides of what one bf16 factor holds."""
     torch, kp = _kp()
-    t = Tree(torch, 2, 1, 128, [64], [1], True, seed=3)
+    t = Tree(torch, 2, 1, 128, [64], [drafts], True, seed=3, q_std=2.0 ** -max(0, exponent))
     codes = t.pages.view(torch.uint8)
-    codes[:] = torch.randint(0, 8, codes.shape, device="cuda", dtype=torch.uint8)   # 0 .. 7/8 2^-6
-    t.exps[:] = 127 + 6
-    t.values = t.pages.double() * 64
+    codes[:] = torch.randint(0, 8, codes.shape, device="cuda", dtype=torch.uint8)
+    t.exps[:] = 127 + exponent
+    t.values = t.pages.double() * 2.0 ** exponent
     t.check(t.run())
 
 
