@@ -695,10 +695,10 @@ KVPRM_API int kvprm_cache_expand(const kvprm_cache* cache, const int32_t* src, c
  * out.  Slots past a length and drafts that no row sees may hold anything; a draft
  * whose value row is not finite makes NaN of the rows that see it, and of no others.
  *  workspace    device, kvprm_tree_workspace() bytes for the same arguments, 256-byte
- *               aligned; its first 8192 bytes zero before its first use.  Every
- *               call leaves them zero; calls that share it must be ordered.  Should
- *               a wait inside the kernel give up (after 2 s), the rows that it
- *               concerns get NaN and the int32 at byte 8188 is set.
+ *               aligned; scratch of any contents.  Calls that share it must be
+ *               ordered.
+ * Should a wait inside the kernel give up (after 2 s), the rows that it concerns get
+ * NaN.
  * Errors: KVPRM_EINVAL, KVPRM_ECAPACITY (workspace too small), KVPRM_ECUDA. */
 typedef struct {
   const void *q, *k, *v;

@@ -14,7 +14,7 @@ BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "libkvprm.so")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 SOURCES = ["kvprm_api.cu", "gemm_tc.cu", "attention.cu", "fused.cu", "noalloc.cu", "grad.cu",
-           "cache_ops.cu", "tree.cu", "tree_tc.cu", "tree_api.cu"]
+           "cache_ops.cu", "tree.cu", "tree_tc.cu", "tree_join.cu", "tree_api.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=hidden",
          "--expt-relaxed-constexpr"] + ARCH

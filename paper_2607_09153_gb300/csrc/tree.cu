@@ -64,26 +64,28 @@ __global__ void __launch_bounds__(kThreads, kTreeRows16PerSm) tree_rows16_kernel
   using F = Frag<HD, E4M3>;
   constexpr int KS = HD / 16;   // 16-dim steps of q . k
   constexpr int NT = HD / 8;    // 8-dim tiles of the output
-  __shared__ int64_t s_off[kTreeSeqs + 1];
-  __shared__ int64_t s_sum[kWarps];
-  __shared__ __align__(16) float s_o[kWarps][kRows][HD];
+  __shared__ int32_t s_off[kTreeSeqs + 1];
+  __shared__ int32_t s_sum[kWarps];
+  __shared__ float s_o[kWarps][kRows][HD + 1];
   __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
-  __shared__ int s_last;
-  tree_line<kRows, kTreePage, kThreads>(a, s_off, s_sum);
-  const int64_t total = s_off[a.n_seqs];
-  const int P = static_cast<int>(min(static_cast<int64_t>(gridDim.x), total)), me = blockIdx.x;
-  if (me >= P) return;
-  const int64_t u_begin = total * me / P, u_end = total * (me + 1) / P;
+  grid_dep_launch();
+  tree_line<TreeRows16, kThreads>(a, s_off, s_sum);
+  const int32_t total = s_off[a.n_seqs];
+  if (total == 0) return;
+  const TreeShares shares(total, gridDim.x, 1);
+  const int me = blockIdx.x;
+  tree_leave_line(a, s_off, shares.ctas);
+  if (me >= shares.ctas) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, c = lane & 3;
   const int64_t block_bytes = static_cast<int64_t>(kTreePage) * HD * (E4M3 ? 1 : 2);   // of one head's keys
-  int s = tree_find(s_off, a.n_seqs, u_begin);
-  for (int64_t u = u_begin; u < u_end;) {
-    while (u >= s_off[s + 1]) ++s;
-    const TreeSeq q = tree_seq<kRows, kTreePage>(a, s);
-    const int64_t local = u - s_off[s];
-    const int pair = static_cast<int>(local / q.blocks), b0 = static_cast<int>(local - static_cast<int64_t>(pair) * q.blocks);
-    const int count = static_cast<int>(min(static_cast<int64_t>(q.blocks - b0), u_end - u));
-    const int g = pair / q.tiles, tile = pair - g * q.tiles, rows = q.drafts * a.group;
+  int32_t u = shares.begin(me);
+  const int32_t u_end = shares.begin(me + 1);
+  int s = tree_find(s_off, a.n_seqs, u);
+  TreePart part;
+  for (bool first_part = true; tree_next<TreeRows16>(a, s_off, u, u_end, s, part); first_part = false) {
+    if (!first_part) __syncthreads();   // the last part's states have been read
+    const TreeSeq& q = part.q;
+    const int g = part.g, tile = part.tp, rows = q.drafts * a.group;
     const int32_t* table = a.t.block_table + static_cast<int64_t>(a.seq0 + s) * a.t.max_blocks;
 
     // ---- query fragments: rows gid and gid + 8
@@ -93,10 +95,10 @@ __global__ void __launch_bounds__(kThreads, kTreeRows16PerSm) tree_rows16_kernel
     for (int h = 0; h < 2; ++h) {
       const int r = tile * kRows + gid + 8 * h;
       const bool live = r < rows;
-      row_t[h] = live ? r / a.group : -1;
+      row_t[h] = live ? tree_token(a, r) : -1;
       const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.t.q) +
                                  (live ? (q.start + static_cast<int64_t>(row_t[h])) * a.t.q_token +
-                                             (g * a.group + r % a.group) * a.t.q_head
+                                             (g * a.group + r - row_t[h] * a.group) * a.t.q_head
                                        : 0);
       const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
       if constexpr (E4M3) {
@@ -197,8 +199,8 @@ __global__ void __launch_bounds__(kThreads, kTreeRows16PerSm) tree_rows16_kernel
       }
     };
 
-    const int b_end = b0 + count;
-    int b = b0 + warp;
+    const int b_end = part.c1;
+    int b = part.c0 + warp;
     int64_t page = -1;
     if (b < min(b_end, q.cached_blocks)) {
       page = page_of(b);
@@ -397,7 +399,7 @@ __global__ void __launch_bounds__(kThreads, kTreeRows16PerSm) tree_rows16_kernel
       }
     __syncthreads();
     constexpr int kPer = kRows * HD / kThreads;   // outputs of a thread: part of one row
-    const int r = threadIdx.x / (HD / kPer), d0 = threadIdx.x % (HD / kPer) * kPer;
+    const int r = threadIdx.x % kRows, d0 = threadIdx.x / kRows * kPer;
     float top = -INFINITY, sum = 0.f, acc[kPer];
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w][r]);
@@ -405,61 +407,22 @@ __global__ void __launch_bounds__(kThreads, kTreeRows16PerSm) tree_rows16_kernel
     for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-      const float f = s_m[w][r] == -INFINITY ? (s_l[w][r] == 0.f ? 0.f : 1.f) : ex2_ftz(s_m[w][r] - top);
+      const float f = s_m[w][r] == -INFINITY ? 0.f : ex2_ftz(s_m[w][r] - top);   // (NaN sums stay NaN)
       sum += s_l[w][r] * f;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) acc[i] += s_o[w][r][d0 + i] * f;
     }
-    bool write = true;
-    if (count < q.blocks) {   // the pair goes on in other CTAs: the last of them to finish joins all parts, in order
-      const int64_t first = s_off[s] + static_cast<int64_t>(pair) * q.blocks;
-      const int i0 = tree_owner(first, total, P), i1 = tree_owner(first + q.blocks - 1, total, P);
-      const int slot = me == i0 ? 2 * me + 1 : 2 * me;
-      float* po = a.part_o + (static_cast<int64_t>(slot) * kRows + r) * HD + d0;
-#pragma unroll
-      for (int i = 0; i < kPer; i += 4) *reinterpret_cast<float4*>(po + i) = make_float4(acc[i], acc[i + 1], acc[i + 2], acc[i + 3]);
-      if (d0 == 0) a.part_ml[slot * kRows + r] = make_float2(top, sum);
-      __threadfence();
-      __syncthreads();
-      if (threadIdx.x == 0) {
-        const int n = atomicAdd(a.tickets + i0, 1);
-        s_last = n == i1 - i0;
-        if (s_last) a.tickets[i0] = 0;
-      }
-      __syncthreads();
-      write = s_last != 0;
-      if (write) {
-        __threadfence();
-        float best = -INFINITY;
-        for (int i = i0; i <= i1; ++i) best = fmaxf(best, __ldcg(a.part_ml + (i == i0 ? 2 * i + 1 : 2 * i) * kRows + r).x);
-        top = best;
-        sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
-#pragma unroll 2
-        for (int i = i0; i <= i1; ++i) {
-          const int sl = i == i0 ? 2 * i + 1 : 2 * i;
-          const float2 ml = __ldcg(a.part_ml + sl * kRows + r);
-          const float f = ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : ex2_ftz(ml.x - best);
-          sum += ml.y * f;
-          const float4* p = reinterpret_cast<const float4*>(a.part_o + (static_cast<int64_t>(sl) * kRows + r) * HD + d0);
-#pragma unroll
-          for (int k = 0; k < kPer / 4; ++k) {
-            const float4 x = __ldcg(p + k);
-            acc[4 * k] += x.x * f;
-            acc[4 * k + 1] += x.y * f;
-            acc[4 * k + 2] += x.z * f;
-            acc[4 * k + 3] += x.w * f;
-          }
-        }
-      }
-    }
     const int out_r = tile * kRows + r;
-    if (write && out_r < rows) {
+    if (!part.whole()) {   // the pair goes on in other CTAs
+      const int slot = me == shares.owner(part.place(0)) ? 2 * me + 1 : 2 * me;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) a.part_o[(static_cast<int64_t>(slot) * HD + d0 + i) * kRows + r] = acc[i];
+      if (d0 == 0) a.part_ml[slot * kRows + r] = make_float2(top, sum);
+    } else if (out_r < rows) {
       const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row that saw nothing: zeros; NaN stays
-      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.t.out) +
-                           (q.start + static_cast<int64_t>(out_r / a.group)) * a.t.out_token +
-                           (g * a.group + out_r % a.group) * a.t.out_head + d0;
+      const int tok = tree_token(a, out_r);
+      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.t.out) + (q.start + static_cast<int64_t>(tok)) * a.t.out_token +
+                           (g * a.group + out_r - tok * a.group) * a.t.out_head + d0;
 #pragma unroll
       for (int i = 0; i < kPer; i += 8) {
         uint4 w;
@@ -470,8 +433,6 @@ __global__ void __launch_bounds__(kThreads, kTreeRows16PerSm) tree_rows16_kernel
         *reinterpret_cast<uint4*>(dst + i) = w;
       }
     }
-    u += count;
-    if (u < u_end) __syncthreads();   // the states are read before the next part's are written
   }
 }
 

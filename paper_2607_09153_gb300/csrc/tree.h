@@ -8,8 +8,7 @@
 
 namespace kvprm {
 
-constexpr int kTreeSeqs = 1024;        // sequences of a launch (longer batches take several)
-constexpr int kTreeTickets = 2048;     // the workspace's first words: a counter per CTA, and the last for waits that gave up
+constexpr int kTreeSeqs = 1024;        // sequences of a launch at most (longer batches take several)
 constexpr int kTreePage = 16;
 
 struct TreeLaunch {
@@ -18,19 +17,24 @@ struct TreeLaunch {
   const uint8_t* exponents;
   int64_t n_pages;
   int32_t n_kv, group, seq0, n_seqs;   // sequences seq0 .. seq0 + n_seqs - 1
+  uint32_t group_m;                    // ceil(2^32 / group), 0 for a group of one (tree_token)
+  int32_t whole;                       // 1: no pair is cut
   float scale_log2;                    // scores in units of log2
-  int32_t* tickets;
-  float* part_o;                       // [2 * CTAs][rows][head_dim]
+  int32_t* line;                       // [n_seqs + 1], then the CTAs that took part: for the join
+  float* part_o;                       // [2 * CTAs][head_dim][rows]
   float2* part_ml;                     // [2 * CTAs][rows]
 };
 
 #ifdef __CUDACC__
 
-// The work of a launch is one line of blocks (of kBlock keys), laid end to end: sequence by sequence, in a
-// sequence (kv head, tile of ROWS query rows) by (kv head, tile) -- a "pair" -- and in a pair the cached blocks,
-// then the blocks of drafted tokens.  CTA i of P takes [W i / P, W (i + 1) / P): equal shares whatever the lengths
-// are, with at most two pairs that it shares with other CTAs.  The line's marks come from the device's own lengths
-// (a prefix sum over the sequences at the start of each CTA), so that nothing is planned on the host.
+// The work of a launch is one line, laid out sequence by sequence, in a sequence (kv head, rows) by (kv head, rows) -- a
+// "pair", with `weight` row tiles -- and in a pair block by block (of kBlock keys), the cached ones first, then those of
+// drafted tokens.  A block takes `weight` places, and a pair begins with LEAD * weight places that stand for what it costs to
+// begin one.  Each CTA takes an equal share of the line, whatever the lengths are: the blocks whose first place it holds,
+// so at most two of its pairs are shared with other CTAs.  Those leave partial results (slot 2 i + 1 of CTA i for a pair
+// that begins in its share, 2 i for one that began before), which a second launch joins in order (tree_join.cu).  With
+// `whole` set a pair goes to the CTA that holds its first block.  The line's marks come from the device's own lengths (a
+// prefix sum over the sequences at the start of each CTA), so that nothing is planned on the host.
 struct TreeSeq {
   int32_t len, start, drafts, cached_blocks, blocks, tiles;
   bool bad;   // a length that cannot be: every output NaN
@@ -52,32 +56,39 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeLaunch& a, int s) {
   return q;
 }
 
-// off[s] = the first block of sequence s on the line, off[n_seqs] = W.  All threads of the CTA.
-template <int ROWS, int BLOCK, int THREADS>
-__device__ __forceinline__ void tree_line(const TreeLaunch& a, int64_t* off, int64_t* warp_sum) {
+// The geometry of a kernel's line: ROWS query rows of a tile, BLOCK keys, pairs of up to TILES tiles, LEAD (above).
+template <int ROWS_, int BLOCK_, int TILES_, int LEAD_>
+struct TreeGeometry {
+  static constexpr int ROWS = ROWS_, BLOCK = BLOCK_, TILES = TILES_, LEAD = LEAD_;
+  static constexpr int kSlotRows = ROWS * TILES;   // of a partial result
+};
+
+// off[s] = the first place of sequence s, off[n_seqs] = the line's length (kept below 2^31 by the host).  All threads.
+template <typename G, int THREADS>
+__device__ __forceinline__ void tree_line(const TreeLaunch& a, int32_t* off, int32_t* warp_sum) {
   constexpr int kPer = (kTreeSeqs + THREADS - 1) / THREADS;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (a.n_seqs + THREADS - 1) / THREADS;   // <= kPer
-  int64_t mine[kPer], sum = 0;
+  int32_t mine[kPer], sum = 0;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     if (k >= per) break;
     const int s = tid * per + k;
     mine[k] = sum;
     if (s < a.n_seqs) {
-      const TreeSeq q = tree_seq<ROWS, BLOCK>(a, s);
-      sum += static_cast<int64_t>(q.blocks) * q.tiles * a.n_kv;
+      const TreeSeq q = tree_seq<G::ROWS, G::BLOCK>(a, s);
+      if (q.drafts > 0) sum += (q.blocks + G::LEAD) * q.tiles * a.n_kv;
     }
   }
-  int64_t scan = sum;
+  int32_t scan = sum;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const int64_t up = __shfl_up_sync(0xffffffffu, scan, d);
+    const int32_t up = __shfl_up_sync(0xffffffffu, scan, d);
     if (lane >= d) scan += up;
   }
   if (lane == 31) warp_sum[warp] = scan;
   __syncthreads();
-  int64_t before = scan - sum;
+  int32_t before = scan - sum;
   for (int w = 0; w < warp; ++w) before += warp_sum[w];
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
@@ -89,8 +100,65 @@ __device__ __forceinline__ void tree_line(const TreeLaunch& a, int64_t* off, int
   __syncthreads();
 }
 
-// The sequence that holds block u of the line.
-__device__ __forceinline__ int tree_find(const int64_t* off, int n, int64_t u) {
+// The CTAs' shares of the line: the first `more` have least + 1 places, the others `least`.  A share is as long as the
+// widest block at least, so that every CTA between a pair's first and last holds a block of it.
+struct TreeShares {
+  int32_t ctas, least, more;
+  __device__ __forceinline__ TreeShares(int32_t total, int grid, int tiles) : ctas(max(1, min(grid, total / tiles))) {
+    least = total / ctas;
+    more = total - least * ctas;
+  }
+  __device__ __forceinline__ int32_t begin(int cta) const { return least * cta + min(cta, more); }
+  __device__ __forceinline__ int owner(int32_t u) const {   // the CTA whose share holds place u
+    const int32_t longer = more * (least + 1);
+    return u < longer ? u / (least + 1) : more + (u - longer) / least;
+  }
+};
+
+// A pair, and one CTA's blocks c0 .. c1 - 1 of it.
+struct TreePart {
+  TreeSeq q;
+  int32_t first;      // the place of its first block
+  int s, g, tp;       // sequence, kv head, which TILES tiles
+  int tiles, c0, c1;  // tiles: its weight
+  __device__ __forceinline__ bool whole() const { return c0 == 0 && c1 == q.blocks; }
+  __device__ __forceinline__ int32_t place(int block) const { return first + block * tiles; }
+};
+
+// Walks a CTA's share [u, u_end); s: the sequence to start looking from (tree_find).
+template <typename G>
+__device__ __forceinline__ bool tree_next(const TreeLaunch& a, const int32_t* off, int32_t& u, int32_t u_end, int& s,
+                                          TreePart& p) {
+  while (u < u_end) {
+    while (u >= off[s + 1]) ++s;
+    p.q = tree_seq<G::ROWS, G::BLOCK>(a, s);
+    p.s = s;
+    const int32_t depth = p.q.blocks + G::LEAD, head = depth * p.q.tiles, local = u - off[s];
+    p.g = local / head;
+    p.tp = (local - p.g * head) / (G::TILES * depth);
+    p.tiles = min(G::TILES, p.q.tiles - G::TILES * p.tp);
+    const int32_t pair0 = off[s] + p.g * head + p.tp * G::TILES * depth;
+    p.first = pair0 + G::LEAD * p.tiles;
+    auto block_at = [&](int32_t place) {   // the first block that begins at a place or after it
+      const int32_t d = place - p.first;
+      return d <= 0 ? 0 : min(p.q.blocks, (d + p.tiles - 1) / p.tiles);
+    };
+    p.c0 = block_at(u);
+    p.c1 = block_at(u_end);
+    if (a.whole) {
+      const bool mine = p.first >= u && p.first < u_end;
+      p.c0 = 0;
+      p.c1 = mine ? p.q.blocks : 0;
+    }
+    const int32_t end = pair0 + depth * p.tiles;
+    u = min(end, u_end);
+    if (p.c0 < p.c1) return true;
+  }
+  return false;
+}
+
+// The sequence that holds place u.
+__device__ __forceinline__ int tree_find(const int32_t* off, int n, int32_t u) {
   int lo = 0, hi = n - 1;
   while (lo < hi) {
     const int mid = (lo + hi + 1) >> 1;
@@ -99,9 +167,16 @@ __device__ __forceinline__ int tree_find(const int64_t* off, int n, int64_t u) {
   return lo;
 }
 
-// The CTA of P whose share holds block u: the largest i with W i / P <= u.
-__device__ __forceinline__ int tree_owner(int64_t u, int64_t total, int p) {
-  return static_cast<int>(((u + 1) * p - 1) / total);
+// Left for the join by the launch's first CTA.
+__device__ __forceinline__ void tree_leave_line(const TreeLaunch& a, const int32_t* off, int ctas) {
+  if (blockIdx.x != 0 || a.whole) return;
+  for (int i = threadIdx.x; i <= a.n_seqs; i += blockDim.x) a.line[i] = off[i];
+  if (threadIdx.x == 0) a.line[a.n_seqs + 1] = ctas;
+}
+
+// A row's drafted token: row / group (rows < 2^21, group <= 2^10).
+__device__ __forceinline__ int tree_token(const TreeLaunch& a, int row) {
+  return a.group_m ? static_cast<int>(__umulhi(static_cast<uint32_t>(row), a.group_m)) : row;
 }
 
 // Whether row's drafted token `t` of sequence q sees drafted tokens j0 .. j0 + 15 (bits; j0 a multiple of 16).
@@ -121,8 +196,14 @@ __device__ __forceinline__ uint32_t tree_sees16(const TreeLaunch& a, const TreeS
 
 // tree.cu: query rows in tiles of 16; CTAs that run at once on an SM.
 constexpr int kTreeRows16PerSm = 3;
+#ifdef __CUDACC__
+using TreeRows16 = TreeGeometry<16, kTreePage, 1, 8>;
+using TreeTc = TreeGeometry<128, 128, 2, 4>;
+#endif
 cudaError_t launch_tree_rows16(const TreeLaunch& a, const kvprm_cache& c, int ctas, cudaStream_t stream);
 // tree_tc.cu: in pairs of tiles of 128, on the tensor cores; one CTA on an SM.  The cache has a page at least.
 cudaError_t launch_tree_tc(const TreeLaunch& a, const kvprm_cache& c, int ctas, cudaStream_t stream);
+// tree_join.cu: joins the partial results that either left.
+cudaError_t launch_tree_join(const TreeLaunch& a, const kvprm_cache& c, bool tc, cudaStream_t stream);
 
 }  // namespace kvprm

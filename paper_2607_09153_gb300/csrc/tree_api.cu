@@ -11,14 +11,14 @@ using namespace kvprm;
 
 namespace {
 
-constexpr int64_t kTicketBytes = 4 * kTreeTickets;
+constexpr int64_t kLineBytes = (4 * (kTreeSeqs + 2) + 255) / 256 * 256;
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct TreePlan {
-  bool tc = false;
-  int ctas = 0, rows = 16;   // rows: of a partial result
+  bool tc = false, whole = false;
+  int ctas = 0, rows = 16, seqs = 0;   // rows: of a partial result; seqs: sequences of a launch
 };
 
 int check(const kvprm_cache* c, const kvprm_tree* t, const char* who) {
@@ -44,24 +44,30 @@ int sm_count(int* sms) {
   return KVPRM_OK;
 }
 
-// More than 16 rows of a kv head go to the tensor cores.  CTAs: as many as run at once, but no more than one per pair
-// while pairs are short (a pair in one CTA needs no joining), and a few blocks for each where they are long.
-TreePlan plan(const kvprm_cache& c, const kvprm_tree& t, int sms) {
+// More than 16 rows of a kv head go to the tensor cores.  CTAs: as many as run at once.  Pairs of so few blocks that
+// cutting one would cost more than it gives, or one per CTA where all are so short, stay whole: no join follows.
+int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   TreePlan p;
   const int64_t rows = int64_t{t.max_drafts} * (t.n_q_heads / c.n_kv_heads);
   p.tc = rows > 16 && c.n_pages > 0;
   p.rows = p.tc ? 256 : 16;
-  const int64_t block = p.tc ? 128 : kTreePage, least = p.tc ? 4 : 16;
+  const int64_t block = p.tc ? 128 : kTreePage, tiles = ceil_div(rows, p.tc ? 128 : 16), lead = 8;
+  // the line of a sequence of any length is shorter than this; a launch's stays within 31 bits
+  const int64_t line = (ceil_div(int64_t{kTreePage} * t.max_blocks, block) + ceil_div(t.max_drafts, block) + lead) * tiles * c.n_kv_heads;
+  if (line > 0x7FFFFFFF) return operator_fail(KVPRM_ECAPACITY, "kvprm_tree: block tables of %d pages", t.max_blocks);
+  p.seqs = static_cast<int>(std::min<int64_t>({t.n_seqs, kTreeSeqs, 0x7FFFFFFF / line}));
   const int64_t len = std::min<int64_t>(t.max_len, int64_t{kTreePage} * t.max_blocks);
-  const int64_t pairs = std::min<int64_t>(t.n_seqs, kTreeSeqs) * c.n_kv_heads * ceil_div(rows, p.rows);
+  const int64_t pairs = int64_t{p.seqs} * c.n_kv_heads * ceil_div(rows, p.rows);
   const int64_t blocks = ceil_div(len, block) + ceil_div(t.max_drafts, block);
-  const int64_t most = std::min<int64_t>(int64_t{sms} * (p.tc ? 1 : kTreeRows16PerSm), kTreeTickets - 1);
-  p.ctas = static_cast<int>(std::max<int64_t>(1, std::min(most, std::max(pairs, pairs * blocks / least))));
-  return p;
+  const int64_t most = int64_t{sms} * (p.tc ? 1 : kTreeRows16PerSm);
+  p.whole = blocks <= (p.tc ? 3 : 16);
+  p.ctas = static_cast<int>(std::max<int64_t>(1, std::min(most, p.whole ? pairs : pairs * blocks / (p.tc ? 2 : 8))));
+  *out = p;
+  return KVPRM_OK;
 }
 
 int64_t workspace_bytes(const kvprm_cache& c, const TreePlan& p) {
-  return kTicketBytes + int64_t{2} * p.ctas * p.rows * (4 * c.head_dim + 8);
+  return kLineBytes + (p.whole ? 0 : int64_t{2} * p.ctas * p.rows * (4 * c.head_dim + 8));
 }
 
 }  // namespace
@@ -74,7 +80,9 @@ int kvprm_tree_workspace(const kvprm_cache* cache, const kvprm_tree* t, int64_t*
   if (const int rc = check(cache, t, who)) return rc;
   int sms = 0;
   if (const int rc = sm_count(&sms)) return rc;
-  *bytes = workspace_bytes(*cache, plan(*cache, *t, sms));
+  TreePlan p;
+  if (const int rc = plan(*cache, *t, sms, &p)) return rc;
+  *bytes = workspace_bytes(*cache, p);
   return KVPRM_OK;
 }
 
@@ -90,7 +98,8 @@ int kvprm_tree_attention(const kvprm_cache* cache, const kvprm_tree* t, void* wo
     return operator_fail(KVPRM_EINVAL, "%s: rows of q, k, v and out have to be 16-byte aligned", who);
   int sms = 0;
   if (const int rc = sm_count(&sms)) return rc;
-  const TreePlan p = plan(*cache, *t, sms);
+  TreePlan p;
+  if (const int rc = plan(*cache, *t, sms, &p)) return rc;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0)
     return operator_fail(KVPRM_EINVAL, "%s: workspace is NULL or not 256-byte aligned", who);
   if (workspace_size < workspace_bytes(*cache, p))
@@ -103,14 +112,17 @@ int kvprm_tree_attention(const kvprm_cache* cache, const kvprm_tree* t, void* wo
   a.n_pages = cache->n_pages;
   a.n_kv = cache->n_kv_heads;
   a.group = t->n_q_heads / cache->n_kv_heads;
+  a.group_m = a.group > 1 ? static_cast<uint32_t>(((uint64_t{1} << 32) + a.group - 1) / a.group) : 0u;
   a.scale_log2 = t->scale * 1.4426950408889634f;
-  a.tickets = static_cast<int32_t*>(workspace);
-  a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kTicketBytes);
+  a.whole = p.whole;
+  a.line = static_cast<int32_t*>(workspace);
+  a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kLineBytes);
   a.part_ml = reinterpret_cast<float2*>(a.part_o + int64_t{2} * p.ctas * p.rows * cache->head_dim);
-  for (a.seq0 = 0; a.seq0 < t->n_seqs; a.seq0 += kTreeSeqs) {
-    a.n_seqs = std::min(kTreeSeqs, t->n_seqs - a.seq0);
-    const cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const cudaError_t e = p.tc ? launch_tree_tc(a, *cache, p.ctas, st) : launch_tree_rows16(a, *cache, p.ctas, st);
+  const cudaStream_t st = static_cast<cudaStream_t>(stream);
+  for (a.seq0 = 0; a.seq0 < t->n_seqs; a.seq0 += p.seqs) {
+    a.n_seqs = std::min(p.seqs, t->n_seqs - a.seq0);
+    cudaError_t e = p.tc ? launch_tree_tc(a, *cache, p.ctas, st) : launch_tree_rows16(a, *cache, p.ctas, st);
+    if (e == cudaSuccess && !p.whole) e = launch_tree_join(a, *cache, p.tc, st);
     if (e != cudaSuccess) return operator_fail(KVPRM_ECUDA, "%s: %s", who, cudaGetErrorString(e));
   }
   return KVPRM_OK;

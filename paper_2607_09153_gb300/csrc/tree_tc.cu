@@ -19,6 +19,8 @@
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
+#include <type_traits>
+
 #include "kernels.h"
 #include "ptx.cuh"
 #include "rope.h"
@@ -29,7 +31,7 @@ namespace kvprm {
 namespace {
 
 constexpr int kThreads = 448;
-constexpr int kRows = 128, kChunk = 128, kPages = kChunk / kTreePage;
+constexpr int kRows = TreeTc::ROWS, kChunk = TreeTc::BLOCK, kPages = kChunk / kTreePage;
 constexpr int kProducers = 128;
 constexpr float kMargin = 8.f;   // log2 units that scores may pass a running maximum by
 constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;   // S buffers at 0 and 128, accumulators at 256 and 384
@@ -51,8 +53,8 @@ struct Smem {
 };
 
 struct Static {   // in static shared memory
-  int64_t off[kTreeSeqs + 1];
-  int64_t sum[kThreads / 32];
+  int32_t off[kTreeSeqs + 1];
+  int32_t sum[kThreads / 32];
   uint64_t slot_full[8], slot_empty[8], raw_full[8], raw_empty[8];
   uint64_t draft_go[8];   // bf16 cache: a free slot that is the producers' to fill
   uint64_t q_full, q_empty, s_full[2], p_full[2], part_done, o_free;
@@ -60,36 +62,25 @@ struct Static {   // in static shared memory
   int bad[kFlagSets];                   // of a part: a page outside the cache, a bad draft (1, 2)
   int raw_bad[8];                       // a page outside the cache, of a raw slot
   uint32_t tmem;
-  int last;
+  int err;   // a wait gave up (after which the CTA's other waits are short, and its rows NaN)
 };
 
-// One CTA's part of a pair.
-struct Part {
-  TreeSeq q;
-  int64_t pair0;          // the pair's first place on the line
-  int s, g, tp, tiles;    // tiles: 1 or 2, and a chunk's weight on the line
-  int c0, c1;             // chunks
-};
-
-__device__ __forceinline__ bool next_part(const TreeLaunch& a, const int64_t* off, int64_t& u, int64_t u_end, int& s,
-                                          Part& p) {
-  while (u < u_end) {
-    while (u >= off[s + 1]) ++s;
-    p.q = tree_seq<kRows, kChunk>(a, s);
-    p.s = s;
-    const int64_t head_len = static_cast<int64_t>(p.q.blocks) * p.q.tiles, local = u - off[s];
-    p.g = static_cast<int>(local / head_len);
-    const int64_t in_head = local - p.g * head_len;
-    p.tp = static_cast<int>(in_head / (2 * p.q.blocks));
-    p.pair0 = off[s] + p.g * head_len + static_cast<int64_t>(p.tp) * 2 * p.q.blocks;
-    p.tiles = min(2, p.q.tiles - 2 * p.tp);
-    p.c0 = static_cast<int>((u - p.pair0 + p.tiles - 1) / p.tiles);
-    p.c1 = static_cast<int>(min(static_cast<int64_t>(p.q.blocks), (u_end - p.pair0 + p.tiles - 1) / p.tiles));
-    u = p.c1 == p.q.blocks ? p.pair0 + static_cast<int64_t>(p.q.blocks) * p.tiles : u_end;
-    if (p.c0 < p.c1) return true;
+// The items of a part: its chunks' keys and values, in the order in which the matrix products take them.  Keys and
+// values in turn where two tiles share a chunk; keys one chunk further ahead where the chunks alternate between the
+// groups (K0 K1 V0 K2 V1 ..): the S that follows an O is then two chunks on, and no slot holds values that wait for
+// their softmax while keys are needed.
+struct Items {
+  int tiles, n;   // n: two per chunk
+  __device__ __forceinline__ explicit Items(const TreePart& p) : tiles(p.tiles), n(2 * (p.c1 - p.c0)) {}
+  __device__ __forceinline__ int keys(int c) const { return tiles == 2 ? 2 * c : c == 0 ? 0 : 2 * c - 1; }
+  __device__ __forceinline__ int values(int c) const { return tiles == 2 || 2 * c == n - 2 ? 2 * c + 1 : 2 * c + 2; }
+  // the chunk of an item, and whether it is its values
+  __device__ __forceinline__ int chunk(int item, int* kv) const {
+    const bool last = item == n - 1;
+    *kv = tiles == 2 ? item & 1 : last || (item > 0 && (item & 1) == 0);
+    return tiles == 2 || last ? item >> 1 : *kv ? (item >> 1) - 1 : (item + 1) >> 1;
   }
-  return false;
-}
+};
 
 __device__ __forceinline__ uint32_t swizzled(int row, int piece) {   // of a 16-byte piece of a tile's row
   return static_cast<uint32_t>(piece >> 3) * (kRows * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
@@ -100,22 +91,54 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
+  float2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;"
+      : "=l"(reinterpret_cast<uint64_t&>(r))
+      : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
+  return r;
+}
+__device__ __forceinline__ float2 add2(float2 a, float2 b) {
+  float2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(reinterpret_cast<uint64_t&>(r)) : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)));
+  return r;
+}
 __device__ __forceinline__ bool not_finite2(uint32_t w) {
   return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
 }
 
-// Four e4m3 codes as bf16 times a row's power of two.  A code's exponent and mantissa at bf16's place are
-// 2^-120 of its value; f1 * f2 is 2^120 times the row's power (f2 = 1 unless that passes bf16's range).
-__device__ __forceinline__ uint2 bf16_of4(uint32_t w, uint32_t f1, uint32_t f2, bool two) {
-  uint32_t e = ((w << 4) & 0x07F007F0u) | ((w << 8) & 0x80008000u);   // bytes 0, 2
-  uint32_t o = ((w >> 4) & 0x07F007F0u) | (w & 0x80008000u);          // bytes 1, 3
-  e = mul_bf16x2(e, f1);
-  o = mul_bf16x2(o, f1);
-  if (two) {
-    e = mul_bf16x2(e, f2);
-    o = mul_bf16x2(o, f2);
+// Sixteen e4m3 codes as bf16 times a row's power of two.  A code's exponent and mantissa at bf16's place are 2^-120 of its
+// value; f1 (times f2, where the two do not fit one factor) is 2^120 times the row's power.  The even and the odd codes of
+// a word each become a pair, so that the head's dimensions come in the order 0 2 1 3, 4 6 5 7 ..: Q and the drafted
+// tokens are laid out alike (paired), and the outputs are put back in order.
+template <bool TWO>
+__device__ __forceinline__ void bf16_of16(const uint4& c, uint32_t f1, uint32_t f2, uint4* lo, uint4* hi) {
+  auto pair = [&](uint32_t w, uint32_t* e, uint32_t* o) {
+    *e = mul_bf16x2(((w << 4) & 0x07F007F0u) | ((w << 8) & 0x80008000u), f1);
+    *o = mul_bf16x2(((w >> 4) & 0x07F007F0u) | (w & 0x80008000u), f1);
+    if (TWO) {
+      *e = mul_bf16x2(*e, f2);
+      *o = mul_bf16x2(*o, f2);
+    }
+  };
+  pair(c.x, &lo->x, &lo->y);
+  pair(c.y, &lo->z, &lo->w);
+  pair(c.z, &hi->x, &hi->y);
+  pair(c.w, &hi->z, &hi->w);
+}
+__device__ __forceinline__ uint4 paired(const uint4& v) {
+  return make_uint4(__byte_perm(v.x, v.y, 0x5410), __byte_perm(v.x, v.y, 0x7632), __byte_perm(v.z, v.w, 0x5410),
+                    __byte_perm(v.z, v.w, 0x7632));
+}
+template <int N>
+__device__ __forceinline__ void in_order(float (&o)[N]) {
+#pragma unroll
+  for (int i = 1; i < N; i += 4) {
+    const float x = o[i];
+    o[i] = o[i + 1];
+    o[i + 1] = x;
   }
-  return make_uint2(__byte_perm(e, o, 0x5410), __byte_perm(e, o, 0x7632));
 }
 
 template <int HD, bool E4M3>
@@ -125,7 +148,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   extern __shared__ uint8_t smem_raw[];
   __shared__ Static st;
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t{1023});
-  int* err = a.tickets + kTreeTickets - 1;
+  int* err = &st.err;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < 8; ++i) {
@@ -141,6 +164,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       mbar_init(&st.s_full[i], 1);
       mbar_init(&st.p_full[i], 4);
     }
+    st.err = 0;
     mbar_init(&st.part_done, 1);
     mbar_init(&st.o_free, 8);
     fence_mbar_init();
@@ -153,88 +177,102 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     tmem_relinquish();
   }
   tc_fence_before();
-  tree_line<kRows, kChunk, kThreads>(a, st.off, st.sum);   // barriers inside
+  grid_dep_launch();
+  tree_line<TreeTc, kThreads>(a, st.off, st.sum);   // barriers inside
   tc_fence_after();
   const uint32_t tmem = st.tmem;
-  const int64_t total = st.off[a.n_seqs];
-  // a share of two or more holds at least one chunk's start of any pair that it lies in
-  const int P = static_cast<int>(min(static_cast<int64_t>(gridDim.x), max(total / 2, int64_t{1})));
+  const int32_t total = st.off[a.n_seqs];
+  const TreeShares shares(total, gridDim.x, TreeTc::TILES);
+  tree_leave_line(a, st.off, shares.ctas);
   const int me = blockIdx.x;
-  const bool idle = me >= P || total == 0;
-  int64_t u = idle ? 0 : total * me / P;
-  const int64_t u_end = idle ? 0 : total * (me + 1) / P;
+  const bool idle = me >= shares.ctas || total == 0;
+  int32_t u = idle ? 0 : shares.begin(me);
+  const int32_t u_end = idle ? 0 : shares.begin(me + 1);
   int s = idle ? 0 : tree_find(st.off, a.n_seqs, u);
-  Part p;
+  TreePart p;
+  auto next_part = [&]() { return tree_next<TreeTc>(a, st.off, u, u_end, s, p); };
 
   if (warp == 12) {
     // ------------------------------------------------ TMA
     const uint64_t pol = policy_evict_normal();
-    uint32_t n = 0;   // items: keys of chunk 0, values of chunk 0, keys of chunk 1 ...
-    uint32_t loaded = 0;
+    uint32_t n = 0, loaded = 0;   // items of earlier parts; raw slots filled
     bool ok = true;
     auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, err)); };
-    for (int part = 0; ok && next_part(a, st.off, u, u_end, s, p); ++part) {
+    for (int part = 0; ok && next_part(); ++part) {
       const int32_t* table = a.t.block_table + static_cast<int64_t>(a.seq0 + p.s) * a.t.max_blocks;
       const int pages = (p.q.len + kTreePage - 1) / kTreePage;
-      for (int c = p.c0; c < p.c1 && ok; ++c, n += 2) {
+      const Items items(p);
+      // page ids of four chunks, a page per lane, and of the next four (loaded long before they are needed); -1: no page
+      // there, -2: not a page of the cache
+      auto ids_of = [&](int four) {
+        const int at = four * 32 + lane;
+        if (at >= pages) return -1;
+        const int32_t page = __ldg(table + at);
+        return page < 0 || page >= a.n_pages ? -2 : page;
+      };
+      int four = p.c0 >> 2;
+      int32_t ids = ids_of(four), ids_next = ids_of(four + 1);
+      for (int item = 0; item < items.n && ok; ++item) {
+        int kv;
+        const int c = p.c0 + items.chunk(item, &kv);
         const bool cached = c < p.q.cached_blocks;
         if (E4M3 && !cached) continue;
-        // lane i < 8: the chunk's i-th page (-1: none there, -2: not a page of the cache)
-        const int at = c * kPages + lane;
-        int32_t page = -1;
-        if (cached && lane < kPages && at < pages) {
-          page = __ldg(table + at);
-          if (page < 0 || page >= a.n_pages) page = -2;
+        if (kv && (c >> 2) > four) {   // (keys are at most a chunk ahead of values)
+          ++four;
+          ids = ids_next;
+          ids_next = ids_of(four + 1);
         }
-        const bool bad = __any_sync(0xffffffffu, page == -2);
+        int32_t id[kPages];
+        bool bad = false;
 #pragma unroll
-        for (int kv = 0; kv < 2; ++kv) {
-          if constexpr (E4M3) {
-            const uint32_t r = loaded % SM::kRaw;
-            if (loaded >= SM::kRaw) ok = ok && wait_all(&st.raw_empty[r], (loaded / SM::kRaw - 1) & 1u);
-            if (!ok) break;
-            constexpr uint32_t kPageBytes = kTreePage * HD;
-            const uint32_t good = __popc(__ballot_sync(0xffffffffu, page >= 0));
-            if (lane == 0) {
-              st.raw_bad[r] = bad;
-              mbar_arrive_expect_tx(&st.raw_full[r], good * (kPageBytes + kTreePage));
-            }
-            __syncwarp();
-            if (page >= 0) {
-              uint8_t* dst = base + SM::kRaw0 + r * SM::kRawBytes;
-              const int64_t row = (static_cast<int64_t>(page) * 2 + kv) * a.n_kv + p.g;
-              bulk_load(dst + lane * kPageBytes, a.pages + row * kPageBytes, kPageBytes, &st.raw_full[r]);
-              bulk_load(dst + SM::kRawCodes + lane * kTreePage, a.exponents + row * kTreePage, kTreePage, &st.raw_full[r]);
-            }
-            __syncwarp();
-            ++loaded;
-          } else {
-            // This warp waits for every use of a slot, also where the producers fill it: a wait by parity sees only
-            // the phase before the present one, so none may be left out.
-            const uint32_t i = n + kv, slot = i % SM::kSlots;
-            if (i >= SM::kSlots) ok = ok && wait_all(&st.slot_empty[slot], (i / SM::kSlots - 1) & 1u);
-            if (!ok) break;
-            if (!cached) {
-              if (lane == 0) mbar_arrive(&st.draft_go[slot]);
-              continue;
-            }
-            if (lane == 0) {
-              // (a part's marks are set once a slot of it is free: no earlier part then holds the same set)
-              if (bad) atomicOr(&st.bad[part % kFlagSets], 1);
-              mbar_arrive_expect_tx(&st.slot_full[slot], SM::kTile);
-            }
-            __syncwarp();
-            // lane (sub, page): a 2 KB box of 16 rows of 64 columns; places without a page read one that does
-            // not exist and arrive as zeros
-            const int32_t pg = __shfl_sync(0xffffffffu, page, lane % kPages);
-            const int sub = lane / kPages;
-            if (sub < HD / 64)
-              tma_load_5d(base + SM::kSlot0 + slot * SM::kTile + sub * (kRows * 128) + (lane % kPages) * 2048, &map,
-                          &st.slot_full[slot], 0, 0, sub, p.g, pg >= 0 ? 2 * pg + kv : -1, pol);
-            __syncwarp();
+        for (int i = 0; i < kPages; ++i) {
+          id[i] = __shfl_sync(0xffffffffu, (c >> 2) > four ? ids_next : ids, (c & 3) * kPages + i);
+          bad = bad || id[i] == -2;
+        }
+        if constexpr (E4M3) {
+          const uint32_t r = loaded % SM::kRaw;
+          if (loaded >= SM::kRaw) ok = wait_all(&st.raw_empty[r], (loaded / SM::kRaw - 1) & 1u);
+          if (!ok) continue;
+          ++loaded;
+          if (lane != 0) continue;
+          constexpr uint32_t kPageBytes = kTreePage * HD;
+          uint32_t good = 0;
+#pragma unroll
+          for (int i = 0; i < kPages; ++i) good += id[i] >= 0 ? 1u : 0u;
+          st.raw_bad[r] = bad;
+          mbar_arrive_expect_tx(&st.raw_full[r], good * (kPageBytes + kTreePage));
+          uint8_t* dst = base + SM::kRaw0 + r * SM::kRawBytes;
+#pragma unroll
+          for (int i = 0; i < kPages; ++i) {
+            if (id[i] < 0) continue;
+            const int64_t row = (static_cast<int64_t>(id[i]) * 2 + kv) * a.n_kv + p.g;
+            bulk_load(dst + i * kPageBytes, a.pages + row * kPageBytes, kPageBytes, &st.raw_full[r]);
+            bulk_load(dst + SM::kRawCodes + i * kTreePage, a.exponents + row * kTreePage, kTreePage, &st.raw_full[r]);
           }
+        } else {
+          // This warp waits for every use of a slot, also where the producers fill it: a wait by parity sees only
+          // the phase before the present one, so none may be left out.
+          const uint32_t i = n + item, slot = i % SM::kSlots;
+          if (i >= SM::kSlots) ok = wait_all(&st.slot_empty[slot], (i / SM::kSlots - 1) & 1u);
+          if (!ok || lane != 0) continue;
+          if (!cached) {
+            mbar_arrive(&st.draft_go[slot]);
+            continue;
+          }
+          // (a part's marks are set once a slot of it is free: no earlier part then holds the same set)
+          if (bad) atomicOr(&st.bad[part % kFlagSets], 1);
+          mbar_arrive_expect_tx(&st.slot_full[slot], SM::kTile);
+          // a box is 16 rows of 64 columns; a place without a page reads one that does not exist and arrives as zeros
+          uint8_t* dst = base + SM::kSlot0 + slot * SM::kTile;
+#pragma unroll
+          for (int k = 0; k < kPages; ++k)
+#pragma unroll
+            for (int sub = 0; sub < HD / 64; ++sub)
+              tma_load_5d(dst + sub * (kRows * 128) + k * 2048, &map, &st.slot_full[slot], 0, 0, sub, p.g,
+                          id[k] >= 0 ? 2 * id[k] + kv : -1, pol);
         }
       }
+      n += items.n;
     }
     // Nothing of this warp's is in flight when the CTA ends: the matrix products (or the producers) waited for every
     // load.  After a wait that gave up, a millisecond is far beyond a load's time.
@@ -248,13 +286,14 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, err)); };
     uint32_t n = 0, uses[2] = {0, 0};
     bool ok = true;
-    for (int part = 0; next_part(a, st.off, u, u_end, s, p); ++part) {
-      const int chunks = p.c1 - p.c0, units = chunks * p.tiles;
+    for (int part = 0; next_part(); ++part) {
+      const Items items(p);
+      const int units = (p.c1 - p.c0) * p.tiles;
       if (!ok) continue;
       ok = wait_all(&st.q_full, part & 1u);
       auto issue_s = [&](int j) {
         const int c = p.tiles == 2 ? j >> 1 : j, g = j & 1;
-        const uint32_t i = n + 2 * c, slot = i % SM::kSlots;
+        const uint32_t i = n + items.keys(c), slot = i % SM::kSlots;
         ok = ok && wait_all(&st.slot_full[slot], (i / SM::kSlots) & 1u);
         if (!ok) return;
         tc_fence_after();
@@ -271,7 +310,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       };
       auto issue_o = [&](int j) {
         const int c = p.tiles == 2 ? j >> 1 : j, g = j & 1;
-        const uint32_t i = n + 2 * c + 1, slot = i % SM::kSlots;
+        const uint32_t i = n + items.values(c), slot = i % SM::kSlots;
         ok = ok && wait_all(&st.slot_full[slot], (i / SM::kSlots) & 1u);
         ok = ok && wait_all(&st.p_full[g], uses[g]++ & 1u);
         if (!ok) return;
@@ -304,7 +343,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         if (j + 2 < units && ok) issue_s(j + 2);
       }
       if (ok) umma_commit_w(&st.part_done);
-      n += 2 * chunks;
+      n += items.n;
     }
   } else if (warp >= 8 && warp < 12) {
     // ------------------------------------------------ producers
@@ -317,97 +356,114 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       if (t == 0) mbar_arrive(bar);
     };
     const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale turns Q's signs instead
-    for (int part = 0; next_part(a, st.off, u, u_end, s, p); ++part) {
+    for (int part = 0; next_part(); ++part) {
       const int rows = p.q.drafts * a.group;
       if (part > 0) ok = ok && mbar_wait(&st.q_empty, (part - 1) & 1u, err);
-      constexpr int kPieces = HD / 8;
+      constexpr int kPieces = HD / 8, kStep = kProducers / kPieces;   // a thread's rows are kStep apart
       for (int tile = 0; tile < p.tiles; ++tile) {
         uint8_t* dst = base + SM::kQ + tile * SM::kTile;
-#pragma unroll 4
-        for (int x = t; x < kRows * kPieces; x += kProducers) {
-          const int r = x / kPieces, piece = x % kPieces, row = (2 * p.tp + tile) * kRows + r;
-          uint4 v = make_uint4(0u, 0u, 0u, 0u);
-          if (row < rows) {
-            const int tok = row / a.group, h = p.g * a.group + row - tok * a.group;
-            v = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.t.q) +
-                                                     (p.q.start + static_cast<int64_t>(tok)) * a.t.q_token +
-                                                     h * a.t.q_head) + piece);
-            v = make_uint4(v.x ^ flip, v.y ^ flip, v.z ^ flip, v.w ^ flip);
+        const int piece = t % kPieces, first = t / kPieces, left = rows - (2 * p.tp + tile) * kRows;
+#pragma unroll
+        for (int half = 0; half < kPieces; half += kPieces / 2) {   // several loads in flight for each thread
+          uint4 v[kPieces / 2];
+#pragma unroll
+          for (int i = 0; i < kPieces / 2; ++i) {
+            const int r = first + (half + i) * kStep;
+            v[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (r < left) {
+              const int row = rows - left + r, tok = tree_token(a, row), h = p.g * a.group + row - tok * a.group;
+              v[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.t.q) +
+                                                          (p.q.start + static_cast<int64_t>(tok)) * a.t.q_token +
+                                                          h * a.t.q_head) + piece);
+            }
           }
-          *reinterpret_cast<uint4*>(dst + swizzled(r, piece)) = v;
+#pragma unroll
+          for (int i = 0; i < kPieces / 2; ++i)
+          {
+            v[i] = make_uint4(v[i].x ^ flip, v[i].y ^ flip, v[i].z ^ flip, v[i].w ^ flip);
+            *reinterpret_cast<uint4*>(dst + swizzled(first + (half + i) * kStep, piece)) = E4M3 ? paired(v[i]) : v[i];
+          }
         }
       }
       filled(&st.q_full);
-      for (int c = p.c0; c < p.c1; ++c, n += 2) {
+      const Items items(p);
+      for (int item = 0; item < items.n; ++item) {
+        int kv;
+        const int c = p.c0 + items.chunk(item, &kv);
         const bool cached = c < p.q.cached_blocks;
         if (cached && !E4M3) continue;
-#pragma unroll 1
-        for (int kv = 0; kv < 2; ++kv) {
-          const uint32_t i = n + kv, slot = i % SM::kSlots;
-          if constexpr (E4M3) {   // every slot is filled here
-            if (i >= SM::kSlots) ok = ok && mbar_wait(&st.slot_empty[slot], (i / SM::kSlots - 1) & 1u, err);
-          } else {
-            ok = ok && mbar_wait(&st.draft_go[slot], (go >> slot) & 1u, err);
-            go ^= 1u << slot;
-          }
-          uint8_t* dst = base + SM::kSlot0 + slot * SM::kTile;
+        const uint32_t i = n + item, slot = i % SM::kSlots;
+        uint8_t* dst = base + SM::kSlot0 + slot * SM::kTile;
+        if constexpr (E4M3) {   // every slot is filled here
+          if (i >= SM::kSlots) ok = ok && mbar_wait(&st.slot_empty[slot], (i / SM::kSlots - 1) & 1u, err);
           if (cached) {
             const uint32_t r = raw % SM::kRaw;
             ok = ok && mbar_wait(&st.raw_full[r], (raw / SM::kRaw) & 1u, err);
             if (t == 0 && st.raw_bad[r]) atomicOr(&st.bad[part % kFlagSets], 1);
             const uint8_t* src = base + SM::kRaw0 + r * SM::kRawBytes;
-            const int have = min(kChunk, p.q.len - c * kChunk);
-            constexpr int kParts = HD / 16;   // 16 codes each
-#pragma unroll 4
-            for (int x = t; x < kChunk * kParts; x += kProducers) {
-              const int row = x / kParts, piece = x % kParts;
-              uint4 lo = make_uint4(0u, 0u, 0u, 0u), hi = lo;
-              if (row < have) {
-                const uint4 w = *reinterpret_cast<const uint4*>(src + row * HD + piece * 16);
-                const uint32_t e = src[SM::kRawCodes + row];
-                // 2^(e - 127 + 120) as bf16; beyond its range (or NaN, 255) in two factors
-                const bool two = e > 134u;
-                const uint32_t f1 = (two ? 254u : e + 120u) << 7, f2 = e == 255u ? 0x7FC0u : (e - 7u) << 7;
-                const uint32_t p1 = f1 * 0x10001u, p2 = f2 * 0x10001u;
-                const uint2 a0 = bf16_of4(w.x, p1, p2, two), a1 = bf16_of4(w.y, p1, p2, two);
-                const uint2 a2 = bf16_of4(w.z, p1, p2, two), a3 = bf16_of4(w.w, p1, p2, two);
-                lo = make_uint4(a0.x, a0.y, a1.x, a1.y);
-                hi = make_uint4(a2.x, a2.y, a3.x, a3.y);
+            const int have = p.q.len - c * kChunk;
+            constexpr int kParts = HD / 16, kTeam = 32 / kParts;       // pieces of a row; rows of a warp's step
+            constexpr int kSteps = kChunk / (kTeam * kProducers / 32);
+            // the factors of the rows that this warp converts, a row per lane: 2^(e - 127 + 120) as bf16, beyond its range
+            // (or NaN, 255) in two; zero past the length, where the codes may be anything
+            const int mine = lane % kTeam + (t >> 5) * kTeam + lane / kTeam * (kTeam * kProducers / 32);
+            const uint32_t e = src[SM::kRawCodes + mine];
+            const bool two = e > 134u && mine < have;
+            uint32_t f = (two ? 254u : e + 120u) << 7 | (two ? (e == 255u ? 0x7FC0u : (e - 7u) << 7) : 0x3F80u) << 16;
+            if (mine >= have) f = 0x3F800000u;
+            const int row0 = t / kParts, piece = t % kParts;
+            auto convert = [&](auto twice) {
+#pragma unroll
+              for (int k = 0; k < kSteps; ++k) {
+                const int row = row0 + k * (kTeam * kProducers / 32);
+                const uint32_t fr = __shfl_sync(0xffffffffu, f, lane / kParts + kTeam * k);
+                uint4 lo, hi;
+                bf16_of16<decltype(twice)::value>(*reinterpret_cast<const uint4*>(src + row * HD + piece * 16),
+                                                  __byte_perm(fr, 0, 0x1010), __byte_perm(fr, 0, 0x3232), &lo, &hi);
+                *reinterpret_cast<uint4*>(dst + swizzled(row, 2 * piece)) = lo;
+                *reinterpret_cast<uint4*>(dst + swizzled(row, 2 * piece + 1)) = hi;
               }
-              *reinterpret_cast<uint4*>(dst + swizzled(row, 2 * piece)) = lo;
-              *reinterpret_cast<uint4*>(dst + swizzled(row, 2 * piece + 1)) = hi;
-            }
+            };
+            if (__any_sync(0xffffffffu, two))
+              convert(std::true_type());
+            else
+              convert(std::false_type());
             ++raw;
             filled(&st.slot_full[slot]);
             if (t == 0) mbar_arrive(&st.raw_empty[r]);
-          } else {
-            const int j0 = (c - p.q.cached_blocks) * kChunk, have = p.q.drafts - j0;
-            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(kv ? a.t.v : a.t.k) +
-                                       (p.q.start + static_cast<int64_t>(j0)) * (kv ? a.t.v_token : a.t.k_token) +
-                                       p.g * (kv ? a.t.v_head : a.t.k_head);
-            const int64_t step = kv ? a.t.v_token : a.t.k_token;
-#pragma unroll 4
-            for (int x = t; x < kChunk * kPieces; x += kProducers) {   // a row's pieces: neighbouring lanes of a warp
-              const int row = x / kPieces, piece = x % kPieces;
-              uint4 v = make_uint4(0u, 0u, 0u, 0u);
-              if (row < have) v = __ldg(reinterpret_cast<const uint4*>(src + row * step) + piece);
-              if (kv) {   // a weight of zero must leave no trace of a value that is not finite: its readers are marked
-                const bool off = not_finite2(v.x) || not_finite2(v.y) || not_finite2(v.z) || not_finite2(v.w);
-                const uint32_t who = __ballot_sync(0xffffffffu, off);
-                if ((who >> (lane / kPieces * kPieces)) & ((1u << kPieces) - 1u)) {
-                  v = make_uint4(0u, 0u, 0u, 0u);
-                  if (piece == 0) {
-                    atomicOr(&st.bad_drafts[part % kFlagSets][(j0 + row) >> 5], 1u << ((j0 + row) & 31));
-                    atomicOr(&st.bad[part % kFlagSets], 2);
-                  }
-                }
-              }
-              *reinterpret_cast<uint4*>(dst + swizzled(row, piece)) = v;
-            }
-            filled(&st.slot_full[slot]);
+            continue;
           }
+        } else {
+          ok = ok && mbar_wait(&st.draft_go[slot], (go >> slot) & 1u, err);
+          go ^= 1u << slot;
         }
+        // ---- drafted tokens: bf16 rows of their own tensors, whatever the cache holds
+        const int j0 = (c - p.q.cached_blocks) * kChunk, have = p.q.drafts - j0;
+        const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(kv ? a.t.v : a.t.k) +
+                                   (p.q.start + static_cast<int64_t>(j0)) * (kv ? a.t.v_token : a.t.k_token) +
+                                   p.g * (kv ? a.t.v_head : a.t.k_head);
+        const int64_t step = kv ? a.t.v_token : a.t.k_token;
+#pragma unroll 4
+        for (int x = t; x < kChunk * kPieces; x += kProducers) {   // a row's pieces: neighbouring lanes of a warp
+          const int row = x / kPieces, piece = x % kPieces;
+          uint4 v = make_uint4(0u, 0u, 0u, 0u);
+          if (row < have) v = __ldg(reinterpret_cast<const uint4*>(src + row * step) + piece);
+          if (kv) {   // a weight of zero must leave no trace of a value that is not finite: its readers are marked
+            const bool off = not_finite2(v.x) || not_finite2(v.y) || not_finite2(v.z) || not_finite2(v.w);
+            const uint32_t who = __ballot_sync(0xffffffffu, off);
+            if ((who >> (lane / kPieces * kPieces)) & ((1u << kPieces) - 1u)) {
+              v = make_uint4(0u, 0u, 0u, 0u);
+              if (piece == 0) {
+                atomicOr(&st.bad_drafts[part % kFlagSets][(j0 + row) >> 5], 1u << ((j0 + row) & 31));
+                atomicOr(&st.bad[part % kFlagSets], 2);
+              }
+            }
+          }
+          *reinterpret_cast<uint4*>(dst + swizzled(row, piece)) = E4M3 ? paired(v) : v;
+        }
+        filled(&st.slot_full[slot]);
       }
+      n += items.n;
     }
   } else if (warp < 8) {
     // ------------------------------------------------ softmax
@@ -418,11 +474,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     float2* s_ml = reinterpret_cast<float2*>(base + SM::kMl);
     uint32_t uses = 0;
     bool ok = true;
-    for (int part = 0; next_part(a, st.off, u, u_end, s, p); ++part) {
+    for (int part = 0; next_part(); ++part) {
       const bool both = p.tiles == 2;   // the groups have a tile each, else alternate chunks of one
       const int rows = p.q.drafts * a.group, row = (2 * p.tp + (both ? g : 0)) * kRows + r;
       const bool live = row < rows;
-      const int tok = live ? row / a.group : 0;
+      const int tok = live ? tree_token(a, row) : 0;
       float m = -INFINITY, l = 0.f;
       bool begun = false;
       for (int c = both ? p.c0 : p.c0 + g; c < p.c1; c += both ? 1 : 2) {
@@ -454,24 +510,39 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         ok = ok && __all_sync(0xffffffffu, mbar_wait(&st.s_full[g], uses & 1u, err));
         tc_fence_after();
         if (ok) {
+          // 32 columns at a time, the next ones on their way
+          float x[2][2][16];
+          auto fetch = [&](int h) {
+            tmem_ld16_nowait(ts + h * 32, x[h & 1][0]);
+            tmem_ld16_nowait(ts + h * 32 + 16, x[h & 1][1]);
+          };
+          auto arrived = [&](int h) {
+            tmem_wait_ld();
+            tmem_hold(x[h & 1][0]);
+            tmem_hold(x[h & 1][1]);
+          };
           float mx = -INFINITY;
+          fetch(0);
 #pragma unroll
           for (int h = 0; h < 4; ++h) {
-            float x0[16], x1[16];
-            tmem_ld16_nowait(ts + h * 32, x0);
-            tmem_ld16_nowait(ts + h * 32 + 16, x1);
-            tmem_wait_ld();
-            tmem_hold(x0);
-            tmem_hold(x1);
+            arrived(h);
+            if (h < 3) fetch(h + 1);
+            const float(&x0)[16] = x[h & 1][0], (&x1)[16] = x[h & 1][1];
             if (all) {
+              float y0 = x0[0], y1 = x1[0];
 #pragma unroll
-              for (int i = 0; i < 16; ++i) mx = fmaxf(mx, fmaxf(x0[i], x1[i]));
+              for (int i = 1; i < 16; ++i) {
+                y0 = fmaxf(y0, x0[i]);
+                y1 = fmaxf(y1, x1[i]);
+              }
+              mx = fmaxf(mx, fmaxf(y0, y1));
             } else {
 #pragma unroll
               for (int i = 0; i < 16; ++i)
                 mx = fmaxf(mx, fmaxf((sees[h] >> i) & 1u ? x0[i] : -INFINITY, (sees[h] >> (16 + i)) & 1u ? x1[i] : -INFINITY));
             }
           }
+          fetch(0);   // again, for the weights
           mx *= scale;
           if (scale == 0.f && mx != mx) mx = 0.f;   // -infinity times zero: nothing seen, or scores of zero
           const bool grow = mx > m + kMargin;
@@ -494,35 +565,29 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
           }
           begun = true;
           const float nm = m == -INFINITY ? 0.f : -m;
+          float2 sum = make_float2(0.f, 0.f);
+          const float2 scale2 = make_float2(scale, scale), nm2 = make_float2(nm, nm);
 #pragma unroll
           for (int h = 0; h < 4; ++h) {
-            float x0[16], x1[16], w[16];
-            tmem_ld16_nowait(ts + h * 32, x0);
-            tmem_ld16_nowait(ts + h * 32 + 16, x1);
-            tmem_wait_ld();
-            tmem_hold(x0);
-            tmem_hold(x1);
-            float l0 = 0.f, l1 = 0.f;
+            arrived(h);
+            if (h < 3) fetch(h + 1);
+            float w[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              x0[i] = ex2_ftz(fmaf(x0[i], scale, nm));
-              x1[i] = ex2_ftz(fmaf(x1[i], scale, nm));
-              if (!all) {
-                x0[i] = (sees[h] >> i) & 1u ? x0[i] : 0.f;
-                x1[i] = (sees[h] >> (16 + i)) & 1u ? x1[i] : 0.f;
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                float2 y = fma2(make_float2(x[h & 1][k][2 * i], x[h & 1][k][2 * i + 1]), scale2, nm2);
+                y = make_float2(ex2_ftz(y.x), ex2_ftz(y.y));
+                if (!all) {
+                  const uint32_t bits = sees[h] >> (16 * k + 2 * i);
+                  y = make_float2(bits & 1u ? y.x : 0.f, bits & 2u ? y.y : 0.f);
+                }
+                sum = add2(sum, y);
+                w[8 * k + i] = __uint_as_float(pack_bf16(y.x, y.y));
               }
-              l0 += x0[i];
-              l1 += x1[i];
-            }
-            l += l0 + l1;
-            // the weights as bf16 (the values' type) over columns of S that have been read
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              w[i] = __uint_as_float(pack_bf16(x0[2 * i], x0[2 * i + 1]));
-              w[8 + i] = __uint_as_float(pack_bf16(x1[2 * i], x1[2 * i + 1]));
-            }
-            tmem_st16(ts + h * 16, w);
+            tmem_st16(ts + h * 16, w);   // the weights as bf16 (the values' type), over columns of S that have been read
           }
+          l += sum.x + sum.y;
           tmem_wait_st();
           tc_fence_before();
         }
@@ -550,30 +615,21 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         if (threadIdx.x == 0) st.bad[set] = 0;
       }
       const float top = fmaxf(mine.x, other.x);
-      auto factor = [&](float2 ml, float best) { return ml.x == -INFINITY ? (ml.y == 0.f ? 0.f : 1.f) : ex2_ftz(ml.x - best); };
+      auto factor = [](float2 ml, float best) { return ml.x == -INFINITY ? 0.f : ex2_ftz(ml.x - best); };   // (NaN sums stay NaN)
       const float f0 = factor(mine, top), f1 = factor(other, top);
-      float sum = mine.y * f0 + other.y * f1;
+      const float sum = mine.y * f0 + other.y * f1;
       const bool two_streams = !both && p.c1 - p.c0 > 1;   // else the second accumulator holds nothing of this part
       const int d_begin = both ? 0 : g * (HD / 2), d_end = both ? HD : d_begin + HD / 2;
-      const bool whole = p.c0 == 0 && p.c1 == p.q.blocks;
+      const bool whole = p.whole();
+      // a partial result: [dim][row], so that a warp's rows are stored side by side
+      const int64_t slot = me == shares.owner(p.place(0)) ? 2 * me + 1 : 2 * me;
       const int slot_row = (both ? g : 0) * kRows + r;
+      float* part_o = a.part_o + slot * (HD * TreeTc::kSlotRows) + slot_row;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row that saw nothing: zeros
       __nv_bfloat16* dst = nullptr;
       if (live)
         dst = static_cast<__nv_bfloat16*>(a.t.out) + (p.q.start + static_cast<int64_t>(tok)) * a.t.out_token +
               (p.g * a.group + row - tok * a.group) * a.t.out_head;
-      auto put = [&](int d, const float (&o)[16], float inv) {
-        uint32_t w[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = pack_bf16(o[2 * i] * inv, o[2 * i + 1] * inv);
-        *reinterpret_cast<uint4*>(dst + d) = make_uint4(w[0], w[1], w[2], w[3]);
-        *reinterpret_cast<uint4*>(dst + d + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-      };
-      int i0 = me, i1 = me;
-      if (!whole) {
-        i0 = tree_owner(p.pair0, total, P);
-        i1 = tree_owner(p.pair0 + static_cast<int64_t>(p.q.blocks - 1) * p.tiles, total, P);
-      }
-      const int64_t mine_at = static_cast<int64_t>(me == i0 ? 2 * me + 1 : 2 * me) * (2 * kRows) + slot_row;
 #pragma unroll 1
       for (int d = d_begin; d < d_end; d += 16) {
         float o[16], o1[16];
@@ -587,60 +643,24 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[i] = ok ? o[i] * f0 + (two_streams ? o1[i] * f1 : 0.f) : 0.f;
+        if (E4M3) in_order(o);
+        if (!live) continue;
         if (whole) {
-          if (live) put(d, o, sum == 0.f ? 0.f : 1.f / sum);   // a row that saw nothing: zeros
-        } else if (live) {
-          float4* to_part = reinterpret_cast<float4*>(a.part_o + mine_at * HD + d);
+          uint32_t w[8];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) to_part[i] = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+          for (int i = 0; i < 8; ++i) w[i] = pack_bf16(o[2 * i] * inv, o[2 * i + 1] * inv);
+          *reinterpret_cast<uint4*>(dst + d) = make_uint4(w[0], w[1], w[2], w[3]);
+          *reinterpret_cast<uint4*>(dst + d + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) part_o[(d + i) * TreeTc::kSlotRows] = o[i];
         }
       }
+      if (!whole && live && d_begin == 0) a.part_ml[slot * TreeTc::kSlotRows + slot_row] = make_float2(top, sum);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive(&st.o_free);
-      if (!whole) {   // the pair goes on in other CTAs: the last of them to finish joins all parts, in order
-        if (live && d_begin == 0) a.part_ml[mine_at] = make_float2(top, sum);
-        __threadfence();
-        named_bar_sync(1, 256);
-        if (threadIdx.x == 0) {
-          st.last = atomicAdd(a.tickets + i0, 1) == i1 - i0;
-          if (st.last) a.tickets[i0] = 0;
-        }
-        named_bar_sync(1, 256);
-        if (st.last && live) {
-          __threadfence();
-          auto at = [&](int i) { return static_cast<int64_t>(i == i0 ? 2 * i + 1 : 2 * i) * (2 * kRows) + slot_row; };
-          float best = -INFINITY;
-          sum = 0.f;
-          for (int i = i0; i <= i1; ++i) best = fmaxf(best, __ldcg(a.part_ml + at(i)).x);
-          for (int i = i0; i <= i1; ++i) {
-            const float2 ml = __ldcg(a.part_ml + at(i));
-            sum += ml.y * factor(ml, best);
-          }
-          const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll 1
-          for (int d = d_begin; d < d_end; d += 16) {
-            float o[16];
-#pragma unroll
-            for (int k = 0; k < 16; ++k) o[k] = 0.f;
-#pragma unroll 2
-            for (int i = i0; i <= i1; ++i) {
-              const float f = factor(__ldcg(a.part_ml + at(i)), best);
-              const float4* src = reinterpret_cast<const float4*>(a.part_o + at(i) * HD + d);
-#pragma unroll
-              for (int k = 0; k < 4; ++k) {
-                const float4 v = __ldcg(src + k);
-                o[4 * k] += v.x * f;
-                o[4 * k + 1] += v.y * f;
-                o[4 * k + 2] += v.z * f;
-                o[4 * k + 3] += v.w * f;
-              }
-            }
-            put(d, o, inv);
-          }
-        }
-      }
-      named_bar_sync(1, 256);   // the states (and st.last) are read before the next part's are written
+      named_bar_sync(1, 256);   // the states are read before the next part's are written
     }
   }
   __syncwarp();

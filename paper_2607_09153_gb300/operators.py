@@ -306,9 +306,9 @@ def tree_mask(parents, start):
 _workspaces: dict = {}
 
 
-def _zeros(T, need: int, device: int, stream):
+def _scratch(T, need: int, device: int, stream):
     with T.torch.cuda.stream(stream):   # (None: the current one)
-        return T.torch.zeros(need, dtype=T.torch.uint8, device=T.torch.device("cuda", device))
+        return T.torch.empty(need, dtype=T.torch.uint8, device=T.torch.device("cuda", device))
 
 
 def _workspace_bytes(c: bytes, t: bytes) -> int:
@@ -357,16 +357,16 @@ def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, ma
     if workspace is not None:
         rc = _call(T, dev, stream, go, c, t, workspace.data_ptr(), workspace.numel())
     else:
-        # Scratch is kept per device and stream: calls on one stream follow one another, so they can share it, and each
-        # leaves its counters at zero.  A call that is being captured gets scratch of its own (the graph's, zeroed by
-        # it): the graph may be replayed on any stream.
+        # Scratch is kept per device and stream: calls on one stream follow one another, so they can share it.  A call
+        # that is being captured gets scratch of its own (the graph's), for the graph may be replayed on any stream.
         key = (dev, T.raw_stream(dev) if stream is None else stream.cuda_stream)
         w = _workspaces.get(key)
-        if T.capturing():
-            w = _zeros(T, _workspace_bytes(c, t), dev, stream)
+        capturing = T.capturing()
+        if capturing:
+            w = _scratch(T, _workspace_bytes(c, t), dev, stream)
         rc = KVPRM_ECAPACITY if w is None else _call(T, dev, stream, go, c, t, w.data_ptr(), w.numel())
-        if rc == KVPRM_ECAPACITY:
-            w = _workspaces[key] = _zeros(T, _workspace_bytes(c, t), dev, stream)
+        if rc == KVPRM_ECAPACITY and not capturing:
+            w = _workspaces[key] = _scratch(T, _workspace_bytes(c, t), dev, stream)
             rc = _call(T, dev, stream, go, c, t, w.data_ptr(), w.numel())
     if rc != KVPRM_OK:
         _check(rc)
