@@ -16,12 +16,12 @@
 // Tiles lie in shared memory as rows of 128 bytes under the 128-byte swizzle, [64-column part][128 rows]: a
 // K-major operand for the keys and an MN-major one for the values.
 #include <cuda.h>
+#include <cudaTypedefs.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
 #include <type_traits>
 
-#include "kernels.h"
 #include "ptx.cuh"
 #include "rope.h"
 #include "tree.h"
@@ -82,14 +82,67 @@ struct Items {
   }
 };
 
-__device__ __forceinline__ uint32_t swizzled(int row, int piece) {   // of a 16-byte piece of a tile's row
+// Tiles in shared memory: rows of 128 bytes (64 columns) under the 128-byte swizzle.  Q, and keys and values that the
+// producers write for an 8-bit cache: [64-column part][128 rows].  Keys and values of a bf16 cache: as one TMA box per
+// page leaves them, [8 pages][64-column part][16 rows], drafted tokens alike; the matrix products then take a page's
+// first or last 8 rows of all pages at a time (8-row groups a page apart), so that the columns of S, and the rows of V,
+// come in the order of column_of below.  (One box for a page's 64 columns, in the first layout, took 32 boxes a chunk:
+// at about 120 cycles a box the TMA unit, not memory, bounded the call.)
+__device__ __forceinline__ uint32_t swizzled(int row, int piece) {   // of a 16-byte piece of a row, first layout
   return static_cast<uint32_t>(piece >> 3) * (kRows * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
+}
+template <int HD, bool PAGED>
+__device__ __forceinline__ uint32_t swizzled_kv(int row, int piece) {
+  if (!PAGED) return swizzled(row, piece);
+  return static_cast<uint32_t>(row >> 4) * (HD * 32) + static_cast<uint32_t>(piece >> 3) * 2048 + (row & 15) * 128 +
+         (((piece & 7) ^ (row & 7)) << 4);
+}
+// Keys' bits (in their order) as bits of S's columns: byte 2 page + half to byte 8 half + page.
+__device__ __forceinline__ void column_of(uint32_t (&w)[4]) {
+  const uint32_t n0 = w[0], n1 = w[1], n2 = w[2], n3 = w[3];
+  w[0] = __byte_perm(n0, n1, 0x6420);
+  w[1] = __byte_perm(n2, n3, 0x6420);
+  w[2] = __byte_perm(n0, n1, 0x7531);
+  w[3] = __byte_perm(n2, n3, 0x7531);
+}
+
+// mbar_wait (ptx.cuh) with the barrier's own suspension: most of this kernel's warps wait most of the time, and polling
+// took two thirds of its instructions.
+__device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, int* err) {
+  const uint32_t at = smem_u32(bar);
+  if (mbar_try_wait(at, parity)) return true;
+  const uint64_t t0 = global_timer_ns();
+  for (;;) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(at), "r"(parity), "r"(20000u)   // ns
+        : "memory");
+    if (ok) return true;
+    const uint64_t dt = global_timer_ns() - t0;
+    if (dt < kErrPollNs) continue;
+    if (*(volatile int*)err != 0) return false;
+    if (dt > kWaitTimeoutNs) {
+      atomicCAS(err, 0, kDevTimeout);
+      return false;
+    }
+  }
 }
 
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
+}
+// As tmem_st16 (ptx.cuh), 8 columns.
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const float (&v)[8]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
+               "r"(__float_as_uint(v[0])), "r"(__float_as_uint(v[1])), "r"(__float_as_uint(v[2])), "r"(__float_as_uint(v[3])),
+               "r"(__float_as_uint(v[4])), "r"(__float_as_uint(v[5])), "r"(__float_as_uint(v[6])), "r"(__float_as_uint(v[7]))
+               : "memory");
 }
 // Two fp32 operations in one instruction.
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
@@ -145,6 +198,7 @@ template <int HD, bool E4M3>
 __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_constant__ TreeLaunch a,
                                                               const __grid_constant__ CUtensorMap map) {
   using SM = Smem<HD, E4M3>;
+  constexpr bool kPaged = !E4M3 && HD == 128;   // (of 64 columns a page's box is in the first layout)
   extern __shared__ uint8_t smem_raw[];
   __shared__ Static st;
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t{1023});
@@ -197,7 +251,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     const uint64_t pol = policy_evict_normal();
     uint32_t n = 0, loaded = 0;   // items of earlier parts; raw slots filled
     bool ok = true;
-    auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, err)); };
+    auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_for(bar, parity, err)); };
     for (int part = 0; ok && next_part(); ++part) {
       const int32_t* table = a.t.block_table + static_cast<int64_t>(a.seq0 + p.s) * a.t.max_blocks;
       const int pages = (p.q.len + kTreePage - 1) / kTreePage;
@@ -262,14 +316,11 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
           // (a part's marks are set once a slot of it is free: no earlier part then holds the same set)
           if (bad) atomicOr(&st.bad[part % kFlagSets], 1);
           mbar_arrive_expect_tx(&st.slot_full[slot], SM::kTile);
-          // a box is 16 rows of 64 columns; a place without a page reads one that does not exist and arrives as zeros
+          // a box is a page's rows of one head; a place without a page reads one that does not exist and arrives as zeros
           uint8_t* dst = base + SM::kSlot0 + slot * SM::kTile;
 #pragma unroll
           for (int k = 0; k < kPages; ++k)
-#pragma unroll
-            for (int sub = 0; sub < HD / 64; ++sub)
-              tma_load_5d(dst + sub * (kRows * 128) + k * 2048, &map, &st.slot_full[slot], 0, 0, sub, p.g,
-                          id[k] >= 0 ? 2 * id[k] + kv : -1, pol);
+            tma_load_5d(dst + k * (HD * 32), &map, &st.slot_full[slot], 0, 0, 0, p.g, id[k] >= 0 ? 2 * id[k] + kv : -1, pol);
         }
       }
       n += items.n;
@@ -282,9 +333,9 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     }
   } else if (warp == 13) {
     // ------------------------------------------------ MMA
-    const uint32_t id_s = idesc_bf16_f32(kRows, kChunk), id_o = idesc_bf16_f32(kRows, HD) | kIdescMnMajorB;
-    auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, err)); };
-    uint32_t n = 0, uses[2] = {0, 0};
+    const uint32_t id_s = idesc_bf16_f32(kRows, kPaged ? kChunk / 2 : kChunk), id_o = idesc_bf16_f32(kRows, HD) | kIdescMnMajorB;
+    auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_for(bar, parity, err)); };
+    uint32_t n = 0, phase = 0;   // phase: per group, the parity of its next p_full
     bool ok = true;
     for (int part = 0; next_part(); ++part) {
       const Items items(p);
@@ -298,11 +349,22 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         if (!ok) return;
         tc_fence_after();
         const uint64_t qd = desc_sw128(smem_u32(base + SM::kQ + (p.tiles == 2 ? g : 0) * SM::kTile));
-        const uint64_t kd = desc_sw128(smem_u32(base + SM::kSlot0 + slot * SM::kTile));
+        const uint32_t keys = smem_u32(base + SM::kSlot0 + slot * SM::kTile);
+        if constexpr (kPaged) {
+          const uint64_t kd = desc_sw128_s(keys, 16, HD * 32);
 #pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-          const uint32_t step = ((k >> 2) * (kRows * 128) + (k & 3) * 32) >> 4;
-          umma_bf16_w(tmem + kColS + g * 128, qd + step, kd + step, id_s, k > 0 ? 1u : 0u);
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int k = 0; k < HD / 16; ++k)
+              umma_bf16_w(tmem + kColS + g * 128 + h * 64, qd + (((k >> 2) * (kRows * 128) + (k & 3) * 32) >> 4),
+                          kd + (((k >> 2) * 2048 + h * 1024 + (k & 3) * 32) >> 4), id_s, k > 0 ? 1u : 0u);
+        } else {
+          const uint64_t kd = desc_sw128(keys);
+#pragma unroll
+          for (int k = 0; k < HD / 16; ++k) {
+            const uint32_t step = ((k >> 2) * (kRows * 128) + (k & 3) * 32) >> 4;
+            umma_bf16_w(tmem + kColS + g * 128, qd + step, kd + step, id_s, k > 0 ? 1u : 0u);
+          }
         }
         umma_commit_w(&st.s_full[g]);
         if (p.tiles == 1 || g == 1) umma_commit_w(&st.slot_empty[slot]);
@@ -312,7 +374,8 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         const int c = p.tiles == 2 ? j >> 1 : j, g = j & 1;
         const uint32_t i = n + items.values(c), slot = i % SM::kSlots;
         ok = ok && wait_all(&st.slot_full[slot], (i / SM::kSlots) & 1u);
-        ok = ok && wait_all(&st.p_full[g], uses[g]++ & 1u);
+        ok = ok && wait_all(&st.p_full[g], (phase >> g) & 1u);
+        phase ^= 1u << g;
         if (!ok) return;
         uint8_t* tile = base + SM::kSlot0 + slot * SM::kTile;
         if constexpr (!E4M3) {
@@ -322,17 +385,20 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
           if (p.c0 + c == p.q.cached_blocks - 1 && (have & 15) != 0 && (p.tiles == 1 || g == 0)) {
             const int rows = 16 - (have & 15);
             for (int x = lane; x < rows * (HD / 8); x += 32)
-              *reinterpret_cast<uint4*>(tile + swizzled(have + x / (HD / 8), x % (HD / 8))) = make_uint4(0u, 0u, 0u, 0u);
+              *reinterpret_cast<uint4*>(tile + swizzled_kv<HD, kPaged>(have + x / (HD / 8), x % (HD / 8))) =
+                  make_uint4(0u, 0u, 0u, 0u);
             fence_proxy_async_smem();
             __syncwarp();
           }
         }
         tc_fence_after();
-        const uint64_t vd = desc_sw128_mn(smem_u32(tile), kRows * 128);
+        const uint64_t vd = kPaged ? desc_sw128_s(smem_u32(tile), 2048, HD * 32) : desc_sw128_mn(smem_u32(tile), kRows * 128);
         const uint32_t pt = tmem + kColS + g * 128;
 #pragma unroll
-        for (int k = 0; k < kChunk / 16; ++k)
-          umma_bf16_ta_w(tmem + kColO + g * 128, pt + k * 8, vd + 128 * k, id_o, k > 0 || j >= 2 ? 1u : 0u);
+        for (int k = 0; k < kChunk / 16; ++k)   // 16 rows: 8 of two pages each, or of their own
+          umma_bf16_ta_w(tmem + kColO + g * 128, pt + k * 8,
+                         vd + ((kPaged ? (k & 3) * 2 * HD * 32 + (k >> 2) * 1024 : k * 2048) >> 4), id_o,
+                         k > 0 || j >= 2 ? 1u : 0u);
         if (p.tiles == 1 || g == 1) umma_commit_w(&st.slot_empty[slot]);
       };
       if (ok) issue_s(0);
@@ -358,7 +424,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale turns Q's signs instead
     for (int part = 0; next_part(); ++part) {
       const int rows = p.q.drafts * a.group;
-      if (part > 0) ok = ok && mbar_wait(&st.q_empty, (part - 1) & 1u, err);
+      if (part > 0) ok = ok && wait_for(&st.q_empty, (part - 1) & 1u, err);
       constexpr int kPieces = HD / 8, kStep = kProducers / kPieces;   // a thread's rows are kStep apart
       for (int tile = 0; tile < p.tiles; ++tile) {
         uint8_t* dst = base + SM::kQ + tile * SM::kTile;
@@ -395,10 +461,10 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
         const uint32_t i = n + item, slot = i % SM::kSlots;
         uint8_t* dst = base + SM::kSlot0 + slot * SM::kTile;
         if constexpr (E4M3) {   // every slot is filled here
-          if (i >= SM::kSlots) ok = ok && mbar_wait(&st.slot_empty[slot], (i / SM::kSlots - 1) & 1u, err);
+          if (i >= SM::kSlots) ok = ok && wait_for(&st.slot_empty[slot], (i / SM::kSlots - 1) & 1u, err);
           if (cached) {
             const uint32_t r = raw % SM::kRaw;
-            ok = ok && mbar_wait(&st.raw_full[r], (raw / SM::kRaw) & 1u, err);
+            ok = ok && wait_for(&st.raw_full[r], (raw / SM::kRaw) & 1u, err);
             if (t == 0 && st.raw_bad[r]) atomicOr(&st.bad[part % kFlagSets], 1);
             const uint8_t* src = base + SM::kRaw0 + r * SM::kRawBytes;
             const int have = p.q.len - c * kChunk;
@@ -411,12 +477,15 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
             const bool two = e > 134u && mine < have;
             uint32_t f = (two ? 254u : e + 120u) << 7 | (two ? (e == 255u ? 0x7FC0u : (e - 7u) << 7) : 0x3F80u) << 16;
             if (mine >= have) f = 0x3F800000u;
-            const int row0 = t / kParts, piece = t % kParts;
+            // A row's 8 pieces fill two 64-column parts, whose equal pieces lie in the same banks: lanes 0 to 3 and 4 to
+            // 7 take neighbouring rows, which the swizzle puts in different ones.
+            const int piece = t % kParts, j = HD == 128 ? (lane >> 4) * 2 + (((lane >> 3) & 1) ^ (piece >> 2)) : lane / kParts;
+            const int row0 = (t >> 5) * kTeam + j;
             auto convert = [&](auto twice) {
-#pragma unroll
+#pragma unroll(decltype(twice)::value ? 1 : 4)
               for (int k = 0; k < kSteps; ++k) {
                 const int row = row0 + k * (kTeam * kProducers / 32);
-                const uint32_t fr = __shfl_sync(0xffffffffu, f, lane / kParts + kTeam * k);
+                const uint32_t fr = __shfl_sync(0xffffffffu, f, j + kTeam * k);
                 uint4 lo, hi;
                 bf16_of16<decltype(twice)::value>(*reinterpret_cast<const uint4*>(src + row * HD + piece * 16),
                                                   __byte_perm(fr, 0, 0x1010), __byte_perm(fr, 0, 0x3232), &lo, &hi);
@@ -434,7 +503,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
             continue;
           }
         } else {
-          ok = ok && mbar_wait(&st.draft_go[slot], (go >> slot) & 1u, err);
+          ok = ok && wait_for(&st.draft_go[slot], (go >> slot) & 1u, err);
           go ^= 1u << slot;
         }
         // ---- drafted tokens: bf16 rows of their own tensors, whatever the cache holds
@@ -459,7 +528,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
               }
             }
           }
-          *reinterpret_cast<uint4*>(dst + swizzled(row, piece)) = E4M3 ? paired(v) : v;
+          *reinterpret_cast<uint4*>(dst + swizzled_kv<HD, kPaged>(row, piece)) = E4M3 ? paired(v) : v;
         }
         filled(&st.slot_full[slot]);
       }
@@ -477,7 +546,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
     for (int part = 0; next_part(); ++part) {
       const bool both = p.tiles == 2;   // the groups have a tile each, else alternate chunks of one
       const int rows = p.q.drafts * a.group, row = (2 * p.tp + (both ? g : 0)) * kRows + r;
-      const bool live = row < rows;
+      const bool live = row < rows, warp_live = row - lane < rows;   // (a dead row's weights, whatever they are, stay in it)
       const int tok = live ? tree_token(a, row) : 0;
       float m = -INFINITY, l = 0.f;
       bool begun = false;
@@ -507,46 +576,51 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                           : 0u;
           }
         }
-        ok = ok && __all_sync(0xffffffffu, mbar_wait(&st.s_full[g], uses & 1u, err));
+        if (kPaged && !all) column_of(sees);
+        ok = ok && __all_sync(0xffffffffu, wait_for(&st.s_full[g], uses & 1u, err));
         tc_fence_after();
-        if (ok) {
-          // 32 columns at a time, the next ones on their way
-          float x[2][2][16];
-          auto fetch = [&](int h) {
-            tmem_ld16_nowait(ts + h * 32, x[h & 1][0]);
-            tmem_ld16_nowait(ts + h * 32 + 16, x[h & 1][1]);
-          };
+        if (ok && warp_live) {
+          // Two passes over the row's S, 16 columns at a time with the next ones on their way: its maximum, then the
+          // weights.  (SEEN: every key; the other form is for a cache's last chunk and for drafted tokens.)
+          float x[2][16];
+          auto fetch = [&](int h) { tmem_ld16_nowait(ts + h * 16, x[h & 1]); };
           auto arrived = [&](int h) {
             tmem_wait_ld();
-            tmem_hold(x[h & 1][0]);
-            tmem_hold(x[h & 1][1]);
+            tmem_hold(x[h & 1]);
+          };
+          auto bits_of = [&](int h) {   // of the keys of columns 16 h ..
+            const uint32_t w = h < 4 ? (h < 2 ? sees[0] : sees[1]) : (h < 6 ? sees[2] : sees[3]);
+            return w >> (16 * (h & 1));
           };
           float mx = -INFINITY;
           fetch(0);
+          if (all) {
+            float my = -INFINITY;
 #pragma unroll
-          for (int h = 0; h < 4; ++h) {
-            arrived(h);
-            if (h < 3) fetch(h + 1);
-            const float(&x0)[16] = x[h & 1][0], (&x1)[16] = x[h & 1][1];
-            if (all) {
-              float y0 = x0[0], y1 = x1[0];
+            for (int h = 0; h < 8; ++h) {
+              arrived(h);
+              if (h < 7) fetch(h + 1);
+              const float(&y)[16] = x[h & 1];
 #pragma unroll
-              for (int i = 1; i < 16; ++i) {
-                y0 = fmaxf(y0, x0[i]);
-                y1 = fmaxf(y1, x1[i]);
+              for (int i = 0; i < 16; i += 4) {
+                mx = fmaxf(mx, fmaxf(y[i], y[i + 1]));
+                my = fmaxf(my, fmaxf(y[i + 2], y[i + 3]));
               }
-              mx = fmaxf(mx, fmaxf(y0, y1));
-            } else {
+            }
+            mx = fmaxf(mx, my);
+          } else {
+#pragma unroll 1
+            for (int h = 0; h < 8; ++h) {
+              tmem_ld16(ts + h * 16, x[0]);
+              const uint32_t bits = bits_of(h);
 #pragma unroll
-              for (int i = 0; i < 16; ++i)
-                mx = fmaxf(mx, fmaxf((sees[h] >> i) & 1u ? x0[i] : -INFINITY, (sees[h] >> (16 + i)) & 1u ? x1[i] : -INFINITY));
+              for (int i = 0; i < 16; ++i) mx = fmaxf(mx, (bits >> i) & 1u ? x[0][i] : -INFINITY);
             }
           }
           fetch(0);   // again, for the weights
           mx *= scale;
           if (scale == 0.f && mx != mx) mx = 0.f;   // -infinity times zero: nothing seen, or scores of zero
           const bool grow = mx > m + kMargin;
-          const float to_m = grow ? mx : m;
           if (__any_sync(0xffffffffu, grow) && begun) {   // the accumulator follows (every MMA on it has completed)
             const float f = grow ? (m == -INFINITY ? 0.f : ex2_ftz(m - mx)) : 1.f;
 #pragma unroll 1
@@ -561,31 +635,44 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
           }
           if (grow) {
             l = m == -INFINITY ? l : l * ex2_ftz(m - mx);
-            m = to_m;
+            m = mx;
           }
           begun = true;
           const float nm = m == -INFINITY ? 0.f : -m;
           float2 sum = make_float2(0.f, 0.f);
           const float2 scale2 = make_float2(scale, scale), nm2 = make_float2(nm, nm);
+          // the weights go as bf16 (the values' type) over columns of S that have been read
+          if (all) {
 #pragma unroll
-          for (int h = 0; h < 4; ++h) {
-            arrived(h);
-            if (h < 3) fetch(h + 1);
-            float w[16];
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
+            for (int h = 0; h < 8; ++h) {
+              arrived(h);
+              if (h < 7) fetch(h + 1);
+              float w[8];
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
-                float2 y = fma2(make_float2(x[h & 1][k][2 * i], x[h & 1][k][2 * i + 1]), scale2, nm2);
+                float2 y = fma2(make_float2(x[h & 1][2 * i], x[h & 1][2 * i + 1]), scale2, nm2);
                 y = make_float2(ex2_ftz(y.x), ex2_ftz(y.y));
-                if (!all) {
-                  const uint32_t bits = sees[h] >> (16 * k + 2 * i);
-                  y = make_float2(bits & 1u ? y.x : 0.f, bits & 2u ? y.y : 0.f);
-                }
                 sum = add2(sum, y);
-                w[8 * k + i] = __uint_as_float(pack_bf16(y.x, y.y));
+                w[i] = __uint_as_float(pack_bf16(y.x, y.y));
               }
-            tmem_st16(ts + h * 16, w);   // the weights as bf16 (the values' type), over columns of S that have been read
+              tmem_st8(ts + h * 8, w);
+            }
+          } else {
+            arrived(0);
+#pragma unroll 1
+            for (int h = 0; h < 8; ++h) {
+              if (h > 0) tmem_ld16(ts + h * 16, x[0]);
+              const uint32_t bits = bits_of(h);
+              float w[8];
+#pragma unroll
+              for (int i = 0; i < 8; ++i) {
+                float2 y = fma2(make_float2(x[0][2 * i], x[0][2 * i + 1]), scale2, nm2);
+                y = make_float2((bits >> (2 * i)) & 1u ? ex2_ftz(y.x) : 0.f, (bits >> (2 * i + 1)) & 1u ? ex2_ftz(y.y) : 0.f);
+                sum = add2(sum, y);
+                w[i] = __uint_as_float(pack_bf16(y.x, y.y));
+              }
+              tmem_st8(ts + h * 8, w);
+            }
           }
           l += sum.x + sum.y;
           tmem_wait_st();
@@ -597,7 +684,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       }
 
       // ---- the part's end
-      ok = ok && __all_sync(0xffffffffu, mbar_wait(&st.part_done, part & 1u, err));
+      ok = ok && __all_sync(0xffffffffu, wait_for(&st.part_done, part & 1u, err));
       tc_fence_after();
       const int set = part % kFlagSets, marks = st.bad[set];
       bool nan = !ok || p.q.bad || (marks & 1) != 0;
@@ -687,6 +774,17 @@ cudaError_t launch(const TreeLaunch& a, const CUtensorMap& map, int ctas, cudaSt
   return cudaLaunchKernelEx(&cfg, tree_tc_kernel<HD, E4M3>, a, map);
 }
 
+// Pages [n_pages][2][n_kv][16][hd] as (column of 64, row, 64-column part, kv head, 2 page + {0: keys, 1: values}); a box is
+// one page's keys or values of one head, landing as [part][16 rows][128 bytes] under the 128-byte swizzle.
+CUresult encode_pages(PFN_cuTensorMapEncodeTiled_v12000 encode, CUtensorMap* map, const kvprm_cache& c) {
+  const cuuint64_t row = static_cast<cuuint64_t>(c.head_dim) * 2, parts = c.head_dim / 64, heads = c.n_kv_heads;
+  const cuuint64_t dims[5] = {64, kTreePage, parts, heads, static_cast<cuuint64_t>(c.n_pages) * 2};
+  const cuuint64_t strides[4] = {row, 128, kTreePage * row, heads * kTreePage * row};
+  const cuuint32_t box[5] = {64, kTreePage, static_cast<cuuint32_t>(parts), 1, 1}, step[5] = {1, 1, 1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, c.pages, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
 }  // namespace
 
 cudaError_t launch_tree_tc(const TreeLaunch& a, const kvprm_cache& c, int ctas, cudaStream_t stream) {
@@ -702,8 +800,7 @@ cudaError_t launch_tree_tc(const TreeLaunch& a, const kvprm_cache& c, int ctas, 
     return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
   }();
   if (!encode) return cudaErrorNotSupported;
-  if (encode_pool_map_tc(encode, &map, c.pages, c.n_pages, c.n_kv_heads, c.head_dim) != CUDA_SUCCESS)
-    return cudaErrorInvalidValue;
+  if (encode_pages(encode, &map, c) != CUDA_SUCCESS) return cudaErrorInvalidValue;
   return c.head_dim == 128 ? launch<128, false>(a, map, ctas, stream) : launch<64, false>(a, map, ctas, stream);
 }
 
