@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(kThreads, kTreeRows16PerSm) tree_rows16_kernel
   tree_line<TreeRows16, kThreads>(a, s_off, s_sum);
   const int32_t total = s_off[a.n_seqs];
   if (total == 0) return;
-  const TreeShares shares(total, gridDim.x, 1);
+  const TreeShares shares(total, gridDim.x, a.weight_full);
   const int me = blockIdx.x;
   tree_leave_line(a, s_off, shares.ctas);
   if (me >= shares.ctas) return;

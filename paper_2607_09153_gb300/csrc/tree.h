@@ -19,6 +19,7 @@ struct TreeLaunch {
   int32_t n_kv, group, seq0, n_seqs;   // sequences seq0 .. seq0 + n_seqs - 1
   uint32_t group_m;                    // ceil(2^32 / group), 0 for a group of one (tree_token)
   int32_t whole;                       // 1: no pair is cut
+  int32_t weight_full, weight_part;    // places of a block of a pair with all its tiles, or with fewer
   float scale_log2;                    // scores in units of log2
   int32_t* line;                       // [n_seqs + 1], then the CTAs that took part: for the join
   float* part_o;                       // [2 * CTAs][head_dim][rows]
@@ -28,9 +29,8 @@ struct TreeLaunch {
 #ifdef __CUDACC__
 
 // The work of a launch is one line, laid out sequence by sequence, in a sequence (kv head, rows) by (kv head, rows) -- a
-// "pair", with `weight` row tiles -- and in a pair block by block (of kBlock keys), the cached ones first, then those of
-// drafted tokens.  A block takes `weight` places, and a pair begins with LEAD * weight places that stand for what it costs to
-// begin one.  Each CTA takes an equal share of the line, whatever the lengths are: the blocks whose first place it holds,
+// "pair" -- and in a pair block by block (of BLOCK keys), the cached ones first, then those of drafted tokens.  A block takes as
+// many places as its time weighs, and a pair begins with the places of LEAD blocks that stand for what it costs to begin one.  Each CTA takes an equal share of the line, whatever the lengths are: the blocks whose first place it holds,
 // so at most two of its pairs are shared with other CTAs.  Those leave partial results (slot 2 i + 1 of CTA i for a pair
 // that begins in its share, 2 i for one that began before), which a second launch joins in order (tree_join.cu).  With
 // `whole` set a pair goes to the CTA that holds its first block.  The line's marks come from the device's own lengths (a
@@ -63,6 +63,12 @@ struct TreeGeometry {
   static constexpr int kSlotRows = ROWS * TILES;   // of a partial result
 };
 
+// Places that a block of all of a head's pairs takes.
+template <typename G>
+__device__ __forceinline__ int32_t tree_width(const TreeLaunch& a, int tiles) {
+  return tiles / G::TILES * a.weight_full + (tiles % G::TILES != 0 ? a.weight_part : 0);
+}
+
 // off[s] = the first place of sequence s, off[n_seqs] = the line's length (kept below 2^31 by the host).  All threads.
 template <typename G, int THREADS>
 __device__ __forceinline__ void tree_line(const TreeLaunch& a, int32_t* off, int32_t* warp_sum) {
@@ -77,7 +83,7 @@ __device__ __forceinline__ void tree_line(const TreeLaunch& a, int32_t* off, int
     mine[k] = sum;
     if (s < a.n_seqs) {
       const TreeSeq q = tree_seq<G::ROWS, G::BLOCK>(a, s);
-      if (q.drafts > 0) sum += (q.blocks + G::LEAD) * q.tiles * a.n_kv;
+      if (q.drafts > 0) sum += (q.blocks + G::LEAD) * tree_width<G>(a, q.tiles) * a.n_kv;
     }
   }
   int32_t scan = sum;
@@ -100,11 +106,11 @@ __device__ __forceinline__ void tree_line(const TreeLaunch& a, int32_t* off, int
   __syncthreads();
 }
 
-// The CTAs' shares of the line: the first `more` have least + 1 places, the others `least`.  A share is as long as the
-// widest block at least, so that every CTA between a pair's first and last holds a block of it.
+// The CTAs' shares of the line: the first `more` have least + 1 places, the others `least`.  A share is as long as a block
+// (`widest`) at least, so that every CTA between a pair's first and last holds a block of it.
 struct TreeShares {
   int32_t ctas, least, more;
-  __device__ __forceinline__ TreeShares(int32_t total, int grid, int tiles) : ctas(max(1, min(grid, total / tiles))) {
+  __device__ __forceinline__ TreeShares(int32_t total, int grid, int widest) : ctas(max(1, min(grid, total / widest))) {
     least = total / ctas;
     more = total - least * ctas;
   }
@@ -120,9 +126,9 @@ struct TreePart {
   TreeSeq q;
   int32_t first;      // the place of its first block
   int s, g, tp;       // sequence, kv head, which TILES tiles
-  int tiles, c0, c1;  // tiles: its weight
+  int tiles, weight, c0, c1;
   __device__ __forceinline__ bool whole() const { return c0 == 0 && c1 == q.blocks; }
-  __device__ __forceinline__ int32_t place(int block) const { return first + block * tiles; }
+  __device__ __forceinline__ int32_t place(int block) const { return first + block * weight; }
 };
 
 // Walks a CTA's share [u, u_end); s: the sequence to start looking from (tree_find).
@@ -133,15 +139,16 @@ __device__ __forceinline__ bool tree_next(const TreeLaunch& a, const int32_t* of
     while (u >= off[s + 1]) ++s;
     p.q = tree_seq<G::ROWS, G::BLOCK>(a, s);
     p.s = s;
-    const int32_t depth = p.q.blocks + G::LEAD, head = depth * p.q.tiles, local = u - off[s];
+    const int32_t depth = p.q.blocks + G::LEAD, head = depth * tree_width<G>(a, p.q.tiles), local = u - off[s];
     p.g = local / head;
-    p.tp = (local - p.g * head) / (G::TILES * depth);
+    p.tp = (local - p.g * head) / (a.weight_full * depth);
     p.tiles = min(G::TILES, p.q.tiles - G::TILES * p.tp);
-    const int32_t pair0 = off[s] + p.g * head + p.tp * G::TILES * depth;
-    p.first = pair0 + G::LEAD * p.tiles;
+    p.weight = p.tiles == G::TILES ? a.weight_full : a.weight_part;
+    const int32_t pair0 = off[s] + p.g * head + p.tp * a.weight_full * depth;
+    p.first = pair0 + G::LEAD * p.weight;
     auto block_at = [&](int32_t place) {   // the first block that begins at a place or after it
       const int32_t d = place - p.first;
-      return d <= 0 ? 0 : min(p.q.blocks, (d + p.tiles - 1) / p.tiles);
+      return d <= 0 ? 0 : min(p.q.blocks, (d + p.weight - 1) / p.weight);
     };
     p.c0 = block_at(u);
     p.c1 = block_at(u_end);
@@ -150,7 +157,7 @@ __device__ __forceinline__ bool tree_next(const TreeLaunch& a, const int32_t* of
       p.c0 = 0;
       p.c1 = mine ? p.q.blocks : 0;
     }
-    const int32_t end = pair0 + depth * p.tiles;
+    const int32_t end = pair0 + depth * p.weight;
     u = min(end, u_end);
     if (p.c0 < p.c1) return true;
   }

@@ -53,7 +53,7 @@ int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   p.rows = p.tc ? 256 : 16;
   const int64_t block = p.tc ? 128 : kTreePage, tiles = ceil_div(rows, p.tc ? 128 : 16), lead = 8;
   // the line of a sequence of any length is shorter than this; a launch's stays within 31 bits
-  const int64_t line = (ceil_div(int64_t{kTreePage} * t.max_blocks, block) + ceil_div(t.max_drafts, block) + lead) * tiles * c.n_kv_heads;
+  const int64_t line = (ceil_div(int64_t{kTreePage} * t.max_blocks, block) + ceil_div(t.max_drafts, block) + lead) * (p.tc ? 4 * ceil_div(tiles, 2) : tiles) * c.n_kv_heads;
   if (line > 0x7FFFFFFF) return operator_fail(KVPRM_ECAPACITY, "kvprm_tree: block tables of %d pages", t.max_blocks);
   p.seqs = static_cast<int>(std::min<int64_t>({t.n_seqs, kTreeSeqs, 0x7FFFFFFF / line}));
   const int64_t len = std::min<int64_t>(t.max_len, int64_t{kTreePage} * t.max_blocks);
@@ -115,6 +115,10 @@ int kvprm_tree_attention(const kvprm_cache* cache, const kvprm_tree* t, void* wo
   a.group_m = a.group > 1 ? static_cast<uint32_t>(((uint64_t{1} << 32) + a.group - 1) / a.group) : 0u;
   a.scale_log2 = t->scale * 1.4426950408889634f;
   a.whole = p.whole;
+  // a chunk with one row tile costs the tensor-core kernel, by what it waits for, 0.75 of one with two (a bf16 cache: memory)
+  // or as much (an 8-bit one: its conversion)
+  a.weight_full = p.tc ? 4 : 1;
+  a.weight_part = !p.tc ? 1 : cache->format == KVPRM_CACHE_E4M3 ? 4 : 3;
   a.line = static_cast<int32_t*>(workspace);
   a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kLineBytes);
   a.part_ml = reinterpret_cast<float2*>(a.part_o + int64_t{2} * p.ctas * p.rows * cache->head_dim);

@@ -32,9 +32,9 @@ __global__ void __launch_bounds__(kThreads) tree_join_kernel(const __grid_consta
   grid_dep_wait();
   const int32_t off = __ldcg(a.line + s), total = __ldcg(a.line + a.n_seqs), ctas = __ldcg(a.line + a.n_seqs + 1);
   const TreeShares shares(total, ctas, 1);
-  const int tiles = min(G::TILES, q.tiles - G::TILES * tp), depth = q.blocks + G::LEAD;
-  const int32_t first = off + g * depth * q.tiles + tp * G::TILES * depth + G::LEAD * tiles;
-  const int i0 = shares.owner(first), i1 = shares.owner(first + (q.blocks - 1) * tiles);
+  const int weight = q.tiles - G::TILES * tp >= G::TILES ? a.weight_full : a.weight_part, depth = q.blocks + G::LEAD;
+  const int32_t first = off + depth * (g * tree_width<G>(a, q.tiles) + tp * a.weight_full) + G::LEAD * weight;
+  const int i0 = shares.owner(first), i1 = shares.owner(first + (q.blocks - 1) * weight);
   if (i0 == i1) return;   // whole: written by its CTA
   const int r = row0 - tp * R + lane % kLaneRows, d0 = warp * (HD / 8) + lane / kLaneRows * kDims;
   float best = -INFINITY, sum = 0.f, o[kDims];

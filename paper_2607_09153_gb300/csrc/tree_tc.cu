@@ -9,10 +9,10 @@
 // streams that meet at the end.  Either way one group's softmax runs beside the other's matrix products, and
 // the groups never wait for each other within a part.
 //   warps 0-3, 4-7   softmax groups (thread = row = lane of tensor memory)
-//   warps 8-11       producers: Q tiles, drafted tokens' keys and values, and with an 8-bit cache every chunk,
+//   warps 8-15       producers: Q tiles, drafted tokens' keys and values, and with an 8-bit cache every chunk,
 //                    converted to bf16 (exact: a power of two per row changes no mantissa)
-//   warp 12          TMA: bf16 pages straight into the tiles, 8-bit pages into a ring of their own
-//   warp 13          issues every MMA, in an order that keeps one unit's S ahead of the other's O
+//   warp 16          TMA: bf16 pages straight into the tiles, 8-bit pages into a ring of their own
+//   warp 17          issues every MMA, in an order that keeps one unit's S ahead of the other's O
 // Tiles lie in shared memory as rows of 128 bytes under the 128-byte swizzle, [64-column part][128 rows]: a
 // K-major operand for the keys and an MN-major one for the values.
 #include <cuda.h>
@@ -30,9 +30,10 @@ namespace kvprm {
 
 namespace {
 
-constexpr int kThreads = 448;
+constexpr int kThreads = 576;
 constexpr int kRows = TreeTc::ROWS, kChunk = TreeTc::BLOCK, kPages = kChunk / kTreePage;
-constexpr int kProducers = 128;
+constexpr int kProducers = 256;
+constexpr int kWarpTma = 16, kWarpMma = 17;
 constexpr float kMargin = 8.f;   // log2 units that scores may pass a running maximum by
 constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;   // S buffers at 0 and 128, accumulators at 256 and 384
 constexpr int kFlagSets = 4;     // parts whose marks may be in flight (the rings hold chunks of at most three)
@@ -194,8 +195,9 @@ __device__ __forceinline__ void in_order(float (&o)[N]) {
   }
 }
 
+// (a bound of 640 threads: 96 registers, what five warps of a scheduler can have)
 template <int HD, bool E4M3>
-__global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_constant__ TreeLaunch a,
+__global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__ TreeLaunch a,
                                                               const __grid_constant__ CUtensorMap map) {
   using SM = Smem<HD, E4M3>;
   constexpr bool kPaged = !E4M3 && HD == 128;   // (of 64 columns a page's box is in the first layout)
@@ -209,7 +211,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       mbar_init(&st.slot_full[i], 1);
       mbar_init(&st.slot_empty[i], 1);
       mbar_init(&st.draft_go[i], 1);
-      mbar_init(&st.raw_full[i], 1);
+      mbar_init(&st.raw_full[i], 33);   // the bulk copies' bytes, and each lane's own copies
       mbar_init(&st.raw_empty[i], 1);
     }
     mbar_init(&st.q_full, 1);
@@ -226,7 +228,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   }
   if (threadIdx.x < kFlagSets * 32) st.bad_drafts[threadIdx.x >> 5][lane] = 0;
   if (threadIdx.x < kFlagSets) st.bad[threadIdx.x] = 0;
-  if (warp == 13) {
+  if (warp == kWarpMma) {
     tmem_alloc(&st.tmem, kTmemCols);
     tmem_relinquish();
   }
@@ -236,7 +238,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   tc_fence_after();
   const uint32_t tmem = st.tmem;
   const int32_t total = st.off[a.n_seqs];
-  const TreeShares shares(total, gridDim.x, TreeTc::TILES);
+  const TreeShares shares(total, gridDim.x, a.weight_full);
   tree_leave_line(a, st.off, shares.ctas);
   const int me = blockIdx.x;
   const bool idle = me >= shares.ctas || total == 0;
@@ -246,7 +248,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   TreePart p;
   auto next_part = [&]() { return tree_next<TreeTc>(a, st.off, u, u_end, s, p); };
 
-  if (warp == 12) {
+  if (warp == kWarpTma) {
     // ------------------------------------------------ TMA
     const uint64_t pol = policy_evict_normal();
     uint32_t n = 0, loaded = 0;   // items of earlier parts; raw slots filled
@@ -288,21 +290,27 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
           if (loaded >= SM::kRaw) ok = wait_all(&st.raw_empty[r], (loaded / SM::kRaw - 1) & 1u);
           if (!ok) continue;
           ++loaded;
-          if (lane != 0) continue;
+          // a page's codes as one bulk copy; its 16 exponents by a lane's own asynchronous copy (a bulk copy costs the TMA
+          // unit about 120 cycles whatever its size)
           constexpr uint32_t kPageBytes = kTreePage * HD;
-          uint32_t good = 0;
-#pragma unroll
-          for (int i = 0; i < kPages; ++i) good += id[i] >= 0 ? 1u : 0u;
-          st.raw_bad[r] = bad;
-          mbar_arrive_expect_tx(&st.raw_full[r], good * (kPageBytes + kTreePage));
           uint8_t* dst = base + SM::kRaw0 + r * SM::kRawBytes;
+          auto row_of = [&](int32_t page) { return (static_cast<int64_t>(page) * 2 + kv) * a.n_kv + p.g; };
+          const int32_t mine = __shfl_sync(0xffffffffu, (c >> 2) > four ? ids_next : ids, (c & 3) * kPages + lane % kPages);
+          if (lane == 0) {
+            uint32_t good = 0;
 #pragma unroll
-          for (int i = 0; i < kPages; ++i) {
-            if (id[i] < 0) continue;
-            const int64_t row = (static_cast<int64_t>(id[i]) * 2 + kv) * a.n_kv + p.g;
-            bulk_load(dst + i * kPageBytes, a.pages + row * kPageBytes, kPageBytes, &st.raw_full[r]);
-            bulk_load(dst + SM::kRawCodes + i * kTreePage, a.exponents + row * kTreePage, kTreePage, &st.raw_full[r]);
+            for (int i = 0; i < kPages; ++i) good += id[i] >= 0 ? 1u : 0u;
+            st.raw_bad[r] = bad;
+            mbar_arrive_expect_tx(&st.raw_full[r], good * kPageBytes);
+#pragma unroll
+            for (int i = 0; i < kPages; ++i)
+              if (id[i] >= 0) bulk_load(dst + i * kPageBytes, a.pages + row_of(id[i]) * kPageBytes, kPageBytes, &st.raw_full[r]);
           }
+          if (lane < kPages && mine >= 0)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst + SM::kRawCodes + lane * kTreePage)),
+                         "l"(a.exponents + row_of(mine) * kTreePage)
+                         : "memory");
+          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&st.raw_full[r])) : "memory");
         } else {
           // This warp waits for every use of a slot, also where the producers fill it: a wait by parity sees only
           // the phase before the present one, so none may be left out.
@@ -331,7 +339,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       const uint64_t t0 = global_timer_ns();
       while (global_timer_ns() - t0 < 1000000ull) __nanosleep(1000);
     }
-  } else if (warp == 13) {
+  } else if (warp == kWarpMma) {
     // ------------------------------------------------ MMA
     const uint32_t id_s = idesc_bf16_f32(kRows, kPaged ? kChunk / 2 : kChunk), id_o = idesc_bf16_f32(kRows, HD) | kIdescMnMajorB;
     auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_for(bar, parity, err)); };
@@ -411,7 +419,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       if (ok) umma_commit_w(&st.part_done);
       n += items.n;
     }
-  } else if (warp >= 8 && warp < 12) {
+  } else if (warp >= 8 && warp < 16) {
     // ------------------------------------------------ producers
     const int t = threadIdx.x - 256;
     uint32_t n = 0, raw = 0, go = 0;   // go: per slot, the parity of its next draft_go
@@ -429,26 +437,22 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
       for (int tile = 0; tile < p.tiles; ++tile) {
         uint8_t* dst = base + SM::kQ + tile * SM::kTile;
         const int piece = t % kPieces, first = t / kPieces, left = rows - (2 * p.tp + tile) * kRows;
+        uint4 v[kRows / kStep];   // all loads in flight
 #pragma unroll
-        for (int half = 0; half < kPieces; half += kPieces / 2) {   // several loads in flight for each thread
-          uint4 v[kPieces / 2];
-#pragma unroll
-          for (int i = 0; i < kPieces / 2; ++i) {
-            const int r = first + (half + i) * kStep;
-            v[i] = make_uint4(0u, 0u, 0u, 0u);
-            if (r < left) {
-              const int row = rows - left + r, tok = tree_token(a, row), h = p.g * a.group + row - tok * a.group;
-              v[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.t.q) +
-                                                          (p.q.start + static_cast<int64_t>(tok)) * a.t.q_token +
-                                                          h * a.t.q_head) + piece);
-            }
+        for (int i = 0; i < kRows / kStep; ++i) {
+          const int r = first + i * kStep;
+          v[i] = make_uint4(0u, 0u, 0u, 0u);
+          if (r < left) {
+            const int row = rows - left + r, tok = tree_token(a, row), h = p.g * a.group + row - tok * a.group;
+            v[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(a.t.q) +
+                                                        (p.q.start + static_cast<int64_t>(tok)) * a.t.q_token +
+                                                        h * a.t.q_head) + piece);
           }
+        }
 #pragma unroll
-          for (int i = 0; i < kPieces / 2; ++i)
-          {
-            v[i] = make_uint4(v[i].x ^ flip, v[i].y ^ flip, v[i].z ^ flip, v[i].w ^ flip);
-            *reinterpret_cast<uint4*>(dst + swizzled(first + (half + i) * kStep, piece)) = E4M3 ? paired(v[i]) : v[i];
-          }
+        for (int i = 0; i < kRows / kStep; ++i) {
+          v[i] = make_uint4(v[i].x ^ flip, v[i].y ^ flip, v[i].z ^ flip, v[i].w ^ flip);
+          *reinterpret_cast<uint4*>(dst + swizzled(first + i * kStep, piece)) = E4M3 ? paired(v[i]) : v[i];
         }
       }
       filled(&st.q_full);
@@ -472,25 +476,27 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
             constexpr int kSteps = kChunk / (kTeam * kProducers / 32);
             // the factors of the rows that this warp converts, a row per lane: 2^(e - 127 + 120) as bf16, beyond its range
             // (or NaN, 255) in two; zero past the length, where the codes may be anything
-            const int mine = lane % kTeam + (t >> 5) * kTeam + lane / kTeam * (kTeam * kProducers / 32);
+            // A row's 8 pieces fill two 64-column parts, whose equal pieces lie in the same banks: lanes 0 to 3 and 4 to
+            // 7 take neighbouring rows, which the swizzle puts in different ones.
+            const int piece = t % kParts, j = HD == 128 ? (lane >> 4) * 2 + (((lane >> 3) & 1) ^ (piece >> 2)) : lane / kParts;
+            constexpr int kApart = kTeam * kProducers / 32;
+            const int row0 = (t >> 5) * kTeam + j;
+            uint4 codes[kSteps];
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) codes[k] = *reinterpret_cast<const uint4*>(src + (row0 + k * kApart) * HD + piece * 16);
+            const int mine = lane % kTeam + (t >> 5) * kTeam + lane / kTeam % kSteps * kApart;
             const uint32_t e = src[SM::kRawCodes + mine];
             const bool two = e > 134u && mine < have;
             uint32_t f = (two ? 254u : e + 120u) << 7 | (two ? (e == 255u ? 0x7FC0u : (e - 7u) << 7) : 0x3F80u) << 16;
             if (mine >= have) f = 0x3F800000u;
-            // A row's 8 pieces fill two 64-column parts, whose equal pieces lie in the same banks: lanes 0 to 3 and 4 to
-            // 7 take neighbouring rows, which the swizzle puts in different ones.
-            const int piece = t % kParts, j = HD == 128 ? (lane >> 4) * 2 + (((lane >> 3) & 1) ^ (piece >> 2)) : lane / kParts;
-            const int row0 = (t >> 5) * kTeam + j;
             auto convert = [&](auto twice) {
-#pragma unroll(decltype(twice)::value ? 1 : 4)
+#pragma unroll
               for (int k = 0; k < kSteps; ++k) {
-                const int row = row0 + k * (kTeam * kProducers / 32);
                 const uint32_t fr = __shfl_sync(0xffffffffu, f, j + kTeam * k);
                 uint4 lo, hi;
-                bf16_of16<decltype(twice)::value>(*reinterpret_cast<const uint4*>(src + row * HD + piece * 16),
-                                                  __byte_perm(fr, 0, 0x1010), __byte_perm(fr, 0, 0x3232), &lo, &hi);
-                *reinterpret_cast<uint4*>(dst + swizzled(row, 2 * piece)) = lo;
-                *reinterpret_cast<uint4*>(dst + swizzled(row, 2 * piece + 1)) = hi;
+                bf16_of16<decltype(twice)::value>(codes[k], __byte_perm(fr, 0, 0x1010), __byte_perm(fr, 0, 0x3232), &lo, &hi);
+                *reinterpret_cast<uint4*>(dst + swizzled(row0 + k * kApart, 2 * piece)) = lo;
+                *reinterpret_cast<uint4*>(dst + swizzled(row0 + k * kApart, 2 * piece + 1)) = hi;
               }
             };
             if (__any_sync(0xffffffffu, two))
@@ -512,7 +518,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
                                    (p.q.start + static_cast<int64_t>(j0)) * (kv ? a.t.v_token : a.t.k_token) +
                                    p.g * (kv ? a.t.v_head : a.t.k_head);
         const int64_t step = kv ? a.t.v_token : a.t.k_token;
-#pragma unroll 4
+#pragma unroll 2
         for (int x = t; x < kChunk * kPieces; x += kProducers) {   // a row's pieces: neighbouring lanes of a warp
           const int row = x / kPieces, piece = x % kPieces;
           uint4 v = make_uint4(0u, 0u, 0u, 0u);
@@ -583,23 +589,22 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
           // Two passes over the row's S, 16 columns at a time with the next ones on their way: its maximum, then the
           // weights.  (SEEN: every key; the other form is for a cache's last chunk and for drafted tokens.)
           float x[2][16];
-          auto fetch = [&](int h) { tmem_ld16_nowait(ts + h * 16, x[h & 1]); };
-          auto arrived = [&](int h) {
+          auto arrived = [&](int b) {
             tmem_wait_ld();
-            tmem_hold(x[h & 1]);
+            tmem_hold(x[b]);
           };
           auto bits_of = [&](int h) {   // of the keys of columns 16 h ..
             const uint32_t w = h < 4 ? (h < 2 ? sees[0] : sees[1]) : (h < 6 ? sees[2] : sees[3]);
             return w >> (16 * (h & 1));
           };
           float mx = -INFINITY;
-          fetch(0);
+          tmem_ld16_nowait(ts, x[0]);
           if (all) {
             float my = -INFINITY;
 #pragma unroll
             for (int h = 0; h < 8; ++h) {
-              arrived(h);
-              if (h < 7) fetch(h + 1);
+              arrived(h & 1);
+              tmem_ld16_nowait(ts + (h < 7 ? (h + 1) * 16 : 0), x[(h + 1) & 1]);   // (at the end the first ones again, for the weights)
               const float(&y)[16] = x[h & 1];
 #pragma unroll
               for (int i = 0; i < 16; i += 4) {
@@ -611,13 +616,12 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
           } else {
 #pragma unroll 1
             for (int h = 0; h < 8; ++h) {
-              tmem_ld16(ts + h * 16, x[0]);
+              tmem_ld16(ts + h * 16, x[0]);   // (waits)
               const uint32_t bits = bits_of(h);
 #pragma unroll
               for (int i = 0; i < 16; ++i) mx = fmaxf(mx, (bits >> i) & 1u ? x[0][i] : -INFINITY);
             }
           }
-          fetch(0);   // again, for the weights
           mx *= scale;
           if (scale == 0.f && mx != mx) mx = 0.f;   // -infinity times zero: nothing seen, or scores of zero
           const bool grow = mx > m + kMargin;
@@ -639,29 +643,28 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
           }
           begun = true;
           const float nm = m == -INFINITY ? 0.f : -m;
-          float2 sum = make_float2(0.f, 0.f);
+          float2 sum = make_float2(0.f, 0.f), sum1 = sum;
           const float2 scale2 = make_float2(scale, scale), nm2 = make_float2(nm, nm);
           // the weights go as bf16 (the values' type) over columns of S that have been read
           if (all) {
 #pragma unroll
             for (int h = 0; h < 8; ++h) {
-              arrived(h);
-              if (h < 7) fetch(h + 1);
+              arrived(h & 1);
+              if (h < 7) tmem_ld16_nowait(ts + (h + 1) * 16, x[(h + 1) & 1]);
               float w[8];
 #pragma unroll
               for (int i = 0; i < 8; ++i) {
                 float2 y = fma2(make_float2(x[h & 1][2 * i], x[h & 1][2 * i + 1]), scale2, nm2);
                 y = make_float2(ex2_ftz(y.x), ex2_ftz(y.y));
-                sum = add2(sum, y);
+                (i & 1 ? sum1 : sum) = add2(i & 1 ? sum1 : sum, y);
                 w[i] = __uint_as_float(pack_bf16(y.x, y.y));
               }
               tmem_st8(ts + h * 8, w);
             }
           } else {
-            arrived(0);
 #pragma unroll 1
             for (int h = 0; h < 8; ++h) {
-              if (h > 0) tmem_ld16(ts + h * 16, x[0]);
+              tmem_ld16(ts + h * 16, x[0]);
               const uint32_t bits = bits_of(h);
               float w[8];
 #pragma unroll
@@ -674,7 +677,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
               tmem_st8(ts + h * 8, w);
             }
           }
-          l += sum.x + sum.y;
+          l += (sum.x + sum1.x) + (sum.y + sum1.y);
           tmem_wait_st();
           tc_fence_before();
         }
@@ -753,7 +756,7 @@ __global__ void __launch_bounds__(kThreads, 1) tree_tc_kernel(const __grid_const
   __syncwarp();
   tc_fence_before();
   __syncthreads();
-  if (warp == 13) {
+  if (warp == kWarpMma) {
     tc_fence_after();
     tmem_dealloc(tmem, kTmemCols);
   }
