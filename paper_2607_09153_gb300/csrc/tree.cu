@@ -1,12 +1,11 @@
-// Attention of drafted tokens over the paged cache, in tiles of 16 query rows (row = drafted token and
-// head of the kv head's group): warp-level matrix instructions on fragments that are loaded straight
-// from the pages.
+// Attention of drafted tokens over the paged cache in tiles of 16 or 32 query rows (row = drafted token and head of the kv
+// head's group): warp-level matrix instructions on fragments that are loaded straight from the pages.
 //
-// Each warp takes every fourth 16-token block of its CTA's part of a pair (tree.h) and keeps its own
-// online softmax; the four meet at the part's end.  A lane's 16-byte loads are its operand fragments:
-// the products q . k run over head dimensions in any order, so a lane takes consecutive ones for both
-// operands, and the output's columns are named by the dimensions that its values' loads held.  Nothing
-// goes through shared memory or waits at a barrier while the cache streams.
+// Each warp takes every fourth 16-token block of its CTA's part of a pair (tree.h) and keeps its own online softmax; the
+// four meet at the part's end.  A lane's 16-byte loads are its operand fragments: the products q . k run over head
+// dimensions in any order, so a lane takes consecutive ones for both operands, and the output's columns are named by the
+// dimensions that its values' loads held.  Only the queries (the same for all warps) lie in shared memory; nothing waits
+// at a barrier while the cache streams.  8-bit codes become bf16 in registers, once for both tiles of 32 rows.
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -18,7 +17,7 @@ namespace kvprm {
 
 namespace {
 
-constexpr int kWarps = 4, kThreads = 32 * kWarps, kRows = 16;
+constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr float kMargin = 8.f;   // a running maximum may be exceeded by so many powers of two
 
 __device__ __forceinline__ uint4 ldg_stream(const void* p) {
@@ -28,8 +27,8 @@ __device__ __forceinline__ uint4 ldg_stream(const void* p) {
                : "l"(p));
   return r;
 }
-__device__ __forceinline__ uint2 ldg_stream2(const void* p) {
-  uint2 r;
+__device__ __forceinline__ uint4 ldg_stream2(const void* p) {   // 8 bytes
+  uint4 r = make_uint4(0u, 0u, 0u, 0u);
   asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
   return r;
 }
@@ -47,29 +46,32 @@ __device__ __forceinline__ uint32_t e4m3_even(uint32_t w) {
 }
 __device__ __forceinline__ uint32_t e4m3_odd(uint32_t w) { return rebias(((w >> 4) & 0x07F007F0u) | (w & 0x80008000u)); }
 
-// Whether one of two bf16 is infinite or NaN.
+// Whether one of two bf16 is infinite or NaN; whether one of four bytes is 255.
 __device__ __forceinline__ bool not_finite2(uint32_t w) {
   return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
 }
+__device__ __forceinline__ bool has_255(uint32_t w) { return ((~w - 0x01010101u) & w & 0x80808080u) != 0u; }
+// A row's power of two from byte k of a word of exponents (255, NaN, is looked for before).
+__device__ __forceinline__ float power(uint32_t w, int k) {
+  const uint32_t bits = (k < 3 ? w << (23 - 8 * k) : w >> 1) & 0x7F800000u;
+  return __uint_as_float(max(bits, 0x00400000u));
+}
 
-template <int HD, bool E4M3>
-struct Frag {
-  // keys: one or two 16-byte loads per token and 64 dims; values: 16 bytes per 64 dims (bf16), HD / 8 bytes (e4m3)
-  static constexpr int kK = E4M3 ? HD / 64 : HD / 32;
-  static constexpr int kV = E4M3 ? 1 : HD / 64;
-};
-
-template <int HD, bool E4M3>
-__global__ void __launch_bounds__(kThreads, kTreeRows16PerSm) tree_rows16_kernel(const __grid_constant__ TreeLaunch a) {
-  using F = Frag<HD, E4M3>;
-  constexpr int KS = HD / 16;   // 16-dim steps of q . k
-  constexpr int NT = HD / 8;    // 8-dim tiles of the output
+template <int HD, bool E4M3, int TILES>
+__global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_rows_kernel(const __grid_constant__ TreeLaunch a) {
+  using G = TreeRows<TILES>;
+  constexpr int KS = HD / 16;                       // 16-dim steps of q . k
+  constexpr int NT = HD / 8;                        // 8-dim tiles of the output
+  constexpr int kK = E4M3 ? HD / 64 : HD / 32;      // a lane's 16-byte pieces of a key row
+  constexpr int kV = E4M3 ? 1 : HD / 64;            // of a value row (of 8 bytes with 64 codes)
+  constexpr int kSize = E4M3 ? 1 : 2;
   __shared__ int32_t s_off[kTreeSeqs + 1];
   __shared__ int32_t s_sum[kWarps];
-  __shared__ float s_o[kWarps][kRows][HD + 1];
-  __shared__ float s_m[kWarps][kRows], s_l[kWarps][kRows];
+  __shared__ uint4 s_q[TILES][KS][32];              // the queries' fragments, by lane
+  __shared__ float s_o[kWarps][16][HD + 1];
+  __shared__ float s_m[kWarps][16], s_l[kWarps][16];
   grid_dep_launch();
-  tree_line<TreeRows16, kThreads>(a, s_off, s_sum);
+  tree_line<G, kThreads>(a, s_off, s_sum);
   const int32_t total = s_off[a.n_seqs];
   if (total == 0) return;
   const TreeShares shares(total, gridDim.x, a.weight_full);
@@ -77,380 +79,391 @@ __global__ void __launch_bounds__(kThreads, kTreeRows16PerSm) tree_rows16_kernel
   tree_leave_line(a, s_off, shares.ctas);
   if (me >= shares.ctas) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, c = lane & 3;
-  const int64_t block_bytes = static_cast<int64_t>(kTreePage) * HD * (E4M3 ? 1 : 2);   // of one head's keys
+  const int64_t head_bytes = static_cast<int64_t>(kTreePage) * HD * kSize, page_bytes = 2 * a.n_kv * head_bytes;
+  const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
   int32_t u = shares.begin(me);
   const int32_t u_end = shares.begin(me + 1);
-  int s = tree_find(s_off, a.n_seqs, u);
+  int s_at = tree_find(s_off, a.n_seqs, u);
   TreePart part;
-  for (bool first_part = true; tree_next<TreeRows16>(a, s_off, u, u_end, s, part); first_part = false) {
-    if (!first_part) __syncthreads();   // the last part's states have been read
+  while (tree_next<G>(a, s_off, u, u_end, s_at, part)) {
     const TreeSeq& q = part.q;
-    const int g = part.g, tile = part.tp, rows = q.drafts * a.group;
-    const int32_t* table = a.t.block_table + static_cast<int64_t>(a.seq0 + s) * a.t.max_blocks;
+    const int g = part.g, row0 = part.tp * G::kSlotRows, rows = q.drafts * a.group;
+    const int32_t* table = a.t.block_table + static_cast<int64_t>(a.seq0 + s_at) * a.t.max_blocks;
+    const uint8_t* keys = a.pages + g * head_bytes;
+    const uint8_t* values = keys + a.n_kv * head_bytes;
+    const uint8_t* exponents = a.exponents + g * kTreePage;
 
-    // ---- query fragments: rows gid and gid + 8
-    uint32_t qa[KS][4];
-    int row_t[2];
+    // ---- query fragments: warp w those of every fourth step; rows gid and gid + 8 of a tile
+    __syncthreads();   // the last part's have been read
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int r = tile * kRows + gid + 8 * h;
-      const bool live = r < rows;
-      row_t[h] = live ? tree_token(a, r) : -1;
-      const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.t.q) +
-                                 (live ? (q.start + static_cast<int64_t>(row_t[h])) * a.t.q_token +
-                                             (g * a.group + r - row_t[h] * a.group) * a.t.q_head
-                                       : 0);
-      const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-      if constexpr (E4M3) {
+    for (int ti = 0; ti < TILES; ++ti)
+      for (int j = warp; j < HD / 32; j += kWarps) {   // 32 dims: two steps
+        uint4 f[2];
 #pragma unroll
-        for (int j = 0; j < HD / 64; ++j)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            const uint4 v = live ? __ldg(reinterpret_cast<const uint4*>(src + 64 * j + 16 * c + 8 * i)) : zero;
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {   // dims of a word: even ones, odd ones
-              const uint32_t lo = word(v, 2 * k), hi = word(v, 2 * k + 1);
-              qa[4 * j + 2 * i + k][h] = __byte_perm(lo, hi, 0x5410);
-              qa[4 * j + 2 * i + k][2 + h] = __byte_perm(lo, hi, 0x7632);
-            }
+        for (int h = 0; h < 2; ++h) {
+          const int r = row0 + 16 * ti + gid + 8 * h;
+          uint4 v = zero;
+          if (r < rows) {
+            const int tok = tree_token(a, r);
+            const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.t.q) + (q.start + static_cast<int64_t>(tok)) * a.t.q_token +
+                                       (g * a.group + r - tok * a.group) * a.t.q_head;
+            // bf16 keys: 8 dims from 32 j + 8 c on; codes: half of 16 dims from 64 (j / 2) + 16 c on
+            v = __ldg(reinterpret_cast<const uint4*>(src + (E4M3 ? 64 * (j >> 1) + 16 * c + 8 * (j & 1) : 32 * j + 8 * c)));
           }
-      } else {
 #pragma unroll
-        for (int j = 0; j < HD / 32; ++j) {
-          const uint4 v = live ? __ldg(reinterpret_cast<const uint4*>(src + 32 * j + 8 * c)) : zero;
-          qa[2 * j][h] = v.x;
-          qa[2 * j][2 + h] = v.y;
-          qa[2 * j + 1][h] = v.z;
-          qa[2 * j + 1][2 + h] = v.w;
+          for (int k = 0; k < 2; ++k) {   // of codes the even dims of a word, then the odd ones
+            const uint32_t lo = word(v, 2 * k), hi = word(v, 2 * k + 1);
+            (h ? f[k].y : f[k].x) = E4M3 ? __byte_perm(lo, hi, 0x5410) : lo;
+            (h ? f[k].w : f[k].z) = E4M3 ? __byte_perm(lo, hi, 0x7632) : hi;
+          }
         }
+        s_q[ti][2 * j][lane] = f[0];
+        s_q[ti][2 * j + 1][lane] = f[1];
       }
+    __syncthreads();
+
+    float o[TILES][NT][4], m[TILES][2], l[TILES][2];
+#pragma unroll
+    for (int ti = 0; ti < TILES; ++ti) {
+#pragma unroll
+      for (int i = 0; i < NT; ++i) o[ti][i][0] = o[ti][i][1] = o[ti][i][2] = o[ti][i][3] = 0.f;
+      m[ti][0] = m[ti][1] = -INFINITY;
+      l[ti][0] = l[ti][1] = 0.f;
     }
-
-    float o[NT][4];
-#pragma unroll
-    for (int i = 0; i < NT; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
-    float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
     bool poison = q.bad;        // of all rows of the sequence
-    bool poison_row[2] = {false, false};
+    uint32_t poison_row = 0;    // bit 2 ti + h: of row gid + 8 h of tile ti
 
-    // ---- one block's fragments
-    struct KeyRegs {
-      uint4 k[2][F::kK];
-    } kr;
-    auto page_of = [&](int b) -> int64_t {   // -1: not a page of the cache
-      const int32_t p = __ldg(table + b);
-      return p >= 0 && p < a.n_pages ? p : -1;
-    };
-    auto draft_row = [&](const void* base, int64_t tok, int64_t head, int j) {
-      return static_cast<const __nv_bfloat16*>(base) + (q.start + static_cast<int64_t>(j)) * tok + g * head;
-    };
-    auto load_keys = [&](int64_t page) {
-      const uint8_t* base = a.pages + (page * 2 * a.n_kv + g) * block_bytes;
-#pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int j = 0; j < F::kK; ++j) {
-          const int at = (8 * n + gid) * HD * (E4M3 ? 1 : 2) + 64 * j + 16 * c;
-          kr.k[n][j] = page >= 0 ? ldg_stream(base + at) : make_uint4(0u, 0u, 0u, 0u);
-        }
-    };
-
-    // One block's softmax step: raw scores s (token 2 c + (i & 1) + 8 n of row gid + 8 (i >> 1)) and the tokens that the
-    // rows see become the weights as an operand, the running maximum, sum and output following.  The maximum moves
-    // only when a score passes it by more than kMargin (the weights then stay below 2^kMargin, and most blocks need
-    // no exchange between lanes).  The weights are rounded to bf16, the values' type: their sum is not.
-    auto softmax = [&](float(&s)[2][4], const uint32_t(&sees)[2], const float(&vf)[4], uint32_t(&pa)[4]) {
+    // One block's softmax step for one tile: scores s in units of log2 (token 2 c + (i & 1) + 8 n of row gid + 8 (i >> 1))
+    // become the weights as an operand, the running maximum, sum and output following.  The maximum moves only when
+    // a score passes it by more than kMargin (the weights then stay below 2^kMargin, and most blocks need no exchange
+    // between lanes).  The weights are rounded to bf16, the values' type: their sum is not.
+    auto softmax = [&](int ti, float(&s)[2][4], const float(&vf)[4], uint32_t(&pa)[4]) {
       float mx[2];
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          s[n][i] = (sees[i >> 1] >> (2 * c + (i & 1) + 8 * n)) & 1u ? s[n][i] * a.scale_log2 : -INFINITY;
-#pragma unroll
       for (int h = 0; h < 2; ++h) mx[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
-      if (__any_sync(0xffffffffu, mx[0] > m[0] + kMargin || mx[1] > m[1] + kMargin)) {
+      if (__any_sync(0xffffffffu, mx[0] > m[ti][0] + kMargin || mx[1] > m[ti][1] + kMargin)) {
         float al[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 1));
           mx[h] = fmaxf(mx[h], __shfl_xor_sync(0xffffffffu, mx[h], 2));
-          mx[h] = fmaxf(mx[h], m[h]);
-          al[h] = mx[h] == m[h] ? 1.f : ex2_ftz(m[h] - mx[h]);
-          m[h] = mx[h];
-          l[h] *= al[h];
+          mx[h] = fmaxf(mx[h], m[ti][h]);
+          al[h] = mx[h] == m[ti][h] ? 1.f : ex2_ftz(m[ti][h] - mx[h]);
+          m[ti][h] = mx[h];
+          l[ti][h] *= al[h];
         }
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
-          o[i][0] *= al[0];
-          o[i][1] *= al[0];
-          o[i][2] *= al[1];
-          o[i][3] *= al[1];
+          o[ti][i][0] *= al[0];
+          o[ti][i][1] *= al[0];
+          o[ti][i][2] *= al[1];
+          o[ti][i][3] *= al[1];
         }
       }
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float nm = m[h] == -INFINITY ? 0.f : -m[h];   // nothing seen yet: every score is -infinity
+        const float nm = m[ti][h] == -INFINITY ? 0.f : -m[ti][h];   // nothing seen yet: every score is -infinity
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
           const float p0 = ex2_ftz(s[n][2 * h] + nm), p1 = ex2_ftz(s[n][2 * h + 1] + nm);
-          l[h] += p0 + p1;
-          pa[2 * n + h] = pack_bf16(p0 * vf[2 * n], p1 * vf[2 * n + 1]);
+          l[ti][h] += p0 + p1;
+          pa[2 * n + h] = E4M3 ? pack_bf16(p0 * vf[2 * n], p1 * vf[2 * n + 1]) : pack_bf16(p0, p1);
         }
       }
     };
 
-    const int b_end = part.c1;
+    const int c_end = min(part.c1, q.cached_blocks);
+    uint4 kr[2][kK];
+    auto page_of = [&](int b) { return b < c_end ? __ldg(table + b) : 0; };
+    auto in_cache = [&](int32_t page) { return page >= 0 && page < a.n_pages; };
+    auto load_keys = [&](int32_t page) {
+      const uint8_t* base = keys + (in_cache(page) ? page : 0) * page_bytes + gid * HD * kSize + 16 * c;
+#pragma unroll
+      for (int n = 0; n < 2; ++n)
+#pragma unroll
+        for (int j = 0; j < kK; ++j) kr[n][j] = a.n_pages > 0 ? ldg_stream(base + (8 * n * HD * kSize + 64 * j)) : zero;
+    };
+
+    // ---- the cache: pages b, b + 4, ..; the next page's keys and the page's own values are on their way while scores are made
     int b = part.c0 + warp;
-    int64_t page = -1;
-    if (b < min(b_end, q.cached_blocks)) {
-      page = page_of(b);
-      load_keys(page);
-    }
-    for (; b < b_end; b += kWarps) {
-      const bool cached = b < q.cached_blocks;
-      const int next = b + kWarps;
-      const bool next_cached = next < min(b_end, q.cached_blocks);
-      const int64_t next_page = next_cached ? page_of(next) : -1;
-      const int j0 = cached ? b * kTreePage : (b - q.cached_blocks) * kTreePage;
-      const int have = cached ? q.len - j0 : q.drafts - j0;   // tokens of the block, 16 or more where it is full
-      float s[2][4];
+    int32_t page = page_of(b), next = page_of(b + kWarps);
+    if (b < c_end) load_keys(page);
+    for (; b < c_end; b += kWarps) {
+      const int32_t after = page_of(b + 2 * kWarps);
+      const int have = q.len - b * kTreePage;   // tokens of the page: 16 or more where it is full
+      poison = poison || !in_cache(page);
+      const int64_t at = (in_cache(page) ? page : 0) * static_cast<int64_t>(2 * a.n_kv);
+      uint4 v[4][kV];
+      uint32_t ke = 0, ve = 0;   // exponents of tokens 2 c, 2 c + 1, 8 + 2 c, 9 + 2 c
+      {
+        const uint8_t* base = values + at * head_bytes + (E4M3 ? gid * (HD / 8) : 16 * gid);
 #pragma unroll
-      for (int n = 0; n < 2; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.f;
-      uint32_t sees[2];   // tokens that rows gid and gid + 8 see
-      if (cached) {
-        poison = poison || page < 0;
-        // values and the rows' powers of two on their way while the scores are made
-        uint4 v[4][F::kV];
-        uint4 ke, ve;
-        {
-          const uint8_t* base = a.pages + ((page * 2 + 1) * a.n_kv + g) * block_bytes;
+        for (int k = 0; k < 4; ++k) {
+          const uint8_t* p = base + (2 * c + (k & 1) + 8 * (k >> 1)) * HD * kSize;
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int tok = 2 * c + (k & 1) + 8 * (k >> 1);
-            const bool live = page >= 0 && tok < have;   // beyond the length: anything, even NaN
-            if constexpr (E4M3) {
-              const uint8_t* p = base + tok * HD + gid * (HD / 8);
-              if constexpr (HD == 128) {
-                v[k][0] = live ? ldg_stream(p) : make_uint4(0u, 0u, 0u, 0u);
-              } else {
-                const uint2 w = live ? ldg_stream2(p) : make_uint2(0u, 0u);
-                v[k][0] = make_uint4(w.x, w.y, 0u, 0u);
-              }
-            } else {
-#pragma unroll
-              for (int h = 0; h < F::kV; ++h)
-                v[k][h] = live ? ldg_stream(base + (tok * HD + 64 * h + 8 * gid) * 2) : make_uint4(0u, 0u, 0u, 0u);
-            }
-          }
-          if constexpr (E4M3) {
-            const uint8_t* e = a.exponents + (page * 2 * a.n_kv + g) * kTreePage;
-            ke = page >= 0 ? __ldg(reinterpret_cast<const uint4*>(e)) : make_uint4(0u, 0u, 0u, 0u);
-            ve = page >= 0 ? __ldg(reinterpret_cast<const uint4*>(e + static_cast<int64_t>(a.n_kv) * kTreePage))
-                           : make_uint4(0u, 0u, 0u, 0u);
-          }
+          for (int h = 0; h < kV; ++h)
+            v[k][h] = a.n_pages > 0 ? (E4M3 && HD == 64 ? ldg_stream2(p) : ldg_stream(p + 128 * h)) : zero;
         }
-#pragma unroll
-        for (int n = 0; n < 2; ++n)
-#pragma unroll
-          for (int j = 0; j < F::kK; ++j) {
-            if constexpr (E4M3) {
-#pragma unroll
-              for (int w = 0; w < 4; ++w) {
-                const uint32_t x = word(kr.k[n][j], w);
-                const uint32_t(&A)[4] = qa[4 * j + w];
-                mma_bf16_16816(s[n], A[0], A[1], A[2], A[3], e4m3_even(x), e4m3_odd(x));
-              }
-            } else {
-              const uint32_t(&A)[4] = qa[2 * j];
-              const uint32_t(&B)[4] = qa[2 * j + 1];
-              mma_bf16_16816(s[n], A[0], A[1], A[2], A[3], kr.k[n][j].x, kr.k[n][j].y);
-              mma_bf16_16816(s[n], B[0], B[1], B[2], B[3], kr.k[n][j].z, kr.k[n][j].w);
-            }
-          }
-        if (next_cached) load_keys(next_page);
-        sees[0] = sees[1] = have >= 16 ? 0xFFFFu : (1u << have) - 1u;
-        float vf[4] = {1.f, 1.f, 1.f, 1.f};
         if constexpr (E4M3) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            const int tok = 2 * c + (k & 1) + 8 * (k >> 1);
-            const uint32_t kw = word(ke, (tok >> 2)), vw = word(ve, (tok >> 2));
-            const float kf = row_factor((kw >> (8 * (tok & 3))) & 0xFFu);
-            vf[k] = tok < have ? row_factor((vw >> (8 * (tok & 3))) & 0xFFu) : 0.f;
-            s[k >> 1][k & 1] *= kf;
-            s[k >> 1][2 + (k & 1)] *= kf;
+          const uint8_t* e = exponents + at * kTreePage + 2 * c;
+          if (a.n_pages > 0) {
+            ke = __ldg(reinterpret_cast<const uint16_t*>(e)) | __ldg(reinterpret_cast<const uint16_t*>(e + 8)) << 16;
+            e += a.n_kv * kTreePage;
+            ve = __ldg(reinterpret_cast<const uint16_t*>(e)) | __ldg(reinterpret_cast<const uint16_t*>(e + 8)) << 16;
           }
         }
-        uint32_t pa[4];
-        softmax(s, sees, vf, pa);
-        if constexpr (E4M3) {
+      }
+      float s[TILES][2][4];
 #pragma unroll
-          for (int w = 0; w < HD / 32; ++w) {
-            const uint32_t x0 = word(v[0][0], w), x1 = word(v[1][0], w), y0 = word(v[2][0], w), y1 = word(v[3][0], w);
-            const uint32_t a0 = __byte_perm(x0, x1, 0x5410), a1 = __byte_perm(x0, x1, 0x7632);
-            const uint32_t c0 = __byte_perm(y0, y1, 0x5410), c1 = __byte_perm(y0, y1, 0x7632);
-            mma_bf16_16816(o[4 * w], pa[0], pa[1], pa[2], pa[3], e4m3_even(a0), e4m3_even(c0));
-            mma_bf16_16816(o[4 * w + 1], pa[0], pa[1], pa[2], pa[3], e4m3_odd(a0), e4m3_odd(c0));
-            mma_bf16_16816(o[4 * w + 2], pa[0], pa[1], pa[2], pa[3], e4m3_even(a1), e4m3_even(c1));
-            mma_bf16_16816(o[4 * w + 3], pa[0], pa[1], pa[2], pa[3], e4m3_odd(a1), e4m3_odd(c1));
-          }
-        } else {
+      for (int ti = 0; ti < TILES; ++ti)
 #pragma unroll
-          for (int h = 0; h < F::kV; ++h)
+        for (int n = 0; n < 2; ++n) s[ti][n][0] = s[ti][n][1] = s[ti][n][2] = s[ti][n][3] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              const uint32_t sel = i & 1 ? 0x7632 : 0x5410;
-              mma_bf16_16816(o[8 * h + i], pa[0], pa[1], pa[2], pa[3],
-                             __byte_perm(word(v[0][h], i >> 1), word(v[1][h], i >> 1), sel),
-                             __byte_perm(word(v[2][h], i >> 1), word(v[3][h], i >> 1), sel));
-            }
-        }
-      } else {
-        // ---- drafted tokens: bf16 rows of their own tensors, whatever the cache holds
-        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+      for (int k = 0; k < KS; ++k) {
+        uint32_t b0[2], b1[2];
 #pragma unroll
         for (int n = 0; n < 2; ++n) {
-          const int j = 8 * n + gid;
-          const __nv_bfloat16* row = draft_row(a.t.k, a.t.k_token, a.t.k_head, j0 + j);
           if constexpr (E4M3) {
-#pragma unroll
-            for (int d = 0; d < HD / 64; ++d)
-#pragma unroll
-              for (int i = 0; i < 2; ++i) {
-                const uint4 x = j < have ? __ldg(reinterpret_cast<const uint4*>(row + 64 * d + 16 * c + 8 * i)) : zero;
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                  const uint32_t(&A)[4] = qa[4 * d + 2 * i + k];
-                  mma_bf16_16816(s[n], A[0], A[1], A[2], A[3], __byte_perm(word(x, 2 * k), word(x, 2 * k + 1), 0x5410),
-                                 __byte_perm(word(x, 2 * k), word(x, 2 * k + 1), 0x7632));
-                }
-              }
+            const uint32_t x = word(kr[n][k / 4], k % 4);
+            b0[n] = e4m3_even(x);
+            b1[n] = e4m3_odd(x);
           } else {
-#pragma unroll
-            for (int d = 0; d < HD / 32; ++d) {
-              const uint4 x = j < have ? __ldg(reinterpret_cast<const uint4*>(row + 32 * d + 8 * c)) : zero;
-              const uint32_t(&A)[4] = qa[2 * d];
-              const uint32_t(&B)[4] = qa[2 * d + 1];
-              mma_bf16_16816(s[n], A[0], A[1], A[2], A[3], x.x, x.y);
-              mma_bf16_16816(s[n], B[0], B[1], B[2], B[3], x.z, x.w);
-            }
+            b0[n] = word(kr[n][k / 2], 2 * (k % 2));
+            b1[n] = word(kr[n][k / 2], 2 * (k % 2) + 1);
           }
         }
-        constexpr int kD = HD / 64;   // 16-byte pieces of a lane's dims of one value row
-        uint4 v[4][kD];
-        uint32_t bad = 0;   // tokens whose value row is not finite
+#pragma unroll
+        for (int ti = 0; ti < TILES; ++ti) {
+          const uint4 f = s_q[ti][k][lane];
+#pragma unroll
+          for (int n = 0; n < 2; ++n) mma_bf16_16816(s[ti][n], f.x, f.y, f.z, f.w, b0[n], b1[n]);
+        }
+      }
+      if (b + kWarps < c_end) load_keys(next);
+      if (have < kTreePage) {   // the last page: its places beyond the length may hold anything, even NaN
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           const int tok = 2 * c + (k & 1) + 8 * (k >> 1);
-          const __nv_bfloat16* row = draft_row(a.t.v, a.t.v_token, a.t.v_head, j0 + tok);
-          bool off = false;
+          if (tok < have) continue;
 #pragma unroll
-          for (int d = 0; d < kD; ++d) {
-            const int dim = E4M3 ? gid * (HD / 8) + 8 * d : 64 * d + 8 * gid;
-            v[k][d] = tok < have ? __ldg(reinterpret_cast<const uint4*>(row + dim)) : zero;
-            off = off || not_finite2(v[k][d].x) || not_finite2(v[k][d].y) || not_finite2(v[k][d].z) || not_finite2(v[k][d].w);
+          for (int h = 0; h < kV; ++h) v[k][h] = zero;
+          ke = (ke & ~(255u << (8 * k))) | 127u << (8 * k);
+          ve = (ve & ~(255u << (8 * k))) | 127u << (8 * k);
+        }
+      }
+      if (E4M3 && __any_sync(0xffffffffu, has_255(ke) || has_255(ve))) poison = true;   // every row sees the page
+      float kf[4], vf[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        kf[k] = E4M3 ? power(ke, k) * a.scale_log2 : a.scale_log2;
+        vf[k] = E4M3 ? power(ve, k) : 1.f;
+      }
+      uint32_t pa[TILES][4];
+#pragma unroll
+      for (int ti = 0; ti < TILES; ++ti) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float x = s[ti][n][i] * kf[2 * n + (i & 1)];
+            s[ti][n][i] = have < kTreePage && 2 * c + (i & 1) + 8 * n >= have ? -INFINITY : x;   // (a scale may be negative)
           }
-          const uint32_t who = __ballot_sync(0xffffffffu, off);
+        softmax(ti, s[ti], vf, pa[ti]);
+      }
+#pragma unroll
+      for (int w = 0; w < NT / 4; ++w) {   // four 8-dim tiles: a word of codes, or two words of bf16, of each of the lane's tokens
+        uint32_t b0[4], b1[4];
+        if constexpr (E4M3) {
+#pragma unroll
+          for (int x = 0; x < 2; ++x) {
+            const uint32_t t0 = __byte_perm(word(v[0][0], w), word(v[1][0], w), x ? 0x7632 : 0x5410);
+            const uint32_t t1 = __byte_perm(word(v[2][0], w), word(v[3][0], w), x ? 0x7632 : 0x5410);
+            b0[2 * x] = e4m3_even(t0);
+            b0[2 * x + 1] = e4m3_odd(t0);
+            b1[2 * x] = e4m3_even(t1);
+            b1[2 * x + 1] = e4m3_odd(t1);
+          }
+        } else {
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int at_word = 2 * (w & 1) + (x >> 1), sel = x & 1 ? 0x7632 : 0x5410;
+            b0[x] = __byte_perm(word(v[0][w / 2], at_word), word(v[1][w / 2], at_word), sel);
+            b1[x] = __byte_perm(word(v[2][w / 2], at_word), word(v[3][w / 2], at_word), sel);
+          }
+        }
+#pragma unroll
+        for (int ti = 0; ti < TILES; ++ti)
 #pragma unroll
           for (int x = 0; x < 4; ++x)
-            if (who & (0x11111111u << x)) bad |= 1u << (2 * x + (k & 1) + 8 * (k >> 1));
-          if ((bad >> tok) & 1u) {   // a weight of zero must leave no trace of it: rows that see it are marked instead
-#pragma unroll
-            for (int d = 0; d < kD; ++d) v[k][d] = zero;
-          }
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          sees[h] = row_t[h] >= 0 ? tree_sees16(a, q, row_t[h], j0) : 0u;
-          poison_row[h] = poison_row[h] || (sees[h] & bad) != 0;
-        }
-        const float vf[4] = {1.f, 1.f, 1.f, 1.f};
-        uint32_t pa[4];
-        softmax(s, sees, vf, pa);
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          const int d = i / 8, w = (i % 8) >> 1;
-          const uint32_t sel = i & 1 ? 0x7632 : 0x5410;
-          mma_bf16_16816(o[i], pa[0], pa[1], pa[2], pa[3], __byte_perm(word(v[0][d], w), word(v[1][d], w), sel),
-                         __byte_perm(word(v[2][d], w), word(v[3][d], w), sel));
-        }
+            mma_bf16_16816(o[ti][4 * w + x], pa[ti][0], pa[ti][1], pa[ti][2], pa[ti][3], b0[x], b1[x]);
       }
-      page = next_page;
+      page = next;
+      next = after;
     }
 
-    // ---- the part's end: the four warps' states meet
+    // ---- drafted tokens: bf16 rows of their own tensors, whatever the cache holds (b is the warp's next block after the cache)
+    for (; b < part.c1; b += kWarps) {
+      const int j0 = (b - q.cached_blocks) * kTreePage, have = q.drafts - j0;
+      const __nv_bfloat16* kd = static_cast<const __nv_bfloat16*>(a.t.k) + (q.start + static_cast<int64_t>(j0)) * a.t.k_token + g * a.t.k_head;
+      const __nv_bfloat16* vd = static_cast<const __nv_bfloat16*>(a.t.v) + (q.start + static_cast<int64_t>(j0)) * a.t.v_token + g * a.t.v_head;
+      float s[TILES][2][4];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-      l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-      if (poison || poison_row[h]) l[h] = NAN;
-      if (c == 0) {
-        s_m[warp][gid + 8 * h] = m[h];
-        s_l[warp][gid + 8 * h] = l[h];
+      for (int ti = 0; ti < TILES; ++ti)
+#pragma unroll
+        for (int n = 0; n < 2; ++n) s[ti][n][0] = s[ti][n][1] = s[ti][n][2] = s[ti][n][3] = 0.f;
+#pragma unroll 1
+      for (int j = 0; j < HD / 32; ++j) {   // two steps
+        uint4 x[2];
+#pragma unroll
+        for (int n = 0; n < 2; ++n)
+          x[n] = 8 * n + gid < have ? __ldg(reinterpret_cast<const uint4*>(
+                                          kd + (8 * n + gid) * a.t.k_token +
+                                          (E4M3 ? 64 * (j >> 1) + 16 * c + 8 * (j & 1) : 32 * j + 8 * c)))
+                                    : zero;
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int ti = 0; ti < TILES; ++ti) {
+            const uint4 f = s_q[ti][2 * j + k][lane];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+              const uint32_t lo = word(x[n], 2 * k), hi = word(x[n], 2 * k + 1);
+              mma_bf16_16816(s[ti][n], f.x, f.y, f.z, f.w, E4M3 ? __byte_perm(lo, hi, 0x5410) : lo,
+                             E4M3 ? __byte_perm(lo, hi, 0x7632) : hi);
+            }
+          }
+      }
+      constexpr int kD = HD / 64;   // 16-byte pieces of a lane's dims of one value row
+      uint4 v[4][kD];
+      uint32_t bad = 0;   // tokens whose value row is not finite
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int tok = 2 * c + (k & 1) + 8 * (k >> 1);
+        bool off = false;
+#pragma unroll
+        for (int d = 0; d < kD; ++d) {
+          const int dim = E4M3 ? gid * (HD / 8) + 8 * d : 64 * d + 8 * gid;
+          v[k][d] = tok < have ? __ldg(reinterpret_cast<const uint4*>(vd + tok * a.t.v_token + dim)) : zero;
+          off = off || not_finite2(v[k][d].x) || not_finite2(v[k][d].y) || not_finite2(v[k][d].z) || not_finite2(v[k][d].w);
+        }
+        const uint32_t who = __ballot_sync(0xffffffffu, off);
+#pragma unroll
+        for (int x = 0; x < 4; ++x)
+          if (who & (0x11111111u << x)) bad |= 1u << (2 * x + (k & 1) + 8 * (k >> 1));
+        if ((bad >> tok) & 1u) {   // a weight of zero must leave no trace of it: rows that see it are marked instead
+#pragma unroll
+          for (int d = 0; d < kD; ++d) v[k][d] = zero;
+        }
+      }
+      uint32_t pa[TILES][4];
+#pragma unroll
+      for (int ti = 0; ti < TILES; ++ti) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int r = row0 + 16 * ti + gid + 8 * h;
+          const uint32_t sees = r < rows ? tree_sees16(a, q, tree_token(a, r), j0) : 0u;
+          if (sees & bad) poison_row |= 1u << (2 * ti + h);
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+              s[ti][n][2 * h + i] = (sees >> (2 * c + i + 8 * n)) & 1u ? s[ti][n][2 * h + i] * a.scale_log2 : -INFINITY;
+        }
+        const float ones[4] = {1.f, 1.f, 1.f, 1.f};
+        softmax(ti, s[ti], ones, pa[ti]);
+      }
+#pragma unroll
+      for (int i = 0; i < NT; ++i) {
+        const int d = i / 8, w = (i % 8) >> 1;
+        const uint32_t sel = i & 1 ? 0x7632 : 0x5410;
+        const uint32_t b0 = __byte_perm(word(v[0][d], w), word(v[1][d], w), sel);
+        const uint32_t b1 = __byte_perm(word(v[2][d], w), word(v[3][d], w), sel);
+#pragma unroll
+        for (int ti = 0; ti < TILES; ++ti) mma_bf16_16816(o[ti][i], pa[ti][0], pa[ti][1], pa[ti][2], pa[ti][3], b0, b1);
       }
     }
+
+    // ---- the part's end: the four warps' states meet, 16 rows at a time
 #pragma unroll
-    for (int i = 0; i < NT; ++i)
+    for (int ti = 0; ti < TILES; ++ti) {
+      if (ti > 0) __syncthreads();
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {   // column 2 c + (e & 1) of tile i: the dimension that its values' load held
-        const int n = 2 * c + (e & 1);
-        const int dim = E4M3 ? n * (HD / 8) + i : 64 * (i / 8) + 8 * n + i % 8;
-        s_o[warp][gid + 8 * (e >> 1)][dim] = o[i][e];
+      for (int h = 0; h < 2; ++h) {
+        float sum = l[ti][h];
+        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        if (poison || (poison_row >> (2 * ti + h)) & 1u) sum = NAN;
+        if (c == 0) {
+          s_m[warp][gid + 8 * h] = m[ti][h];
+          s_l[warp][gid + 8 * h] = sum;
+        }
       }
-    __syncthreads();
-    constexpr int kPer = kRows * HD / kThreads;   // outputs of a thread: part of one row
-    const int r = threadIdx.x % kRows, d0 = threadIdx.x / kRows * kPer;
-    float top = -INFINITY, sum = 0.f, acc[kPer];
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w][r]);
+      for (int i = 0; i < NT; ++i)
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
+        for (int e = 0; e < 4; ++e) {   // column 2 c + (e & 1) of tile i: the dimension that its values' load held
+          const int n = 2 * c + (e & 1);
+          const int dim = E4M3 ? n * (HD / 8) + i : 64 * (i / 8) + 8 * n + i % 8;
+          s_o[warp][gid + 8 * (e >> 1)][dim] = o[ti][i][e];
+        }
+      __syncthreads();
+      constexpr int kPer = 16 * HD / kThreads;   // outputs of a thread: part of one row
+      const int r = threadIdx.x % 16, d0 = threadIdx.x / 16 * kPer;
+      float top = -INFINITY, sum = 0.f, acc[kPer];
 #pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-      const float f = s_m[w][r] == -INFINITY ? 0.f : ex2_ftz(s_m[w][r] - top);   // (NaN sums stay NaN)
-      sum += s_l[w][r] * f;
+      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w][r]);
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) acc[i] += s_o[w][r][d0 + i] * f;
-    }
-    const int out_r = tile * kRows + r;
-    if (!part.whole()) {   // the pair goes on in other CTAs
-      const int slot = me == shares.owner(part.place(0)) ? 2 * me + 1 : 2 * me;
+      for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) a.part_o[(static_cast<int64_t>(slot) * HD + d0 + i) * kRows + r] = acc[i];
-      if (d0 == 0) a.part_ml[slot * kRows + r] = make_float2(top, sum);
-    } else if (out_r < rows) {
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row that saw nothing: zeros; NaN stays
-      const int tok = tree_token(a, out_r);
-      __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.t.out) + (q.start + static_cast<int64_t>(tok)) * a.t.out_token +
-                           (g * a.group + out_r - tok * a.group) * a.t.out_head + d0;
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = s_m[w][r] == -INFINITY ? 0.f : ex2_ftz(s_m[w][r] - top);   // (NaN sums stay NaN)
+        sum += s_l[w][r] * f;
 #pragma unroll
-      for (int i = 0; i < kPer; i += 8) {
-        uint4 w;
-        w.x = pack_bf16(acc[i] * inv, acc[i + 1] * inv);
-        w.y = pack_bf16(acc[i + 2] * inv, acc[i + 3] * inv);
-        w.z = pack_bf16(acc[i + 4] * inv, acc[i + 5] * inv);
-        w.w = pack_bf16(acc[i + 6] * inv, acc[i + 7] * inv);
-        *reinterpret_cast<uint4*>(dst + i) = w;
+        for (int i = 0; i < kPer; ++i) acc[i] += s_o[w][r][d0 + i] * f;
+      }
+      const int out_r = row0 + 16 * ti + r;
+      if (!part.whole()) {   // the pair goes on in other CTAs: [dim][row]
+        const int64_t slot = me == shares.owner(part.place(0)) ? 2 * me + 1 : 2 * me;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) a.part_o[(slot * HD + d0 + i) * G::kSlotRows + 16 * ti + r] = acc[i];
+        if (d0 == 0) a.part_ml[slot * G::kSlotRows + 16 * ti + r] = make_float2(top, sum);
+      } else if (out_r < rows) {
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row that saw nothing: zeros; NaN stays
+        const int tok = tree_token(a, out_r);
+        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.t.out) + (q.start + static_cast<int64_t>(tok)) * a.t.out_token +
+                             (g * a.group + out_r - tok * a.group) * a.t.out_head + d0;
+#pragma unroll
+        for (int i = 0; i < kPer; i += 8) {
+          uint4 w;
+          w.x = pack_bf16(acc[i] * inv, acc[i + 1] * inv);
+          w.y = pack_bf16(acc[i + 2] * inv, acc[i + 3] * inv);
+          w.z = pack_bf16(acc[i + 4] * inv, acc[i + 5] * inv);
+          w.w = pack_bf16(acc[i + 6] * inv, acc[i + 7] * inv);
+          *reinterpret_cast<uint4*>(dst + i) = w;
+        }
       }
     }
   }
 }
 
-template <int HD, bool E4M3>
+template <int HD, bool E4M3, int TILES>
 cudaError_t launch(const TreeLaunch& a, int ctas, cudaStream_t stream) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(ctas));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = stream;
-  return cudaLaunchKernelEx(&cfg, tree_rows16_kernel<HD, E4M3>, a);
+  return cudaLaunchKernelEx(&cfg, tree_rows_kernel<HD, E4M3, TILES>, a);
 }
 
 }  // namespace
 
-cudaError_t launch_tree_rows16(const TreeLaunch& a, const kvprm_cache& c, int ctas, cudaStream_t stream) {
-  if (c.head_dim == 128)
-    return c.format == KVPRM_CACHE_E4M3 ? launch<128, true>(a, ctas, stream) : launch<128, false>(a, ctas, stream);
-  return c.format == KVPRM_CACHE_E4M3 ? launch<64, true>(a, ctas, stream) : launch<64, false>(a, ctas, stream);
+cudaError_t launch_tree_rows(const TreeLaunch& a, const kvprm_cache& c, int tiles, int ctas, cudaStream_t stream) {
+  const bool wide = c.head_dim == 128, codes = c.format == KVPRM_CACHE_E4M3;
+  if (tiles == 2)
+    return codes ? (wide ? launch<128, true, 2>(a, ctas, stream) : launch<64, true, 2>(a, ctas, stream))
+                 : (wide ? launch<128, false, 2>(a, ctas, stream) : launch<64, false, 2>(a, ctas, stream));
+  return codes ? (wide ? launch<128, true, 1>(a, ctas, stream) : launch<64, true, 1>(a, ctas, stream))
+               : (wide ? launch<128, false, 1>(a, ctas, stream) : launch<64, false, 1>(a, ctas, stream));
 }
 
 }  // namespace kvprm

@@ -201,16 +201,18 @@ __device__ __forceinline__ uint32_t tree_sees16(const TreeLaunch& a, const TreeS
 
 #endif  // __CUDACC__
 
-// tree.cu: query rows in tiles of 16; CTAs that run at once on an SM.
-constexpr int kTreeRows16PerSm = 3;
+// tree.cu: query rows in tiles of 16 (tiles 1) or 32 (tiles 2); CTAs of four warps that run at once on an SM, by the
+// registers that a warp's outputs and loads in flight take.
+constexpr int tree_rows_per_sm(bool, int tiles) { return tiles == 2 ? 2 : 3; }
 #ifdef __CUDACC__
-using TreeRows16 = TreeGeometry<16, kTreePage, 1, 8>;
+template <int TILES>
+using TreeRows = TreeGeometry<16 * TILES, kTreePage, 1, 8>;
 using TreeTc = TreeGeometry<128, 128, 2, 4>;
 #endif
-cudaError_t launch_tree_rows16(const TreeLaunch& a, const kvprm_cache& c, int ctas, cudaStream_t stream);
+cudaError_t launch_tree_rows(const TreeLaunch& a, const kvprm_cache& c, int tiles, int ctas, cudaStream_t stream);
 // tree_tc.cu: in pairs of tiles of 128, on the tensor cores; one CTA on an SM.  The cache has a page at least.
 cudaError_t launch_tree_tc(const TreeLaunch& a, const kvprm_cache& c, int ctas, cudaStream_t stream);
-// tree_join.cu: joins the partial results that either left.
-cudaError_t launch_tree_join(const TreeLaunch& a, const kvprm_cache& c, bool tc, cudaStream_t stream);
+// tree_join.cu: joins the partial results that either left; rows: of a partial result (16, 32 or 256).
+cudaError_t launch_tree_join(const TreeLaunch& a, const kvprm_cache& c, int rows, cudaStream_t stream);
 
 }  // namespace kvprm

@@ -49,9 +49,10 @@ int sm_count(int* sms) {
 int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   TreePlan p;
   const int64_t rows = int64_t{t.max_drafts} * (t.n_q_heads / c.n_kv_heads);
-  p.tc = rows > 16 && c.n_pages > 0;
-  p.rows = p.tc ? 256 : 16;
-  const int64_t block = p.tc ? 128 : kTreePage, tiles = ceil_div(rows, p.tc ? 128 : 16), lead = 8;
+  const bool e4m3 = c.format == KVPRM_CACHE_E4M3;
+  p.tc = rows > (e4m3 ? 64 : 16) && c.n_pages > 0;
+  p.rows = p.tc ? 256 : rows > 16 ? 32 : 16;
+  const int64_t block = p.tc ? 128 : kTreePage, tiles = ceil_div(rows, p.tc ? 128 : p.rows), lead = 8;
   // the line of a sequence of any length is shorter than this; a launch's stays within 31 bits
   const int64_t line = (ceil_div(int64_t{kTreePage} * t.max_blocks, block) + ceil_div(t.max_drafts, block) + lead) * (p.tc ? 4 * ceil_div(tiles, 2) : tiles) * c.n_kv_heads;
   if (line > 0x7FFFFFFF) return operator_fail(KVPRM_ECAPACITY, "kvprm_tree: block tables of %d pages", t.max_blocks);
@@ -59,7 +60,7 @@ int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   const int64_t len = std::min<int64_t>(t.max_len, int64_t{kTreePage} * t.max_blocks);
   const int64_t pairs = int64_t{p.seqs} * c.n_kv_heads * ceil_div(rows, p.rows);
   const int64_t blocks = ceil_div(len, block) + ceil_div(t.max_drafts, block);
-  const int64_t most = int64_t{sms} * (p.tc ? 1 : kTreeRows16PerSm);
+  const int64_t most = int64_t{sms} * (p.tc ? 1 : tree_rows_per_sm(e4m3, p.rows / 16));
   p.whole = blocks <= (p.tc ? 3 : 16);
   p.ctas = static_cast<int>(std::max<int64_t>(1, std::min(most, p.whole ? pairs : pairs * blocks / (p.tc ? 2 : 8))));
   *out = p;
@@ -125,8 +126,8 @@ int kvprm_tree_attention(const kvprm_cache* cache, const kvprm_tree* t, void* wo
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   for (a.seq0 = 0; a.seq0 < t->n_seqs; a.seq0 += p.seqs) {
     a.n_seqs = std::min(p.seqs, t->n_seqs - a.seq0);
-    cudaError_t e = p.tc ? launch_tree_tc(a, *cache, p.ctas, st) : launch_tree_rows16(a, *cache, p.ctas, st);
-    if (e == cudaSuccess && !p.whole) e = launch_tree_join(a, *cache, p.tc, st);
+    cudaError_t e = p.tc ? launch_tree_tc(a, *cache, p.ctas, st) : launch_tree_rows(a, *cache, p.rows / 16, p.ctas, st);
+    if (e == cudaSuccess && !p.whole) e = launch_tree_join(a, *cache, p.rows, st);
     if (e != cudaSuccess) return operator_fail(KVPRM_ECUDA, "%s: %s", who, cudaGetErrorString(e));
   }
   return KVPRM_OK;

@@ -85,9 +85,11 @@ cudaError_t launch(const TreeLaunch& a, cudaStream_t stream) {
 
 }  // namespace
 
-cudaError_t launch_tree_join(const TreeLaunch& a, const kvprm_cache& c, bool tc, cudaStream_t stream) {
-  if (tc) return c.head_dim == 128 ? launch<TreeTc, 128>(a, stream) : launch<TreeTc, 64>(a, stream);
-  return c.head_dim == 128 ? launch<TreeRows16, 128>(a, stream) : launch<TreeRows16, 64>(a, stream);
+cudaError_t launch_tree_join(const TreeLaunch& a, const kvprm_cache& c, int rows, cudaStream_t stream) {
+  const bool wide = c.head_dim == 128;
+  if (rows == TreeTc::kSlotRows) return wide ? launch<TreeTc, 128>(a, stream) : launch<TreeTc, 64>(a, stream);
+  if (rows == 32) return wide ? launch<TreeRows<2>, 128>(a, stream) : launch<TreeRows<2>, 64>(a, stream);
+  return wide ? launch<TreeRows<1>, 128>(a, stream) : launch<TreeRows<1>, 64>(a, stream);
 }
 
 }  // namespace kvprm
