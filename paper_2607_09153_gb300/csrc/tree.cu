@@ -5,9 +5,18 @@
 // four meet at the part's end.  A lane's 16-byte loads are its operand fragments: the products q . k run over head
 // dimensions in any order, so a lane takes consecutive ones for both operands, and the output's columns are named by the
 // dimensions that its values' loads held.  Only the queries (the same for all warps) lie in shared memory; nothing waits
-// at a barrier while the cache streams.  8-bit codes become bf16 in registers, once for both tiles of 32 rows.
+// at a barrier while the cache streams.
+//
+// 8-bit codes become fp16 in registers (one instruction for two; to bf16 it takes nine for four, and ran at 0.7 of this
+// rate), once for both tiles of 32 rows.  What fp16 lacks in range is kept beside it as powers of two: a query row is
+// scaled to a largest magnitude of 1 to 2 (exact but for elements 2^-14 of that and smaller, which lose what is below
+// 2^-25 of it), a key row's power multiplies the scores in fp32, and a value row's multiplies the weights, relative to the
+// largest one met, E: a weight p becomes p 2^(e - E + 10), whose fp16 steps end at 2^-34 of a full weight's.
 #include <cuda_bf16.h>
+#include <cuda_fp16.h>
 #include <cuda_runtime.h>
+
+#include <type_traits>
 
 #include "ptx.cuh"
 #include "rope.h"
@@ -18,7 +27,8 @@ namespace kvprm {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr float kMargin = 8.f;   // a running maximum may be exceeded by so many powers of two
+// A running maximum may be exceeded by so many powers of two (of fp16 weights times 2^12 less, to stay below 65504).
+constexpr float margin(bool e4m3) { return e4m3 ? 3.f : 8.f; }
 
 __device__ __forceinline__ uint4 ldg_stream(const void* p) {
   uint4 r;
@@ -34,17 +44,29 @@ __device__ __forceinline__ uint4 ldg_stream2(const void* p) {   // 8 bytes
 }
 __device__ __forceinline__ uint32_t word(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
-// Two e4m3 codes as bf16: the even or the odd bytes of a word.  A code's exponent and mantissa at bf16's
-// place are 2^-120 of its value (the biases differ by 120), subnormals included.
-__device__ __forceinline__ uint32_t rebias(uint32_t v) {
+// The low or the high two e4m3 codes of a word as fp16 (exact, in one instruction).
+__device__ __forceinline__ uint32_t codes_lo(uint32_t w) {
   uint32_t r;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(0x7B807B80u));   // 2^120
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\t}" : "=r"(r) : "r"(w));
   return r;
 }
-__device__ __forceinline__ uint32_t e4m3_even(uint32_t w) {
-  return rebias(((w << 4) & 0x07F007F0u) | ((w << 8) & 0x80008000u));
+__device__ __forceinline__ uint32_t codes_hi(uint32_t w) {
+  uint32_t r;
+  asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %1;\n\tcvt.rn.f16x2.e4m3x2 %0, h;\n\t}" : "=r"(r) : "r"(w));
+  return r;
 }
-__device__ __forceinline__ uint32_t e4m3_odd(uint32_t w) { return rebias(((w >> 4) & 0x07F007F0u) | (w & 0x80008000u)); }
+// mma_bf16_16816 (ptx.cuh) on fp16 operands.
+__device__ __forceinline__ void mma_f16_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                              uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+  const __half2 v = __floats2half2_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ float power_of(int field) { return __uint_as_float(static_cast<uint32_t>(field) << 23); }
 
 // Whether one of two bf16 is infinite or NaN; whether one of four bytes is 255.
 __device__ __forceinline__ bool not_finite2(uint32_t w) {
@@ -67,8 +89,17 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
   constexpr int kSize = E4M3 ? 1 : 2;
   __shared__ int32_t s_off[kTreeSeqs + 1];
   __shared__ int32_t s_sum[kWarps];
-  __shared__ uint4 s_q[TILES][KS][32];              // the queries' fragments, by lane
-  __shared__ float s_o[kWarps][16][HD + 1];
+  __shared__ union {
+    struct {
+      uint4 bf16[TILES][KS][32];                              // the queries' fragments, by lane
+      uint4 fp16[E4M3 ? TILES : 1][E4M3 ? KS : 1][32];        // and, for codes, scaled
+    } q;
+    float o[kWarps][16][HD + 1];                              // at a part's end, the warps' outputs
+  } sh;
+  auto& s_q = sh.q.bf16;
+  auto& s_qh = sh.q.fp16;
+  auto& s_o = sh.o;
+  __shared__ float s_most[TILES][16][HD / 32];      // largest magnitude of 32 dims of a query row
   __shared__ float s_m[kWarps][16], s_l[kWarps][16];
   grid_dep_launch();
   tree_line<G, kThreads>(a, s_off, s_sum);
@@ -93,12 +124,15 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
     const uint8_t* values = keys + a.n_kv * head_bytes;
     const uint8_t* exponents = a.exponents + g * kTreePage;
 
-    // ---- query fragments: warp w those of every fourth step; rows gid and gid + 8 of a tile
+    // ---- query fragments: rows gid and gid + 8 of a tile; warp w dims 32 w .. (two steps)
     __syncthreads();   // the last part's have been read
+    float rs[TILES][2];   // what a row's scores are to be multiplied by
+    {
+      uint4 f[TILES][2];
 #pragma unroll
-    for (int ti = 0; ti < TILES; ++ti)
-      for (int j = warp; j < HD / 32; j += kWarps) {   // 32 dims: two steps
-        uint4 f[2];
+      for (int ti = 0; ti < TILES; ++ti) {
+        f[ti][0] = f[ti][1] = zero;
+        if (warp >= HD / 32) continue;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const int r = row0 + 16 * ti + gid + 8 * h;
@@ -107,20 +141,59 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
             const int tok = tree_token(a, r);
             const __nv_bfloat16* src = static_cast<const __nv_bfloat16*>(a.t.q) + (q.start + static_cast<int64_t>(tok)) * a.t.q_token +
                                        (g * a.group + r - tok * a.group) * a.t.q_head;
-            // bf16 keys: 8 dims from 32 j + 8 c on; codes: half of 16 dims from 64 (j / 2) + 16 c on
-            v = __ldg(reinterpret_cast<const uint4*>(src + (E4M3 ? 64 * (j >> 1) + 16 * c + 8 * (j & 1) : 32 * j + 8 * c)));
+            // bf16 keys: 8 dims from 32 w + 8 c on; codes: half of 16 dims from 64 (w / 2) + 16 c on
+            v = __ldg(reinterpret_cast<const uint4*>(src + (E4M3 ? 64 * (warp >> 1) + 16 * c + 8 * (warp & 1) : 32 * warp + 8 * c)));
           }
+          (h ? f[ti][0].y : f[ti][0].x) = v.x;
+          (h ? f[ti][0].w : f[ti][0].z) = v.y;
+          (h ? f[ti][1].y : f[ti][1].x) = v.z;
+          (h ? f[ti][1].w : f[ti][1].z) = v.w;
+          if (E4M3) {
+            float most = 0.f;
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {   // of codes the even dims of a word, then the odd ones
-            const uint32_t lo = word(v, 2 * k), hi = word(v, 2 * k + 1);
-            (h ? f[k].y : f[k].x) = E4M3 ? __byte_perm(lo, hi, 0x5410) : lo;
-            (h ? f[k].w : f[k].z) = E4M3 ? __byte_perm(lo, hi, 0x7632) : hi;
+            for (int k = 0; k < 4; ++k) {
+              const uint32_t x = word(v, k);
+              most = fmaxf(most, fmaxf(fabsf(__uint_as_float(x << 16)), fabsf(__uint_as_float(x & 0xFFFF0000u))));
+            }
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+            if (c == 0) s_most[ti][gid + 8 * h][warp] = most;
           }
         }
-        s_q[ti][2 * j][lane] = f[0];
-        s_q[ti][2 * j + 1][lane] = f[1];
+        s_q[ti][2 * warp][lane] = f[ti][0];
+        s_q[ti][2 * warp + 1][lane] = f[ti][1];
       }
-    __syncthreads();
+      __syncthreads();
+      if constexpr (E4M3) {
+#pragma unroll
+        for (int ti = 0; ti < TILES; ++ti) {
+          float up[2];
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            float most = 0.f;
+#pragma unroll
+            for (int k = 0; k < HD / 32; ++k) most = fmaxf(most, s_most[ti][gid + 8 * h][k]);
+            int e = static_cast<int>(__float_as_uint(most) >> 23);   // (infinite or all zero: any scale does)
+            e = e < 1 || e > 253 ? 127 : e;
+            rs[ti][h] = power_of(e);
+            up[h] = power_of(254 - e);
+          }
+          if (warp < HD / 32) {
+            auto scaled = [&](uint32_t x, float by) {
+              return pack_f16(__uint_as_float(x << 16) * by, __uint_as_float(x & 0xFFFF0000u) * by);
+            };
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+              s_qh[ti][2 * warp + k][lane] = make_uint4(scaled(f[ti][k].x, up[0]), scaled(f[ti][k].y, up[1]),
+                                                        scaled(f[ti][k].z, up[0]), scaled(f[ti][k].w, up[1]));
+          }
+        }
+        __syncthreads();
+      } else {
+#pragma unroll
+        for (int ti = 0; ti < TILES; ++ti) rs[ti][0] = rs[ti][1] = 1.f;
+      }
+    }
 
     float o[TILES][NT][4], m[TILES][2], l[TILES][2];
 #pragma unroll
@@ -132,16 +205,20 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
     }
     bool poison = q.bad;        // of all rows of the sequence
     uint32_t poison_row = 0;    // bit 2 ti + h: of row gid + 8 h of tile ti
+    // E, the exponent byte that the weights are relative to (from the first page on, at least 64: 2^-63; 0: none yet), and
+    // 2^(10 + 127 - E), which the outputs are multiplied by
+    int top_e = 0;
+    float rel = 1.f;
 
     // One block's softmax step for one tile: scores s in units of log2 (token 2 c + (i & 1) + 8 n of row gid + 8 (i >> 1))
     // become the weights as an operand, the running maximum, sum and output following.  The maximum moves only when
-    // a score passes it by more than kMargin (the weights then stay below 2^kMargin, and most blocks need no exchange
+    // a score passes it by more than a margin (the weights then stay below 2^margin, and most blocks need no exchange
     // between lanes).  The weights are rounded to bf16, the values' type: their sum is not.
-    auto softmax = [&](int ti, float(&s)[2][4], const float(&vf)[4], uint32_t(&pa)[4]) {
+    auto softmax = [&](int ti, float(&s)[2][4], const float(&vf)[4], uint32_t(&pa)[4], auto codes) {
       float mx[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) mx[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
-      if (__any_sync(0xffffffffu, mx[0] > m[ti][0] + kMargin || mx[1] > m[ti][1] + kMargin)) {
+      if (__any_sync(0xffffffffu, mx[0] > m[ti][0] + margin(E4M3) || mx[1] > m[ti][1] + margin(E4M3))) {
         float al[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -167,7 +244,8 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
         for (int n = 0; n < 2; ++n) {
           const float p0 = ex2_ftz(s[n][2 * h] + nm), p1 = ex2_ftz(s[n][2 * h + 1] + nm);
           l[ti][h] += p0 + p1;
-          pa[2 * n + h] = E4M3 ? pack_bf16(p0 * vf[2 * n], p1 * vf[2 * n + 1]) : pack_bf16(p0, p1);
+          const float w0 = E4M3 ? p0 * vf[2 * n] : p0, w1 = E4M3 ? p1 * vf[2 * n + 1] : p1;
+          pa[2 * n + h] = decltype(codes)::value ? pack_f16(w0, w1) : pack_bf16(w0, w1);
         }
       }
     };
@@ -225,8 +303,8 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
         for (int n = 0; n < 2; ++n) {
           if constexpr (E4M3) {
             const uint32_t x = word(kr[n][k / 4], k % 4);
-            b0[n] = e4m3_even(x);
-            b1[n] = e4m3_odd(x);
+            b0[n] = codes_lo(x);
+            b1[n] = codes_hi(x);
           } else {
             b0[n] = word(kr[n][k / 2], 2 * (k % 2));
             b1[n] = word(kr[n][k / 2], 2 * (k % 2) + 1);
@@ -234,9 +312,14 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
         }
 #pragma unroll
         for (int ti = 0; ti < TILES; ++ti) {
-          const uint4 f = s_q[ti][k][lane];
+          const uint4 f = E4M3 ? s_qh[E4M3 ? ti : 0][E4M3 ? k : 0][lane] : s_q[ti][k][lane];
 #pragma unroll
-          for (int n = 0; n < 2; ++n) mma_bf16_16816(s[ti][n], f.x, f.y, f.z, f.w, b0[n], b1[n]);
+          for (int n = 0; n < 2; ++n) {
+            if constexpr (E4M3)
+              mma_f16_16816(s[ti][n], f.x, f.y, f.z, f.w, b0[n], b1[n]);
+            else
+              mma_bf16_16816(s[ti][n], f.x, f.y, f.z, f.w, b0[n], b1[n]);
+          }
         }
       }
       if (b + kWarps < c_end) load_keys(next);
@@ -247,16 +330,35 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
           if (tok < have) continue;
 #pragma unroll
           for (int h = 0; h < kV; ++h) v[k][h] = zero;
-          ke = (ke & ~(255u << (8 * k))) | 127u << (8 * k);
-          ve = (ve & ~(255u << (8 * k))) | 127u << (8 * k);
+          ke = (ke & ~(255u << (8 * k))) | 1u << (8 * k);
+          ve = (ve & ~(255u << (8 * k))) | 1u << (8 * k);
         }
       }
-      if (E4M3 && __any_sync(0xffffffffu, has_255(ke) || has_255(ve))) poison = true;   // every row sees the page
+      if constexpr (E4M3) {
+        // a value row's power beyond E + 2 (NaN among them): E moves there and the outputs with it
+        const uint32_t most = max(max(ve & 255u, (ve >> 8) & 255u), max((ve >> 16) & 255u, ve >> 24));
+        if (__any_sync(0xffffffffu, static_cast<int>(most) > top_e + 2 || has_255(ke)) || top_e == 0) {
+          if (__any_sync(0xffffffffu, has_255(ke) || has_255(ve))) poison = true;   // every row sees the page
+          uint32_t e = most;
+          e = max(e, __shfl_xor_sync(0xffffffffu, e, 1));
+          e = max(e, __shfl_xor_sync(0xffffffffu, e, 2));
+          const int now = max(min(static_cast<int>(e), 254), max(top_e, 64));
+          const float f = power_of(max(127 + top_e - now, 0));
+#pragma unroll
+          for (int ti = 0; ti < TILES; ++ti)
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) o[ti][i][k] *= f;
+          top_e = now;
+          rel = power_of(264 - now);
+        }
+      }
       float kf[4], vf[4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         kf[k] = E4M3 ? power(ke, k) * a.scale_log2 : a.scale_log2;
-        vf[k] = E4M3 ? power(ve, k) : 1.f;
+        vf[k] = E4M3 ? power(ve, k) * rel : 1.f;
       }
       uint32_t pa[TILES][4];
 #pragma unroll
@@ -265,10 +367,10 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
         for (int n = 0; n < 2; ++n)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const float x = s[ti][n][i] * kf[2 * n + (i & 1)];
+            const float x = s[ti][n][i] * (E4M3 ? kf[2 * n + (i & 1)] * rs[ti][i >> 1] : kf[0]);
             s[ti][n][i] = have < kTreePage && 2 * c + (i & 1) + 8 * n >= have ? -INFINITY : x;   // (a scale may be negative)
           }
-        softmax(ti, s[ti], vf, pa[ti]);
+        softmax(ti, s[ti], vf, pa[ti], std::integral_constant<bool, E4M3>());
       }
 #pragma unroll
       for (int w = 0; w < NT / 4; ++w) {   // four 8-dim tiles: a word of codes, or two words of bf16, of each of the lane's tokens
@@ -276,12 +378,12 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
         if constexpr (E4M3) {
 #pragma unroll
           for (int x = 0; x < 2; ++x) {
-            const uint32_t t0 = __byte_perm(word(v[0][0], w), word(v[1][0], w), x ? 0x7632 : 0x5410);
-            const uint32_t t1 = __byte_perm(word(v[2][0], w), word(v[3][0], w), x ? 0x7632 : 0x5410);
-            b0[2 * x] = e4m3_even(t0);
-            b0[2 * x + 1] = e4m3_odd(t0);
-            b1[2 * x] = e4m3_even(t1);
-            b1[2 * x + 1] = e4m3_odd(t1);
+            const uint32_t t0 = __byte_perm(word(v[0][0], w), word(v[1][0], w), x ? 0x7362 : 0x5140);   // tokens side by side
+            const uint32_t t1 = __byte_perm(word(v[2][0], w), word(v[3][0], w), x ? 0x7362 : 0x5140);
+            b0[2 * x] = codes_lo(t0);
+            b0[2 * x + 1] = codes_hi(t0);
+            b1[2 * x] = codes_lo(t1);
+            b1[2 * x + 1] = codes_hi(t1);
           }
         } else {
 #pragma unroll
@@ -294,14 +396,22 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
 #pragma unroll
         for (int ti = 0; ti < TILES; ++ti)
 #pragma unroll
-          for (int x = 0; x < 4; ++x)
-            mma_bf16_16816(o[ti][4 * w + x], pa[ti][0], pa[ti][1], pa[ti][2], pa[ti][3], b0[x], b1[x]);
+          for (int x = 0; x < 4; ++x) {
+            if constexpr (E4M3)
+              mma_f16_16816(o[ti][4 * w + x], pa[ti][0], pa[ti][1], pa[ti][2], pa[ti][3], b0[x], b1[x]);
+            else
+              mma_bf16_16816(o[ti][4 * w + x], pa[ti][0], pa[ti][1], pa[ti][2], pa[ti][3], b0[x], b1[x]);
+          }
       }
       page = next;
       next = after;
     }
 
     // ---- drafted tokens: bf16 rows of their own tensors, whatever the cache holds (b is the warp's next block after the cache)
+    if (E4M3 && top_e == 0) {
+      top_e = 127;
+      rel = power_of(137);
+    }
     for (; b < part.c1; b += kWarps) {
       const int j0 = (b - q.cached_blocks) * kTreePage, have = q.drafts - j0;
       const __nv_bfloat16* kd = static_cast<const __nv_bfloat16*>(a.t.k) + (q.start + static_cast<int64_t>(j0)) * a.t.k_token + g * a.t.k_head;
@@ -328,8 +438,7 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
               const uint32_t lo = word(x[n], 2 * k), hi = word(x[n], 2 * k + 1);
-              mma_bf16_16816(s[ti][n], f.x, f.y, f.z, f.w, E4M3 ? __byte_perm(lo, hi, 0x5410) : lo,
-                             E4M3 ? __byte_perm(lo, hi, 0x7632) : hi);
+              mma_bf16_16816(s[ti][n], f.x, f.y, f.z, f.w, lo, hi);
             }
           }
       }
@@ -369,8 +478,8 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
             for (int i = 0; i < 2; ++i)
               s[ti][n][2 * h + i] = (sees >> (2 * c + i + 8 * n)) & 1u ? s[ti][n][2 * h + i] * a.scale_log2 : -INFINITY;
         }
-        const float ones[4] = {1.f, 1.f, 1.f, 1.f};
-        softmax(ti, s[ti], ones, pa[ti]);
+        const float same[4] = {rel, rel, rel, rel};
+        softmax(ti, s[ti], same, pa[ti], std::false_type());
       }
 #pragma unroll
       for (int i = 0; i < NT; ++i) {
@@ -384,9 +493,10 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
     }
 
     // ---- the part's end: the four warps' states meet, 16 rows at a time
+    const float down = power_of(max(top_e - 10, 1));   // 1 / rel
 #pragma unroll
     for (int ti = 0; ti < TILES; ++ti) {
-      if (ti > 0) __syncthreads();
+      __syncthreads();   // the queries (or the last 16 rows) have been read
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float sum = l[ti][h];
@@ -404,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
         for (int e = 0; e < 4; ++e) {   // column 2 c + (e & 1) of tile i: the dimension that its values' load held
           const int n = 2 * c + (e & 1);
           const int dim = E4M3 ? n * (HD / 8) + i : 64 * (i / 8) + 8 * n + i % 8;
-          s_o[warp][gid + 8 * (e >> 1)][dim] = o[ti][i][e];
+          s_o[warp][gid + 8 * (e >> 1)][dim] = E4M3 ? o[ti][i][e] * down : o[ti][i][e];
         }
       __syncthreads();
       constexpr int kPer = 16 * HD / kThreads;   // outputs of a thread: part of one row
