@@ -34,7 +34,7 @@ int operator_fail(int code, const char* fmt, ...) {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxTokens = 8;   // tokens of a CTA
+constexpr int kRopeTokens = 4, kWriteTokens = 8;   // tokens of a CTA at most
 constexpr int kMaxHeads = 1024, kMaxHeadDim = 512;
 
 // ---------------------------------------------------------------- elements
@@ -91,7 +91,7 @@ __device__ __forceinline__ void store_n(T* p, const float (&x)[N]) {
   }
 }
 
-// Division by a number that a launch keeps: exact for n * d < 2^32 (kMaxTokens * kMaxHeads * kMaxHeadDim^2
+// Division by a number that a launch keeps: exact for n * d < 2^32 (8 tokens * kMaxHeads * kMaxHeadDim^2
 // is the most that happens here).
 struct FastDiv {
   uint32_t d, m;
@@ -103,11 +103,11 @@ struct FastDiv {
 // angle is pos * turns in whole numbers modulo one turn: its upper 32 bits as a signed fraction of a
 // turn are within 2^-32 turns at every position, where a 32-bit product of a position of 131,072 and
 // a frequency would be 2^-8 radians off.
-__device__ __forceinline__ void fill_rotations(const RopeTable& tab, const int32_t* __restrict__ positions,
+__device__ __forceinline__ void fill_rotations(const RopeTable& tab, const FastDiv& by_pairs, const int32_t* __restrict__ positions,
                                                int64_t first, int tokens, float sign, float* s_cos, float* s_sin) {
   const int pairs = tab.dim >> 1;
   for (int i = threadIdx.x; i < tokens * pairs; i += blockDim.x) {
-    const int t = i / pairs, pair = i - t * pairs;
+    const int t = static_cast<int>(by_pairs.div(i)), pair = i - t * pairs;
     const uint64_t a = static_cast<uint64_t>(static_cast<int64_t>(__ldg(positions + first + t))) * tab.turns[pair];
     const float half_turns = static_cast<float>(static_cast<int32_t>(a >> 32)) * 0x1p-31f;
     float sn, cs;
@@ -122,7 +122,7 @@ struct RopeLaunch {
   RopeTable tab;
   kvprm_heads x[4];
   int32_t n_x, heads, head_dim, tokens;   // heads of all tensors; tokens of a CTA
-  FastDiv by_unit, by_heads, by_rest;
+  FastDiv by_unit, by_heads, by_rest, by_pairs;
   const int32_t* positions;
   int64_t n_tokens;
   float sign;
@@ -141,19 +141,18 @@ __device__ __forceinline__ void locate(const RopeLaunch& a, int64_t token, int h
 // 16 bytes of neighbouring pairs (interleaved); single pairs without VEC.
 template <typename T, bool INTERLEAVED, bool VEC>
 __global__ void __launch_bounds__(kThreads) rope_kernel(const __grid_constant__ RopeLaunch a) {
-  extern __shared__ float s_rot[];
+  extern __shared__ __align__(16) float s_rot[];
   const int pairs = a.tab.dim >> 1;
   const int64_t first = static_cast<int64_t>(blockIdx.x) * a.tokens;
   const int tokens = static_cast<int>(min(static_cast<int64_t>(a.tokens), a.n_tokens - first));
   float* s_cos = s_rot;
   float* s_sin = s_rot + a.tokens * pairs;
-  fill_rotations(a.tab, a.positions, first, tokens, a.sign, s_cos, s_sin);
+  fill_rotations(a.tab, a.by_pairs, a.positions, first, tokens, a.sign, s_cos, s_sin);
   __syncthreads();
   constexpr int kV = VEC ? 16 / sizeof(T) : (INTERLEAVED ? 2 : 1);   // elements of an access
   constexpr int kP = INTERLEAVED ? kV / 2 : kV;                      // pairs of a unit
   const uint32_t units = a.by_unit.d;                                // of a head
   const uint32_t total = static_cast<uint32_t>(tokens) * a.heads * units;
-#pragma unroll 2
   for (uint32_t i = threadIdx.x; i < total; i += kThreads) {
     const uint32_t row = a.by_unit.div(i), u = i - row * units;
     const uint32_t t = a.by_heads.div(row), h = row - t * a.heads;
@@ -218,7 +217,7 @@ struct WriteLaunch {
   uint8_t* pages;
   uint8_t* exponents;
   int32_t heads, head_dim, tokens;
-  FastDiv by_rows;         // 2 * heads
+  FastDiv by_rows, by_pairs;   // 2 * heads
 };
 
 // Eight elements from `i` on of a key row, rotated.  Partners outside the eight are read again (they
@@ -266,6 +265,12 @@ __device__ __forceinline__ int row_exponent(float most) {
   return max(e, -127);
 }
 
+__device__ __forceinline__ float max_nan(float a, float b) {   // NaN if either is
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
 __device__ __forceinline__ uint2 e4m3_of8(const float (&x)[8], float f) {
   uint32_t w[2];
 #pragma unroll
@@ -281,45 +286,50 @@ __device__ __forceinline__ uint2 e4m3_of8(const float (&x)[8], float f) {
 // rotated pair of the half layout meets in one thread, and the row's maximum in as many shuffles.
 template <typename T, bool E4M3, bool VEC>
 __global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__ WriteLaunch a) {
-  extern __shared__ float s_rot[];
+  extern __shared__ __align__(16) float s_rot[];
   const int pairs = a.tab.dim >> 1;
   const int64_t first = static_cast<int64_t>(blockIdx.x) * a.tokens;
   const int tokens = static_cast<int>(min(static_cast<int64_t>(a.tokens), a.n_tokens - first));
   float* s_cos = s_rot;
   float* s_sin = s_rot + a.tokens * pairs;
   if (pairs > 0) {
-    fill_rotations(a.tab, a.positions, first, tokens, 1.f, s_cos, s_sin);
+    fill_rotations(a.tab, a.by_pairs, a.positions, first, tokens, 1.f, s_cos, s_sin);
     __syncthreads();
   }
-  const int per_row = a.head_dim >> 4, half = a.head_dim >> 1;
-  const int j = threadIdx.x & (per_row - 1);
-  const uint32_t rows = static_cast<uint32_t>(tokens) * 2 * a.heads, step = kThreads / per_row;
-  for (uint32_t r0 = 0; r0 < rows; r0 += step) {
-    const uint32_t r = r0 + threadIdx.x / per_row;
+  const int per_row = a.head_dim >> 4, half = a.head_dim >> 1, j = threadIdx.x & (per_row - 1);
+  // A thread keeps its row of a token (its head's keys or values) and goes from token to token, as many tokens at a time
+  // as the CTA's threads cover; a token of more rows than that takes several rounds.
+  const int rows = 2 * a.heads, lane_row = threadIdx.x / per_row, at_once = kThreads / per_row;
+  const int side = rows < at_once ? static_cast<int>(a.by_rows.div(lane_row)) : 0;   // which of the tokens at a time
+  const int side_tokens = rows < at_once ? at_once / rows : 1;
+  for (int r0 = 0; r0 < rows; r0 += at_once) {
+   const int r = rows < at_once ? lane_row - side * rows : r0 + lane_row;
+   const bool mine = r < rows && side < side_tokens;
+   const bool kv = r >= a.heads;
+   const int h = kv ? r - a.heads : r;
+   const T* base = kv ? static_cast<const T*>(a.v) + h * a.v_head : static_cast<const T*>(a.k) + h * a.k_head;
+   const int64_t token_step = kv ? a.v_token : a.k_token;
+   for (int t0 = 0; t0 < tokens; t0 += side_tokens) {
+    const int t = t0 + side;
     int64_t slot = -1;
-    uint32_t t = 0, kv = 0, h = 0;
-    if (r < rows) {
-      t = a.by_rows.div(r);
-      const uint32_t in_token = r - t * 2 * a.heads;
-      kv = in_token >= static_cast<uint32_t>(a.heads) ? 1 : 0;
-      h = in_token - kv * a.heads;
-      slot = __ldg(a.slots + first + t);
-    }
+    if (mine && t < tokens) slot = __ldg(a.slots + first + t);
     const bool live = slot >= 0 && slot < a.n_slots;
     float x0[8], x1[8];
     if (live) {
-      const T* row = kv ? static_cast<const T*>(a.v) + (first + t) * a.v_token + h * a.v_head
-                        : static_cast<const T*>(a.k) + (first + t) * a.k_token + h * a.k_head;
+      const T* row = base + (first + t) * token_step;
       load_n<T, 8, VEC>(row + 8 * j, x0);
       load_n<T, 8, VEC>(row + half + 8 * j, x1);
-      if (pairs > 0 && kv == 0) {
+      if (pairs > 0 && !kv) {
         const float *cs = s_cos + t * pairs, *sn = s_sin + t * pairs;
         if (!a.tab.interleaved && pairs == half) {
+          float c[8], s[8];
+          load_n<float, 8, true>(cs + 8 * j, c);
+          load_n<float, 8, true>(sn + 8 * j, s);
 #pragma unroll
           for (int k = 0; k < 8; ++k) {
-            const float c = cs[8 * j + k], s = sn[8 * j + k], p = x0[k], q = x1[k];
-            x0[k] = p * c - q * s;
-            x1[k] = q * c + p * s;
+            const float p = x0[k], q = x1[k];
+            x0[k] = p * c[k] - q * s[k];
+            x1[k] = q * c[k] + p * s[k];
           }
         } else {
           rotate8<T, VEC>(a.tab, cs, sn, row, 8 * j, x0);
@@ -327,20 +337,29 @@ __global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__
         }
       }
     }
-    const int64_t page = slot >> 4;
-    const int64_t out_row = ((page * 2 + kv) * a.heads + h) * 16 + (slot & 15);
+    const int64_t out_row = ((slot >> 4) * rows + r) * 16 + (slot & 15);   // (rows of a page: keys' heads, then values')
     if constexpr (E4M3) {
-      float most = 0.f;   // the largest finite magnitude, or infinity for a row with a NaN
+      // the largest magnitude, NaN if there is one
+      float most = 0.f;
       if (live) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const float p = fabsf(x0[k]), q = fabsf(x1[k]);
-          most = fmaxf(most, fmaxf(p < INFINITY ? p : p > 0.f ? 0.f : INFINITY, q < INFINITY ? q : q > 0.f ? 0.f : INFINITY));
-        }
+        for (int k = 0; k < 8; ++k) most = max_nan(most, max_nan(fabsf(x0[k]), fabsf(x1[k])));
       }
-      for (int off = per_row >> 1; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, off));
+      for (int off = per_row >> 1; off > 0; off >>= 1) most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, off));
+      const bool nan = most != most;
+      if (__any_sync(0xffffffffu, most == INFINITY)) {   // the largest finite one, then
+        float finite = 0.f;
+        if (live) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) {
+            const float p = fabsf(x0[k]), q = fabsf(x1[k]);
+            finite = fmaxf(finite, fmaxf(p < INFINITY ? p : 0.f, q < INFINITY ? q : 0.f));
+          }
+        }
+        for (int off = per_row >> 1; off > 0; off >>= 1) finite = fmaxf(finite, __shfl_xor_sync(0xffffffffu, finite, off));
+        most = finite;
+      }
       if (!live) continue;
-      const bool nan = most == INFINITY;
       const int e = nan ? 0 : row_exponent(most);
       const float f = __uint_as_float(static_cast<uint32_t>(127 - e) << 23);   // 2^-e, e in [-127, 120]
       uint8_t* out = a.pages + out_row * a.head_dim;
@@ -353,13 +372,15 @@ __global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__
       store_n<__nv_bfloat16, 8, true>(out + 8 * j, x0);
       store_n<__nv_bfloat16, 8, true>(out + half + 8 * j, x1);
     }
+   }
   }
 }
 
 // ---------------------------------------------------------------- expand
-// 16 codes per thread: a 16-byte load, the row's power of two, two 16-byte stores.
-constexpr int kExpandPer = 2;   // pieces of 16 codes per thread
-__global__ void __launch_bounds__(kThreads) expand_kernel(const uint4* __restrict__ pages,
+// Pieces of 8 codes: an 8-byte load, the row's power of two, a 16-byte store, so that a warp's stores are 512 bytes side by
+// side (with 16 codes a thread each store left every other 16 bytes out: 86 % of the copy rate).
+constexpr int kExpandPer = 4;   // pieces of a thread
+__global__ void __launch_bounds__(kThreads) expand_kernel(const uint2* __restrict__ pages,
                                                           const uint8_t* __restrict__ exponents,
                                                           const int32_t* __restrict__ src,
                                                           const int32_t* __restrict__ dst, int64_t n_pages,
@@ -369,7 +390,7 @@ __global__ void __launch_bounds__(kThreads) expand_kernel(const uint4* __restric
   if (s < 0 || s >= n_pages || d < 0 || d >= out_pages) return;
   const int pieces = rows << row_shift;   // of a page
   const int p0 = blockIdx.y * (kThreads * kExpandPer) + threadIdx.x;
-  uint4 c[kExpandPer];
+  uint2 c[kExpandPer];
   float f[kExpandPer];
 #pragma unroll
   for (int i = 0; i < kExpandPer; ++i) {
@@ -382,17 +403,15 @@ __global__ void __launch_bounds__(kThreads) expand_kernel(const uint4* __restric
   for (int i = 0; i < kExpandPer; ++i) {
     const int p = p0 + i * kThreads;
     if (p >= pieces) continue;
-    const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
-    uint32_t r[8];
+    uint32_t r[4];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) {
-      const __half2_raw h2 = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w[k >> 1] >> (16 * (k & 1))), __NV_E4M3);
+    for (int k = 0; k < 4; ++k) {
+      const __half2_raw h2 = __nv_cvt_fp8x2_to_halfraw2(
+          static_cast<__nv_fp8x2_storage_t>((k < 2 ? c[i].x : c[i].y) >> (16 * (k & 1))), __NV_E4M3);
       const float2 v = __half22float2(__half2(h2));
       r[k] = pack_bf16(v.x * f[i], v.y * f[i]);
     }
-    uint4* o = out + 2 * (d * pieces + p);
-    o[0] = make_uint4(r[0], r[1], r[2], r[3]);
-    o[1] = make_uint4(r[4], r[5], r[6], r[7]);
+    out[d * pieces + p] = make_uint4(r[0], r[1], r[2], r[3]);
   }
 }
 
@@ -408,10 +427,10 @@ int sm_count() {
 }
 
 // Tokens of a CTA: one while there are fewer than four CTAs per SM, so that a step's few tokens spread
-// over the SMs; then up to kMaxTokens, which share a launch's fixed costs.
-int tokens_per_cta(int64_t n, int sms) {
+// over the SMs; then up to `most`, which share a launch's fixed costs.
+int tokens_per_cta(int64_t n, int sms, int most) {
   const int64_t t = n / (4 * static_cast<int64_t>(sms));
-  return static_cast<int>(t < 1 ? 1 : t > kMaxTokens ? kMaxTokens : t);
+  return static_cast<int>(t < 1 ? 1 : t > most ? most : t);
 }
 
 template <typename K, typename A>
@@ -558,11 +577,12 @@ int kvprm_rope_rotate(const kvprm_rope* rope, int32_t dtype, int32_t head_dim, c
   if (sms == 0) return operator_fail(KVPRM_ECUDA, "%s: no device", who);
   a.n_x = n_x;
   a.head_dim = head_dim;
-  a.tokens = tokens_per_cta(n_tokens, sms);
+  a.tokens = tokens_per_cta(n_tokens, sms, kRopeTokens);
   const int64_t grid = (n_tokens + a.tokens - 1) / a.tokens;
   if (grid > 0x7FFFFFFF) return operator_fail(KVPRM_EINVAL, "%s: n_tokens %lld", who, static_cast<long long>(n_tokens));
   a.by_unit = FastDiv(static_cast<uint32_t>(vec ? (a.tab.interleaved ? dim : dim / 2) / per : dim / 2));
   a.by_heads = FastDiv(static_cast<uint32_t>(a.heads));
+  a.by_pairs = FastDiv(static_cast<uint32_t>(dim / 2));
   a.by_rest = FastDiv(static_cast<uint32_t>(head_dim > dim ? (head_dim - dim) / (vec ? per : 1) : 1));
   a.positions = positions;
   a.n_tokens = n_tokens;
@@ -612,8 +632,9 @@ int kvprm_cache_write(const kvprm_cache* cache, int32_t dtype, const void* k, in
   a.exponents = static_cast<uint8_t*>(cache->exponents);
   a.heads = cache->n_kv_heads;
   a.head_dim = cache->head_dim;
-  a.tokens = tokens_per_cta(n_tokens, sms);
+  a.tokens = tokens_per_cta(n_tokens, sms, kWriteTokens);
   a.by_rows = FastDiv(static_cast<uint32_t>(2 * a.heads));
+  a.by_pairs = FastDiv(static_cast<uint32_t>(a.tab.dim > 0 ? a.tab.dim / 2 : 1));
   const int64_t grid = (n_tokens + a.tokens - 1) / a.tokens;
   if (grid > 0x7FFFFFFF) return operator_fail(KVPRM_EINVAL, "%s: n_tokens %lld", who, static_cast<long long>(n_tokens));
   const unsigned g = static_cast<unsigned>(grid);
@@ -631,13 +652,13 @@ int kvprm_cache_expand(const kvprm_cache* cache, const int32_t* src, const int32
   if (n < 0 || n > 0x7FFFFFFF || out_pages < 0) return operator_fail(KVPRM_EINVAL, "%s: n %lld, out_pages %lld", who, static_cast<long long>(n), static_cast<long long>(out_pages));
   if (n == 0 || cache->n_pages == 0 || out_pages == 0) return KVPRM_OK;
   if (!src || !dst || !out || !aligned16(out)) return operator_fail(KVPRM_EINVAL, "%s: src, dst or out are NULL, or out is not 16-byte aligned", who);
-  const int rows = 2 * cache->n_kv_heads * 16, shift = cache->head_dim == 128 ? 3 : 2;
+  const int rows = 2 * cache->n_kv_heads * 16, shift = cache->head_dim == 128 ? 4 : 3;
   const int pieces = rows << shift;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(n), static_cast<unsigned>((pieces + kThreads * kExpandPer - 1) / (kThreads * kExpandPer)), 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.stream = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, expand_kernel, static_cast<const uint4*>(cache->pages),
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, expand_kernel, static_cast<const uint2*>(cache->pages),
                                            static_cast<const uint8_t*>(cache->exponents), src, dst, cache->n_pages,
                                            out_pages, rows, shift, static_cast<uint4*>(out));
   if (e != cudaSuccess) return operator_fail(KVPRM_ECUDA, "%s: %s", who, cudaGetErrorString(e));

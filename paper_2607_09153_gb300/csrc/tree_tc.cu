@@ -212,7 +212,7 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
       mbar_init(&st.slot_empty[i], 1);
       mbar_init(&st.draft_go[i], 1);
       mbar_init(&st.raw_full[i], 33);   // the bulk copies' bytes, and each lane's own copies
-      mbar_init(&st.raw_empty[i], kProducers / 32);
+      mbar_init(&st.raw_empty[i], 1);
     }
     mbar_init(&st.q_full, 1);
     mbar_init(&st.q_empty, 1);
@@ -465,9 +465,11 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
         const uint32_t i = n + item, slot = i % SM::kSlots;
         uint8_t* dst = base + SM::kSlot0 + slot * SM::kTile;
         if constexpr (E4M3) {   // every slot is filled here
+          if (i >= SM::kSlots) ok = ok && wait_for(&st.slot_empty[slot], (i / SM::kSlots - 1) & 1u, err);
           if (cached) {
             const uint32_t r = raw % SM::kRaw;
             ok = ok && wait_for(&st.raw_full[r], (raw / SM::kRaw) & 1u, err);
+            if (t == 0 && st.raw_bad[r]) atomicOr(&st.bad[part % kFlagSets], 1);
             const uint8_t* src = base + SM::kRaw0 + r * SM::kRawBytes;
             const int have = p.q.len - c * kChunk;
             constexpr int kParts = HD / 16, kTeam = 32 / kParts;       // pieces of a row; rows of a warp's step
@@ -487,11 +489,6 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
             const bool two = e > 134u && mine < have;
             uint32_t f = (two ? 254u : e + 120u) << 7 | (two ? (e == 255u ? 0x7FC0u : (e - 7u) << 7) : 0x3F80u) << 16;
             if (mine >= have) f = 0x3F800000u;
-            if (t == 0 && st.raw_bad[r]) atomicOr(&st.bad[part % kFlagSets], 1);
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&st.raw_empty[r]);   // the codes are in registers: the next ones may come
-            ++raw;
-            if (i >= SM::kSlots) ok = ok && wait_for(&st.slot_empty[slot], (i / SM::kSlots - 1) & 1u, err);
             auto convert = [&](auto twice) {
 #pragma unroll
               for (int k = 0; k < kSteps; ++k) {
@@ -506,10 +503,11 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
               convert(std::true_type());
             else
               convert(std::false_type());
+            ++raw;
             filled(&st.slot_full[slot]);
+            if (t == 0) mbar_arrive(&st.raw_empty[r]);
             continue;
           }
-          if (i >= SM::kSlots) ok = ok && wait_for(&st.slot_empty[slot], (i / SM::kSlots - 1) & 1u, err);
         } else {
           ok = ok && wait_for(&st.draft_go[slot], (go >> slot) & 1u, err);
           go ^= 1u << slot;
