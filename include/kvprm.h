@@ -688,7 +688,8 @@ KVPRM_API int kvprm_cache_expand(const kvprm_cache* cache, const int32_t* src, c
  *  max_len      about the longest cached length; it sizes the launch, and results
  *               do not depend on it beyond the order of sums
  * Scores, weights' sums and accumulators are fp32; the weights that multiply the
- * values are rounded to bf16, as the output is.
+ * values are rounded to bf16 (an 8-bit cache with up to 32 query rows of a kv
+ * head: fp16, near the sequence's largest power of two), as the output is to bf16.
  * What the host cannot see: a sequence whose length is negative or beyond its
  * block table, or that has a page outside the cache, gets NaN in every output; one whose
  * drafted tokens are not within [0, n_tokens), or more than max_drafts, is left

@@ -7,11 +7,18 @@
 // dimensions that its values' loads held.  Only the queries (the same for all warps) lie in shared memory; nothing waits
 // at a barrier while the cache streams.
 //
-// 8-bit codes become fp16 in registers (one instruction for two; to bf16 it takes nine for four, and ran at 0.7 of this
-// rate), once for both tiles of 32 rows.  What fp16 lacks in range is kept beside it as powers of two: a query row is
+// 8-bit codes become fp16 in registers (one instruction for two; to bf16 it takes nine for four: 8 x 32,768 tokens of 8 kv
+// heads 129 us, so 113), once for both tiles of 32 rows.  What fp16 lacks in range is kept beside it as powers of two: a query row is
 // scaled to a largest magnitude of 1 to 2 (exact but for elements 2^-14 of that and smaller, which lose what is below
 // 2^-25 of it), a key row's power multiplies the scores in fp32, and a value row's multiplies the weights, relative to the
-// largest one met, E: a weight p becomes p 2^(e - E + 10), whose fp16 steps end at 2^-34 of a full weight's.
+// largest one met, E: a weight p becomes p 2^(e - E + 10), whose fp16 steps end at 2^-34 of a full weight's.  A page with a
+// power below 2^-10 of E takes its values' product in bf16 instead, whose range is fp32's: its weights would lose what E,
+// which may stand for a row that is not looked at, leaves out.
+//
+// What bounds it, measured on a GB300, a drafted token per sequence: a bf16 cache memory (8 kv heads of 128, 4 query heads
+// each, 8 x 32,768 tokens in 169 us, 6,370 GB/s), an 8-bit one the instructions of a page (the same in 113 us, 4,790 GB/s;
+// with 7 query heads each over 64 ragged sequences 79 us, 4,260 GB/s): neither more loads in flight, by registers or
+// asynchronous copies, nor a fourth CTA made that faster.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -66,6 +73,10 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
   const __half2 v = __floats2half2_rn(lo, hi);
   return *reinterpret_cast<const uint32_t*>(&v);
 }
+__device__ __forceinline__ uint32_t bf16_of_f16(uint32_t v) {   // exact for codes
+  const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&v));
+  return pack_bf16(f.x, f.y);
+}
 __device__ __forceinline__ float power_of(int field) { return __uint_as_float(static_cast<uint32_t>(field) << 23); }
 
 // Whether one of two bf16 is infinite or NaN; whether one of four bytes is 255.
@@ -80,7 +91,8 @@ __device__ __forceinline__ float power(uint32_t w, int k) {
 }
 
 template <int HD, bool E4M3, int TILES>
-__global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_rows_kernel(const __grid_constant__ TreeLaunch a) {
+__global__ void __launch_bounds__(kThreads, tree_rows_per_sm(TILES))
+    tree_rows_kernel(const __grid_constant__ TreeLaunch a) {
   using G = TreeRows<TILES>;
   constexpr int KS = HD / 16;                       // 16-dim steps of q . k
   constexpr int NT = HD / 8;                        // 8-dim tiles of the output
@@ -213,8 +225,8 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
     // One block's softmax step for one tile: scores s in units of log2 (token 2 c + (i & 1) + 8 n of row gid + 8 (i >> 1))
     // become the weights as an operand, the running maximum, sum and output following.  The maximum moves only when
     // a score passes it by more than a margin (the weights then stay below 2^margin, and most blocks need no exchange
-    // between lanes).  The weights are rounded to bf16, the values' type: their sum is not.
-    auto softmax = [&](int ti, float(&s)[2][4], const float(&vf)[4], uint32_t(&pa)[4], auto codes) {
+    // between lanes).  The weights are rounded to bf16 or fp16, the values' type: their sum is not.
+    auto softmax = [&](int ti, float(&s)[2][4], const float(&vf)[4], uint32_t(&pa)[4], bool fp16) {
       float mx[2];
 #pragma unroll
       for (int h = 0; h < 2; ++h) mx[h] = fmaxf(fmaxf(s[0][2 * h], s[0][2 * h + 1]), fmaxf(s[1][2 * h], s[1][2 * h + 1]));
@@ -245,7 +257,7 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
           const float p0 = ex2_ftz(s[n][2 * h] + nm), p1 = ex2_ftz(s[n][2 * h + 1] + nm);
           l[ti][h] += p0 + p1;
           const float w0 = E4M3 ? p0 * vf[2 * n] : p0, w1 = E4M3 ? p1 * vf[2 * n + 1] : p1;
-          pa[2 * n + h] = decltype(codes)::value ? pack_f16(w0, w1) : pack_bf16(w0, w1);
+          pa[2 * n + h] = E4M3 && fp16 ? pack_f16(w0, w1) : pack_bf16(w0, w1);
         }
       }
     };
@@ -334,10 +346,13 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
           ve = (ve & ~(255u << (8 * k))) | 1u << (8 * k);
         }
       }
+      bool wide = false;   // a value row's power far below E
       if constexpr (E4M3) {
         // a value row's power beyond E + 2 (NaN among them): E moves there and the outputs with it
         const uint32_t most = max(max(ve & 255u, (ve >> 8) & 255u), max((ve >> 16) & 255u, ve >> 24));
-        if (__any_sync(0xffffffffu, static_cast<int>(most) > top_e + 2 || has_255(ke)) || top_e == 0) {
+        const uint32_t least = min(min(ve & 255u, (ve >> 8) & 255u), min((ve >> 16) & 255u, ve >> 24));
+        if (__any_sync(0xffffffffu, static_cast<int>(most) > top_e + 2 || static_cast<int>(least) < top_e - 10 || has_255(ke)) ||
+            top_e == 0) {
           if (__any_sync(0xffffffffu, has_255(ke) || has_255(ve))) poison = true;   // every row sees the page
           uint32_t e = most;
           e = max(e, __shfl_xor_sync(0xffffffffu, e, 1));
@@ -352,6 +367,7 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
               for (int k = 0; k < 4; ++k) o[ti][i][k] *= f;
           top_e = now;
           rel = power_of(264 - now);
+          wide = __any_sync(0xffffffffu, static_cast<int>(least) < now - 10);
         }
       }
       float kf[4], vf[4];
@@ -370,39 +386,49 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
             const float x = s[ti][n][i] * (E4M3 ? kf[2 * n + (i & 1)] * rs[ti][i >> 1] : kf[0]);
             s[ti][n][i] = have < kTreePage && 2 * c + (i & 1) + 8 * n >= have ? -INFINITY : x;   // (a scale may be negative)
           }
-        softmax(ti, s[ti], vf, pa[ti], std::integral_constant<bool, E4M3>());
+        softmax(ti, s[ti], vf, pa[ti], !wide);
       }
+      // the weights' product with the values
+      auto product = [&](auto codes) {
 #pragma unroll
-      for (int w = 0; w < NT / 4; ++w) {   // four 8-dim tiles: a word of codes, or two words of bf16, of each of the lane's tokens
-        uint32_t b0[4], b1[4];
-        if constexpr (E4M3) {
+        for (int w = 0; w < NT / 4; ++w) {   // four 8-dim tiles: a word of codes, or two words of bf16, of each of the lane's tokens
+          uint32_t b0[4], b1[4];
+          if constexpr (E4M3) {
 #pragma unroll
-          for (int x = 0; x < 2; ++x) {
-            const uint32_t t0 = __byte_perm(word(v[0][0], w), word(v[1][0], w), x ? 0x7362 : 0x5140);   // tokens side by side
-            const uint32_t t1 = __byte_perm(word(v[2][0], w), word(v[3][0], w), x ? 0x7362 : 0x5140);
-            b0[2 * x] = codes_lo(t0);
-            b0[2 * x + 1] = codes_hi(t0);
-            b1[2 * x] = codes_lo(t1);
-            b1[2 * x + 1] = codes_hi(t1);
+            for (int x = 0; x < 2; ++x) {
+              const uint32_t t0 = __byte_perm(word(v[0][0], w), word(v[1][0], w), x ? 0x7362 : 0x5140);   // tokens side by side
+              const uint32_t t1 = __byte_perm(word(v[2][0], w), word(v[3][0], w), x ? 0x7362 : 0x5140);
+              b0[2 * x] = codes_lo(t0);
+              b0[2 * x + 1] = codes_hi(t0);
+              b1[2 * x] = codes_lo(t1);
+              b1[2 * x + 1] = codes_hi(t1);
+            }
+          } else {
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const int at_word = 2 * (w & 1) + (x >> 1), sel = x & 1 ? 0x7632 : 0x5410;
+              b0[x] = __byte_perm(word(v[0][w / 2], at_word), word(v[1][w / 2], at_word), sel);
+              b1[x] = __byte_perm(word(v[2][w / 2], at_word), word(v[3][w / 2], at_word), sel);
+            }
           }
-        } else {
 #pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int at_word = 2 * (w & 1) + (x >> 1), sel = x & 1 ? 0x7632 : 0x5410;
-            b0[x] = __byte_perm(word(v[0][w / 2], at_word), word(v[1][w / 2], at_word), sel);
-            b1[x] = __byte_perm(word(v[2][w / 2], at_word), word(v[3][w / 2], at_word), sel);
-          }
+          for (int ti = 0; ti < TILES; ++ti)
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              float(&d)[4] = o[ti][4 * w + x];
+              if constexpr (decltype(codes)::value)
+                mma_f16_16816(d, pa[ti][0], pa[ti][1], pa[ti][2], pa[ti][3], b0[x], b1[x]);
+              else if constexpr (E4M3)
+                mma_bf16_16816(d, pa[ti][0], pa[ti][1], pa[ti][2], pa[ti][3], bf16_of_f16(b0[x]), bf16_of_f16(b1[x]));
+              else
+                mma_bf16_16816(d, pa[ti][0], pa[ti][1], pa[ti][2], pa[ti][3], b0[x], b1[x]);
+            }
         }
-#pragma unroll
-        for (int ti = 0; ti < TILES; ++ti)
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            if constexpr (E4M3)
-              mma_f16_16816(o[ti][4 * w + x], pa[ti][0], pa[ti][1], pa[ti][2], pa[ti][3], b0[x], b1[x]);
-            else
-              mma_bf16_16816(o[ti][4 * w + x], pa[ti][0], pa[ti][1], pa[ti][2], pa[ti][3], b0[x], b1[x]);
-          }
-      }
+      };
+      if (E4M3 && !wide)
+        product(std::integral_constant<bool, E4M3>());
+      else
+        product(std::false_type());
       page = next;
       next = after;
     }
@@ -479,7 +505,7 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(E4M3, TILES)) tree_
               s[ti][n][2 * h + i] = (sees >> (2 * c + i + 8 * n)) & 1u ? s[ti][n][2 * h + i] * a.scale_log2 : -INFINITY;
         }
         const float same[4] = {rel, rel, rel, rel};
-        softmax(ti, s[ti], same, pa[ti], std::false_type());
+        softmax(ti, s[ti], same, pa[ti], false);
       }
 #pragma unroll
       for (int i = 0; i < NT; ++i) {

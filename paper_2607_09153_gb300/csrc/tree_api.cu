@@ -44,23 +44,25 @@ int sm_count(int* sms) {
   return KVPRM_OK;
 }
 
-// More than 16 rows of a kv head go to the tensor cores.  CTAs: as many as run at once.  Pairs of so few blocks that
-// cutting one would cost more than it gives, or one per CTA where all are so short, stay whole: no join follows.
+// More than 32 rows of a kv head go to the tensor cores (us a call, registers / tensor cores: 16 sequences of 4 heads with
+// 28 rows over 400 bf16 tokens 20 / 25, over 3,900 43 / 46; 8 heads with 32 rows over 8 x 32,768 191 / 188, with 24 over
+// ragged 20,000 99 / 82; 63 rows over 3,900 8-bit tokens 57 / 57, 98 rows 92 / 57).  CTAs: as many as run at once.  Pairs of
+// so few blocks that cutting one would cost more than it gives stay whole: no join follows.
 int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   TreePlan p;
   const int64_t rows = int64_t{t.max_drafts} * (t.n_q_heads / c.n_kv_heads);
-  const bool e4m3 = c.format == KVPRM_CACHE_E4M3;
-  p.tc = rows > (e4m3 ? 64 : 16) && c.n_pages > 0;
+  p.tc = rows > 32 && c.n_pages > 0;
   p.rows = p.tc ? 256 : rows > 16 ? 32 : 16;
   const int64_t block = p.tc ? 128 : kTreePage, tiles = ceil_div(rows, p.tc ? 128 : p.rows), lead = 8;
   // the line of a sequence of any length is shorter than this; a launch's stays within 31 bits
-  const int64_t line = (ceil_div(int64_t{kTreePage} * t.max_blocks, block) + ceil_div(t.max_drafts, block) + lead) * (p.tc ? 4 * ceil_div(tiles, 2) : tiles) * c.n_kv_heads;
+  const int64_t depth = ceil_div(int64_t{kTreePage} * t.max_blocks, block) + ceil_div(t.max_drafts, block) + lead;
+  const int64_t line = depth * (p.tc ? 4 * ceil_div(tiles, 2) : tiles) * c.n_kv_heads;
   if (line > 0x7FFFFFFF) return operator_fail(KVPRM_ECAPACITY, "kvprm_tree: block tables of %d pages", t.max_blocks);
   p.seqs = static_cast<int>(std::min<int64_t>({t.n_seqs, kTreeSeqs, 0x7FFFFFFF / line}));
   const int64_t len = std::min<int64_t>(t.max_len, int64_t{kTreePage} * t.max_blocks);
   const int64_t pairs = int64_t{p.seqs} * c.n_kv_heads * ceil_div(rows, p.rows);
   const int64_t blocks = ceil_div(len, block) + ceil_div(t.max_drafts, block);
-  const int64_t most = int64_t{sms} * (p.tc ? 1 : tree_rows_per_sm(e4m3, p.rows / 16));
+  const int64_t most = int64_t{sms} * (p.tc ? 1 : tree_rows_per_sm(p.rows / 16));
   p.whole = blocks <= (p.tc ? 3 : 16);
   p.ctas = static_cast<int>(std::max<int64_t>(1, std::min(most, p.whole ? pairs : pairs * blocks / (p.tc ? 2 : 8))));
   *out = p;

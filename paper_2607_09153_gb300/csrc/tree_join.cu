@@ -27,7 +27,10 @@ __global__ void __launch_bounds__(kThreads) tree_join_kernel(const __grid_consta
   const int group = blockIdx.x % groups, head = blockIdx.x / groups, g = head % a.n_kv, s = head / a.n_kv;
   const TreeSeq q = tree_seq<G::ROWS, G::BLOCK>(a, s);
   const int rows = q.drafts * a.group, row0 = group * kLaneRows;
-  if (row0 >= rows) return;
+  if (row0 >= rows) {
+    if (blockIdx.x == 0) grid_dep_wait();   // no launch of this kernel ends before the attention kernel
+    return;
+  }
   const int tp = row0 / R;
   grid_dep_wait();
   const int32_t off = __ldcg(a.line + s), total = __ldcg(a.line + a.n_seqs), ctas = __ldcg(a.line + a.n_seqs + 1);

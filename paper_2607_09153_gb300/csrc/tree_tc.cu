@@ -1,4 +1,4 @@
-// Attention of drafted tokens over the paged cache on the tensor cores (tcgen05), for more than 16 query
+// Attention of drafted tokens over the paged cache on the tensor cores (tcgen05), for more than 32 query
 // rows (drafted token and head of the kv head's group) per sequence and kv head.
 //
 // A pair (tree.h) is one kv head of a sequence and one or two tiles of 128 query rows; its keys come in
@@ -13,8 +13,12 @@
 //                    converted to bf16 (exact: a power of two per row changes no mantissa)
 //   warp 16          TMA: bf16 pages straight into the tiles, 8-bit pages into a ring of their own
 //   warp 17          issues every MMA, in an order that keeps one unit's S ahead of the other's O
-// Tiles lie in shared memory as rows of 128 bytes under the 128-byte swizzle, [64-column part][128 rows]: a
-// K-major operand for the keys and an MN-major one for the values.
+//
+// What bounds it, measured on a GB300.  Two tiles: the softmax, about 2,100 cycles of the two groups for the
+// chunk's two units, beside 1,024 of matrix products: 8 kv heads, 64 tokens of 4 heads each over 4 x 16,384
+// bf16 tokens in 88 us, 780 TFLOP/s.  One tile: a bf16 chunk memory (its two units overlap), an 8-bit one its
+// conversion, about 2,000 cycles of the eight producer warps for a tile of 128 x 128.  Short calls: what a
+// part begins and ends with, 4 to 5 us, and the join's launch.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>
@@ -107,8 +111,8 @@ __device__ __forceinline__ void column_of(uint32_t (&w)[4]) {
   w[3] = __byte_perm(n2, n3, 0x7531);
 }
 
-// mbar_wait (ptx.cuh) with the barrier's own suspension: most of this kernel's warps wait most of the time, and polling
-// took two thirds of its instructions.
+// mbar_wait (ptx.cuh) with the barrier's own suspension: most of this kernel's warps wait most of the time, and share
+// their schedulers with the softmax.
 __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, int* err) {
   const uint32_t at = smem_u32(bar);
   if (mbar_try_wait(at, parity)) return true;
@@ -198,7 +202,7 @@ __device__ __forceinline__ void in_order(float (&o)[N]) {
 // (a bound of 640 threads: 96 registers, what five warps of a scheduler can have)
 template <int HD, bool E4M3>
 __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__ TreeLaunch a,
-                                                              const __grid_constant__ CUtensorMap map) {
+                                                         const __grid_constant__ CUtensorMap map) {
   using SM = Smem<HD, E4M3>;
   constexpr bool kPaged = !E4M3 && HD == 128;   // (of 64 columns a page's box is in the first layout)
   extern __shared__ uint8_t smem_raw[];
@@ -472,18 +476,17 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
             if (t == 0 && st.raw_bad[r]) atomicOr(&st.bad[part % kFlagSets], 1);
             const uint8_t* src = base + SM::kRaw0 + r * SM::kRawBytes;
             const int have = p.q.len - c * kChunk;
-            constexpr int kParts = HD / 16, kTeam = 32 / kParts;       // pieces of a row; rows of a warp's step
-            constexpr int kSteps = kChunk / (kTeam * kProducers / 32);
-            // the factors of the rows that this warp converts, a row per lane: 2^(e - 127 + 120) as bf16, beyond its range
-            // (or NaN, 255) in two; zero past the length, where the codes may be anything
+            constexpr int kParts = HD / 16, kTeam = 32 / kParts;   // 16-byte pieces of a row; rows of a warp's step
+            constexpr int kApart = kTeam * kProducers / 32, kSteps = kChunk / kApart;   // rows from step to step
             // A row's 8 pieces fill two 64-column parts, whose equal pieces lie in the same banks: lanes 0 to 3 and 4 to
             // 7 take neighbouring rows, which the swizzle puts in different ones.
             const int piece = t % kParts, j = HD == 128 ? (lane >> 4) * 2 + (((lane >> 3) & 1) ^ (piece >> 2)) : lane / kParts;
-            constexpr int kApart = kTeam * kProducers / 32;
             const int row0 = (t >> 5) * kTeam + j;
             uint4 codes[kSteps];
 #pragma unroll
             for (int k = 0; k < kSteps; ++k) codes[k] = *reinterpret_cast<const uint4*>(src + (row0 + k * kApart) * HD + piece * 16);
+            // the factors of the rows that this warp converts, a row per lane: 2^(e - 127 + 120) as bf16, beyond its range
+            // (or NaN, 255) in two; zero past the length, where the codes may be anything
             const int mine = lane % kTeam + (t >> 5) * kTeam + lane / kTeam % kSteps * kApart;
             const uint32_t e = src[SM::kRawCodes + mine];
             const bool two = e > 134u && mine < have;

@@ -454,6 +454,29 @@ def test_tree_small_codes_count(drafts, exponent):
     t.check(t.run())
 
 
+@pytest.mark.parametrize("drafts", [1, 12, 20])
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("weight", ["none", "alike"])
+def test_tree_value_powers_apart(weight, hd, drafts):
+    """Value rows up to 2^70 apart.  "none": the large ones have no weight at all; "alike": weights that fall as the powers
+    rise, so that every power's rows count."""
+    torch, kp = _kp()
+    t = Tree(torch, 2, 1, hd, [333, 40], [drafts, 1], True, seed=13, q_std=0.25)
+    t.q[..., 0] = 16.0
+    away = torch.randint(-30, 41, t.exps[:, 1].shape, generator=_gen(torch, 14), device="cuda")
+    nat = away.double() * math.log(2.0) * hd ** 0.5 / 16   # of dimension 0 of a key: e^-(away ln 2)
+    if weight == "none":
+        nat = torch.where(away > 0, 400.0, 0.0)
+    t.exps[:, 0], t.exps[:, 1] = 127, (120 + away).to(torch.uint8)
+    t.pages[:, 0, ..., 0] = (-nat).clamp(-448, 448).to(torch.float8_e4m3fn)
+    t.pages[:, 0, ..., 1:] = (_randn(torch, t.pages[:, 0, ..., 1:].shape, _gen(torch, 15), torch.float32) * 0.5).to(
+        torch.float8_e4m3fn)
+    t.pages[:, 1] = (_randn(torch, t.pages[:, 1].shape, _gen(torch, 16), torch.float32) * 100).clamp(-448, 448).to(
+        torch.float8_e4m3fn)
+    t.values = t.pages.double() * torch.exp2(t.exps.double() - 127)[..., None]
+    t.check(t.run())
+
+
 @pytest.mark.parametrize("e4m3", [False, True])
 def test_tree_not_finite(e4m3):
     """Drafts that are not finite reach the rows that see them and no others; a NaN in the cache reaches its sequence."""
