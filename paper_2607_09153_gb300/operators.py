@@ -311,6 +311,11 @@ def _scratch(T, need: int, device: int, stream):
         return T.torch.empty(need, dtype=T.torch.uint8, device=T.torch.device("cuda", device))
 
 
+def _capturing(T, stream) -> bool:
+    with T.torch.cuda.stream(stream):
+        return T.capturing()
+
+
 def _workspace_bytes(c: bytes, t: bytes) -> int:
     need = ctypes.c_int64()
     _check(lib().kvprm_tree_workspace(c, t, ctypes.byref(need)))
@@ -361,7 +366,7 @@ def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, ma
         # that is being captured gets scratch of its own (the graph's), for the graph may be replayed on any stream.
         key = (dev, T.raw_stream(dev) if stream is None else stream.cuda_stream)
         w = _workspaces.get(key)
-        capturing = T.capturing()
+        capturing = T.capturing() if stream is None else _capturing(T, stream)
         if capturing:
             w = _scratch(T, _workspace_bytes(c, t), dev, stream)
         rc = KVPRM_ECAPACITY if w is None else _call(T, dev, stream, go, c, t, w.data_ptr(), w.numel())
