@@ -11,14 +11,15 @@
 //   warps 0-3, 4-7   softmax groups (thread = row = lane of tensor memory)
 //   warps 8-15       producers: Q tiles, drafted tokens' keys and values, and with an 8-bit cache every chunk,
 //                    converted to bf16 (exact: a power of two per row changes no mantissa)
-//   warp 16          TMA: bf16 pages straight into the tiles, 8-bit pages into a ring of their own
+//   warp 16          TMA: bf16 pages straight into the tiles
 //   warp 17          issues every MMA, in an order that keeps one unit's S ahead of the other's O
 //
-// What bounds it, measured on a GB300.  Two tiles: the softmax, about 2,100 cycles of the two groups for the
-// chunk's two units, beside 1,024 of matrix products: 8 kv heads, 64 tokens of 4 heads each over 4 x 16,384
-// bf16 tokens in 88 us, 780 TFLOP/s.  One tile: a bf16 chunk memory (its two units overlap), an 8-bit one its
-// conversion, about 2,000 cycles of the eight producer warps for a tile of 128 x 128.  Short calls: what a
-// part begins and ends with, 4 to 5 us, and the join's launch.
+// What bounds it, measured on a GB300.  Two tiles: a group's chain of S (800 cycles: its operands take all of
+// shared memory's bandwidth), softmax (1,500) and O (500), 3,400 cycles a chunk for both groups: 8 kv heads, 64
+// tokens of 4 heads each over 4 x 16,384 bf16 tokens in 81 us, 845 TFLOP/s.  An 8-bit chunk: its conversion, some
+// 2,000 cycles of the eight producer warps for a tile of 128 x 128, which beside two tiles' products takes
+// 3,000: 16 sequences of 4 heads with 126 rows over 9,001 tokens in 94 us (bf16: 71).  Short calls: what a part
+// begins and ends with, 5 and 2 us, and the join.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>
@@ -45,10 +46,9 @@ constexpr int kFlagSets = 8;     // parts whose marks may be in flight (a ring o
 template <int HD, bool E4M3>
 struct Smem {
   static constexpr uint32_t kTile = kChunk * HD * 2;             // one chunk's keys or values, or one tile of Q
-  static constexpr int kSlots = HD == 128 ? (E4M3 ? 3 : 4) : (E4M3 ? 4 : 8);
-  static constexpr int kRaw = E4M3 ? (HD == 128 ? 3 : 6) : 1;
-  static constexpr uint32_t kRawCodes = kChunk * HD;
-  static constexpr uint32_t kRawBytes = kRawCodes + kChunk;      // codes, then the rows' exponents
+  static constexpr int kSlots = HD == 128 ? (E4M3 ? 3 : 4) : 8;
+  static constexpr uint32_t kRaw = 3, kRawCodes = kChunk * HD;     // an 8-bit cache's ring: a chunk's codes,
+  static constexpr uint32_t kRawBytes = kRawCodes + kChunk;        // and its rows' exponents
   static constexpr uint32_t kQ = 0;                              // two tiles
   static constexpr uint32_t kSlot0 = kQ + 2 * kTile;
   static constexpr uint32_t kRaw0 = kSlot0 + kSlots * kTile;
@@ -60,12 +60,11 @@ struct Smem {
 struct Static {   // in static shared memory
   int32_t off[kTreeSeqs + 1];
   int32_t sum[kThreads / 32];
-  uint64_t slot_full[8], slot_empty[8], raw_full[8], raw_empty[8];
+  uint64_t slot_full[8], slot_empty[8];
   uint64_t draft_go[8];   // bf16 cache: a free slot that is the producers' to fill
   uint64_t q_full, q_empty, s_full[2], p_full[2], part_done, o_free;
   uint32_t bad_drafts[kFlagSets][32];   // drafted tokens of a part whose values are not finite
   int bad[kFlagSets];                   // of a part: a page outside the cache, a bad draft (1, 2)
-  int raw_bad[8];                       // a page outside the cache, of a raw slot
   uint32_t tmem;
   int err;   // a wait gave up (after which the CTA's other waits are short, and its rows NaN)
 };
@@ -87,28 +86,15 @@ struct Items {
   }
 };
 
-// Tiles in shared memory: rows of 128 bytes (64 columns) under the 128-byte swizzle.  Q, and keys and values that the
-// producers write for an 8-bit cache: [64-column part][128 rows].  Keys and values of a bf16 cache: as one TMA box per
-// page leaves them, [8 pages][64-column part][16 rows], drafted tokens alike; the matrix products then take a page's
-// first or last 8 rows of all pages at a time (8-row groups a page apart), so that the columns of S, and the rows of V,
-// come in the order of column_of below.  (One box for a page's 64 columns, in the first layout, took 32 boxes a chunk:
-// at about 120 cycles a box the TMA unit, not memory, bounded the call.)
-__device__ __forceinline__ uint32_t swizzled(int row, int piece) {   // of a 16-byte piece of a row, first layout
-  return static_cast<uint32_t>(piece >> 3) * (kRows * 128) + row * 128 + (((piece & 7) ^ (row & 7)) << 4);
-}
-template <int HD, bool PAGED>
-__device__ __forceinline__ uint32_t swizzled_kv(int row, int piece) {
-  if (!PAGED) return swizzled(row, piece);
-  return static_cast<uint32_t>(row >> 4) * (HD * 32) + static_cast<uint32_t>(piece >> 3) * 2048 + (row & 15) * 128 +
+// Tiles in shared memory, 128 rows of HD columns: [8-row group][64-column part][8 rows][128 bytes] under the 128-byte
+// swizzle, a K-major operand (Q, keys) and an MN-major one (values) alike, and what one TMA box per page leaves.  (With
+// [part][128 rows] a page took a box per part, and at about 120 cycles a box the TMA unit, not memory, bounded the call;
+// with [page][part][16 rows] S took twice the instructions of half the columns, and they bounded it.)
+constexpr uint32_t kAtom = 1024;   // eight rows of a part
+template <int HD>
+__device__ __forceinline__ uint32_t swizzled(int row, int piece) {   // of a 16-byte piece of a row
+  return static_cast<uint32_t>(row >> 3) * (HD * 16) + static_cast<uint32_t>(piece >> 3) * kAtom + (row & 7) * 128 +
          (((piece & 7) ^ (row & 7)) << 4);
-}
-// Keys' bits (in their order) as bits of S's columns: byte 2 page + half to byte 8 half + page.
-__device__ __forceinline__ void column_of(uint32_t (&w)[4]) {
-  const uint32_t n0 = w[0], n1 = w[1], n2 = w[2], n3 = w[3];
-  w[0] = __byte_perm(n0, n1, 0x6420);
-  w[1] = __byte_perm(n2, n3, 0x6420);
-  w[2] = __byte_perm(n0, n1, 0x7531);
-  w[3] = __byte_perm(n2, n3, 0x7531);
 }
 
 // mbar_wait (ptx.cuh) with the barrier's own suspension: most of this kernel's warps wait most of the time, and share
@@ -137,6 +123,14 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, int* er
   }
 }
 
+__device__ __forceinline__ void cp_async16(void* dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -204,7 +198,6 @@ template <int HD, bool E4M3>
 __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__ TreeLaunch a,
                                                          const __grid_constant__ CUtensorMap map) {
   using SM = Smem<HD, E4M3>;
-  constexpr bool kPaged = !E4M3 && HD == 128;   // (of 64 columns a page's box is in the first layout)
   extern __shared__ uint8_t smem_raw[];
   __shared__ Static st;
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t{1023});
@@ -212,11 +205,9 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < 8; ++i) {
-      mbar_init(&st.slot_full[i], 1);
+      mbar_init(&st.slot_full[i], E4M3 ? kProducers / 32 : 1);
       mbar_init(&st.slot_empty[i], 1);
       mbar_init(&st.draft_go[i], 1);
-      mbar_init(&st.raw_full[i], 33);   // the bulk copies' bytes, and each lane's own copies
-      mbar_init(&st.raw_empty[i], 1);
     }
     mbar_init(&st.q_full, 1);
     mbar_init(&st.q_empty, 1);
@@ -255,10 +246,10 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
   if (warp == kWarpTma) {
     // ------------------------------------------------ TMA
     const uint64_t pol = policy_evict_normal();
-    uint32_t n = 0, loaded = 0;   // items of earlier parts; raw slots filled
+    uint32_t n = 0;   // items of earlier parts
     bool ok = true;
     auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_for(bar, parity, err)); };
-    for (int part = 0; ok && next_part(); ++part) {
+    for (int part = 0; !E4M3 && ok && next_part(); ++part) {
       const int32_t* table = a.t.block_table + static_cast<int64_t>(a.seq0 + p.s) * a.t.max_blocks;
       const int pages = (p.q.len + kTreePage - 1) / kTreePage;
       const Items items(p);
@@ -276,7 +267,6 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
         int kv;
         const int c = p.c0 + items.chunk(item, &kv);
         const bool cached = c < p.q.cached_blocks;
-        if (E4M3 && !cached) continue;
         if (kv && (c >> 2) > four) {   // (keys are at most a chunk ahead of values)
           ++four;
           ids = ids_next;
@@ -289,63 +279,36 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
           id[i] = __shfl_sync(0xffffffffu, (c >> 2) > four ? ids_next : ids, (c & 3) * kPages + i);
           bad = bad || id[i] == -2;
         }
-        if constexpr (E4M3) {
-          const uint32_t r = loaded % SM::kRaw;
-          if (loaded >= SM::kRaw) ok = wait_all(&st.raw_empty[r], (loaded / SM::kRaw - 1) & 1u);
-          if (!ok) continue;
-          ++loaded;
-          // a page's codes as one bulk copy; its 16 exponents by a lane's own asynchronous copy (a bulk copy costs the TMA
-          // unit about 120 cycles whatever its size)
-          constexpr uint32_t kPageBytes = kTreePage * HD;
-          uint8_t* dst = base + SM::kRaw0 + r * SM::kRawBytes;
-          auto row_of = [&](int32_t page) { return (static_cast<int64_t>(page) * 2 + kv) * a.n_kv + p.g; };
-          const int32_t mine = __shfl_sync(0xffffffffu, (c >> 2) > four ? ids_next : ids, (c & 3) * kPages + lane % kPages);
-          if (lane == 0) {
-            uint32_t good = 0;
-#pragma unroll
-            for (int i = 0; i < kPages; ++i) good += id[i] >= 0 ? 1u : 0u;
-            st.raw_bad[r] = bad;
-            mbar_arrive_expect_tx(&st.raw_full[r], good * kPageBytes);
-#pragma unroll
-            for (int i = 0; i < kPages; ++i)
-              if (id[i] >= 0) bulk_load(dst + i * kPageBytes, a.pages + row_of(id[i]) * kPageBytes, kPageBytes, &st.raw_full[r]);
-          }
-          if (lane < kPages && mine >= 0)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst + SM::kRawCodes + lane * kTreePage)),
-                         "l"(a.exponents + row_of(mine) * kTreePage)
-                         : "memory");
-          asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&st.raw_full[r])) : "memory");
-        } else {
-          // This warp waits for every use of a slot, also where the producers fill it: a wait by parity sees only
-          // the phase before the present one, so none may be left out.
-          const uint32_t i = n + item, slot = i % SM::kSlots;
-          if (i >= SM::kSlots) ok = wait_all(&st.slot_empty[slot], (i / SM::kSlots - 1) & 1u);
-          if (!ok || lane != 0) continue;
-          if (!cached) {
-            mbar_arrive(&st.draft_go[slot]);
-            continue;
-          }
-          // (a part's marks are set once a slot of it is free: no earlier part then holds the same set)
-          if (bad) atomicOr(&st.bad[part % kFlagSets], 1);
-          mbar_arrive_expect_tx(&st.slot_full[slot], SM::kTile);
-          // a box is a page's rows of one head; a place without a page reads one that does not exist and arrives as zeros
-          uint8_t* dst = base + SM::kSlot0 + slot * SM::kTile;
-#pragma unroll
-          for (int k = 0; k < kPages; ++k)
-            tma_load_5d(dst + k * (HD * 32), &map, &st.slot_full[slot], 0, 0, 0, p.g, id[k] >= 0 ? 2 * id[k] + kv : -1, pol);
+        // This warp waits for every use of a slot, also where the producers fill it: a wait by parity sees only
+        // the phase before the present one, so none may be left out.
+        const uint32_t i = n + item, slot = i % SM::kSlots;
+        if (i >= SM::kSlots) ok = wait_all(&st.slot_empty[slot], (i / SM::kSlots - 1) & 1u);
+        if (!ok || lane != 0) continue;
+        if (!cached) {
+          mbar_arrive(&st.draft_go[slot]);
+          continue;
         }
+        // (a part's marks are set once a slot of it is free: no earlier part then holds the same set)
+        if (bad) atomicOr(&st.bad[part % kFlagSets], 1);
+        mbar_arrive_expect_tx(&st.slot_full[slot], SM::kTile);
+        // a box is a page's rows of one head; a place without a page reads one that does not exist and arrives as zeros
+        uint8_t* dst = base + SM::kSlot0 + slot * SM::kTile;
+#pragma unroll
+        for (int k = 0; k < kPages; ++k)
+          tma_load_5d(dst + k * (HD * 32), &map, &st.slot_full[slot], 0, 0, 0, 0,
+                      id[k] >= 0 ? (2 * id[k] + kv) * a.n_kv + p.g : -1, pol);
       }
       n += items.n;
     }
-    // Nothing of this warp's is in flight when the CTA ends: the matrix products (or the producers) waited for every
-    // load.  After a wait that gave up, a millisecond is far beyond a load's time.
+    // Nothing of this warp's is in flight when the CTA ends: the matrix products waited for every load.  After a wait
+    // that gave up, a millisecond is far beyond a load's time.
     if (!ok) {
       const uint64_t t0 = global_timer_ns();
       while (global_timer_ns() - t0 < 1000000ull) __nanosleep(1000);
     }
   } else if (warp == kWarpMma) {
     // ------------------------------------------------ MMA
-    const uint32_t id_s = idesc_bf16_f32(kRows, kPaged ? kChunk / 2 : kChunk), id_o = idesc_bf16_f32(kRows, HD) | kIdescMnMajorB;
+    const uint32_t id_s = idesc_bf16_f32(kRows, kChunk), id_o = idesc_bf16_f32(kRows, HD) | kIdescMnMajorB;
     auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_for(bar, parity, err)); };
     uint32_t n = 0, phase = 0;   // phase: per group, the parity of its next p_full
     bool ok = true;
@@ -360,23 +323,12 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
         ok = ok && wait_all(&st.slot_full[slot], (i / SM::kSlots) & 1u);
         if (!ok) return;
         tc_fence_after();
-        const uint64_t qd = desc_sw128(smem_u32(base + SM::kQ + (p.tiles == 2 ? g : 0) * SM::kTile));
-        const uint32_t keys = smem_u32(base + SM::kSlot0 + slot * SM::kTile);
-        if constexpr (kPaged) {
-          const uint64_t kd = desc_sw128_s(keys, 16, HD * 32);
+        const uint64_t qd = desc_sw128_s(smem_u32(base + SM::kQ + (p.tiles == 2 ? g : 0) * SM::kTile), 16, HD * 16);
+        const uint64_t kd = desc_sw128_s(smem_u32(base + SM::kSlot0 + slot * SM::kTile), 16, HD * 16);
 #pragma unroll
-          for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int k = 0; k < HD / 16; ++k)
-              umma_bf16_w(tmem + kColS + g * 128 + h * 64, qd + (((k >> 2) * (kRows * 128) + (k & 3) * 32) >> 4),
-                          kd + (((k >> 2) * 2048 + h * 1024 + (k & 3) * 32) >> 4), id_s, k > 0 ? 1u : 0u);
-        } else {
-          const uint64_t kd = desc_sw128(keys);
-#pragma unroll
-          for (int k = 0; k < HD / 16; ++k) {
-            const uint32_t step = ((k >> 2) * (kRows * 128) + (k & 3) * 32) >> 4;
-            umma_bf16_w(tmem + kColS + g * 128, qd + step, kd + step, id_s, k > 0 ? 1u : 0u);
-          }
+        for (int k = 0; k < HD / 16; ++k) {
+          const uint32_t step = ((k >> 2) * kAtom + (k & 3) * 32) >> 4;
+          umma_bf16_w(tmem + kColS + g * 128, qd + step, kd + step, id_s, k > 0 ? 1u : 0u);
         }
         umma_commit_w(&st.s_full[g]);
         if (p.tiles == 1 || g == 1) umma_commit_w(&st.slot_empty[slot]);
@@ -397,20 +349,18 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
           if (p.c0 + c == p.q.cached_blocks - 1 && (have & 15) != 0 && (p.tiles == 1 || g == 0)) {
             const int rows = 16 - (have & 15);
             for (int x = lane; x < rows * (HD / 8); x += 32)
-              *reinterpret_cast<uint4*>(tile + swizzled_kv<HD, kPaged>(have + x / (HD / 8), x % (HD / 8))) =
+              *reinterpret_cast<uint4*>(tile + swizzled<HD>(have + x / (HD / 8), x % (HD / 8))) =
                   make_uint4(0u, 0u, 0u, 0u);
             fence_proxy_async_smem();
             __syncwarp();
           }
         }
         tc_fence_after();
-        const uint64_t vd = kPaged ? desc_sw128_s(smem_u32(tile), 2048, HD * 32) : desc_sw128_mn(smem_u32(tile), kRows * 128);
+        const uint64_t vd = desc_sw128_s(smem_u32(tile), kAtom, HD * 16);
         const uint32_t pt = tmem + kColS + g * 128;
 #pragma unroll
-        for (int k = 0; k < kChunk / 16; ++k)   // 16 rows: 8 of two pages each, or of their own
-          umma_bf16_ta_w(tmem + kColO + g * 128, pt + k * 8,
-                         vd + ((kPaged ? (k & 3) * 2 * HD * 32 + (k >> 2) * 1024 : k * 2048) >> 4), id_o,
-                         k > 0 || j >= 2 ? 1u : 0u);
+        for (int k = 0; k < kChunk / 16; ++k)
+          umma_bf16_ta_w(tmem + kColO + g * 128, pt + k * 8, vd + (k * (HD * 32) >> 4), id_o, k > 0 || j >= 2 ? 1u : 0u);
         if (p.tiles == 1 || g == 1) umma_commit_w(&st.slot_empty[slot]);
       };
       if (ok) issue_s(0);
@@ -426,16 +376,63 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
   } else if (warp >= 8 && warp < 16) {
     // ------------------------------------------------ producers
     const int t = threadIdx.x - 256;
-    uint32_t n = 0, raw = 0, go = 0;   // go: per slot, the parity of its next draft_go
+    uint32_t n = 0, go = 0;   // go: per slot, the parity of its next draft_go
     bool ok = true;
     auto filled = [&](uint64_t* bar) {   // this tile's writes, seen by the tensor cores, then its barrier
       fence_proxy_async_smem();
       named_bar_sync(2, kProducers);
       if (t == 0) mbar_arrive(bar);
     };
+    auto slot_filled = [&](uint64_t* bar) {   // a slot's: with an 8-bit cache each warp goes on by itself
+      if constexpr (E4M3) {
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(bar);
+      } else {
+        filled(bar);
+      }
+    };
+    // An 8-bit chunk's keys or values: a warp has one page, which it copies into its own places of a ring two items ahead
+    // and converts kTeam rows at a time.  A row's 8 pieces fill two 64-column parts, whose equal pieces lie in the same
+    // banks: lanes 0 to 3 and 4 to 7 take neighbouring rows, which the swizzle puts in different ones.
+    constexpr int kParts = HD / 16, kTeam = 32 / kParts, kSteps = kTreePage / kTeam;   // 16-byte pieces of a row
+    constexpr uint32_t kPageBytes = kTreePage * HD;
+    const int my_page = t >> 5, my_piece = lane % kParts;
+    const int my_row = HD == 128 ? (lane >> 4) * 2 + (((lane >> 3) & 1) ^ (my_piece >> 2)) : lane / kParts;   // of a step's
     const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale turns Q's signs instead
     for (int part = 0; next_part(); ++part) {
       const int rows = p.q.drafts * a.group;
+      const Items items(p);
+      const int32_t* table = a.t.block_table + static_cast<int64_t>(a.seq0 + p.s) * a.t.max_blocks;
+      const int pages = (p.q.len + kTreePage - 1) / kTreePage;
+      auto page_of = [&](int item) {   // -1: no page there, -2: not a page of the cache
+        int kv;
+        const int at = item < items.n ? (p.c0 + items.chunk(item, &kv)) * kPages + my_page : pages;
+        if (at >= pages) return -1;
+        const int32_t page = __ldg(table + at);
+        return page < 0 || page >= a.n_pages ? -2 : page;
+      };
+      uint32_t bad = 0;   // items (modulo 4) with a page outside the cache
+      auto load = [&](int item, int32_t page) {
+        if (page == -2) bad |= 1u << (item & 3);
+        if (page < 0) return;
+        int kv;
+        items.chunk(item, &kv);
+        uint8_t* dst = base + SM::kRaw0 + (n + item) % SM::kRaw * SM::kRawBytes + my_page * kPageBytes;
+        const int64_t row = ((static_cast<int64_t>(page) * 2 + kv) * a.n_kv + p.g) * kTreePage;
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) cp_async16(dst + k * 512 + lane * 16, a.pages + row * HD + k * 512 + lane * 16);
+        if (lane == 0) cp_async16(dst + SM::kRawCodes - my_page * (kPageBytes - kTreePage), a.exponents + row);
+      };
+      int32_t page = -1;
+      if constexpr (E4M3) {
+        const int32_t page0 = page_of(0), page1 = page_of(1);
+        page = page_of(2);
+        load(0, page0);
+        cp_async_commit();
+        load(1, page1);
+        cp_async_commit();
+      }
       if (part > 0) ok = ok && wait_for(&st.q_empty, (part - 1) & 1u, err);
       constexpr int kPieces = HD / 8, kStep = kProducers / kPieces;   // a thread's rows are kStep apart
       for (int tile = 0; tile < p.tiles; ++tile) {
@@ -456,11 +453,10 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
 #pragma unroll
         for (int i = 0; i < kRows / kStep; ++i) {
           v[i] = make_uint4(v[i].x ^ flip, v[i].y ^ flip, v[i].z ^ flip, v[i].w ^ flip);
-          *reinterpret_cast<uint4*>(dst + swizzled(first + i * kStep, piece)) = E4M3 ? paired(v[i]) : v[i];
+          *reinterpret_cast<uint4*>(dst + swizzled<HD>(first + i * kStep, piece)) = E4M3 ? paired(v[i]) : v[i];
         }
       }
       filled(&st.q_full);
-      const Items items(p);
       for (int item = 0; item < items.n; ++item) {
         int kv;
         const int c = p.c0 + items.chunk(item, &kv);
@@ -469,46 +465,42 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
         const uint32_t i = n + item, slot = i % SM::kSlots;
         uint8_t* dst = base + SM::kSlot0 + slot * SM::kTile;
         if constexpr (E4M3) {   // every slot is filled here
+          load(item + 2, page);
+          cp_async_commit();
+          page = page_of(item + 3);
+          cp_async_wait<2>();
+          __syncwarp();
           if (i >= SM::kSlots) ok = ok && wait_for(&st.slot_empty[slot], (i / SM::kSlots - 1) & 1u, err);
           if (cached) {
-            const uint32_t r = raw % SM::kRaw;
-            ok = ok && wait_for(&st.raw_full[r], (raw / SM::kRaw) & 1u, err);
-            if (t == 0 && st.raw_bad[r]) atomicOr(&st.bad[part % kFlagSets], 1);
-            const uint8_t* src = base + SM::kRaw0 + r * SM::kRawBytes;
-            const int have = p.q.len - c * kChunk;
-            constexpr int kParts = HD / 16, kTeam = 32 / kParts;   // 16-byte pieces of a row; rows of a warp's step
-            constexpr int kApart = kTeam * kProducers / 32, kSteps = kChunk / kApart;   // rows from step to step
-            // A row's 8 pieces fill two 64-column parts, whose equal pieces lie in the same banks: lanes 0 to 3 and 4 to
-            // 7 take neighbouring rows, which the swizzle puts in different ones.
-            const int piece = t % kParts, j = HD == 128 ? (lane >> 4) * 2 + (((lane >> 3) & 1) ^ (piece >> 2)) : lane / kParts;
-            const int row0 = (t >> 5) * kTeam + j;
+            if (lane == 0 && (bad >> (item & 3)) & 1u) atomicOr(&st.bad[part % kFlagSets], 1);
+            bad &= ~(1u << (item & 3));
+            const uint8_t* src = base + SM::kRaw0 + i % SM::kRaw * SM::kRawBytes;
             uint4 codes[kSteps];
 #pragma unroll
-            for (int k = 0; k < kSteps; ++k) codes[k] = *reinterpret_cast<const uint4*>(src + (row0 + k * kApart) * HD + piece * 16);
-            // the factors of the rows that this warp converts, a row per lane: 2^(e - 127 + 120) as bf16, beyond its range
-            // (or NaN, 255) in two; zero past the length, where the codes may be anything
-            const int mine = lane % kTeam + (t >> 5) * kTeam + lane / kTeam % kSteps * kApart;
-            const uint32_t e = src[SM::kRawCodes + mine];
-            const bool two = e > 134u && mine < have;
+            for (int k = 0; k < kSteps; ++k)
+              codes[k] = *reinterpret_cast<const uint4*>(src + my_page * kPageBytes + (k * kTeam + my_row) * HD + my_piece * 16);
+            // the factor of a row, per lane: 2^(e - 127 + 120) as bf16, beyond its range (or NaN, 255) in two; zero past the
+            // length, where the codes may be anything
+            const uint32_t e = src[SM::kRawCodes + my_page * kTreePage + lane % kTreePage];
+            const bool live = my_page * kTreePage + lane % kTreePage < p.q.len - c * kChunk, two = e > 134u && live;
             uint32_t f = (two ? 254u : e + 120u) << 7 | (two ? (e == 255u ? 0x7FC0u : (e - 7u) << 7) : 0x3F80u) << 16;
-            if (mine >= have) f = 0x3F800000u;
+            if (!live) f = 0x3F800000u;
             auto convert = [&](auto twice) {
 #pragma unroll
               for (int k = 0; k < kSteps; ++k) {
-                const uint32_t fr = __shfl_sync(0xffffffffu, f, j + kTeam * k);
+                const uint32_t fr = __shfl_sync(0xffffffffu, f, my_row + kTeam * k);
                 uint4 lo, hi;
                 bf16_of16<decltype(twice)::value>(codes[k], __byte_perm(fr, 0, 0x1010), __byte_perm(fr, 0, 0x3232), &lo, &hi);
-                *reinterpret_cast<uint4*>(dst + swizzled(row0 + k * kApart, 2 * piece)) = lo;
-                *reinterpret_cast<uint4*>(dst + swizzled(row0 + k * kApart, 2 * piece + 1)) = hi;
+                const int row = my_page * kTreePage + k * kTeam + my_row;
+                *reinterpret_cast<uint4*>(dst + swizzled<HD>(row, 2 * my_piece)) = lo;
+                *reinterpret_cast<uint4*>(dst + swizzled<HD>(row, 2 * my_piece + 1)) = hi;
               }
             };
             if (__any_sync(0xffffffffu, two))
               convert(std::true_type());
             else
               convert(std::false_type());
-            ++raw;
-            filled(&st.slot_full[slot]);
-            if (t == 0) mbar_arrive(&st.raw_empty[r]);
+            slot_filled(&st.slot_full[slot]);
             continue;
           }
         } else {
@@ -537,9 +529,9 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
               }
             }
           }
-          *reinterpret_cast<uint4*>(dst + swizzled_kv<HD, kPaged>(row, piece)) = E4M3 ? paired(v) : v;
+          *reinterpret_cast<uint4*>(dst + swizzled<HD>(row, piece)) = E4M3 ? paired(v) : v;
         }
-        filled(&st.slot_full[slot]);
+        slot_filled(&st.slot_full[slot]);
       }
       n += items.n;
     }
@@ -585,7 +577,6 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
                           : 0u;
           }
         }
-        if (kPaged && !all) column_of(sees);
         ok = ok && __all_sync(0xffffffffu, wait_for(&st.s_full[g], uses & 1u, err));
         tc_fence_after();
         if (ok && warp_live) {
@@ -780,13 +771,14 @@ cudaError_t launch(const TreeLaunch& a, const CUtensorMap& map, int ctas, cudaSt
   return cudaLaunchKernelEx(&cfg, tree_tc_kernel<HD, E4M3>, a, map);
 }
 
-// Pages [n_pages][2][n_kv][16][hd] as (column of 64, row, 64-column part, kv head, 2 page + {0: keys, 1: values}); a box is
-// one page's keys or values of one head, landing as [part][16 rows][128 bytes] under the 128-byte swizzle.
+// Pages [n_pages][2][n_kv][16][hd] as (column of 64, row of 8, 64-column part, half of the page's rows, (2 page + {0: keys,
+// 1: values}) n_kv + kv head); a box is one page's keys or values of one head.
 CUresult encode_pages(PFN_cuTensorMapEncodeTiled_v12000 encode, CUtensorMap* map, const kvprm_cache& c) {
-  const cuuint64_t row = static_cast<cuuint64_t>(c.head_dim) * 2, parts = c.head_dim / 64, heads = c.n_kv_heads;
-  const cuuint64_t dims[5] = {64, kTreePage, parts, heads, static_cast<cuuint64_t>(c.n_pages) * 2};
-  const cuuint64_t strides[4] = {row, 128, kTreePage * row, heads * kTreePage * row};
-  const cuuint32_t box[5] = {64, kTreePage, static_cast<cuuint32_t>(parts), 1, 1}, step[5] = {1, 1, 1, 1, 1};
+  const cuuint64_t row = static_cast<cuuint64_t>(c.head_dim) * 2, parts = c.head_dim / 64;
+  if (c.n_pages > 0x7FFFFFFF / (2 * int64_t{c.n_kv_heads})) return CUDA_ERROR_INVALID_VALUE;   // coordinates are 32-bit
+  const cuuint64_t dims[5] = {64, 8, parts, 2, static_cast<cuuint64_t>(c.n_pages) * 2 * c.n_kv_heads};
+  const cuuint64_t strides[4] = {row, 128, 8 * row, kTreePage * row};
+  const cuuint32_t box[5] = {64, 8, static_cast<cuuint32_t>(parts), 2, 1}, step[5] = {1, 1, 1, 1, 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, c.pages, dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
