@@ -16,9 +16,9 @@
 //
 // What bounds it, measured on a GB300.  Two tiles: a group's chain of S (800 cycles: its operands take all of
 // shared memory's bandwidth), softmax (1,500) and O (500), 3,400 cycles a chunk for both groups: 8 kv heads, 64
-// tokens of 4 heads each over 4 x 16,384 bf16 tokens in 81 us, 845 TFLOP/s.  An 8-bit chunk: its conversion, some
-// 2,000 cycles of the eight producer warps for a tile of 128 x 128, which beside two tiles' products takes
-// 3,000: 16 sequences of 4 heads with 126 rows over 9,001 tokens in 94 us (bf16: 71).  Short calls: what a part
+// tokens of 4 heads each over 4 x 16,384 bf16 tokens in 80 us, 860 TFLOP/s.  An 8-bit chunk: its conversion, some
+// 1,800 cycles of the eight producer warps for a tile of 128 x 128, which beside two tiles' products takes
+// 2,800: 16 sequences of 4 heads with 126 rows over 9,001 tokens in 84 us (bf16: 70).  Short calls: what a part
 // begins and ends with, 5 and 2 us, and the join.
 #include <cuda.h>
 #include <cudaTypedefs.h>
@@ -47,12 +47,9 @@ template <int HD, bool E4M3>
 struct Smem {
   static constexpr uint32_t kTile = kChunk * HD * 2;             // one chunk's keys or values, or one tile of Q
   static constexpr int kSlots = HD == 128 ? (E4M3 ? 3 : 4) : 8;
-  static constexpr uint32_t kRaw = 3, kRawCodes = kChunk * HD;     // an 8-bit cache's ring: a chunk's codes,
-  static constexpr uint32_t kRawBytes = kRawCodes + kChunk;        // and its rows' exponents
   static constexpr uint32_t kQ = 0;                              // two tiles
   static constexpr uint32_t kSlot0 = kQ + 2 * kTile;
-  static constexpr uint32_t kRaw0 = kSlot0 + kSlots * kTile;
-  static constexpr uint32_t kMl = kRaw0 + (E4M3 ? kRaw * kRawBytes : 0);   // float2 [2][128]
+  static constexpr uint32_t kMl = kSlot0 + kSlots * kTile;   // float2 [2][128]
   static constexpr uint32_t kEnd = kMl + 2 * kRows * 8;
   static constexpr size_t kDynamic = kEnd + 1024;
 };
@@ -66,6 +63,8 @@ struct Static {   // in static shared memory
   uint32_t bad_drafts[kFlagSets][32];   // drafted tokens of a part whose values are not finite
   int bad[kFlagSets];                   // of a part: a page outside the cache, a bad draft (1, 2)
   uint32_t tmem;
+  TreePart part[8];                     // of the softmax warps, and where they are on the line (in registers the two made
+  int4 walk[8];                         // the loop over chunks spill)
   int err;   // a wait gave up (after which the CTA's other waits are short, and its rows NaN)
 };
 
@@ -123,13 +122,12 @@ __device__ __forceinline__ bool wait_for(uint64_t* bar, uint32_t parity, int* er
   }
 }
 
-__device__ __forceinline__ void cp_async16(void* dst, const void* src) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(dst)), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+__device__ __forceinline__ uint4 ldg_stream(const void* p) {
+  uint4 r;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+               : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
+               : "l"(p));
+  return r;
 }
 __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   uint32_t r;
@@ -150,6 +148,25 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c) {
       : "=l"(reinterpret_cast<uint64_t&>(r))
       : "l"(reinterpret_cast<uint64_t&>(a)), "l"(reinterpret_cast<uint64_t&>(b)), "l"(reinterpret_cast<uint64_t&>(c)));
   return r;
+}
+// A product's steps are issued by one lane in a branch of its own, with descriptors at fixed steps from a base: some ten
+// instructions a step.  (With the warp converged, an elected lane per step, each took forty.)
+__device__ __forceinline__ bool elect_lane() {
+  uint32_t r;
+  asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xffffffff;\n\tselp.u32 %0, 1, 0, e;\n\t}" : "=r"(r));
+  return r != 0;
+}
+__device__ __forceinline__ void umma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void umma_ta(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate)
+      : "memory");
 }
 __device__ __forceinline__ float2 add2(float2 a, float2 b) {
   float2 r;
@@ -238,7 +255,7 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
   const int me = blockIdx.x;
   const bool idle = me >= shares.ctas || total == 0;
   int32_t u = idle ? 0 : shares.begin(me);
-  const int32_t u_end = idle ? 0 : shares.begin(me + 1);
+  int32_t u_end = idle ? 0 : shares.begin(me + 1);
   int s = idle ? 0 : tree_find(st.off, a.n_seqs, u);
   TreePart p;
   auto next_part = [&]() { return tree_next<TreeTc>(a, st.off, u, u_end, s, p); };
@@ -325,11 +342,14 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
         tc_fence_after();
         const uint64_t qd = desc_sw128_s(smem_u32(base + SM::kQ + (p.tiles == 2 ? g : 0) * SM::kTile), 16, HD * 16);
         const uint64_t kd = desc_sw128_s(smem_u32(base + SM::kSlot0 + slot * SM::kTile), 16, HD * 16);
+        if (elect_lane()) {
 #pragma unroll
-        for (int k = 0; k < HD / 16; ++k) {
-          const uint32_t step = ((k >> 2) * kAtom + (k & 3) * 32) >> 4;
-          umma_bf16_w(tmem + kColS + g * 128, qd + step, kd + step, id_s, k > 0 ? 1u : 0u);
+          for (int k = 0; k < HD / 16; ++k) {
+            const uint32_t step = ((k >> 2) * kAtom + (k & 3) * 32) >> 4;
+            umma(tmem + kColS + g * 128, qd + step, kd + step, id_s, k > 0 ? 1u : 0u);
+          }
         }
+        __syncwarp();
         umma_commit_w(&st.s_full[g]);
         if (p.tiles == 1 || g == 1) umma_commit_w(&st.slot_empty[slot]);
         if (j == units - 1) umma_commit_w(&st.q_empty);
@@ -358,9 +378,12 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
         tc_fence_after();
         const uint64_t vd = desc_sw128_s(smem_u32(tile), kAtom, HD * 16);
         const uint32_t pt = tmem + kColS + g * 128;
+        if (elect_lane()) {
 #pragma unroll
-        for (int k = 0; k < kChunk / 16; ++k)
-          umma_bf16_ta_w(tmem + kColO + g * 128, pt + k * 8, vd + (k * (HD * 32) >> 4), id_o, k > 0 || j >= 2 ? 1u : 0u);
+          for (int k = 0; k < kChunk / 16; ++k)
+            umma_ta(tmem + kColO + g * 128, pt + k * 8, vd + (k * (HD * 32) >> 4), id_o, k > 0 || j >= 2 ? 1u : 0u);
+        }
+        __syncwarp();
         if (p.tiles == 1 || g == 1) umma_commit_w(&st.slot_empty[slot]);
       };
       if (ok) issue_s(0);
@@ -392,11 +415,11 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
         filled(bar);
       }
     };
-    // An 8-bit chunk's keys or values: a warp has one page, which it copies into its own places of a ring two items ahead
-    // and converts kTeam rows at a time.  A row's 8 pieces fill two 64-column parts, whose equal pieces lie in the same
-    // banks: lanes 0 to 3 and 4 to 7 take neighbouring rows, which the swizzle puts in different ones.
+    // An 8-bit chunk's keys or values: a warp has one page, whose codes it loads an item ahead and converts kTeam rows at
+    // a time; it waits for slots and hands them on by itself.  A row's 8 pieces fill two 64-column parts, whose equal
+    // pieces lie in the same banks: lanes 0 to 3 and 4 to 7 take neighbouring rows, which the swizzle puts in different
+    // ones.
     constexpr int kParts = HD / 16, kTeam = 32 / kParts, kSteps = kTreePage / kTeam;   // 16-byte pieces of a row
-    constexpr uint32_t kPageBytes = kTreePage * HD;
     const int my_page = t >> 5, my_piece = lane % kParts;
     const int my_row = HD == 128 ? (lane >> 4) * 2 + (((lane >> 3) & 1) ^ (my_piece >> 2)) : lane / kParts;   // of a step's
     const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale turns Q's signs instead
@@ -413,25 +436,26 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
         return page < 0 || page >= a.n_pages ? -2 : page;
       };
       uint32_t bad = 0;   // items (modulo 4) with a page outside the cache
+      uint4 next[kSteps];
+      uint32_t next_e = 0;
       auto load = [&](int item, int32_t page) {
         if (page == -2) bad |= 1u << (item & 3);
         if (page < 0) return;
         int kv;
         items.chunk(item, &kv);
-        uint8_t* dst = base + SM::kRaw0 + (n + item) % SM::kRaw * SM::kRawBytes + my_page * kPageBytes;
         const int64_t row = ((static_cast<int64_t>(page) * 2 + kv) * a.n_kv + p.g) * kTreePage;
+        const uint8_t* src = a.pages + row * HD + my_row * HD + my_piece * 16;
 #pragma unroll
-        for (int k = 0; k < kSteps; ++k) cp_async16(dst + k * 512 + lane * 16, a.pages + row * HD + k * 512 + lane * 16);
-        if (lane == 0) cp_async16(dst + SM::kRawCodes - my_page * (kPageBytes - kTreePage), a.exponents + row);
+        for (int k = 0; k < kSteps; ++k) next[k] = ldg_stream(src + k * 512);
+        next_e = __ldg(a.exponents + row + lane % kTreePage);
       };
       int32_t page = -1;
       if constexpr (E4M3) {
-        const int32_t page0 = page_of(0), page1 = page_of(1);
-        page = page_of(2);
+#pragma unroll
+        for (int k = 0; k < kSteps; ++k) next[k] = make_uint4(0u, 0u, 0u, 0u);
+        const int32_t page0 = page_of(0);
+        page = page_of(1);
         load(0, page0);
-        cp_async_commit();
-        load(1, page1);
-        cp_async_commit();
       }
       if (part > 0) ok = ok && wait_for(&st.q_empty, (part - 1) & 1u, err);
       constexpr int kPieces = HD / 8, kStep = kProducers / kPieces;   // a thread's rows are kStep apart
@@ -465,23 +489,18 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
         const uint32_t i = n + item, slot = i % SM::kSlots;
         uint8_t* dst = base + SM::kSlot0 + slot * SM::kTile;
         if constexpr (E4M3) {   // every slot is filled here
-          load(item + 2, page);
-          cp_async_commit();
-          page = page_of(item + 3);
-          cp_async_wait<2>();
-          __syncwarp();
           if (i >= SM::kSlots) ok = ok && wait_for(&st.slot_empty[slot], (i / SM::kSlots - 1) & 1u, err);
+          uint4 codes[kSteps];
+#pragma unroll
+          for (int k = 0; k < kSteps; ++k) codes[k] = next[k];
+          const uint32_t e = next_e;
+          load(item + 1, page);
+          page = page_of(item + 2);
           if (cached) {
             if (lane == 0 && (bad >> (item & 3)) & 1u) atomicOr(&st.bad[part % kFlagSets], 1);
             bad &= ~(1u << (item & 3));
-            const uint8_t* src = base + SM::kRaw0 + i % SM::kRaw * SM::kRawBytes;
-            uint4 codes[kSteps];
-#pragma unroll
-            for (int k = 0; k < kSteps; ++k)
-              codes[k] = *reinterpret_cast<const uint4*>(src + my_page * kPageBytes + (k * kTeam + my_row) * HD + my_piece * 16);
             // the factor of a row, per lane: 2^(e - 127 + 120) as bf16, beyond its range (or NaN, 255) in two; zero past the
             // length, where the codes may be anything
-            const uint32_t e = src[SM::kRawCodes + my_page * kTreePage + lane % kTreePage];
             const bool live = my_page * kTreePage + lane % kTreePage < p.q.len - c * kChunk, two = e > 134u && live;
             uint32_t f = (two ? 254u : e + 120u) << 7 | (two ? (e == 255u ? 0x7FC0u : (e - 7u) << 7) : 0x3F80u) << 16;
             if (!live) f = 0x3F800000u;
@@ -545,19 +564,26 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
     uint32_t uses = 0;
     bool ok = true;
     for (int part = 0; next_part(); ++part) {
-      const bool both = p.tiles == 2;   // the groups have a tile each, else alternate chunks of one
-      const int rows = p.q.drafts * a.group, row = (2 * p.tp + (both ? g : 0)) * kRows + r;
+      TreePart& sp = st.part[warp];
+      __syncwarp();
+      if (lane == 0) {
+        sp = p;
+        st.walk[warp] = make_int4(u, u_end, s, 0);
+      }
+      __syncwarp();
+      const bool both = sp.tiles == 2;   // the groups have a tile each, else alternate chunks of one
+      const int rows = sp.q.drafts * a.group, row = (2 * sp.tp + (both ? g : 0)) * kRows + r;
       const bool live = row < rows, warp_live = row - lane < rows;   // (a dead row's weights, whatever they are, stay in it)
       const int tok = live ? tree_token(a, row) : 0;
       float m = -INFINITY, l = 0.f;
       bool begun = false;
-      for (int c = both ? p.c0 : p.c0 + g; c < p.c1; c += both ? 1 : 2) {
-        const bool cached = c < p.q.cached_blocks;
+      for (int c = both ? sp.c0 : sp.c0 + g; c < sp.c1; c += both ? 1 : 2) {
+        const bool cached = c < sp.q.cached_blocks;
         // which of the chunk's keys this row sees
         uint32_t sees[4] = {~0u, ~0u, ~0u, ~0u};
         bool all = true;
         if (cached) {
-          const int have = p.q.len - c * kChunk;
+          const int have = sp.q.len - c * kChunk;
           if (have < kChunk) {
             all = false;
 #pragma unroll
@@ -568,12 +594,12 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
           }
         } else {
           all = false;
-          const int j0 = (c - p.q.cached_blocks) * kChunk;
+          const int j0 = (c - sp.q.cached_blocks) * kChunk;
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             const int j = j0 + 32 * w;
-            sees[w] = live && j < p.q.drafts
-                          ? tree_sees16(a, p.q, tok, j) | (j + 16 < p.q.drafts ? tree_sees16(a, p.q, tok, j + 16) << 16 : 0u)
+            sees[w] = live && j < sp.q.drafts
+                          ? tree_sees16(a, sp.q, tok, j) | (j + 16 < sp.q.drafts ? tree_sees16(a, sp.q, tok, j + 16) << 16 : 0u)
                           : 0u;
           }
         }
@@ -684,10 +710,10 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
       ok = ok && __all_sync(0xffffffffu, wait_for(&st.part_done, part & 1u, err));
       tc_fence_after();
       const int set = part % kFlagSets, marks = st.bad[set];
-      bool nan = !ok || p.q.bad || (marks & 1) != 0;
+      bool nan = !ok || sp.q.bad || (marks & 1) != 0;
       if ((marks & 2) && live) {
-        for (int j = 0; j < p.q.drafts; j += 16)
-          if (tree_sees16(a, p.q, tok, j) & (st.bad_drafts[set][j >> 5] >> (j & 31))) nan = true;
+        for (int j = 0; j < sp.q.drafts; j += 16)
+          if (tree_sees16(a, sp.q, tok, j) & (st.bad_drafts[set][j >> 5] >> (j & 31))) nan = true;
       }
       if (nan) l = NAN;
       s_ml[g * kRows + r] = make_float2(m, l);
@@ -702,18 +728,18 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
       auto factor = [](float2 ml, float best) { return ml.x == -INFINITY ? 0.f : ex2_ftz(ml.x - best); };   // (NaN sums stay NaN)
       const float f0 = factor(mine, top), f1 = factor(other, top);
       const float sum = mine.y * f0 + other.y * f1;
-      const bool two_streams = !both && p.c1 - p.c0 > 1;   // else the second accumulator holds nothing of this part
+      const bool two_streams = !both && sp.c1 - sp.c0 > 1;   // else the second accumulator holds nothing of this part
       const int d_begin = both ? 0 : g * (HD / 2), d_end = both ? HD : d_begin + HD / 2;
-      const bool whole = p.whole();
+      const bool whole = sp.whole();
       // a partial result: [dim][row], so that a warp's rows are stored side by side
-      const int64_t slot = me == shares.owner(p.place(0)) ? 2 * me + 1 : 2 * me;
+      const int64_t slot = me == TreeShares(st.off[a.n_seqs], gridDim.x, a.weight_full).owner(sp.place(0)) ? 2 * me + 1 : 2 * me;
       const int slot_row = (both ? g : 0) * kRows + r;
       float* part_o = a.part_o + slot * (HD * TreeTc::kSlotRows) + slot_row;
       const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row that saw nothing: zeros
       __nv_bfloat16* dst = nullptr;
       if (live)
-        dst = static_cast<__nv_bfloat16*>(a.t.out) + (p.q.start + static_cast<int64_t>(tok)) * a.t.out_token +
-              (p.g * a.group + row - tok * a.group) * a.t.out_head;
+        dst = static_cast<__nv_bfloat16*>(a.t.out) + (sp.q.start + static_cast<int64_t>(tok)) * a.t.out_token +
+              (sp.g * a.group + row - tok * a.group) * a.t.out_head;
 #pragma unroll 1
       for (int d = d_begin; d < d_end; d += 16) {
         float o[16], o1[16];
@@ -745,6 +771,9 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
       __syncwarp();
       if (lane == 0) mbar_arrive(&st.o_free);
       named_bar_sync(1, 256);   // the states are read before the next part's are written
+      u = st.walk[warp].x;
+      u_end = st.walk[warp].y;
+      s = st.walk[warp].z;
     }
   }
   __syncwarp();
