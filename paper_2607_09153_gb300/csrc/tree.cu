@@ -274,17 +274,34 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(TILES))
         for (int j = 0; j < kK; ++j) kr[n][j] = a.n_pages > 0 ? ldg_stream(base + (8 * n * HD * kSize + 64 * j)) : zero;
     };
 
-    // ---- the cache: pages b, b + 4, ..; the next page's keys and the page's own values are on their way while scores are made
+    uint32_t e4[4] = {0u, 0u, 0u, 0u};   // (as loaded: to put them together is to wait for them)
+    auto load_exponents = [&](int32_t page) {
+      if constexpr (E4M3) {
+        if (a.n_pages == 0) return;
+        const uint8_t* e = exponents + (in_cache(page) ? page : 0) * static_cast<int64_t>(2 * a.n_kv) * kTreePage + 2 * c;
+        e4[0] = __ldg(reinterpret_cast<const uint16_t*>(e));
+        e4[1] = __ldg(reinterpret_cast<const uint16_t*>(e + 8));
+        e += a.n_kv * kTreePage;
+        e4[2] = __ldg(reinterpret_cast<const uint16_t*>(e));
+        e4[3] = __ldg(reinterpret_cast<const uint16_t*>(e + 8));
+      }
+    };
+
+    // ---- the cache: pages b, b + 4, ..; the next page's keys and exponents and the page's own values are on their way while
+    // scores are made
     int b = part.c0 + warp;
     int32_t page = page_of(b), next = page_of(b + kWarps);
-    if (b < c_end) load_keys(page);
+    if (b < c_end) {
+      load_keys(page);
+      load_exponents(page);
+    }
     for (; b < c_end; b += kWarps) {
       const int32_t after = page_of(b + 2 * kWarps);
       const int have = q.len - b * kTreePage;   // tokens of the page: 16 or more where it is full
       poison = poison || !in_cache(page);
       const int64_t at = (in_cache(page) ? page : 0) * static_cast<int64_t>(2 * a.n_kv);
       uint4 v[4][kV];
-      uint32_t ke = 0, ve = 0;   // exponents of tokens 2 c, 2 c + 1, 8 + 2 c, 9 + 2 c
+      uint32_t ke = e4[0] | e4[1] << 16, ve = e4[2] | e4[3] << 16;   // exponents of tokens 2 c, 2 c + 1, 8 + 2 c, 9 + 2 c
       {
         const uint8_t* base = values + at * head_bytes + (E4M3 ? gid * (HD / 8) : 16 * gid);
 #pragma unroll
@@ -293,14 +310,6 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(TILES))
 #pragma unroll
           for (int h = 0; h < kV; ++h)
             v[k][h] = a.n_pages > 0 ? (E4M3 && HD == 64 ? ldg_stream2(p) : ldg_stream(p + 128 * h)) : zero;
-        }
-        if constexpr (E4M3) {
-          const uint8_t* e = exponents + at * kTreePage + 2 * c;
-          if (a.n_pages > 0) {
-            ke = __ldg(reinterpret_cast<const uint16_t*>(e)) | __ldg(reinterpret_cast<const uint16_t*>(e + 8)) << 16;
-            e += a.n_kv * kTreePage;
-            ve = __ldg(reinterpret_cast<const uint16_t*>(e)) | __ldg(reinterpret_cast<const uint16_t*>(e + 8)) << 16;
-          }
         }
       }
       float s[TILES][2][4];
@@ -334,7 +343,10 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(TILES))
           }
         }
       }
-      if (b + kWarps < c_end) load_keys(next);
+      if (b + kWarps < c_end) {
+        load_keys(next);
+        load_exponents(next);
+      }
       if (have < kTreePage) {   // the last page: its places beyond the length may hold anything, even NaN
 #pragma unroll
         for (int k = 0; k < 4; ++k) {

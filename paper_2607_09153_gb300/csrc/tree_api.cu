@@ -44,14 +44,16 @@ int sm_count(int* sms) {
   return KVPRM_OK;
 }
 
-// More than 32 rows of a kv head go to the tensor cores (us a call, registers / tensor cores: 16 sequences of 4 heads with
-// 28 rows over 400 bf16 tokens 20 / 25, over 3,900 43 / 46; 8 heads with 32 rows over 8 x 32,768 191 / 188, with 24 over
-// ragged 20,000 99 / 82; 63 rows over 3,900 8-bit tokens 57 / 57, 98 rows 92 / 57).  CTAs: as many as run at once.  Pairs of
-// so few blocks that cutting one would cost more than it gives stay whole: no join follows.
+// More than 32 rows of a kv head go to the tensor cores, and with bf16 pages of 128 more than 16 beside long caches (us a call,
+// registers / tensor cores: 8 heads with 24 rows over ragged 20,000 bf16 tokens 95 / 78, 8-bit 93 / 88; with 32 over 8 x
+// 32,768 bf16 tokens 189 / 186, 8-bit 159 / 220, over ragged 9,000 of 64-wide heads 36 / 42; 4 heads with 28 over 3,900 40 /
+// 41, over 400 20 / 23; 63 rows over 3,900 8-bit tokens 57 / 57).  CTAs: as many as run at once.  Pairs of so few blocks that
+// cutting one would cost more than it gives stay whole: no join follows.
 int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   TreePlan p;
   const int64_t rows = int64_t{t.max_drafts} * (t.n_q_heads / c.n_kv_heads);
-  p.tc = rows > 32 && c.n_pages > 0;
+  const bool long_bf16 = c.format == KVPRM_CACHE_BF16 && c.head_dim == 128 && t.max_len > 4096;
+  p.tc = rows > (long_bf16 ? 16 : 32) && c.n_pages > 0;
   p.rows = p.tc ? 256 : rows > 16 ? 32 : 16;
   const int64_t block = p.tc ? 128 : kTreePage, tiles = ceil_div(rows, p.tc ? 128 : p.rows), lead = 8;
   // the line of a sequence of any length is shorter than this; a launch's stays within 31 bits
