@@ -208,7 +208,7 @@ __device__ __forceinline__ uint32_t tree_sees16(const TreeLaunch& a, const TreeS
 constexpr int tree_rows_per_sm(int tiles) { return tiles == 2 ? 2 : 3; }
 #ifdef __CUDACC__
 template <int TILES>
-using TreeRows = TreeGeometry<16 * TILES, kTreePage, 1, 8>;
+using TreeRows = TreeGeometry<16 * TILES, kTreePage, 1, TILES == 1 ? 16 : 20>;
 using TreeTc = TreeGeometry<128, 128, 2, 4>;
 #endif
 cudaError_t launch_tree_rows(const TreeLaunch& a, const kvprm_cache& c, int tiles, int ctas, cudaStream_t stream);

@@ -52,10 +52,9 @@ int sm_count(int* sms) {
 int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   TreePlan p;
   const int64_t rows = int64_t{t.max_drafts} * (t.n_q_heads / c.n_kv_heads);
-  const bool long_bf16 = c.format == KVPRM_CACHE_BF16 && c.head_dim == 128 && t.max_len > 4096;
-  p.tc = rows > (long_bf16 ? 16 : 32) && c.n_pages > 0;
+  p.tc = rows > 32 && c.n_pages > 0;
   p.rows = p.tc ? 256 : rows > 16 ? 32 : 16;
-  const int64_t block = p.tc ? 128 : kTreePage, tiles = ceil_div(rows, p.tc ? 128 : p.rows), lead = 8;
+  const int64_t block = p.tc ? 128 : kTreePage, tiles = ceil_div(rows, p.tc ? 128 : p.rows), lead = 20;
   // the line of a sequence of any length is shorter than this; a launch's stays within 31 bits
   const int64_t depth = ceil_div(int64_t{kTreePage} * t.max_blocks, block) + ceil_div(t.max_drafts, block) + lead;
   const int64_t line = depth * (p.tc ? 4 * ceil_div(tiles, 2) : tiles) * c.n_kv_heads;
