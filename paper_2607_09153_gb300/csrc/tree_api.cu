@@ -44,11 +44,12 @@ int sm_count(int* sms) {
   return KVPRM_OK;
 }
 
-// More than 32 rows of a kv head go to the tensor cores, and with bf16 pages of 128 more than 16 beside long caches (us a call,
-// registers / tensor cores: 8 heads with 24 rows over ragged 20,000 bf16 tokens 95 / 78, 8-bit 93 / 88; with 32 over 8 x
-// 32,768 bf16 tokens 189 / 186, 8-bit 159 / 220, over ragged 9,000 of 64-wide heads 36 / 42; 4 heads with 28 over 3,900 40 /
-// 41, over 400 20 / 23; 63 rows over 3,900 8-bit tokens 57 / 57).  CTAs: as many as run at once.  Pairs of so few blocks that
-// cutting one would cost more than it gives stay whole: no join follows.
+// More than 32 rows of a kv head go to the tensor cores (us a call, registers / tensor cores: 8 heads with 24 rows over ragged
+// 20,000 bf16 tokens 76 / 78, 8-bit 66 / 89; with 32 over 8 x 32,768 bf16 tokens 187 / 186, 8-bit 155 / 221; 4 heads with 63 over
+// 16 x 9,001 8-bit tokens 97 / 79; 2 heads with 42 over ragged 1,000 bf16 tokens 19 / 21, with 126 22 / 21).  CTAs: as many as
+// run at once.  Pairs that have a CTA each and few blocks stay whole, for a cut one needs the join (cut / whole: registers, 2 x 8
+// heads over 400 tokens 18 / 13, 16 x 4 heads with 28 rows 21 / 15, over 900 22 / 25; tensor cores, 16 x 2 heads with 126 rows
+// over ragged 300 8-bit tokens 23 / 18, over 600 21 / 23); where CTAs have several, uneven shares cost more, and fewer do.
 int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   TreePlan p;
   const int64_t rows = int64_t{t.max_drafts} * (t.n_q_heads / c.n_kv_heads);
@@ -64,7 +65,7 @@ int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   const int64_t pairs = int64_t{p.seqs} * c.n_kv_heads * ceil_div(rows, p.rows);
   const int64_t blocks = ceil_div(len, block) + ceil_div(t.max_drafts, block);
   const int64_t most = int64_t{sms} * (p.tc ? 1 : tree_rows_per_sm(p.rows / 16));
-  p.whole = blocks <= (p.tc ? 3 : 16);
+  p.whole = blocks <= (pairs <= most ? (p.tc ? 4 : 32) : (p.tc ? 3 : 16));
   p.ctas = static_cast<int>(std::max<int64_t>(1, std::min(most, p.whole ? pairs : pairs * blocks / (p.tc ? 2 : 8))));
   *out = p;
   return KVPRM_OK;
