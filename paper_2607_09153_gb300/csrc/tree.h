@@ -207,6 +207,9 @@ __device__ __forceinline__ uint32_t tree_sees16(const TreeLaunch& a, const TreeS
 // 8 x 32,768 bf16 tokens of 8 kv heads 199 us, three 169).
 constexpr int tree_rows_per_sm(int tiles) { return tiles == 2 ? 2 : 3; }
 #ifdef __CUDACC__
+// A pair's start in blocks (us, one draft over 64 ragged 8-bit sequences: 8 pages 77, 16 75, 32 76; 21 rows of 4 heads over 32
+// ragged ones: 8 73, 20 58, 32 58; in chunks, 64 drafts over 16 ragged 8-bit sequences and 21 over 16 bf16 ones: 2 160 and 30,
+// 4 162 and 27, 7 167 and 27).
 template <int TILES>
 using TreeRows = TreeGeometry<16 * TILES, kTreePage, 1, TILES == 1 ? 16 : 20>;
 using TreeTc = TreeGeometry<128, 128, 2, 4>;
