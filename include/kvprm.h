@@ -633,8 +633,9 @@ KVPRM_API int kvprm_rope_rotate(const kvprm_rope* rope, int32_t dtype, int32_t h
  * calls read -- or of 8-bit floating point (4 exponent and 3 mantissa bits,
  * largest value 448, no infinities) with a power of two for each row of head_dim
  * elements: exponents, uint8 [n_pages][2][n_kv_heads][16] (16-byte aligned), a
- * row's values being code * 2^(exponent - 127), NaN where the exponent is 255.  A power of two costs an 8-bit
- * float nothing in precision, never rounds, and a byte per row. */
+ * row's values being code * 2^(exponent - 127), NaN where the exponent is 255 or the
+ * code 0x7F or 0xFF (kvprm_cache_write leaves the former only).  A power of two costs an
+ * 8-bit float nothing in precision, never rounds, and a byte per row. */
 enum { KVPRM_CACHE_BF16 = 0, KVPRM_CACHE_E4M3 = 1 };
 typedef struct {
   void* pages;

@@ -181,14 +181,24 @@ __device__ __forceinline__ bool not_finite2(uint32_t w) {
 // value; f1 (times f2, where the two do not fit one factor) is 2^120 times the row's power.  The even and the odd codes of
 // a word each become a pair, so that the head's dimensions come in the order 0 2 1 3, 4 6 5 7 ..: Q and the drafted
 // tokens are laid out alike (paired), and the outputs are put back in order.
-template <bool TWO>
+//   bf16 has no place for the NaN codes, 0x7F and 0xFF: there they would be 480, so a page that has one (nan_carries) is converted
+// with NANS; a factor of zero, a row past the length, keeps them out.
+template <bool TWO, bool NANS>
 __device__ __forceinline__ void bf16_of16(const uint4& c, uint32_t f1, uint32_t f2, uint4* lo, uint4* hi) {
   auto pair = [&](uint32_t w, uint32_t* e, uint32_t* o) {
-    *e = mul_bf16x2(((w << 4) & 0x07F007F0u) | ((w << 8) & 0x80008000u), f1);
-    *o = mul_bf16x2(((w >> 4) & 0x07F007F0u) | (w & 0x80008000u), f1);
+    const uint32_t even = (w << 4) & 0x07F007F0u, odd = (w >> 4) & 0x07F007F0u;
+    *e = mul_bf16x2(even | ((w << 8) & 0x80008000u), f1);
+    *o = mul_bf16x2(odd | (w & 0x80008000u), f1);
     if (TWO) {
       *e = mul_bf16x2(*e, f2);
       *o = mul_bf16x2(*o, f2);
+    }
+    if (NANS) {
+      auto nans = [](uint32_t v) {
+        return ((v & 0xFFFFu) == 0x07F0u ? 0x7FC0u : 0u) | (v >> 16 == 0x07F0u ? 0x7FC00000u : 0u);
+      };
+      *e |= f1 != 0u ? nans(even) : 0u;
+      *o |= f1 != 0u ? nans(odd) : 0u;
     }
   };
   pair(c.x, &lo->x, &lo->y);
@@ -196,6 +206,9 @@ __device__ __forceinline__ void bf16_of16(const uint4& c, uint32_t f1, uint32_t 
   pair(c.z, &hi->x, &hi->y);
   pair(c.w, &hi->z, &hi->w);
 }
+// Bit 7 of a byte is set in the result where w's byte is a NaN code, and there is no such bit where none is: a carry into it,
+// or out of the byte below, comes of seven ones alone.
+__device__ __forceinline__ uint32_t nan_carries(uint32_t w) { return (w + 0x01010101u) ^ w; }
 __device__ __forceinline__ uint4 paired(const uint4& v) {
   return make_uint4(__byte_perm(v.x, v.y, 0x5410), __byte_perm(v.x, v.y, 0x7632), __byte_perm(v.z, v.w, 0x5410),
                     __byte_perm(v.z, v.w, 0x7632));
@@ -504,21 +517,38 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
             const bool live = my_page * kTreePage + lane % kTreePage < p.q.len - c * kChunk, two = e > 134u && live;
             uint32_t f = (two ? 254u : e + 120u) << 7 | (two ? (e == 255u ? 0x7FC0u : (e - 7u) << 7) : 0x3F80u) << 16;
             if (!live) f = 0x3F800000u;
+            // (looked for before the conversion, whose instructions then hide the vote: 64 drafts over 16 ragged sequences
+            // 162 us without the check, 164 with it, 168 with the vote at the end)
+            uint32_t carries = 0;
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k)
+              carries |= nan_carries(codes[k].x) | nan_carries(codes[k].y) | nan_carries(codes[k].z) | nan_carries(codes[k].w);
+            const bool nan = __any_sync(0xffffffffu, (carries & 0x80808080u) != 0u);
+            auto step = [&](int k, const uint4& x, auto twice, auto nans) {   // kTeam rows
+              const uint32_t fr = __shfl_sync(0xffffffffu, f, my_row + kTeam * k);
+              uint4 lo, hi;
+              bf16_of16<decltype(twice)::value, decltype(nans)::value>(x, __byte_perm(fr, 0, 0x1010), __byte_perm(fr, 0, 0x3232), &lo,
+                                                                       &hi);
+              const int row = my_page * kTreePage + k * kTeam + my_row;
+              *reinterpret_cast<uint4*>(dst + swizzled<HD>(row, 2 * my_piece)) = lo;
+              *reinterpret_cast<uint4*>(dst + swizzled<HD>(row, 2 * my_piece + 1)) = hi;
+            };
             auto convert = [&](auto twice) {
 #pragma unroll
-              for (int k = 0; k < kSteps; ++k) {
-                const uint32_t fr = __shfl_sync(0xffffffffu, f, my_row + kTeam * k);
-                uint4 lo, hi;
-                bf16_of16<decltype(twice)::value>(codes[k], __byte_perm(fr, 0, 0x1010), __byte_perm(fr, 0, 0x3232), &lo, &hi);
-                const int row = my_page * kTreePage + k * kTeam + my_row;
-                *reinterpret_cast<uint4*>(dst + swizzled<HD>(row, 2 * my_piece)) = lo;
-                *reinterpret_cast<uint4*>(dst + swizzled<HD>(row, 2 * my_piece + 1)) = hi;
-              }
+              for (int k = 0; k < kSteps; ++k) step(k, codes[k], twice, std::false_type());
             };
-            if (__any_sync(0xffffffffu, two))
+            if (nan) {   // rare: a loop, on the codes loaded again
+              const int32_t at = page_of(item);
+              const uint8_t* src = a.pages + ((static_cast<int64_t>(max(at, 0)) * 2 + kv) * a.n_kv + p.g) * kTreePage * HD +
+                                   my_row * HD + my_piece * 16;
+#pragma unroll 1
+              for (int k = 0; k < kSteps; ++k)
+                step(k, at >= 0 ? ldg_stream(src + k * 512) : make_uint4(0u, 0u, 0u, 0u), std::true_type(), std::true_type());
+            } else if (__any_sync(0xffffffffu, two)) {
               convert(std::true_type());
-            else
+            } else {
               convert(std::false_type());
+            }
             slot_filled(&st.slot_full[slot]);
             continue;
           }
