@@ -2,8 +2,9 @@
 or quantised to 8 bits, quantised pages expanded for the scorer, and the attention of drafted tokens over the pages.
 
 Like kvprm.py this module only marshals arguments: shapes, types and devices are checked here, everything else by the
-library, and every step runs in its CUDA kernels.  Calls are enqueued on `stream` (default: torch's current one); a
-tensor that belongs to another stream has to be ordered by the caller, as for any torch operation.
+library, and every step runs in its CUDA kernels.  Calls are enqueued on `stream` (default: torch's current one), and the
+tensors that they return belong to it; a tensor that belongs to another stream has to be ordered by the caller, as for
+any torch operation.
 
 A decoding step's calls take a few microseconds on the GPU, so what is spent here counts: arguments are read once, and
 the C structs are packed as bytes (a ctypes structure takes about 0.2 us a field).
@@ -146,6 +147,14 @@ def _call(T, device: int, stream, function, *args) -> int:
         return function(*args, handle)
 
 
+def _result(T, shape, dtype, device, stream):
+    """A tensor of the stream that the call writes it on: one of another stream might still be in use there."""
+    if stream is None:
+        return T.empty(shape, dtype=dtype, device=device)
+    with T.torch.cuda.stream(stream):
+        return T.empty(shape, dtype=dtype, device=device)
+
+
 class Rope:
     """Rotary positions of `rotary_dim` elements per head (kvprm_rope_create; see include/kvprm.h for the layouts and
     the ways the frequencies are stretched)."""
@@ -197,7 +206,7 @@ class Rope:
                 raise ValueError(f"a tensor is {tuple(shape)}, expected [{n}][heads][{hd}]")
             st = _heads("a tensor", x, shape, dtype, dev)
             if out is None:
-                o = T.empty(shape, dtype=dtype, device=x.device)   # dense, also where x is a slice of wider rows
+                o = _result(T, shape, dtype, x.device, stream)   # dense, also where x is a slice of wider rows
                 so = (shape[1] * hd, hd)
             else:
                 o = out[i]
@@ -349,7 +358,7 @@ def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, ma
         words = mask.shape[1]
         bits = _ints("mask", mask, i32, (tokens, words), dev)
     if out is None:
-        out = T.empty(shape, dtype=bf16, device=q.device)
+        out = _result(T, shape, bf16, q.device, stream)
         so = (nq * hd, hd)
     else:
         so = _heads("out", out, shape, bf16, dev)
