@@ -14,6 +14,7 @@ from __future__ import annotations
 import ctypes
 import math
 import struct
+import threading
 
 from .kvprm import KVPRM_ECAPACITY, KVPRM_OK, KvprmError
 from .kvprm import lib as _base_lib
@@ -312,7 +313,16 @@ def tree_mask(parents, start):
     return torch.from_numpy(mask.view(np.int32))
 
 
-_workspaces: dict = {}
+class _Stream:
+    """Scratch of the calls on one stream.  They follow one another there, so they can share it; `lock` is held while one
+    of them enqueues its launches, for those of two host threads must not be mixed."""
+    __slots__ = ("lock", "scratch")
+
+    def __init__(self):
+        self.lock, self.scratch = threading.RLock(), None
+
+
+_streams: dict = {}   # by device and stream handle
 
 
 def _scratch(T, need: int, device: int, stream):
@@ -371,17 +381,20 @@ def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, ma
     if workspace is not None:
         rc = _call(T, dev, stream, go, c, t, workspace.data_ptr(), workspace.numel())
     else:
-        # Scratch is kept per device and stream: calls on one stream follow one another, so they can share it.  A call
-        # that is being captured gets scratch of its own (the graph's), for the graph may be replayed on any stream.
-        key = (dev, T.raw_stream(dev) if stream is None else stream.cuda_stream)
-        w = _workspaces.get(key)
+        # A call that is being captured gets scratch of its own (the graph's), for the graph may be replayed on any stream.
         capturing = T.capturing() if stream is None else _capturing(T, stream)
         if capturing:
             w = _scratch(T, _workspace_bytes(c, t), dev, stream)
-        rc = KVPRM_ECAPACITY if w is None else _call(T, dev, stream, go, c, t, w.data_ptr(), w.numel())
-        if rc == KVPRM_ECAPACITY and not capturing:
-            w = _workspaces[key] = _scratch(T, _workspace_bytes(c, t), dev, stream)
             rc = _call(T, dev, stream, go, c, t, w.data_ptr(), w.numel())
+        else:
+            key = (dev, T.raw_stream(dev) if stream is None else stream.cuda_stream)
+            mine = _streams.get(key) or _streams.setdefault(key, _Stream())
+            with mine.lock:
+                w = mine.scratch
+                rc = KVPRM_ECAPACITY if w is None else _call(T, dev, stream, go, c, t, w.data_ptr(), w.numel())
+                if rc == KVPRM_ECAPACITY:
+                    w = mine.scratch = _scratch(T, _workspace_bytes(c, t), dev, stream)
+                    rc = _call(T, dev, stream, go, c, t, w.data_ptr(), w.numel())
     if rc != KVPRM_OK:
         _check(rc)
     return out

@@ -1,4 +1,6 @@
 """The operators' calls as torch's allocator, threads and gradients meet them."""
+import threading
+
 import pytest
 
 from tests.gpu_util import require_gpu
@@ -26,3 +28,28 @@ def test_results_of_a_side_stream():
         del y
         kept = [torch.empty(shape, dtype=dtype, device="cuda") for _ in range(8)]
         assert at not in [z.data_ptr() for z in kept]
+
+
+def test_threads_on_one_stream():
+    """Host threads that call on one stream, each with sequences of its own that several CTAs share: what each call gives
+    alone, bit for bit."""
+    torch = require_gpu()
+    trees = [Tree(torch, 8, 2, 128, [9000 + 1000 * i, 5000], [1 + 3 * i, 2], i % 2 == 1, seed=i) for i in range(4)]
+    args = [dict(lens=torch.tensor(t.lens, dtype=torch.int32).cuda(), start=torch.tensor(t.start, dtype=torch.int32).cuda())
+            for t in trees]
+    alone = [t.run(**a) for t, a in zip(trees, args)]
+    torch.cuda.synchronize()
+    results, barrier = [None] * 4, threading.Barrier(4)
+
+    def work(i):
+        barrier.wait()
+        results[i] = [trees[i].run(**args[i]) for _ in range(100)]
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    for x in threads:
+        x.start()
+    for x in threads:
+        x.join()
+    torch.cuda.synchronize()
+    for a, many in zip(alone, results):
+        assert all(torch.equal(a, o) for o in many)

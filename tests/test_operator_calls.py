@@ -1,7 +1,9 @@
 """What the operators' torch face asks of torch and hands to the library, with both replaced by stand-ins that keep a record:
 which stream a tensor is made on, who holds scratch when.  (No GPU.)"""
 import contextlib
+import itertools
 import threading
+import time
 
 import pytest
 import torch
@@ -11,8 +13,10 @@ from paper_2607_09153_gb300 import operators as ops
 
 class Tensor:
     """As much of a contiguous CUDA tensor as the calls look at."""
+    addresses = itertools.count(1 << 20, 1 << 20)
 
     def __init__(self, shape, dtype, stream=None, device=0):
+        self.address = next(Tensor.addresses)
         self.shape, self.dtype, self.made_on, self.index = torch.Size(shape), dtype, stream, device
         self.device, self.requires_grad = f"cuda:{device}", False
 
@@ -35,7 +39,7 @@ class Tensor:
         return True
 
     def data_ptr(self):
-        return 0x100000 + id(self) % 4096 * 256
+        return self.address
 
 
 class Stream:
@@ -121,7 +125,7 @@ def face(monkeypatch):
     T, L = Torch(), Library()
     monkeypatch.setattr(ops, "_t", T)
     monkeypatch.setattr(ops, "lib", lambda: L)
-    monkeypatch.setattr(ops, "_workspaces", {})
+    monkeypatch.setattr(ops, "_streams", {})
     return T, L
 
 
@@ -146,3 +150,41 @@ def test_results_belong_to_the_stream_that_writes_them(face):
         assert all(x.made_on == handle for x in T.made[-4:])
         assert [c[1][-1] for c in L.calls if "create" not in c[0]] == [handle] * 3
     assert T.cuda.handle() == 1
+
+
+def test_threads_share_a_streams_scratch_in_turn(face, monkeypatch):
+    """A call enqueues several launches that leave and read partial results: another thread's on the same stream and scratch
+    must not come between them.  Calls on other streams have scratch of their own and need not wait."""
+    T, L = face
+    held, overlaps, together, lock = {}, [], [], threading.Lock()
+
+    def enqueue(c, t, workspace, size, stream):
+        if size < L.need:
+            return ops.KVPRM_ECAPACITY
+        with lock:
+            if held.get(workspace):
+                overlaps.append(workspace)
+            together.append(sum(held.values()))
+            held[workspace] = 1
+        time.sleep(0.002)   # as long as ctypes holds no lock of Python's
+        with lock:
+            held[workspace] = 0
+        return 0
+
+    monkeypatch.setattr(L, "kvprm_tree_attention", enqueue, raising=False)
+    barrier = threading.Barrier(6)
+
+    def work(i):
+        barrier.wait()
+        for k in range(20):
+            if i == 0:
+                L.need = 4096 * (1 + k // 4)   # scratch that is outgrown meanwhile
+            attend(stream=Stream(5) if i < 4 else None)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(6)]
+    for x in threads:
+        x.start()
+    for x in threads:
+        x.join()
+    assert not overlaps
+    assert max(together) == 1   # the two streams' calls did run beside each other
