@@ -330,15 +330,32 @@ def _scratch(T, need: int, device: int, stream):
         return T.torch.empty(need, dtype=T.torch.uint8, device=T.torch.device("cuda", device))
 
 
-def _capturing(T, stream) -> bool:
-    with T.torch.cuda.stream(stream):
-        return T.capturing()
-
-
 def _workspace_bytes(c: bytes, t: bytes) -> int:
     need = ctypes.c_int64()
     _check(lib().kvprm_tree_workspace(c, t, ctypes.byref(need)))
     return need.value
+
+
+def _attend(T, c: bytes, t: bytes, device: int, stream) -> int:
+    """kvprm_tree_attention with scratch of the stream's, the tensors' device being current; the status."""
+    go = lib().kvprm_tree_attention
+    if stream is None:
+        handle, capturing = T.raw_stream(device), T.capturing()
+    else:
+        handle = stream.cuda_stream
+        with T.torch.cuda.stream(stream):
+            capturing = T.capturing()
+    if capturing:   # scratch of the graph's own, for the graph may be replayed on any stream
+        w = _scratch(T, _workspace_bytes(c, t), device, stream)
+        return go(c, t, w.data_ptr(), w.numel(), handle)
+    mine = _streams.get((device, handle)) or _streams.setdefault((device, handle), _Stream())
+    with mine.lock:
+        w = mine.scratch
+        rc = KVPRM_ECAPACITY if w is None else go(c, t, w.data_ptr(), w.numel(), handle)
+        if rc == KVPRM_ECAPACITY:
+            w = mine.scratch = _scratch(T, _workspace_bytes(c, t), device, stream)
+            rc = go(c, t, w.data_ptr(), w.numel(), handle)
+    return rc
 
 
 def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, max_len: int | None = None,
@@ -377,24 +394,13 @@ def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, ma
                    _ints("lens", lens, i32, (n,), dev), _ints("start", start, i32, (n + 1,), dev), bits, width, n,
                    tokens, nq, max_drafts, PAGE * width if max_len is None else max_len, words,
                    1.0 / math.sqrt(hd) if scale is None else scale)
-    go = lib().kvprm_tree_attention
     if workspace is not None:
-        rc = _call(T, dev, stream, go, c, t, workspace.data_ptr(), workspace.numel())
+        rc = _call(T, dev, stream, lib().kvprm_tree_attention, c, t, workspace.data_ptr(), workspace.numel())
+    elif T.device() == dev:
+        rc = _attend(T, c, t, dev, stream)
     else:
-        # A call that is being captured gets scratch of its own (the graph's), for the graph may be replayed on any stream.
-        capturing = T.capturing() if stream is None else _capturing(T, stream)
-        if capturing:
-            w = _scratch(T, _workspace_bytes(c, t), dev, stream)
-            rc = _call(T, dev, stream, go, c, t, w.data_ptr(), w.numel())
-        else:
-            key = (dev, T.raw_stream(dev) if stream is None else stream.cuda_stream)
-            mine = _streams.get(key) or _streams.setdefault(key, _Stream())
-            with mine.lock:
-                w = mine.scratch
-                rc = KVPRM_ECAPACITY if w is None else _call(T, dev, stream, go, c, t, w.data_ptr(), w.numel())
-                if rc == KVPRM_ECAPACITY:
-                    w = mine.scratch = _scratch(T, _workspace_bytes(c, t), dev, stream)
-                    rc = _call(T, dev, stream, go, c, t, w.data_ptr(), w.numel())
+        with T.torch.cuda.device(dev):
+            rc = _attend(T, c, t, dev, stream)
     if rc != KVPRM_OK:
         _check(rc)
     return out

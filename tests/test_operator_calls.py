@@ -129,9 +129,9 @@ def face(monkeypatch):
     return T, L
 
 
-def attend(tokens=3, n=2, **kw):
-    t = lambda *shape: Tensor(shape, torch.bfloat16)  # noqa: E731
-    i = lambda *shape: Tensor(shape, torch.int32)  # noqa: E731
+def attend(tokens=3, n=2, device=0, **kw):
+    t = lambda *shape: Tensor(shape, torch.bfloat16, device=device)  # noqa: E731
+    i = lambda *shape: Tensor(shape, torch.int32, device=device)  # noqa: E731
     return ops.tree_attention(t(tokens, 4, 64), t(tokens, 2, 64), t(tokens, 2, 64), t(8, 2, 2, 16, 64), i(n, 4), i(n), i(n + 1),
                               max_drafts=2, **kw)
 
@@ -188,3 +188,25 @@ def test_threads_share_a_streams_scratch_in_turn(face, monkeypatch):
         x.join()
     assert not overlaps
     assert max(together) == 1   # the two streams' calls did run beside each other
+
+
+def test_scratch_of_another_device(face, monkeypatch):
+    """With another device current: whether a call is being captured, and what scratch it needs, are the tensors' device's
+    to say."""
+    T, L = face
+    capturing, asked = set(), []
+    monkeypatch.setattr(T, "capturing", lambda: T.cuda.index in capturing)
+
+    def workspace(c, t, need):
+        asked.append(T.cuda.index)
+        need._obj.value = L.need
+        return 0
+
+    monkeypatch.setattr(L, "kvprm_tree_workspace", workspace, raising=False)
+    capturing.add(1)
+    attend(device=1)
+    assert ops._streams == {} and asked == [1]   # the graph's own scratch
+    capturing.clear()
+    capturing.add(0)
+    attend(device=1)
+    assert list(ops._streams) == [(1, 1)] and asked == [1, 1] and T.cuda.index == 0
