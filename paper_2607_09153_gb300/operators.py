@@ -395,7 +395,10 @@ def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, ma
                    tokens, nq, max_drafts, PAGE * width if max_len is None else max_len, words,
                    1.0 / math.sqrt(hd) if scale is None else scale)
     if workspace is not None:
-        rc = _call(T, dev, stream, lib().kvprm_tree_attention, c, t, workspace.data_ptr(), workspace.numel())
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError(f"workspace is a contiguous tensor on CUDA device {dev}, got one on {workspace.device}")
+        rc = _call(T, dev, stream, lib().kvprm_tree_attention, c, t, workspace.data_ptr(),
+                   workspace.numel() * workspace.element_size())
     elif T.device() == dev:
         rc = _attend(T, c, t, dev, stream)
     else:

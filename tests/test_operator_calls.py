@@ -32,6 +32,9 @@ class Tensor:
     def dim(self):
         return len(self.shape)
 
+    def element_size(self):
+        return self.dtype.itemsize
+
     def numel(self):
         return self.shape.numel()
 
@@ -210,3 +213,21 @@ def test_scratch_of_another_device(face, monkeypatch):
     capturing.add(0)
     attend(device=1)
     assert list(ops._streams) == [(1, 1)] and asked == [1, 1] and T.cuda.index == 0
+
+
+def test_workspace_of_the_callers(face):
+    """Scratch that the caller passes: on the tensors' device and contiguous, as its address alone is handed on; its size is
+    counted in bytes."""
+    T, L = face
+    good = Tensor((1024,), torch.float32)
+    attend(workspace=good)
+    assert L.calls[-1][1][:2] == (good.address, 4096)
+    host = Tensor((4096,), torch.uint8, device=-1)
+    other = Tensor((4096,), torch.uint8, device=1)
+    gaps = Tensor((4096,), torch.uint8)
+    gaps.is_contiguous = lambda: False
+    calls = len(L.calls)
+    for bad in (host, other, gaps):
+        with pytest.raises(ValueError, match="workspace"):
+            attend(workspace=bad)
+    assert len(L.calls) == calls
