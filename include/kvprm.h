@@ -714,6 +714,10 @@ typedef struct {
 KVPRM_API int kvprm_tree_workspace(const kvprm_cache* cache, const kvprm_tree* t, int64_t* bytes);
 KVPRM_API int kvprm_tree_attention(const kvprm_cache* cache, const kvprm_tree* t, void* workspace,
                                    int64_t workspace_bytes, void* stream);
+/* The same, for an `out` that nobody has written: the rows of tokens that no
+ * sequence has become zeros, those of a sequence that is left out NaN. */
+KVPRM_API int kvprm_tree_attention_filled(const kvprm_cache* cache, const kvprm_tree* t, void* workspace,
+                                          int64_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -114,7 +114,7 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(TILES))
   __shared__ float s_most[TILES][16][HD / 32];      // largest magnitude of 32 dims of a query row
   __shared__ float s_m[kWarps][16], s_l[kWarps][16];
   grid_dep_launch();
-  tree_line<G, kThreads>(a, s_off, s_sum);
+  tree_line<G, kThreads, HD>(a, s_off, s_sum);
   const int32_t total = s_off[a.n_seqs];
   if (total == 0) return;
   const TreeShares shares(total, gridDim.x, a.weight_full);

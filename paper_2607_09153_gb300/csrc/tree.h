@@ -1,6 +1,7 @@
 // Attention of drafted tokens over the paged cache (internal): what the two kernels share.
 #pragma once
 
+#include <cuda_bf16.h>
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -19,6 +20,7 @@ struct TreeLaunch {
   int32_t n_kv, group, seq0, n_seqs;   // sequences seq0 .. seq0 + n_seqs - 1
   uint32_t group_m;                    // ceil(2^32 / group), 0 for a group of one (tree_token)
   int32_t whole;                       // 1: no pair is cut
+  int32_t fill;                        // 1: rows that no sequence writes are written too (tree_fill)
   int32_t weight_full, weight_part;    // places of a block of a pair with all its tiles, or with fewer
   float scale_log2;                    // scores in units of log2
   int32_t* line;                       // [n_seqs + 1], then the CTAs that took part: for the join
@@ -38,7 +40,8 @@ struct TreeLaunch {
 // prefix sum over the sequences at the start of each CTA), so that nothing is planned on the host.
 struct TreeSeq {
   int32_t len, start, drafts, cached_blocks, blocks, tiles;
-  bool bad;   // a length that cannot be: every output NaN
+  bool bad;        // a length that cannot be: every output NaN
+  bool left_out;   // drafts that cannot be
 };
 
 template <int ROWS, int BLOCK>
@@ -49,6 +52,7 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeLaunch& a, int s) {
   const int64_t drafts = static_cast<int64_t>(__ldg(a.t.start + a.seq0 + s + 1)) - q.start;
   const bool none = drafts <= 0 || drafts > a.t.max_drafts || q.start < 0 || q.start + drafts > a.t.n_tokens;
   q.drafts = none ? 0 : static_cast<int32_t>(drafts);
+  q.left_out = drafts != q.drafts;
   q.bad = q.len < 0 || (static_cast<int64_t>(q.len) + kTreePage - 1) / kTreePage > a.t.max_blocks;
   if (q.bad) q.len = 0;
   q.tiles = (q.drafts * a.group + ROWS - 1) / ROWS;
@@ -70,13 +74,37 @@ __device__ __forceinline__ int32_t tree_width(const TreeLaunch& a, int tiles) {
   return tiles / G::TILES * a.weight_full + (tiles % G::TILES != 0 ? a.weight_part : 0);
 }
 
+// Writes the rows of tokens that no sequence has: zeros (they see nothing), or NaN where the sequence is left out.  A warp a
+// token, over the launch's CTAs; only where tree_line found that there may be such tokens.
+template <int HD>
+__device__ __forceinline__ void tree_fill(const TreeLaunch& a) {
+  const int lane = threadIdx.x & 31, warps = blockDim.x >> 5;
+  for (int64_t t = static_cast<int64_t>(blockIdx.x) * warps + (threadIdx.x >> 5); t < a.t.n_tokens; t += int64_t{gridDim.x} * warps) {
+    bool own = false, lost = false;
+    for (int s = lane; s < a.t.n_seqs; s += 32) {
+      const int64_t s0 = __ldg(a.t.start + s), s1 = __ldg(a.t.start + s + 1);
+      if (t < s0 || t >= s1) continue;
+      const bool fine = s1 - s0 <= a.t.max_drafts && s0 >= 0 && s1 <= a.t.n_tokens;
+      own = own || fine;
+      lost = lost || !fine;
+    }
+    if (__any_sync(0xffffffffu, own)) continue;
+    const uint32_t two = __any_sync(0xffffffffu, lost) ? 0x7FC07FC0u : 0u;
+    __nv_bfloat16* row = static_cast<__nv_bfloat16*>(a.t.out) + t * a.t.out_token;
+    for (int i = lane; i < a.t.n_q_heads * (HD / 8); i += 32)
+      *reinterpret_cast<uint4*>(row + i / (HD / 8) * a.t.out_head + i % (HD / 8) * 8) = make_uint4(two, two, two, two);
+  }
+}
+
 // off[s] = the first place of sequence s, off[n_seqs] = the line's length (kept below 2^31 by the host).  All threads.
-template <typename G, int THREADS>
+template <typename G, int THREADS, int HD>
 __device__ __forceinline__ void tree_line(const TreeLaunch& a, int32_t* off, int32_t* warp_sum) {
   constexpr int kPer = (kTreeSeqs + THREADS - 1) / THREADS;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int per = (a.n_seqs + THREADS - 1) / THREADS;   // <= kPer
   int32_t mine[kPer], sum = 0;
+  // sequences follow one another from token 0 to the last one, unless one of these says otherwise
+  bool gaps = a.n_seqs == 0;
 #pragma unroll
   for (int k = 0; k < kPer; ++k) {
     if (k >= per) break;
@@ -85,6 +113,8 @@ __device__ __forceinline__ void tree_line(const TreeLaunch& a, int32_t* off, int
     if (s < a.n_seqs) {
       const TreeSeq q = tree_seq<G::ROWS, G::BLOCK>(a, s);
       if (q.drafts > 0) sum += (q.blocks + G::LEAD) * tree_width<G>(a, q.tiles) * a.n_kv;
+      gaps = gaps || q.left_out || (a.seq0 + s == 0 && q.start != 0) ||
+             (a.seq0 + s == a.t.n_seqs - 1 && q.start + q.drafts != a.t.n_tokens);
     }
   }
   int32_t scan = sum;
@@ -94,7 +124,7 @@ __device__ __forceinline__ void tree_line(const TreeLaunch& a, int32_t* off, int
     if (lane >= d) scan += up;
   }
   if (lane == 31) warp_sum[warp] = scan;
-  __syncthreads();
+  if (__syncthreads_or(gaps && a.fill)) tree_fill<HD>(a);
   int32_t before = scan - sum;
   for (int w = 0; w < warp; ++w) before += warp_sum[w];
 #pragma unroll
@@ -104,6 +134,7 @@ __device__ __forceinline__ void tree_line(const TreeLaunch& a, int32_t* off, int
     if (s < a.n_seqs) off[s] = before + mine[k];
     if (s == a.n_seqs - 1) off[a.n_seqs] = before + sum;
   }
+  if (a.n_seqs == 0 && tid == 0) off[0] = 0;
   __syncthreads();
 }
 

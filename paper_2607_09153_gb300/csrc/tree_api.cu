@@ -75,28 +75,12 @@ int64_t workspace_bytes(const kvprm_cache& c, const TreePlan& p) {
   return kLineBytes + (p.whole ? 0 : int64_t{2} * p.ctas * p.rows * (4 * c.head_dim + 8));
 }
 
-}  // namespace
-
-extern "C" {
-
-int kvprm_tree_workspace(const kvprm_cache* cache, const kvprm_tree* t, int64_t* bytes) {
-  const char* who = "kvprm_tree_workspace";
-  if (!bytes) return operator_fail(KVPRM_EINVAL, "%s: bytes is NULL", who);
+int attend(const kvprm_cache* cache, const kvprm_tree* t, void* workspace, int64_t workspace_size, void* stream, bool fill,
+           const char* who) {
   if (const int rc = check(cache, t, who)) return rc;
-  int sms = 0;
-  if (const int rc = sm_count(&sms)) return rc;
-  TreePlan p;
-  if (const int rc = plan(*cache, *t, sms, &p)) return rc;
-  *bytes = workspace_bytes(*cache, p);
-  return KVPRM_OK;
-}
-
-int kvprm_tree_attention(const kvprm_cache* cache, const kvprm_tree* t, void* workspace, int64_t workspace_size,
-                         void* stream) {
-  const char* who = "kvprm_tree_attention";
-  if (const int rc = check(cache, t, who)) return rc;
-  if (t->n_seqs == 0 || t->n_tokens == 0) return KVPRM_OK;
-  if (!t->q || !t->k || !t->v || !t->out || !t->lens || !t->start || (t->max_blocks > 0 && !t->block_table))
+  if ((t->n_seqs == 0 && !fill) || t->n_tokens == 0) return KVPRM_OK;
+  const bool seqs = t->n_seqs > 0;
+  if (!t->q || !t->k || !t->v || !t->out || !t->start || (seqs && !t->lens) || (seqs && t->max_blocks > 0 && !t->block_table))
     return operator_fail(KVPRM_EINVAL, "%s: NULL argument", who);
   if (!aligned16(t->q) || !aligned16(t->k) || !aligned16(t->v) || !aligned16(t->out) ||
       ((t->q_token | t->q_head | t->k_token | t->k_head | t->v_token | t->v_head | t->out_token | t->out_head) & 7) != 0)
@@ -120,6 +104,7 @@ int kvprm_tree_attention(const kvprm_cache* cache, const kvprm_tree* t, void* wo
   a.group_m = a.group > 1 ? static_cast<uint32_t>(((uint64_t{1} << 32) + a.group - 1) / a.group) : 0u;
   a.scale_log2 = t->scale * 1.4426950408889634f;
   a.whole = p.whole;
+  a.fill = fill;
   // a chunk with one row tile costs the tensor-core kernel, by what it waits for, 0.75 of one with two (a bf16 cache: memory)
   // or as much (an 8-bit one: its conversion)
   a.weight_full = p.tc ? 4 : 1;
@@ -128,13 +113,41 @@ int kvprm_tree_attention(const kvprm_cache* cache, const kvprm_tree* t, void* wo
   a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kLineBytes);
   a.part_ml = reinterpret_cast<float2*>(a.part_o + int64_t{2} * p.ctas * p.rows * cache->head_dim);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  for (a.seq0 = 0; a.seq0 < t->n_seqs; a.seq0 += p.seqs) {
+  a.seq0 = 0;
+  do {   // (once without sequences, which is to fill only)
     a.n_seqs = std::min(p.seqs, t->n_seqs - a.seq0);
     cudaError_t e = p.tc ? launch_tree_tc(a, *cache, p.ctas, st) : launch_tree_rows(a, *cache, p.rows / 16, p.ctas, st);
-    if (e == cudaSuccess && !p.whole) e = launch_tree_join(a, *cache, p.rows, st);
+    if (e == cudaSuccess && !p.whole && seqs) e = launch_tree_join(a, *cache, p.rows, st);
     if (e != cudaSuccess) return operator_fail(KVPRM_ECUDA, "%s: %s", who, cudaGetErrorString(e));
-  }
+    a.seq0 += p.seqs;
+  } while (a.seq0 < t->n_seqs);
   return KVPRM_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int kvprm_tree_workspace(const kvprm_cache* cache, const kvprm_tree* t, int64_t* bytes) {
+  const char* who = "kvprm_tree_workspace";
+  if (!bytes) return operator_fail(KVPRM_EINVAL, "%s: bytes is NULL", who);
+  if (const int rc = check(cache, t, who)) return rc;
+  int sms = 0;
+  if (const int rc = sm_count(&sms)) return rc;
+  TreePlan p;
+  if (const int rc = plan(*cache, *t, sms, &p)) return rc;
+  *bytes = workspace_bytes(*cache, p);
+  return KVPRM_OK;
+}
+
+int kvprm_tree_attention(const kvprm_cache* cache, const kvprm_tree* t, void* workspace, int64_t workspace_bytes,
+                         void* stream) {
+  return attend(cache, t, workspace, workspace_bytes, stream, false, "kvprm_tree_attention");
+}
+
+int kvprm_tree_attention_filled(const kvprm_cache* cache, const kvprm_tree* t, void* workspace, int64_t workspace_bytes,
+                                void* stream) {
+  return attend(cache, t, workspace, workspace_bytes, stream, true, "kvprm_tree_attention_filled");
 }
 
 }  // extern "C"

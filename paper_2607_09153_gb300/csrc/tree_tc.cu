@@ -259,7 +259,7 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
   }
   tc_fence_before();
   grid_dep_launch();
-  tree_line<TreeTc, kThreads>(a, st.off, st.sum);   // barriers inside
+  tree_line<TreeTc, kThreads, HD>(a, st.off, st.sum);   // barriers inside
   tc_fence_after();
   const uint32_t tmem = st.tmem;
   const int32_t total = st.off[a.n_seqs];

@@ -69,7 +69,7 @@ def lib() -> ctypes.CDLL:
         L.kvprm_cache_write.argtypes = [vp, i32, vp, i64, i64, vp, i64, i64, vp, i64, vp, vp, vp]
         L.kvprm_cache_expand.argtypes = [vp, vp, vp, i64, vp, i64, vp]
         L.kvprm_tree_workspace.argtypes = [vp, vp, vp]
-        L.kvprm_tree_attention.argtypes = [vp, vp, vp, i64, vp]
+        L.kvprm_tree_attention.argtypes = L.kvprm_tree_attention_filled.argtypes = [vp, vp, vp, i64, vp]
         _lib = L
     return _lib
 
@@ -336,9 +336,8 @@ def _workspace_bytes(c: bytes, t: bytes) -> int:
     return need.value
 
 
-def _attend(T, c: bytes, t: bytes, device: int, stream) -> int:
-    """kvprm_tree_attention with scratch of the stream's, the tensors' device being current; the status."""
-    go = lib().kvprm_tree_attention
+def _attend(T, go, c: bytes, t: bytes, device: int, stream) -> int:
+    """`go`, an attention entry point, with scratch of the stream's, the tensors' device being current; the status."""
     if stream is None:
         handle, capturing = T.raw_stream(device), T.capturing()
     else:
@@ -366,7 +365,8 @@ def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, ma
     drafted tokens start[s] .. start[s + 1] - 1 (int32 [n_seqs + 1], at most max_drafts each) and lens[s] (int32)
     cached ones in pages block_table[s][0 ..] (int32).  mask: int32 [tokens][words], bit j of a token's row: it sees
     drafted token j of its sequence (tree_mask); None: those up to itself.  max_len sizes the launch (default: the
-    block table's width).  Returns [tokens][n_q_heads][head_dim]."""
+    block table's width).  Returns [tokens][n_q_heads][head_dim]: `out`, where rows of tokens that no sequence has, or one
+    with more than max_drafts, are left as they are, or a new tensor, where they are zeros and NaN."""
     T = _t or _torch()
     c, heads, hd, dev = _cache(T, pages, exponents)
     shape, _ = _rows("q", q)
@@ -387,8 +387,10 @@ def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, ma
     if out is None:
         out = _result(T, shape, bf16, q.device, stream)
         so = (nq * hd, hd)
+        go = lib().kvprm_tree_attention_filled
     else:
         so = _heads("out", out, shape, bf16, dev)
+        go = lib().kvprm_tree_attention
     t = _TREE.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), sq[0], sq[1], sk[0], sk[1], sv[0], sv[1],
                    so[0], so[1], _ints("block_table", block_table, i32, (n, width), dev),
                    _ints("lens", lens, i32, (n,), dev), _ints("start", start, i32, (n + 1,), dev), bits, width, n,
@@ -397,13 +399,13 @@ def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, ma
     if workspace is not None:
         if workspace.get_device() != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace is a contiguous tensor on CUDA device {dev}, got one on {workspace.device}")
-        rc = _call(T, dev, stream, lib().kvprm_tree_attention, c, t, workspace.data_ptr(),
+        rc = _call(T, dev, stream, go, c, t, workspace.data_ptr(),
                    workspace.numel() * workspace.element_size())
     elif T.device() == dev:
-        rc = _attend(T, c, t, dev, stream)
+        rc = _attend(T, go, c, t, dev, stream)
     else:
         with T.torch.cuda.device(dev):
-            rc = _attend(T, c, t, dev, stream)
+            rc = _attend(T, go, c, t, dev, stream)
     if rc != KVPRM_OK:
         _check(rc)
     return out

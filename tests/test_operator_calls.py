@@ -122,6 +122,9 @@ class Library:
         self.calls.append(("kvprm_tree_attention", (workspace, size, stream)))
         return 0 if size >= self.need else ops.KVPRM_ECAPACITY
 
+    def kvprm_tree_attention_filled(self, *args):
+        return self.kvprm_tree_attention(*args)
+
 
 @pytest.fixture
 def face(monkeypatch):
