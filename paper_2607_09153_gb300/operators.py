@@ -92,6 +92,42 @@ class _Torch:
         self.device = torch._C._cuda_getDevice                  # the calls' tensors have initialised CUDA
         self.capturing = torch.cuda.is_current_stream_capturing
         self.empty = torch.empty   # 1.8 us; Tensor.new_empty takes 3.3
+        self.grad_enabled = torch.is_grad_enabled
+        self.rotation, self.attention = _functions(torch)
+
+
+def _functions(torch):
+    """What autograd is told of the calls: the rotation's gradient, and that the attention has none."""
+
+    class Rotation(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, rope, positions, inverse, *tensors):
+            ctx.rope, ctx.inverse = rope, inverse
+            ctx.save_for_backward(positions)
+            out = rope._run(positions, tensors, None, inverse, None)
+            ctx.mark_non_differentiable(*[o for o, need in zip(out, ctx.needs_input_grad[3:]) if not need])
+            return out
+
+        @staticmethod
+        def backward(ctx, *grads):
+            (positions,) = ctx.saved_tensors
+            need = [i for i, n in enumerate(ctx.needs_input_grad[3:]) if n]
+            dense = [g if g.stride(2) == 1 else g.contiguous() for g in (grads[i] for i in need)]
+            result = [None] * (3 + len(grads))
+            for i, g in zip(need, ctx.rope._run(positions, dense, None, 1 - ctx.inverse, None)):
+                result[3 + i] = g
+            return tuple(result)
+
+    class Attention(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, call, *tensors):
+            return call()
+
+        @staticmethod
+        def backward(ctx, grad):
+            raise RuntimeError("tree_attention has no gradient: call it under torch.no_grad(), or on detached tensors")
+
+    return Rotation, Attention
 
 
 _t = None
@@ -149,9 +185,7 @@ def _call(T, device: int, stream, function, *args) -> int:
 
 
 def _result(T, shape, dtype, device, stream):
-    """A tensor of the stream that the call writes it on: one of another stream might still be in use there."""
-    if stream is None:
-        return T.empty(shape, dtype=dtype, device=device)
+    """A tensor of the stream that the call writes it on (one of another stream might still be in use there)."""
     with T.torch.cuda.stream(stream):
         return T.empty(shape, dtype=dtype, device=device)
 
@@ -181,7 +215,7 @@ class Rope:
 
     def rotate(self, positions, *tensors, out=None, stream=None) -> tuple:
         """Each of up to four tensors [tokens][heads][head_dim] (queries, keys) rotated by its tokens' int32
-        positions; `out`: tensors to write instead of new ones (the inputs themselves: in place)."""
+        positions; `out`: tensors to write instead of new ones (the inputs themselves: in place).  Differentiable."""
         return self._run(positions, tensors, out, 0, stream)
 
     def rotate_backward(self, positions, *grads, out=None, stream=None) -> tuple:
@@ -205,9 +239,11 @@ class Rope:
             shape = x.shape
             if len(shape) != 3 or shape[0] != n or shape[2] != hd:
                 raise ValueError(f"a tensor is {tuple(shape)}, expected [{n}][heads][{hd}]")
+            if x.requires_grad and T.grad_enabled():
+                return self._differentiable(T, positions, tensors, out, inverse, stream)
             st = _heads("a tensor", x, shape, dtype, dev)
-            if out is None:
-                o = _result(T, shape, dtype, x.device, stream)   # dense, also where x is a slice of wider rows
+            if out is None:   # dense, also where x is a slice of wider rows
+                o = T.empty(shape, dtype=dtype, device=x.device) if stream is None else _result(T, shape, dtype, x.device, stream)
                 so = (shape[1] * hd, hd)
             else:
                 o = out[i]
@@ -219,6 +255,12 @@ class Rope:
         if rc != KVPRM_OK:
             _check(rc)
         return tuple(result)
+
+    def _differentiable(self, T, positions, tensors, out, inverse, stream):
+        if out is not None:
+            raise ValueError("out= has no gradient: leave it away, or call under torch.no_grad()")
+        with T.torch.cuda.stream(stream):   # (autograd orders the backward pass by the current stream)
+            return T.rotation.apply(self, positions, inverse, *tensors)
 
     def __del__(self):
         try:
@@ -252,7 +294,8 @@ def _cache(T, pages, exponents) -> tuple:
 
 def cache_write(pages, slots, k, v, exponents=None, rope: Rope | None = None, positions=None, stream=None) -> None:
     """Writes tokens' keys and values [tokens][n_kv_heads][head_dim] into their slots (int64: 16 * page + place; below
-    zero: not written), quantised where the pages are, the keys rotated on the way with `rope` and int32 `positions`."""
+    zero: not written), quantised where the pages are, the keys rotated on the way with `rope` and int32 `positions`.  No
+    gradient passes through the pages."""
     T = _t or _torch()
     c, heads, hd, dev = _cache(T, pages, exponents)
     n, dtype = k.shape[0], k.dtype
@@ -316,10 +359,10 @@ def tree_mask(parents, start):
 class _Stream:
     """Scratch of the calls on one stream.  They follow one another there, so they can share it; `lock` is held while one
     of them enqueues its launches, for those of two host threads must not be mixed."""
-    __slots__ = ("lock", "scratch")
+    __slots__ = ("lock", "scratch", "address", "bytes")
 
     def __init__(self):
-        self.lock, self.scratch = threading.RLock(), None
+        self.lock, self.scratch, self.address, self.bytes = threading.RLock(), None, 0, 0
 
 
 _streams: dict = {}   # by device and stream handle
@@ -347,14 +390,24 @@ def _attend(T, go, c: bytes, t: bytes, device: int, stream) -> int:
     if capturing:   # scratch of the graph's own, for the graph may be replayed on any stream
         w = _scratch(T, _workspace_bytes(c, t), device, stream)
         return go(c, t, w.data_ptr(), w.numel(), handle)
-    mine = _streams.get((device, handle)) or _streams.setdefault((device, handle), _Stream())
+    key = (device, handle)
+    mine = _streams.get(key) or _streams.setdefault(key, _Stream())
     with mine.lock:
-        w = mine.scratch
-        rc = KVPRM_ECAPACITY if w is None else go(c, t, w.data_ptr(), w.numel(), handle)
+        rc = go(c, t, mine.address, mine.bytes, handle) if mine.bytes else KVPRM_ECAPACITY
         if rc == KVPRM_ECAPACITY:
             w = mine.scratch = _scratch(T, _workspace_bytes(c, t), device, stream)
-            rc = go(c, t, w.data_ptr(), w.numel(), handle)
+            mine.address, mine.bytes = w.data_ptr(), w.numel()
+            rc = go(c, t, mine.address, mine.bytes, handle)
     return rc
+
+
+def _attend_without_gradient(T, args):
+    """tree_attention(*args) on tensors that require gradients."""
+    *_, out, _, stream = args
+    if out is not None:
+        raise ValueError("out= has no gradient: call under torch.no_grad()")
+    with T.torch.cuda.stream(stream):
+        return T.attention.apply(lambda: tree_attention(*args), *args[:4])
 
 
 def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, max_len: int | None = None,
@@ -366,8 +419,12 @@ def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, ma
     cached ones in pages block_table[s][0 ..] (int32).  mask: int32 [tokens][words], bit j of a token's row: it sees
     drafted token j of its sequence (tree_mask); None: those up to itself.  max_len sizes the launch (default: the
     block table's width).  Returns [tokens][n_q_heads][head_dim]: `out`, where rows of tokens that no sequence has, or one
-    with more than max_drafts, are left as they are, or a new tensor, where they are zeros and NaN."""
+    with more than max_drafts, are left as they are, or a new tensor, where they are zeros and NaN.  There is no gradient: a
+    backward pass that reaches the call raises."""
     T = _t or _torch()
+    if (q.requires_grad or k.requires_grad or v.requires_grad or pages.requires_grad) and T.grad_enabled():
+        return _attend_without_gradient(T, (q, k, v, pages, block_table, lens, start, max_drafts, max_len, exponents, mask, scale,
+                                            out, workspace, stream))
     c, heads, hd, dev = _cache(T, pages, exponents)
     shape, _ = _rows("q", q)
     tokens, nq, _ = shape
@@ -385,7 +442,7 @@ def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, ma
         words = mask.shape[1]
         bits = _ints("mask", mask, i32, (tokens, words), dev)
     if out is None:
-        out = _result(T, shape, bf16, q.device, stream)
+        out = T.empty(shape, dtype=bf16, device=q.device) if stream is None else _result(T, shape, bf16, q.device, stream)
         so = (nq * hd, hd)
         go = lib().kvprm_tree_attention_filled
     else:
