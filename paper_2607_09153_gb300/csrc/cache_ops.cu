@@ -607,11 +607,11 @@ int kvprm_cache_write(const kvprm_cache* cache, int32_t dtype, const void* k, in
   const int size = size_of(dtype);
   if (size == 0) return operator_fail(KVPRM_EINVAL, "%s: dtype %d", who, dtype);
   if (n_tokens < 0) return operator_fail(KVPRM_EINVAL, "%s: n_tokens %lld", who, static_cast<long long>(n_tokens));
-  if ((rope == nullptr) != (positions == nullptr))
-    return operator_fail(KVPRM_EINVAL, "%s: rope and positions come together", who);
   if (rope && rope->table.dim > cache->head_dim)
     return operator_fail(KVPRM_EINVAL, "%s: %d elements rotated of head_dim %d", who, rope->table.dim, cache->head_dim);
   if (n_tokens == 0) return KVPRM_OK;
+  if ((rope == nullptr) != (positions == nullptr))
+    return operator_fail(KVPRM_EINVAL, "%s: rope and positions come together", who);
   if (!k || !v || !slots) return operator_fail(KVPRM_EINVAL, "%s: k, v or slots are NULL", who);
   if ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v)) % size || reinterpret_cast<uintptr_t>(slots) % 8)
     return operator_fail(KVPRM_EINVAL, "%s: k, v or slots are not aligned to their elements", who);
