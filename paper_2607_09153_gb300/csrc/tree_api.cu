@@ -82,8 +82,11 @@ int attend(const kvprm_cache* cache, const kvprm_tree* t, void* workspace, int64
   const bool seqs = t->n_seqs > 0;
   if (!t->q || !t->k || !t->v || !t->out || !t->start || (seqs && !t->lens) || (seqs && t->max_blocks > 0 && !t->block_table))
     return operator_fail(KVPRM_EINVAL, "%s: NULL argument", who);
-  if (!aligned16(t->q) || !aligned16(t->k) || !aligned16(t->v) || !aligned16(t->out) ||
-      ((t->q_token | t->q_head | t->k_token | t->k_head | t->v_token | t->v_head | t->out_token | t->out_head) & 7) != 0)
+  // (the stride of a dimension of one is nobody's)
+  int64_t strides = t->n_tokens > 1 ? t->q_token | t->k_token | t->v_token | t->out_token : 0;
+  if (t->n_q_heads > 1) strides |= t->q_head | t->out_head;
+  if (cache->n_kv_heads > 1) strides |= t->k_head | t->v_head;
+  if (!aligned16(t->q) || !aligned16(t->k) || !aligned16(t->v) || !aligned16(t->out) || (strides & 7) != 0)
     return operator_fail(KVPRM_EINVAL, "%s: rows of q, k, v and out have to be 16-byte aligned", who);
   int sms = 0;
   if (const int rc = sm_count(&sms)) return rc;

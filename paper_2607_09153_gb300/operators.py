@@ -155,7 +155,7 @@ def _heads(name: str, t, shape, dtype, device: int) -> tuple:
             raise TypeError(f"{name} is {t.dtype}, expected {dtype}")
         raise ValueError(f"{name} is {tuple(t.shape)} on {t.device}, expected {tuple(shape)} on CUDA device {device}")
     st = t.stride()
-    if st[2] != 1 and shape[2] > 1:
+    if st[2] != 1 and shape[2] > 1 and t.numel() > 0:
         raise ValueError(f"the elements of a head of {name} are not side by side: strides {st}")
     return st
 
