@@ -592,9 +592,11 @@ KVPRM_API const char* kvprm_operator_error(void);
  *            (2 ln base) the pair that turns n times (clamped to 0 and
  *            rotary_dim - 1; 0 < low < high).
  *  magnitude    finite; 1 unless the stretching asks for another.
- * The handle holds the f_i as 64-bit fractions of a turn, on the host: a
- * position's angle is their product in whole numbers modulo one turn, exact at
- * every int32 position, before a sine and cosine in 32 bits. */
+ * The handle holds the f_i / 2 pi, computed in 64-bit floating point, as 64-bit
+ * fractions of a turn on the host.  A position's angle is their product in whole
+ * numbers modulo one turn, so it is off by 2^-53 turns for each position at most
+ * (2^-36 at 131,072) and by the 2^-26 turns of a 24-bit fraction, of which a sine
+ * and cosine are taken in 32 bits. */
 enum { KVPRM_ROPE_NONE = 0, KVPRM_ROPE_LINEAR = 1, KVPRM_ROPE_BASE = 2, KVPRM_ROPE_RAMP = 3, KVPRM_ROPE_SMOOTH = 4 };
 typedef struct {
   int32_t rotary_dim, interleaved, scaling, original_len;

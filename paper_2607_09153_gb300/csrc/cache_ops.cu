@@ -106,9 +106,10 @@ struct FastDiv {
 };
 
 // Cosines and sines (times the magnitude) of a CTA's tokens, [token][pair] in shared memory.  The
-// angle is pos * turns in whole numbers modulo one turn: its upper 32 bits as a signed fraction of a
-// turn are within 2^-32 turns at every position, where a 32-bit product of a position of 131,072 and
-// a frequency would be 2^-8 radians off.
+// angle is pos * turns in whole numbers modulo one turn, which rounds nothing: it is off by the
+// table's own error (2^-53 turns for each position at most), the lower half that is left out (2^-32)
+// and a float's 24 bits (2^-26), where a 32-bit product of a position of 131,072 and a frequency would
+// be 2^-8 radians off.
 __device__ __forceinline__ void fill_rotations(const RopeTable& tab, const FastDiv& by_pairs, const int32_t* __restrict__ positions,
                                                int64_t first, int tokens, float sign, float* s_cos, float* s_sin) {
   const int pairs = tab.dim >> 1;
