@@ -591,7 +591,8 @@ KVPRM_API const char* kvprm_operator_error(void);
  *            ceil(i(low)), i(n) = rotary_dim ln(original_len / (2 pi n)) /
  *            (2 ln base) the pair that turns n times (clamped to 0 and
  *            rotary_dim - 1; 0 < low < high).
- *  magnitude    finite; 1 unless the stretching asks for another.
+ *  magnitude    finite in 32 bits; 1 unless the stretching asks for another (RAMP's
+ *               usual one, 0.1 ln(factor) + 1, is the caller's to give).
  * The handle holds the f_i / 2 pi, computed in 64-bit floating point, as 64-bit
  * fractions of a turn on the host.  A position's angle is their product in whole
  * numbers modulo one turn, so it is off by 2^-53 turns for each position at most

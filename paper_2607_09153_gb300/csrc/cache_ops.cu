@@ -505,7 +505,7 @@ int kvprm_rope_create(const kvprm_rope_config* c, kvprm_rope** out) {
     return operator_fail(KVPRM_EINVAL, "kvprm_rope_create: interleaved %d", c->interleaved);
   if (c->scaling < KVPRM_ROPE_NONE || c->scaling > KVPRM_ROPE_SMOOTH)
     return operator_fail(KVPRM_EINVAL, "kvprm_rope_create: scaling %d", c->scaling);
-  if (!(c->base > 1.0) || !std::isfinite(c->base) || !std::isfinite(c->magnitude))
+  if (!(c->base > 1.0) || !std::isfinite(c->base) || !std::isfinite(static_cast<float>(c->magnitude)))
     return operator_fail(KVPRM_EINVAL, "kvprm_rope_create: base %g, magnitude %g", c->base, c->magnitude);
   if (c->scaling != KVPRM_ROPE_NONE && (!(c->factor >= 1.0) || !std::isfinite(c->factor)))
     return operator_fail(KVPRM_EINVAL, "kvprm_rope_create: factor %g", c->factor);
@@ -514,11 +514,12 @@ int kvprm_rope_create(const kvprm_rope_config* c, kvprm_rope** out) {
   const bool turns_matter = c->scaling == KVPRM_ROPE_RAMP || c->scaling == KVPRM_ROPE_SMOOTH;
   if (turns_matter && (c->original_len < 1 || !(c->low > 0.0) || !(c->high > c->low) || !std::isfinite(c->high)))
     return operator_fail(KVPRM_EINVAL, "kvprm_rope_create: original_len %d, low %g, high %g", c->original_len, c->low, c->high);
+  double base = c->base;
+  if (c->scaling == KVPRM_ROPE_BASE) base *= std::pow(c->factor, static_cast<double>(rd) / (rd - 2));
+  if (!std::isfinite(base)) return operator_fail(KVPRM_EINVAL, "kvprm_rope_create: base %g times factor %g", c->base, c->factor);
   kvprm_rope* r = new (std::nothrow) kvprm_rope();
   if (!r) return operator_fail(KVPRM_ENOMEM, "kvprm_rope_create: out of memory");
   constexpr double kTwoPi = 6.283185307179586476925286766559;
-  double base = c->base;
-  if (c->scaling == KVPRM_ROPE_BASE) base *= std::pow(c->factor, static_cast<double>(rd) / (rd - 2));
   double first = 0.0, last = 0.0;   // RAMP: the pairs between which the weight falls
   if (c->scaling == KVPRM_ROPE_RAMP) {
     auto pair_at = [&](double n) { return rd * std::log(c->original_len / (kTwoPi * n)) / (2.0 * std::log(base)); };
