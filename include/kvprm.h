@@ -633,7 +633,8 @@ KVPRM_API int kvprm_rope_rotate(const kvprm_rope* rope, int32_t dtype, int32_t h
 
 /* One layer of a paged cache (at most 2^30 pages): pages [n_pages][2][n_kv_heads][16][head_dim] (keys,
  * then values; head_dim 64 or 128), 16-byte aligned, of bf16 -- what the scoring
- * calls read -- or of 8-bit floating point (4 exponent and 3 mantissa bits,
+ * calls read, its keys rotated over the whole head in halves, not interleaved or
+ * stretched, with the context's rope_base: they rotate their query so -- or of 8-bit floating point (4 exponent and 3 mantissa bits,
  * largest value 448, no infinities) with a power of two for each row of head_dim
  * elements: exponents, uint8 [n_pages][2][n_kv_heads][16] (16-byte aligned), a
  * row's values being code * 2^(exponent - 127), NaN where the exponent is 255 or the
@@ -648,8 +649,8 @@ typedef struct {
 } kvprm_cache;
 /* Writes tokens into their slots: token t's keys and values of every head go to
  * slot slots[t] = 16 * page + place in the page (device int64).  A token whose
- * slot is outside [0, 16 n_pages) is not written (padding, rejected drafts); of
- * several tokens with one slot any may win.
+ * slot is outside [0, 16 n_pages) is not written (padding, rejected drafts).  A
+ * slot is for one token of a call: of several, pieces of each may end up in it.
  *  k, v       device [n_tokens][n_kv_heads][head_dim] of `dtype`, with strides
  *  rope, positions  keys are rotated on the way (both NULL: k is rotated already)
  * The values are rounded once, from 32 bits: to bf16, or scaled by the smallest
@@ -662,8 +663,8 @@ KVPRM_API int kvprm_cache_write(const kvprm_cache* cache, int32_t dtype, const v
                                 int64_t n_tokens, const kvprm_rope* rope, const int32_t* positions, void* stream);
 /* Quantised pages into bf16 pages (that the scoring calls read): page src[i] of
  * `cache` (KVPRM_CACHE_E4M3) becomes page dst[i] of out, a bf16 layer of
- * out_pages pages with the same heads; src, dst device int32 [n].  A pair with a
- * page outside its layer is left out.  Exact, but for magnitudes below bf16's
+ * out_pages pages with the same heads; src, dst device int32 [n], no dst twice.  A
+ * pair with a page outside its layer is left out.  Exact, but for magnitudes below bf16's
  * least normal number.
  * Errors: KVPRM_EINVAL, KVPRM_ECUDA. */
 KVPRM_API int kvprm_cache_expand(const kvprm_cache* cache, const int32_t* src, const int32_t* dst, int64_t n, void* out,

@@ -294,8 +294,8 @@ def _cache(T, pages, exponents) -> tuple:
 
 def cache_write(pages, slots, k, v, exponents=None, rope: Rope | None = None, positions=None, stream=None) -> None:
     """Writes tokens' keys and values [tokens][n_kv_heads][head_dim] into their slots (int64: 16 * page + place; below
-    zero: not written), quantised where the pages are, the keys rotated on the way with `rope` and int32 `positions`.  No
-    gradient passes through the pages."""
+    zero: not written; one token each), quantised where the pages are, the keys rotated on the way with `rope` and int32
+    `positions`.  No gradient passes through the pages."""
     T = _t or _torch()
     c, heads, hd, dev = _cache(T, pages, exponents)
     n, dtype = k.shape[0], k.dtype
@@ -315,8 +315,8 @@ def cache_write(pages, slots, k, v, exponents=None, rope: Rope | None = None, po
 
 
 def cache_expand(pages, exponents, src, out, dst=None, stream=None):
-    """Quantised pages src[i] (int32) as bf16 pages dst[i] (int32; default: i) of `out`, a layer that the scoring calls
-    read; returns `out`."""
+    """Quantised pages src[i] (int32) as bf16 pages dst[i] (int32, none twice; default: i) of `out`, a layer that the
+    scoring calls read; returns `out`."""
     T = _t or _torch()
     c, _, _, dev = _cache(T, pages, exponents)
     shape = out.shape
@@ -420,7 +420,8 @@ def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, ma
     drafted token j of its sequence (tree_mask); None: those up to itself.  max_len sizes the launch (default: the
     block table's width).  Returns [tokens][n_q_heads][head_dim]: `out`, where rows of tokens that no sequence has, or one
     with more than max_drafts, are left as they are, or a new tensor, where they are zeros and NaN.  There is no gradient: a
-    backward pass that reaches the call raises."""
+    backward pass that reaches the call raises.  Scratch is kept for each stream, as large as its largest call wanted;
+    workspace: a contiguous tensor to use instead (one that is too small is refused with the bytes that are needed)."""
     T = _t or _torch()
     if (q.requires_grad or k.requires_grad or v.requires_grad or pages.requires_grad) and T.grad_enabled():
         return _attend_without_gradient(T, (q, k, v, pages, block_table, lens, start, max_drafts, max_len, exponents, mask, scale,
