@@ -18,7 +18,7 @@
 // shared memory's bandwidth), softmax (1,500) and O (500), 3,400 cycles a chunk for both groups: 8 kv heads, 64
 // tokens of 4 heads each over 4 x 16,384 bf16 tokens in 80 us, 860 TFLOP/s.  An 8-bit chunk: its conversion, some
 // 1,800 cycles of the eight producer warps for a tile of 128 x 128, which beside two tiles' products takes
-// 2,800: 16 sequences of 4 heads with 126 rows over 9,001 tokens in 84 us (bf16: 70).  Short calls: what a part
+// 2,800: 16 sequences of 4 heads with 126 rows over 9,001 tokens in 86 us (bf16: 70).  Short calls: what a part
 // begins and ends with, 5 and 2 us, and the join.
 #include <cuda.h>
 #include <cudaTypedefs.h>
@@ -181,25 +181,20 @@ __device__ __forceinline__ bool not_finite2(uint32_t w) {
 // value; f1 (times f2, where the two do not fit one factor) is 2^120 times the row's power.  The even and the odd codes of
 // a word each become a pair, so that the head's dimensions come in the order 0 2 1 3, 4 6 5 7 ..: Q and the drafted
 // tokens are laid out alike (paired), and the outputs are put back in order.
-//   bf16 has no place for the NaN codes, 0x7F and 0xFF: there they would be 480, so a page that has one (nan_carries) is converted
-// with NANS; a factor of zero, a row past the length, keeps them out.
-template <bool TWO, bool NANS>
+//   bf16 has no place for the NaN codes, 0x7F and 0xFF: there they would be 480.  So where a page has one, or a row that needs
+// two factors, it takes the longer form (not PLAIN); a factor of zero, a row past the length, keeps NaN out.
+template <bool PLAIN>
 __device__ __forceinline__ void bf16_of16(const uint4& c, uint32_t f1, uint32_t f2, uint4* lo, uint4* hi) {
   auto pair = [&](uint32_t w, uint32_t* e, uint32_t* o) {
     const uint32_t even = (w << 4) & 0x07F007F0u, odd = (w >> 4) & 0x07F007F0u;
     *e = mul_bf16x2(even | ((w << 8) & 0x80008000u), f1);
     *o = mul_bf16x2(odd | (w & 0x80008000u), f1);
-    if (TWO) {
-      *e = mul_bf16x2(*e, f2);
-      *o = mul_bf16x2(*o, f2);
-    }
-    if (NANS) {
-      auto nans = [](uint32_t v) {
-        return ((v & 0xFFFFu) == 0x07F0u ? 0x7FC0u : 0u) | (v >> 16 == 0x07F0u ? 0x7FC00000u : 0u);
-      };
-      *e |= f1 != 0u ? nans(even) : 0u;
-      *o |= f1 != 0u ? nans(odd) : 0u;
-    }
+    if (PLAIN) return;
+    auto nans = [&](uint32_t v) {
+      return f1 == 0u ? 0u : ((v & 0xFFFFu) == 0x07F0u ? 0x7FC0u : 0u) | (v >> 16 == 0x07F0u ? 0x7FC00000u : 0u);
+    };
+    *e = mul_bf16x2(*e, f2) | nans(even);
+    *o = mul_bf16x2(*o, f2) | nans(odd);
   };
   pair(c.x, &lo->x, &lo->y);
   pair(c.y, &lo->z, &lo->w);
@@ -517,38 +512,27 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
             const bool live = my_page * kTreePage + lane % kTreePage < p.q.len - c * kChunk, two = e > 134u && live;
             uint32_t f = (two ? 254u : e + 120u) << 7 | (two ? (e == 255u ? 0x7FC0u : (e - 7u) << 7) : 0x3F80u) << 16;
             if (!live) f = 0x3F800000u;
-            // (looked for before the conversion, whose instructions then hide the vote: 64 drafts over 16 ragged sequences
-            // 162 us without the check, 164 with it, 168 with the vote at the end)
+            // (126 rows of 4 heads over 16 x 9,001 tokens: 84 us without the check for NaN codes, 86 with it, 91 with a vote and a
+            // loop of its own, whose loads made every item wait for those ahead)
             uint32_t carries = 0;
 #pragma unroll
             for (int k = 0; k < kSteps; ++k)
               carries |= nan_carries(codes[k].x) | nan_carries(codes[k].y) | nan_carries(codes[k].z) | nan_carries(codes[k].w);
-            const bool nan = __any_sync(0xffffffffu, (carries & 0x80808080u) != 0u);
-            auto step = [&](int k, const uint4& x, auto twice, auto nans) {   // kTeam rows
-              const uint32_t fr = __shfl_sync(0xffffffffu, f, my_row + kTeam * k);
-              uint4 lo, hi;
-              bf16_of16<decltype(twice)::value, decltype(nans)::value>(x, __byte_perm(fr, 0, 0x1010), __byte_perm(fr, 0, 0x3232), &lo,
-                                                                       &hi);
-              const int row = my_page * kTreePage + k * kTeam + my_row;
-              *reinterpret_cast<uint4*>(dst + swizzled<HD>(row, 2 * my_piece)) = lo;
-              *reinterpret_cast<uint4*>(dst + swizzled<HD>(row, 2 * my_piece + 1)) = hi;
-            };
-            auto convert = [&](auto twice) {
+            auto convert = [&](auto plain) {
 #pragma unroll
-              for (int k = 0; k < kSteps; ++k) step(k, codes[k], twice, std::false_type());
+              for (int k = 0; k < kSteps; ++k) {
+                const uint32_t fr = __shfl_sync(0xffffffffu, f, my_row + kTeam * k);
+                uint4 lo, hi;
+                bf16_of16<decltype(plain)::value>(codes[k], __byte_perm(fr, 0, 0x1010), __byte_perm(fr, 0, 0x3232), &lo, &hi);
+                const int row = my_page * kTreePage + k * kTeam + my_row;
+                *reinterpret_cast<uint4*>(dst + swizzled<HD>(row, 2 * my_piece)) = lo;
+                *reinterpret_cast<uint4*>(dst + swizzled<HD>(row, 2 * my_piece + 1)) = hi;
+              }
             };
-            if (nan) {   // rare: a loop, on the codes loaded again
-              const int32_t at = page_of(item);
-              const uint8_t* src = a.pages + ((static_cast<int64_t>(max(at, 0)) * 2 + kv) * a.n_kv + p.g) * kTreePage * HD +
-                                   my_row * HD + my_piece * 16;
-#pragma unroll 1
-              for (int k = 0; k < kSteps; ++k)
-                step(k, at >= 0 ? ldg_stream(src + k * 512) : make_uint4(0u, 0u, 0u, 0u), std::true_type(), std::true_type());
-            } else if (__any_sync(0xffffffffu, two)) {
-              convert(std::true_type());
-            } else {
+            if (__any_sync(0xffffffffu, two || (carries & 0x80808080u) != 0u))
               convert(std::false_type());
-            }
+            else
+              convert(std::true_type());
             slot_filled(&st.slot_full[slot]);
             continue;
           }
