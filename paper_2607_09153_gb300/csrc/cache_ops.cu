@@ -5,11 +5,12 @@
 // by one launch's latency (a decoding step).  What they share: a CTA takes a few tokens, makes each
 // token's cosines and sines once in shared memory, and its threads then run over the tokens' heads.
 // Measured on a GB300 (copy rate 6,773 GB/s): 32,768 tokens of 32 + 8 heads of 128 rotated in bf16 in
-// 103 us (6,540 GB/s; with eight tokens a CTA 106), 9,001 tokens of 16 + 4 heads of 64, fp32 gradients,
-// in 20 us (4,500 GB/s: one wave of CTAs), 4,099 e4m3 pages of 8 heads expanded in 67 us (6,040 GB/s),
-// 30,001 tokens of 8 heads rotated and written as e4m3 in 47 us (3,930 GB/s: the
-// largest magnitude, the exponent and the codes of a row take instructions that two bytes a value do not
-// hide).  Steps of 16 to 64 tokens take 2 to 2.5 us of the GPU's time.
+// 103 us (6,540 GB/s; with eight tokens a CTA 106; neighbouring pairs 110), 9,001 tokens of 16 + 4 heads
+// of 64, fp32 gradients, in 20 us (4,500 GB/s: not two waves of CTAs, whose loads wait behind a barrier
+// for their sines), 4,099 e4m3 pages of 8 heads expanded in 67 us (6,040 GB/s), 30,001 tokens of 8 heads
+// rotated and written as e4m3 in 47 us (3,930 GB/s: a chain of slot, row, shuffles and store for each
+// token of a thread, whose loads stall it most, with 0.62 of the issue slots in use; not rotated 39 us,
+// from fp32 55, into bf16 pages 49).  Steps of 16 to 64 tokens take 2 to 2.5 us of the GPU's time.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>

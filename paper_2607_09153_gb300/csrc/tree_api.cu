@@ -46,7 +46,7 @@ int sm_count(int* sms) {
 
 // More than 32 rows of a kv head go to the tensor cores (us a call, registers / tensor cores: 8 heads with 24 rows over ragged
 // 20,000 bf16 tokens 76 / 78, 8-bit 66 / 89; with 32 over 8 x 32,768 bf16 tokens 187 / 186, 8-bit 155 / 221; 4 heads with 63 over
-// 16 x 9,001 8-bit tokens 97 / 79; 2 heads with 42 over ragged 1,000 bf16 tokens 19 / 21, with 126 22 / 21).  CTAs: as many as
+// 16 x 9,001 8-bit tokens 97 / 80; 2 heads with 42 over ragged 1,000 bf16 tokens 19 / 21, with 126 22 / 21).  CTAs: as many as
 // run at once.  Pairs that have a CTA each and few blocks stay whole, for a cut one needs the join (cut / whole: registers, 2 x 8
 // heads over 400 tokens 18 / 13, 16 x 4 heads with 28 rows 21 / 15, over 900 22 / 25; tensor cores, 16 x 2 heads with 126 rows
 // over ragged 300 8-bit tokens 23 / 18, over 600 21 / 23); where CTAs have several, uneven shares cost more, and fewer do.
