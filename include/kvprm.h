@@ -639,11 +639,14 @@ KVPRM_API int kvprm_rope_rotate(const kvprm_rope* rope, int32_t dtype, int32_t h
  * elements: exponents, uint8 [n_pages][2][n_kv_heads][16] (16-byte aligned), a
  * row's values being code * 2^(exponent - 127), NaN where the exponent is 255 or the
  * code 0x7F or 0xFF (kvprm_cache_write leaves the former only).  A power of two costs an
- * 8-bit float nothing in precision, never rounds, and a byte per row. */
-enum { KVPRM_CACHE_BF16 = 0, KVPRM_CACHE_E4M3 = 1 };
+ * 8-bit float nothing in precision, never rounds, and a byte per row.  Or of 4-bit floating point
+ * (2 exponent bits and 1 mantissa bit: 0, 1/2, 1, 3/2, 2, 3, 4, 6 and a sign; nothing that is not finite), pages uint8
+ * [n_pages][2][n_kv_heads][16][head_dim / 2], element 2 i in the low half of byte i and 2 i + 1 in the high one, with
+ * a power of two for each 32 elements: exponents uint8 [n_pages][2][n_kv_heads][16][head_dim / 32], read likewise. */
+enum { KVPRM_CACHE_BF16 = 0, KVPRM_CACHE_E4M3 = 1, KVPRM_CACHE_E2M1 = 2 };
 typedef struct {
   void* pages;
-  void* exponents;   /* KVPRM_CACHE_E4M3 only, else NULL */
+  void* exponents;   /* KVPRM_CACHE_E4M3 and KVPRM_CACHE_E2M1, else NULL */
   int64_t n_pages;
   int32_t n_kv_heads, head_dim, format;
 } kvprm_cache;
@@ -656,13 +659,14 @@ typedef struct {
  * The values are rounded once, from 32 bits: to bf16, or scaled by the smallest
  * 2^e (e >= -127) that brings the row's largest finite magnitude to 448 or less
  * and rounded to 8 bits, to nearest even; infinities become +-448 2^e, and a row
- * with a NaN gets the exponent 255, which makes all of it read as NaN.
+ * with a NaN gets the exponent 255, which makes all of it read as NaN.  4-bit pages
+ * the same, by blocks of 32 elements and with 6 in the place of 448.
  * Errors: KVPRM_EINVAL, KVPRM_ECUDA. */
 KVPRM_API int kvprm_cache_write(const kvprm_cache* cache, int32_t dtype, const void* k, int64_t k_token, int64_t k_head,
                                 const void* v, int64_t v_token, int64_t v_head, const int64_t* slots,
                                 int64_t n_tokens, const kvprm_rope* rope, const int32_t* positions, void* stream);
 /* Quantised pages into bf16 pages (that the scoring calls read): page src[i] of
- * `cache` (KVPRM_CACHE_E4M3) becomes page dst[i] of out, a bf16 layer of
+ * `cache` (not KVPRM_CACHE_BF16) becomes page dst[i] of out, a bf16 layer of
  * out_pages pages with the same heads; src, dst device int32 [n], no dst twice.  A
  * pair with a page outside its layer is left out.  Exact, but for magnitudes below bf16's
  * least normal number.
@@ -694,7 +698,8 @@ KVPRM_API int kvprm_cache_expand(const kvprm_cache* cache, const int32_t* src, c
  *               do not depend on it beyond the order of sums
  * Scores, weights' sums and accumulators are fp32; the weights that multiply the
  * values are rounded to bf16 (an 8-bit cache with up to 32 query rows of a kv
- * head: fp16, near the sequence's largest power of two), as the output is to bf16.
+ * head: fp16, near the sequence's largest power of two; a 4-bit one likewise, weights
+ * below 2^-26 of the largest in steps of 2^-36 of it), as the output is to bf16.
  * What the host cannot see: a sequence whose length is negative or beyond its
  * block table, or that has a page outside the cache, gets NaN in every output; one whose
  * drafted tokens are not within [0, n_tokens), or more than max_drafts, is left
@@ -722,6 +727,65 @@ KVPRM_API int kvprm_tree_attention(const kvprm_cache* cache, const kvprm_tree* t
  * sequence has become zeros, those of a sequence that is left out NaN. */
 KVPRM_API int kvprm_tree_attention_filled(const kvprm_cache* cache, const kvprm_tree* t, void* workspace,
                                           int64_t workspace_bytes, void* stream);
+
+/* Pages between two steps of a search.  A pool is what a block table's page numbers index: `layers` times
+ * n_pages pages of page_bytes consecutive bytes, page p of layer l at base + l * layer_stride + p * page_stride
+ * (bytes; all multiples of 16, base 16-byte aligned).  A cache of several layers is one such pool, its exponents are
+ * another; layers that were allocated apart are pools of one layer each.  What a page holds does not matter. */
+enum { KVPRM_MAX_POOLS = 96 };
+typedef struct {
+  void* base;
+  int64_t layer_stride, page_stride, page_bytes;
+  int32_t layers;
+} kvprm_pool;
+/* Replaces n_seqs sequences by n_new ones, each of which continues one of them or begins: sequences that nobody
+ * continues are dropped, those that several do are doubled, and each is given the pages for the tokens to come.
+ *  n_pages      of every pool
+ *  refs         int32 [n_pages]: who holds a page, each sequence that lists it and whoever else; 0 or less: it is free
+ *  block_table  int32 [n_seqs][max_blocks], lens int32 [n_seqs]: the first ceil(lens[s] / 16) entries of a row are its pages
+ *  parents      int32 [n_new]: the sequence that is continued; any other number begins an empty one
+ *  room         int32 [n_new] (may be NULL): tokens that a new sequence is to have pages for beyond its cached ones
+ * Written (none may overlap another or an input):
+ *  table_out    int32 [n_new][width]: the pages, -1 behind them
+ *  lens_out     int32 [n_new]: the cached tokens, lens[parents[i]] or 0
+ *  refs_out     int32 [n_pages]: refs without the old tables' references and with the new ones'
+ *  counts       int32 [2]: pages that are free now, and pages that were wanted and not to be had
+ * Full pages are shared.  A last page that has places left, which its sequence is to write, is kept by the first of
+ * the new sequences that end in it, if nobody else holds it; the others get a copy of it, in every pool.  Copies and
+ * new pages are taken from the free ones, those that the dropped sequences held among them, the lowest first,
+ * sequence by sequence (a copy before the pages to come).  Where none is left, the entry is -1 and a copy is left out:
+ * such a table makes NaN in kvprm_tree_attention, and its slots are not written by kvprm_cache_write.  Pages for which
+ * a row of `width` has no place count as wanted.  What the host cannot see: a sequence whose length is negative or
+ * beyond its block table keeps its references, and those that continue it get its length and no pages; an entry
+ * outside the pool is taken over as it is.
+ *  workspace    as for kvprm_tree_attention, of kvprm_fork_workspace() bytes for the same arguments
+ * Errors: KVPRM_EINVAL (also for more than 2^24 sequences, or new tables of 2^30 pages together), KVPRM_ECAPACITY, KVPRM_ECUDA. */
+typedef struct {
+  const int32_t *refs, *block_table, *lens, *parents, *room;
+  int32_t *refs_out, *table_out, *lens_out, *counts;
+  int64_t n_pages;
+  int32_t n_pools, n_seqs, max_blocks, n_new, width;
+} kvprm_fork;
+KVPRM_API int kvprm_fork_workspace(const kvprm_pool* pools, const kvprm_fork* f, int64_t* bytes);
+KVPRM_API int kvprm_cache_fork(const kvprm_pool* pools, const kvprm_fork* f, void* workspace, int64_t workspace_bytes, void* stream);
+/* Closes a pool up: of n pages in use (refs > 0), those that are not among the first n move, in order, to the free ones
+ * there, in every pool; their old places keep what they held.
+ *  refs, block_table, lens  as above
+ * Written:
+ *  refs_out     int32 [n_pages], table_out int32 [n_seqs][max_blocks]: as above, with the new numbers (-1 behind a row's pages; an
+ *               entry that is free becomes -1)
+ *  moved        int32 [n_pages]: where each page is now (-1: it was free), for other tables and holders
+ *  counts       int32 [2]: pages in use, and pages that moved
+ * Errors: as above. */
+typedef struct {
+  const int32_t *refs, *block_table, *lens;
+  int32_t *refs_out, *table_out, *moved, *counts;
+  int64_t n_pages;
+  int32_t n_pools, n_seqs, max_blocks;
+} kvprm_compact;
+KVPRM_API int kvprm_compact_workspace(const kvprm_pool* pools, const kvprm_compact* f, int64_t* bytes);
+KVPRM_API int kvprm_cache_compact(const kvprm_pool* pools, const kvprm_compact* f, void* workspace, int64_t workspace_bytes,
+                                  void* stream);
 
 #ifdef __cplusplus
 }

@@ -290,9 +290,63 @@ __device__ __forceinline__ uint2 e4m3_of8(const float (&x)[8], float f) {
   return make_uint2(w[0], w[1]);
 }
 
+// The exponent of a block of 4-bit elements, likewise with most <= 6 * 2^e = 1.5 * 2^(2 + e).
+__device__ __forceinline__ int block_exponent(float most) {
+  const uint32_t u = __float_as_uint(most);
+  const int e = static_cast<int>(u >> 23) - 127 - 2 + ((u & 0x7FFFFFu) > 0x400000u ? 1 : 0);
+  return max(e, -127);
+}
+
+// Eight e2m1 codes, the first element's in the lowest four bits.  (A cvt's first operand becomes the high half of its byte.)
+__device__ __forceinline__ uint32_t e2m1_of8(const float (&x)[8], float f) {
+  uint32_t w;
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t}"
+      : "=r"(w)
+      : "f"(x[0] * f), "f"(x[1] * f), "f"(x[2] * f), "f"(x[3] * f), "f"(x[4] * f), "f"(x[5] * f), "f"(x[6] * f), "f"(x[7] * f));
+  return w;
+}
+
+// The largest magnitude of eight elements, of which infinities may be left out; NaN if there is one (and none is left out).
+__device__ __forceinline__ float most_of8(const float (&x)[8]) {
+  float most = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) most = max_nan(most, fabsf(x[k]));
+  return most;
+}
+__device__ __forceinline__ float finite_of8(const float (&x)[8]) {
+  float most = 0.f;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) most = fmaxf(most, fabsf(x[k]) < INFINITY ? fabsf(x[k]) : 0.f);
+  return most;
+}
+
+// Eight elements of a block of 32, which four neighbouring lanes share (all of a warp's take part): the codes, and the
+// block's exponent byte.
+__device__ __forceinline__ uint32_t block_of32(const float (&x)[8], uint8_t* exponent) {
+  float most = most_of8(x);
+  most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, 1));
+  most = max_nan(most, __shfl_xor_sync(0xffffffffu, most, 2));
+  const bool nan = most != most;
+  if (__any_sync(0xffffffffu, most == INFINITY)) {   // the largest finite one, then
+    float finite = finite_of8(x);
+    finite = fmaxf(finite, __shfl_xor_sync(0xffffffffu, finite, 1));
+    finite = fmaxf(finite, __shfl_xor_sync(0xffffffffu, finite, 2));
+    most = finite;
+  }
+  const int e = nan ? 0 : block_exponent(most);
+  *exponent = nan ? 255 : static_cast<uint8_t>(e + 127);
+  return e2m1_of8(x, __uint_as_float(static_cast<uint32_t>(127 - e) << 23));   // 2^-e, e in [-127, 126]
+}
+
 // head_dim / 16 threads per row: each takes eight elements of either half of the row, so that a
-// rotated pair of the half layout meets in one thread, and the row's maximum in as many shuffles.
-template <typename T, bool E4M3, bool VEC>
+// rotated pair of the half layout meets in one thread, and the row's maximum in as many shuffles (a
+// 4-bit block's, in two).
+template <typename T, int FORMAT, bool VEC>
 __global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__ WriteLaunch a) {
   extern __shared__ __align__(16) float s_rot[];
   const int pairs = a.tab.dim >> 1;
@@ -323,6 +377,10 @@ __global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__
       if (mine && t < tokens) slot = __ldg(a.slots + first + t);
       const bool live = slot >= 0 && slot < a.n_slots;
       float x0[8], x1[8];
+      if (FORMAT == KVPRM_CACHE_E2M1 && !live) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x0[k] = x1[k] = 0.f;
+      }
       if (live) {
         const T* row = base + (first + t) * token_step;
         load_n<T, 8, VEC>(row + 8 * j, x0);
@@ -346,7 +404,19 @@ __global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__
         }
       }
       const int64_t out_row = ((slot >> 4) * rows + r) * 16 + (slot & 15);   // (rows of a page: keys' heads, then values')
-      if constexpr (E4M3) {
+      if constexpr (FORMAT == KVPRM_CACHE_E2M1) {
+        uint8_t e0, e1;
+        const uint32_t w0 = block_of32(x0, &e0), w1 = block_of32(x1, &e1);
+        if (!live) continue;
+        uint8_t* out = a.pages + out_row * half;
+        *reinterpret_cast<uint32_t*>(out + 4 * j) = w0;
+        *reinterpret_cast<uint32_t*>(out + (half >> 1) + 4 * j) = w1;
+        if ((j & 3) == 0) {
+          uint8_t* e = a.exponents + out_row * (a.head_dim >> 5) + (j >> 2);
+          e[0] = e0;
+          e[half >> 5] = e1;
+        }
+      } else if constexpr (FORMAT == KVPRM_CACHE_E4M3) {
         // the largest magnitude, NaN if there is one
         float most = 0.f;
         if (live) {
@@ -423,6 +493,40 @@ __global__ void __launch_bounds__(kThreads) expand_kernel(const uint2* __restric
   }
 }
 
+// 4-bit pages likewise: eight codes are four bytes, and a block's exponent is that of four such words.
+constexpr int kExpand4Per = 4;
+__global__ void __launch_bounds__(kThreads) expand4_kernel(const uint32_t* __restrict__ pages,
+                                                           const uint8_t* __restrict__ exponents,
+                                                           const int32_t* __restrict__ src,
+                                                           const int32_t* __restrict__ dst, int64_t n_pages,
+                                                           int64_t out_pages, int pieces, uint4* __restrict__ out) {
+  const int64_t s = __ldg(src + blockIdx.x), d = __ldg(dst + blockIdx.x);
+  if (s < 0 || s >= n_pages || d < 0 || d >= out_pages) return;
+  const int p0 = blockIdx.y * (kThreads * kExpand4Per) + threadIdx.x;
+  uint32_t c[kExpand4Per];
+  float f[kExpand4Per];
+#pragma unroll
+  for (int i = 0; i < kExpand4Per; ++i) {
+    const int p = p0 + i * kThreads;
+    if (p >= pieces) continue;
+    c[i] = __ldg(pages + s * pieces + p);
+    f[i] = row_factor(__ldg(exponents + s * (pieces >> 2) + (p >> 2)));
+  }
+#pragma unroll
+  for (int i = 0; i < kExpand4Per; ++i) {
+    const int p = p0 + i * kThreads;
+    if (p >= pieces) continue;
+    uint32_t h[4], r[4];
+    f16_of_e2m1(c[i], h);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h[k]));
+      r[k] = pack_bf16(v.x * f[i], v.y * f[i]);
+    }
+    out[d * pieces + p] = make_uint4(r[0], r[1], r[2], r[3]);
+  }
+}
+
 // ---------------------------------------------------------------- host
 int size_of(int32_t dtype) { return dtype == KVPRM_F32 ? 4 : dtype == KVPRM_BF16 || dtype == KVPRM_F16 ? 2 : 0; }
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -462,10 +566,11 @@ int launch_rope(const RopeLaunch& a, bool vec, unsigned grid, void* stream) {
 }
 
 template <typename T>
-int launch_write(const WriteLaunch& a, bool e4m3, bool vec, unsigned grid, void* stream) {
+int launch_write(const WriteLaunch& a, int format, bool vec, unsigned grid, void* stream) {
   const size_t smem = static_cast<size_t>(a.tokens) * a.tab.dim * sizeof(float);
-  auto k = e4m3 ? (vec ? write_kernel<T, true, true> : write_kernel<T, true, false>)
-                : (vec ? write_kernel<T, false, true> : write_kernel<T, false, false>);
+  auto k = format == KVPRM_CACHE_E2M1   ? (vec ? write_kernel<T, KVPRM_CACHE_E2M1, true> : write_kernel<T, KVPRM_CACHE_E2M1, false>)
+           : format == KVPRM_CACHE_E4M3 ? (vec ? write_kernel<T, KVPRM_CACHE_E4M3, true> : write_kernel<T, KVPRM_CACHE_E4M3, false>)
+                                        : (vec ? write_kernel<T, KVPRM_CACHE_BF16, true> : write_kernel<T, KVPRM_CACHE_BF16, false>);
   return launch(k, dim3(grid), smem, a, stream, "cache write launch");
 }
 
@@ -473,7 +578,7 @@ int launch_write(const WriteLaunch& a, bool e4m3, bool vec, unsigned grid, void*
 
 int check_cache(const kvprm_cache* c, const char* who) {
   if (!c) return operator_fail(KVPRM_EINVAL, "%s: no cache", who);
-  if (c->format != KVPRM_CACHE_BF16 && c->format != KVPRM_CACHE_E4M3)
+  if (c->format != KVPRM_CACHE_BF16 && c->format != KVPRM_CACHE_E4M3 && c->format != KVPRM_CACHE_E2M1)
     return operator_fail(KVPRM_EINVAL, "%s: cache format %d", who, c->format);
   if (c->head_dim != 64 && c->head_dim != 128)
     return operator_fail(KVPRM_EINVAL, "%s: head_dim %d is not 64 or 128", who, c->head_dim);
@@ -482,7 +587,7 @@ int check_cache(const kvprm_cache* c, const char* who) {
                          static_cast<long long>(c->n_pages));
   if ((c->n_pages > 0 && !c->pages) || !aligned16(c->pages))
     return operator_fail(KVPRM_EINVAL, "%s: pages are NULL or not 16-byte aligned", who);
-  if (c->format == KVPRM_CACHE_E4M3 && ((c->n_pages > 0 && !c->exponents) || !aligned16(c->exponents)))
+  if (c->format != KVPRM_CACHE_BF16 && ((c->n_pages > 0 && !c->exponents) || !aligned16(c->exponents)))
     return operator_fail(KVPRM_EINVAL, "%s: exponents are NULL or not 16-byte aligned", who);
   return KVPRM_OK;
 }
@@ -647,29 +752,33 @@ int kvprm_cache_write(const kvprm_cache* cache, int32_t dtype, const void* k, in
   const int64_t grid = (n_tokens + a.tokens - 1) / a.tokens;
   if (grid > 0x7FFFFFFF) return operator_fail(KVPRM_EINVAL, "%s: n_tokens %lld", who, static_cast<long long>(n_tokens));
   const unsigned g = static_cast<unsigned>(grid);
-  const bool e4m3 = cache->format == KVPRM_CACHE_E4M3;
-  if (dtype == KVPRM_F32) return launch_write<float>(a, e4m3, vec, g, stream);
-  if (dtype == KVPRM_BF16) return launch_write<__nv_bfloat16>(a, e4m3, vec, g, stream);
-  return launch_write<__half>(a, e4m3, vec, g, stream);
+  if (dtype == KVPRM_F32) return launch_write<float>(a, cache->format, vec, g, stream);
+  if (dtype == KVPRM_BF16) return launch_write<__nv_bfloat16>(a, cache->format, vec, g, stream);
+  return launch_write<__half>(a, cache->format, vec, g, stream);
 }
 
 int kvprm_cache_expand(const kvprm_cache* cache, const int32_t* src, const int32_t* dst, int64_t n, void* out,
                        int64_t out_pages, void* stream) {
   const char* who = "kvprm_cache_expand";
   if (const int rc = check_cache(cache, who)) return rc;
-  if (cache->format != KVPRM_CACHE_E4M3) return operator_fail(KVPRM_EINVAL, "%s: the cache is not quantised", who);
+  if (cache->format == KVPRM_CACHE_BF16) return operator_fail(KVPRM_EINVAL, "%s: the cache is not quantised", who);
   if (n < 0 || n > 0x7FFFFFFF || out_pages < 0) return operator_fail(KVPRM_EINVAL, "%s: n %lld, out_pages %lld", who, static_cast<long long>(n), static_cast<long long>(out_pages));
   if (n == 0 || cache->n_pages == 0 || out_pages == 0) return KVPRM_OK;
   if (!src || !dst || !out || !aligned16(out)) return operator_fail(KVPRM_EINVAL, "%s: src, dst or out are NULL, or out is not 16-byte aligned", who);
   const int rows = 2 * cache->n_kv_heads * 16, shift = cache->head_dim == 128 ? 4 : 3;
-  const int pieces = rows << shift;
+  const int pieces = rows << shift;   // of eight codes
+  const int per = kThreads * (cache->format == KVPRM_CACHE_E2M1 ? kExpand4Per : kExpandPer);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(n), static_cast<unsigned>((pieces + kThreads * kExpandPer - 1) / (kThreads * kExpandPer)), 1);
+  cfg.gridDim = dim3(static_cast<unsigned>(n), static_cast<unsigned>((pieces + per - 1) / per), 1);
   cfg.blockDim = dim3(kThreads, 1, 1);
   cfg.stream = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, expand_kernel, static_cast<const uint2*>(cache->pages),
-                                           static_cast<const uint8_t*>(cache->exponents), src, dst, cache->n_pages,
-                                           out_pages, rows, shift, static_cast<uint4*>(out));
+  const uint8_t* exponents = static_cast<const uint8_t*>(cache->exponents);
+  const cudaError_t e =
+      cache->format == KVPRM_CACHE_E2M1
+          ? cudaLaunchKernelEx(&cfg, expand4_kernel, static_cast<const uint32_t*>(cache->pages), exponents, src, dst, cache->n_pages,
+                               out_pages, pieces, static_cast<uint4*>(out))
+          : cudaLaunchKernelEx(&cfg, expand_kernel, static_cast<const uint2*>(cache->pages), exponents, src, dst, cache->n_pages,
+                               out_pages, rows, shift, static_cast<uint4*>(out));
   if (e != cudaSuccess) return operator_fail(KVPRM_ECUDA, "%s: %s", who, cudaGetErrorString(e));
   return KVPRM_OK;
 }

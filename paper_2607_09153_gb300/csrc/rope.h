@@ -21,6 +21,17 @@ struct RopeTable {
 __device__ __forceinline__ float row_factor(uint32_t e) {
   return __uint_as_float((e << 23) | (((e + 1u) & 0xFEu) == 0u ? 0x400000u : 0u));
 }
+// Eight e2m1 codes of a word as fp16 pairs, in their order (exact, an instruction a pair).
+__device__ __forceinline__ void f16_of_e2m1(uint32_t w, uint32_t (&h)[4]) {
+  asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+      "mov.b32 {a, b, c, d}, %4;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+      "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}"
+      : "=r"(h[0]), "=r"(h[1]), "=r"(h[2]), "=r"(h[3])
+      : "r"(w));
+}
 #endif
 
 // Argument checks that the cache's entry points share.

@@ -246,6 +246,9 @@ using TreeRows = TreeGeometry<16 * TILES, kTreePage, 1, TILES == 1 ? 16 : 20>;
 using TreeTc = TreeGeometry<128, 128, 2, 4>;
 #endif
 cudaError_t launch_tree_rows(const TreeLaunch& a, const kvprm_cache& c, int tiles, int ctas, cudaStream_t stream);
+// tree_e2m1.cu: 4-bit pages, tiles of 8, 16 or 32 query rows (tiles of 8: 1, 2 or 4).
+constexpr int tree_e2m1_per_sm(int tiles) { return tiles == 1 ? 4 : tiles == 2 ? 3 : 2; }
+cudaError_t launch_tree_e2m1(const TreeLaunch& a, const kvprm_cache& c, int tiles, int ctas, cudaStream_t stream);
 // tree_tc.cu: in pairs of tiles of 128, on the tensor cores; one CTA on an SM.  The cache has a page at least.
 cudaError_t launch_tree_tc(const TreeLaunch& a, const kvprm_cache& c, int ctas, cudaStream_t stream);
 // tree_join.cu: joins the partial results that either left; rows: of a partial result (16, 32 or 256).

@@ -18,6 +18,7 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct TreePlan {
   bool tc = false, whole = false;
+  int tiles8 = 0;                      // 4-bit pages on registers: tiles of 8 rows
   int ctas = 0, rows = 16, seqs = 0;   // rows: of a partial result; seqs: sequences of a launch
 };
 
@@ -53,7 +54,9 @@ int sm_count(int* sms) {
 int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   TreePlan p;
   const int64_t rows = int64_t{t.max_drafts} * (t.n_q_heads / c.n_kv_heads);
-  p.tc = rows > 32 && c.n_pages > 0;
+  const bool e2m1 = c.format == KVPRM_CACHE_E2M1;
+  p.tc = !e2m1 && rows > 32 && c.n_pages > 0;
+  p.tiles8 = !e2m1 || p.tc ? 0 : rows > 16 ? 4 : rows > 8 ? 2 : 1;
   p.rows = p.tc ? 256 : rows > 16 ? 32 : 16;
   const int64_t block = p.tc ? 128 : kTreePage, tiles = ceil_div(rows, p.tc ? 128 : p.rows), lead = 20;
   // the line of a sequence of any length is shorter than this; a launch's stays within 31 bits
@@ -64,7 +67,7 @@ int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   const int64_t len = std::min<int64_t>(t.max_len, int64_t{kTreePage} * t.max_blocks);
   const int64_t pairs = int64_t{p.seqs} * c.n_kv_heads * ceil_div(rows, p.rows);
   const int64_t blocks = ceil_div(len, block) + ceil_div(t.max_drafts, block);
-  const int64_t most = int64_t{sms} * (p.tc ? 1 : tree_rows_per_sm(p.rows / 16));
+  const int64_t most = int64_t{sms} * (p.tc ? 1 : e2m1 ? tree_e2m1_per_sm(p.tiles8) : tree_rows_per_sm(p.rows / 16));
   p.whole = blocks <= (pairs <= most ? (p.tc ? 4 : 32) : (p.tc ? 3 : 16));
   p.ctas = static_cast<int>(std::max<int64_t>(1, std::min(most, p.whole ? pairs : pairs * blocks / (p.tc ? 2 : 8))));
   *out = p;
@@ -119,7 +122,9 @@ int attend(const kvprm_cache* cache, const kvprm_tree* t, void* workspace, int64
   a.seq0 = 0;
   do {   // (once without sequences, which is to fill only)
     a.n_seqs = std::min(p.seqs, t->n_seqs - a.seq0);
-    cudaError_t e = p.tc ? launch_tree_tc(a, *cache, p.ctas, st) : launch_tree_rows(a, *cache, p.rows / 16, p.ctas, st);
+    cudaError_t e = p.tc       ? launch_tree_tc(a, *cache, p.ctas, st)
+                    : p.tiles8 ? launch_tree_e2m1(a, *cache, p.tiles8, p.ctas, st)
+                               : launch_tree_rows(a, *cache, p.rows / 16, p.ctas, st);
     if (e == cudaSuccess && !p.whole && seqs) e = launch_tree_join(a, *cache, p.rows, st);
     if (e != cudaSuccess) return operator_fail(KVPRM_ECUDA, "%s: %s", who, cudaGetErrorString(e));
     a.seq0 += p.seqs;

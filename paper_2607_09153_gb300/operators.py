@@ -1,5 +1,5 @@
 """torch face of the operators around the cache (include/kvprm.h): rotary positions, the paged cache written in bf16
-or quantised to 8 bits, quantised pages expanded for the scorer, and the attention of drafted tokens over the pages.
+or quantised to 8 or 4 bits, quantised pages expanded for the scorer, and the attention of drafted tokens over the pages.
 
 Like kvprm.py this module only marshals arguments: shapes, types and devices are checked here, everything else by the
 library, and every step runs in its CUDA kernels.  Calls are enqueued on `stream` (default: torch's current one), and the
@@ -20,7 +20,7 @@ from .kvprm import KVPRM_ECAPACITY, KVPRM_OK, KvprmError
 from .kvprm import lib as _base_lib
 
 KVPRM_F32, KVPRM_BF16, KVPRM_F16 = range(3)
-KVPRM_CACHE_BF16, KVPRM_CACHE_E4M3 = range(2)
+KVPRM_CACHE_BF16, KVPRM_CACHE_E4M3, KVPRM_CACHE_E2M1 = range(3)
 ROPE_SCALINGS = ("none", "linear", "base", "ramp", "smooth")
 PAGE = 16
 
@@ -40,6 +40,22 @@ class KvprmHeads(ctypes.Structure):
 class KvprmCache(ctypes.Structure):
     _fields_ = [("pages", ctypes.c_void_p), ("exponents", ctypes.c_void_p), ("n_pages", ctypes.c_int64),
                 ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32)]
+
+
+class KvprmPool(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("layer_stride", ctypes.c_int64), ("page_stride", ctypes.c_int64),
+                ("page_bytes", ctypes.c_int64), ("layers", ctypes.c_int32)]
+
+
+class KvprmFork(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("refs", "block_table", "lens", "parents", "room", "refs_out", "table_out",
+                                                "lens_out", "counts")] + [("n_pages", ctypes.c_int64)] +
+                [(k, ctypes.c_int32) for k in ("n_pools", "n_seqs", "max_blocks", "n_new", "width")])
+
+
+class KvprmCompact(ctypes.Structure):
+    _fields_ = ([(k, ctypes.c_void_p) for k in ("refs", "block_table", "lens", "refs_out", "table_out", "moved", "counts")] +
+                [("n_pages", ctypes.c_int64)] + [(k, ctypes.c_int32) for k in ("n_pools", "n_seqs", "max_blocks")])
 
 
 class KvprmTree(ctypes.Structure):
@@ -70,6 +86,8 @@ def lib() -> ctypes.CDLL:
         L.kvprm_cache_expand.argtypes = [vp, vp, vp, i64, vp, i64, vp]
         L.kvprm_tree_workspace.argtypes = [vp, vp, vp]
         L.kvprm_tree_attention.argtypes = L.kvprm_tree_attention_filled.argtypes = [vp, vp, vp, i64, vp]
+        L.kvprm_fork_workspace.argtypes = L.kvprm_compact_workspace.argtypes = [vp, vp, vp]
+        L.kvprm_cache_fork.argtypes = L.kvprm_cache_compact.argtypes = [vp, vp, vp, i64, vp]
         _lib = L
     return _lib
 
@@ -145,6 +163,11 @@ _HEADS = struct.Struct("@PPiqqqq")
 _CACHE = struct.Struct("@PPqiii0q")
 _TREE = struct.Struct("@PPPPqqqqqqqqPPPPiiiiiiif0q")
 assert _HEADS.size == ctypes.sizeof(KvprmHeads) and _CACHE.size == ctypes.sizeof(KvprmCache)
+_POOL = struct.Struct("@Pqqqi0q")
+_FORK = struct.Struct("@PPPPPPPPPqiiiii0q")
+_COMPACT = struct.Struct("@PPPPPPPqiii0q")
+assert _POOL.size == ctypes.sizeof(KvprmPool) and _FORK.size == ctypes.sizeof(KvprmFork)
+assert _COMPACT.size == ctypes.sizeof(KvprmCompact)
 assert _TREE.size == ctypes.sizeof(KvprmTree)
 
 
@@ -273,7 +296,7 @@ class Rope:
 
 def _cache(T, pages, exponents) -> tuple:
     """(C struct, kv heads, head_dim, device index) of one layer's pages [n_pages][2][n_kv_heads][16][head_dim]:
-    bfloat16, or float8_e4m3fn with exponents [n_pages][2][n_kv_heads][16] (uint8 or float8_e8m0fnu)."""
+    bfloat16, or float8_e4m3fn with exponents [n_pages][2][n_kv_heads][16] (uint8 or float8_e8m0fnu), or 4-bit codes."""
     shape, device = pages.shape, pages.get_device()
     if len(shape) != 5 or shape[1] != 2 or shape[3] != PAGE or device < 0 or not pages.is_contiguous():
         raise ValueError(f"pages are a contiguous CUDA tensor [n_pages][2][n_kv_heads][16][head_dim], got "
@@ -283,13 +306,26 @@ def _cache(T, pages, exponents) -> tuple:
             raise ValueError("bfloat16 pages have no exponents")
         return _CACHE.pack(pages.data_ptr(), 0, shape[0], shape[2], shape[4], KVPRM_CACHE_BF16), shape[2], shape[4], device
     if pages.dtype is not T.e4m3:
-        raise TypeError(f"pages are bfloat16 or float8_e4m3fn, got {pages.dtype}")
+        return _cache4(T, pages, exponents, shape, device)
     if exponents is None or exponents.dtype not in T.bytes or exponents.shape != shape[:4] or \
             exponents.get_device() != device or not exponents.is_contiguous():
         raise ValueError("float8_e4m3fn pages need contiguous uint8 or float8_e8m0fnu exponents "
                          "[n_pages][2][n_kv_heads][16]")
     return (_CACHE.pack(pages.data_ptr(), exponents.data_ptr(), shape[0], shape[2], shape[4], KVPRM_CACHE_E4M3),
             shape[2], shape[4], device)
+
+
+def _cache4(T, pages, exponents, shape, device) -> tuple:
+    """_cache of 4-bit pages [n_pages][2][n_kv_heads][16][head_dim / 2]: uint8 or float4_e2m1fn_x2, with exponents
+    [n_pages][2][n_kv_heads][16][head_dim / 32]."""
+    if pages.dtype is not T.bytes[0] and pages.dtype is not getattr(T.torch, "float4_e2m1fn_x2", T.bytes[0]):
+        raise TypeError(f"pages are bfloat16, float8_e4m3fn, or uint8 (float4_e2m1fn_x2) of two codes each, got {pages.dtype}")
+    if exponents is None or exponents.dtype not in T.bytes or exponents.shape != shape[:4] + (shape[4] // 16,) or \
+            exponents.get_device() != device or not exponents.is_contiguous():
+        raise ValueError("4-bit pages [n_pages][2][n_kv_heads][16][head_dim / 2] need contiguous uint8 or float8_e8m0fnu "
+                         "exponents [n_pages][2][n_kv_heads][16][head_dim / 32]")
+    return (_CACHE.pack(pages.data_ptr(), exponents.data_ptr(), shape[0], shape[2], 2 * shape[4], KVPRM_CACHE_E2M1),
+            shape[2], 2 * shape[4], device)
 
 
 def cache_write(pages, slots, k, v, exponents=None, rope: Rope | None = None, positions=None, stream=None) -> None:
@@ -318,11 +354,11 @@ def cache_expand(pages, exponents, src, out, dst=None, stream=None):
     """Quantised pages src[i] (int32) as bf16 pages dst[i] (int32, none twice; default: i) of `out`, a layer that the
     scoring calls read; returns `out`."""
     T = _t or _torch()
-    c, _, _, dev = _cache(T, pages, exponents)
+    c, _, hd, dev = _cache(T, pages, exponents)
     shape = out.shape
-    if out.dtype is not T.bf16 or len(shape) != 5 or shape[1:] != pages.shape[1:] or out.get_device() != dev or \
-            not out.is_contiguous():
-        raise ValueError(f"out is a contiguous bfloat16 tensor [pages]{list(pages.shape[1:])} on {pages.device}")
+    if out.dtype is not T.bf16 or len(shape) != 5 or shape[1:4] != pages.shape[1:4] or shape[4] != hd or \
+            out.get_device() != dev or not out.is_contiguous():
+        raise ValueError(f"out is a contiguous bfloat16 tensor [pages]{list(pages.shape[1:4]) + [hd]} on {pages.device}")
     n = src.shape[0]
     if dst is None:
         with T.torch.cuda.stream(stream):
@@ -373,14 +409,15 @@ def _scratch(T, need: int, device: int, stream):
         return T.torch.empty(need, dtype=T.torch.uint8, device=T.torch.device("cuda", device))
 
 
-def _workspace_bytes(c: bytes, t: bytes) -> int:
+def _workspace_bytes(c: bytes, t: bytes, ask=None) -> int:
     need = ctypes.c_int64()
-    _check(lib().kvprm_tree_workspace(c, t, ctypes.byref(need)))
+    _check((ask or lib().kvprm_tree_workspace)(c, t, ctypes.byref(need)))
     return need.value
 
 
-def _attend(T, go, c: bytes, t: bytes, device: int, stream) -> int:
-    """`go`, an attention entry point, with scratch of the stream's, the tensors' device being current; the status."""
+def _attend(T, go, c: bytes, t: bytes, device: int, stream, ask=None) -> int:
+    """`go`, an entry point (attention's, or one whose workspace `ask` tells), with scratch of the stream's, the tensors'
+    device being current; the status."""
     if stream is None:
         handle, capturing = T.raw_stream(device), T.capturing()
     else:
@@ -388,14 +425,14 @@ def _attend(T, go, c: bytes, t: bytes, device: int, stream) -> int:
         with T.torch.cuda.stream(stream):
             capturing = T.capturing()
     if capturing:   # scratch of the graph's own, for the graph may be replayed on any stream
-        w = _scratch(T, _workspace_bytes(c, t), device, stream)
+        w = _scratch(T, _workspace_bytes(c, t, ask), device, stream)
         return go(c, t, w.data_ptr(), w.numel(), handle)
     key = (device, handle)
     mine = _streams.get(key) or _streams.setdefault(key, _Stream())
     with mine.lock:
         rc = go(c, t, mine.address, mine.bytes, handle) if mine.bytes else KVPRM_ECAPACITY
         if rc == KVPRM_ECAPACITY:
-            w = mine.scratch = _scratch(T, _workspace_bytes(c, t), device, stream)
+            w = mine.scratch = _scratch(T, _workspace_bytes(c, t, ask), device, stream)
             mine.address, mine.bytes = w.data_ptr(), w.numel()
             rc = go(c, t, mine.address, mine.bytes, handle)
     return rc
@@ -454,16 +491,105 @@ def tree_attention(q, k, v, pages, block_table, lens, start, max_drafts: int, ma
                    _ints("lens", lens, i32, (n,), dev), _ints("start", start, i32, (n + 1,), dev), bits, width, n,
                    tokens, nq, max_drafts, PAGE * width if max_len is None else max_len, words,
                    1.0 / math.sqrt(hd) if scale is None else scale)
+    _run(T, go, c, t, dev, stream, workspace)
+    return out
+
+
+def _run(T, go, c: bytes, t: bytes, dev: int, stream, workspace, ask=None) -> None:
+    """An entry point with the caller's workspace or scratch of the stream's."""
     if workspace is not None:
         if workspace.get_device() != dev or not workspace.is_contiguous():
             raise ValueError(f"workspace is a contiguous tensor on CUDA device {dev}, got one on {workspace.device}")
         rc = _call(T, dev, stream, go, c, t, workspace.data_ptr(),
                    workspace.numel() * workspace.element_size())
     elif T.device() == dev:
-        rc = _attend(T, go, c, t, dev, stream)
+        rc = _attend(T, go, c, t, dev, stream, ask)
     else:
         with T.torch.cuda.device(dev):
-            rc = _attend(T, go, c, t, dev, stream)
+            rc = _attend(T, go, c, t, dev, stream, ask)
     if rc != KVPRM_OK:
         _check(rc)
+
+
+def _pools(pools, n_pages: int, device: int) -> bytes:
+    """C structs of pools [layers][n_pages]...: the elements of a page are side by side."""
+    packed = b""
+    for x in pools:
+        shape, size = x.shape, x.element_size()
+        if len(shape) < 3 or shape[1] != n_pages or x.get_device() != device:
+            raise ValueError(f"a pool is a tensor [layers][{n_pages}]... on CUDA device {device}, got {tuple(shape)} on {x.device}")
+        stride, elements = x.stride(), 1
+        for n, st in zip(reversed(shape[2:]), reversed(stride[2:])):
+            if n > 1 and st != elements and x.numel() > 0:
+                raise ValueError(f"the elements of a pool's page are not side by side: shape {tuple(shape)}, strides {stride}")
+            elements *= n
+        # (the stride of a dimension of one is nobody's)
+        packed += _POOL.pack(x.data_ptr(), size * stride[0] if shape[0] > 1 else 0, size * stride[1] if shape[1] > 1 else 0,
+                             size * elements, shape[0])
+    return packed
+
+
+def _page_table(T, refs, block_table, lens) -> tuple:
+    """(device index, n_pages, n_seqs, max_blocks, addresses of refs, table, lens)."""
+    dev = refs.get_device()
+    if len(refs.shape) != 1 or len(block_table.shape) != 2 or dev < 0:
+        raise ValueError(f"refs is a CUDA tensor [n_pages], block_table [n_seqs][max_blocks]; got {tuple(refs.shape)} on "
+                         f"{refs.device}, {tuple(block_table.shape)}")
+    n, width = block_table.shape
+    return (dev, refs.shape[0], n, width, _ints("refs", refs, T.i32, (refs.shape[0],), dev),
+            _ints("block_table", block_table, T.i32, (n, width), dev), _ints("lens", lens, T.i32, (n,), dev))
+
+
+def _outputs(T, out, names, shapes, device, index: int, stream) -> tuple:
+    """`out`, looked over, or new int32 tensors; and their addresses."""
+    if out is None:
+        make = (lambda shape: T.empty(shape, dtype=T.i32, device=device)) if stream is None else \
+            (lambda shape: _result(T, shape, T.i32, device, stream))
+        out = tuple(make(shape) for shape in shapes)
+        return out, [o.data_ptr() for o in out]
+    if len(out) != len(shapes):
+        raise ValueError(f"out is {', '.join(names)}; got {len(out)} tensors")
+    return tuple(out), [_ints(name, o, T.i32, shape, index) for name, o, shape in zip(names, out, shapes)]
+
+
+def cache_fork(pools, refs, block_table, lens, parents, room=None, width: int | None = None, out=None, workspace=None,
+               stream=None):
+    """The sequences of a search's next step: the i-th continues sequence parents[i] (int32; -1: it begins empty) and has pages
+    for room[i] (int32) tokens more.  Full pages are shared, a page that ends inside is kept by the first that continues it
+    and copied in every pool for the others, pages that nobody holds any more are free.
+
+    pools: tensors [layers][n_pages]... that block_table's numbers index -- pages and exponents, of any type; a single layer's
+    as x[None].  refs (int32 [n_pages]): how many hold a page; 0: it is free.  Returns (block_table [n_new][width], -1 behind a
+    row's pages; lens; refs; counts: pages that are free now, and pages that were wanted and not to be had, which are -1 in
+    the table).  width: default that of `out`, else of block_table, which has to have places for the pages to come.  out: a
+    tuple of four tensors to write instead of new ones; none may share memory with the inputs."""
+    T = _t or _torch()
+    dev, n_pages, n, blocks, *at = _page_table(T, refs, block_table, lens)
+    m = parents.shape[0]
+    if width is None:
+        width = blocks if out is None else out[0].shape[-1]
+    at.append(_ints("parents", parents, T.i32, (m,), dev))
+    at.append(0 if room is None else _ints("room", room, T.i32, (m,), dev))
+    packed = _pools(pools, n_pages, dev)
+    out, to = _outputs(T, out, ("block_table", "lens", "refs", "counts"), ((m, width), (m,), (n_pages,), (2,)), refs.device, dev,
+                       stream)
+    f = _FORK.pack(*at, to[2], to[0], to[1], to[3], n_pages, len(packed) // _POOL.size, n, blocks, m, width)
+    L = lib()
+    _run(T, L.kvprm_cache_fork, packed, f, dev, stream, workspace, L.kvprm_fork_workspace)
+    return out
+
+
+def cache_compact(pools, refs, block_table, lens, out=None, workspace=None, stream=None):
+    """Moves the pages in use (refs > 0) behind the first as many into the free ones before them, in every pool (cache_fork).
+    Returns (block_table, refs, moved, counts): the table and references by the new numbers, where each page is now (-1: it
+    was free), and how many pages are in use and moved.  out: a tuple of four tensors to write instead of new ones; none may
+    share memory with the inputs."""
+    T = _t or _torch()
+    dev, n_pages, n, blocks, *at = _page_table(T, refs, block_table, lens)
+    packed = _pools(pools, n_pages, dev)
+    out, to = _outputs(T, out, ("block_table", "refs", "moved", "counts"), ((n, blocks), (n_pages,), (n_pages,), (2,)),
+                       refs.device, dev, stream)
+    f = _COMPACT.pack(*at, to[1], to[0], to[2], to[3], n_pages, len(packed) // _POOL.size, n, blocks)
+    L = lib()
+    _run(T, L.kvprm_cache_compact, packed, f, dev, stream, workspace, L.kvprm_compact_workspace)
     return out
