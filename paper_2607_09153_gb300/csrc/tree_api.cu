@@ -55,7 +55,7 @@ int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   TreePlan p;
   const int64_t rows = int64_t{t.max_drafts} * (t.n_q_heads / c.n_kv_heads);
   const bool e2m1 = c.format == KVPRM_CACHE_E2M1;
-  p.tc = !e2m1 && rows > 32 && c.n_pages > 0;
+  p.tc = rows > 32 && c.n_pages > 0;
   p.tiles8 = !e2m1 || p.tc ? 0 : rows > 16 ? 4 : rows > 8 ? 2 : 1;
   p.rows = p.tc ? 256 : rows > 16 ? 32 : 16;
   const int64_t block = p.tc ? 128 : kTreePage, tiles = ceil_div(rows, p.tc ? 128 : p.rows), lead = 20;
@@ -114,7 +114,7 @@ int attend(const kvprm_cache* cache, const kvprm_tree* t, void* workspace, int64
   // a chunk with one row tile costs the tensor-core kernel, by what it waits for, 0.75 of one with two (a bf16 cache: memory)
   // or as much (an 8-bit one: its conversion)
   a.weight_full = p.tc ? 4 : 1;
-  a.weight_part = !p.tc ? 1 : cache->format == KVPRM_CACHE_E4M3 ? 4 : 3;
+  a.weight_part = !p.tc ? 1 : cache->format != KVPRM_CACHE_BF16 ? 4 : 3;
   a.line = static_cast<int32_t*>(workspace);
   a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kLineBytes);
   a.part_ml = reinterpret_cast<float2*>(a.part_o + int64_t{2} * p.ctas * p.rows * cache->head_dim);

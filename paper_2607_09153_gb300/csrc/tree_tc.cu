@@ -9,8 +9,8 @@
 // streams that meet at the end.  Either way one group's softmax runs beside the other's matrix products, and
 // the groups never wait for each other within a part.
 //   warps 0-3, 4-7   softmax groups (thread = row = lane of tensor memory)
-//   warps 8-15       producers: Q tiles, drafted tokens' keys and values, and with an 8-bit cache every chunk,
-//                    converted to bf16 (exact: a power of two per row changes no mantissa)
+//   warps 8-15       producers: Q tiles, drafted tokens' keys and values, and with an 8- or 4-bit cache every chunk,
+//                    converted to bf16 (exact: a power of two changes no mantissa)
 //   warp 16          TMA: bf16 pages straight into the tiles
 //   warp 17          issues every MMA, in an order that keeps one unit's S ahead of the other's O
 //
@@ -43,10 +43,10 @@ constexpr float kMargin = 8.f;   // log2 units that scores may pass a running ma
 constexpr uint32_t kTmemCols = 512, kColS = 0, kColO = 256;   // S buffers at 0 and 128, accumulators at 256 and 384
 constexpr int kFlagSets = 8;     // parts whose marks may be in flight (a ring of eight slots reaches five parts ahead)
 
-template <int HD, bool E4M3>
+template <int HD, bool CODES>
 struct Smem {
   static constexpr uint32_t kTile = kChunk * HD * 2;             // one chunk's keys or values, or one tile of Q
-  static constexpr int kSlots = HD == 128 ? (E4M3 ? 3 : 4) : 8;
+  static constexpr int kSlots = HD == 128 ? (CODES ? 3 : 4) : 8;
   static constexpr uint32_t kQ = 0;                              // two tiles
   static constexpr uint32_t kSlot0 = kQ + 2 * kTile;
   static constexpr uint32_t kMl = kSlot0 + kSlots * kTile;   // float2 [2][128]
@@ -201,6 +201,17 @@ __device__ __forceinline__ void bf16_of16(const uint4& c, uint32_t f1, uint32_t 
   pair(c.z, &hi->x, &hi->y);
   pair(c.w, &hi->z, &hi->w);
 }
+// Thirty-two e2m1 codes, a block, likewise: a code's exponent and mantissa at bf16's place are 2^-126 of its value, f1 (times f2)
+// 2^126 times the block's power.  A word's nibbles j and j + 4 become a pair, so that the order is 0 4 1 5 2 6 3 7.  NaN is the
+// factor's alone.
+template <bool PLAIN>
+__device__ __forceinline__ uint4 bf16_of8(uint32_t w, uint32_t f1, uint32_t f2) {
+  auto pair = [&](uint32_t magnitude, uint32_t sign) {
+    const uint32_t v = mul_bf16x2((magnitude & 0x01C001C0u) | (sign & 0x80008000u), f1);
+    return PLAIN ? v : mul_bf16x2(v, f2);
+  };
+  return make_uint4(pair(w << 6, w << 12), pair(w << 2, w << 8), pair(w >> 2, w << 4), pair(w >> 6, w));
+}
 // Bit 7 of a byte is set in the result where w's byte is a NaN code, and there is no such bit where none is: a carry into it,
 // or out of the byte below, comes of seven ones alone.
 __device__ __forceinline__ uint32_t nan_carries(uint32_t w) { return (w + 0x01010101u) ^ w; }
@@ -208,21 +219,37 @@ __device__ __forceinline__ uint4 paired(const uint4& v) {
   return make_uint4(__byte_perm(v.x, v.y, 0x5410), __byte_perm(v.x, v.y, 0x7632), __byte_perm(v.z, v.w, 0x5410),
                     __byte_perm(v.z, v.w, 0x7632));
 }
-template <int N>
+__device__ __forceinline__ uint4 paired4(const uint4& v) {   // as bf16_of8
+  return make_uint4(__byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632), __byte_perm(v.y, v.w, 0x5410),
+                    __byte_perm(v.y, v.w, 0x7632));
+}
+template <int FORMAT, int N>
 __device__ __forceinline__ void in_order(float (&o)[N]) {
+  if constexpr (FORMAT == KVPRM_CACHE_E4M3) {
 #pragma unroll
-  for (int i = 1; i < N; i += 4) {
-    const float x = o[i];
-    o[i] = o[i + 1];
-    o[i + 1] = x;
+    for (int i = 1; i < N; i += 4) {
+      const float x = o[i];
+      o[i] = o[i + 1];
+      o[i + 1] = x;
+    }
+  } else if constexpr (FORMAT == KVPRM_CACHE_E2M1) {
+#pragma unroll
+    for (int i = 0; i < N; i += 8) {
+      float x[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] = o[i + k];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) o[i + (k >> 1) + 4 * (k & 1)] = x[k];
+    }
   }
 }
 
 // (a bound of 640 threads: 96 registers, what five warps of a scheduler can have)
-template <int HD, bool E4M3>
+template <int HD, int FORMAT>
 __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__ TreeLaunch a,
                                                          const __grid_constant__ CUtensorMap map) {
-  using SM = Smem<HD, E4M3>;
+  constexpr bool CODES = FORMAT != KVPRM_CACHE_BF16, E2M1 = FORMAT == KVPRM_CACHE_E2M1;
+  using SM = Smem<HD, CODES>;
   extern __shared__ uint8_t smem_raw[];
   __shared__ Static st;
   uint8_t* base = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t{1023});
@@ -230,7 +257,7 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
     for (int i = 0; i < 8; ++i) {
-      mbar_init(&st.slot_full[i], E4M3 ? kProducers / 32 : 1);
+      mbar_init(&st.slot_full[i], CODES ? kProducers / 32 : 1);
       mbar_init(&st.slot_empty[i], 1);
       mbar_init(&st.draft_go[i], 1);
     }
@@ -244,7 +271,7 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
     mbar_init(&st.part_done, 1);
     mbar_init(&st.o_free, 8);
     fence_mbar_init();
-    if constexpr (!E4M3) tma_prefetch_desc(&map);
+    if constexpr (!CODES) tma_prefetch_desc(&map);
   }
   if (threadIdx.x < kFlagSets * 32) st.bad_drafts[threadIdx.x >> 5][lane] = 0;
   if (threadIdx.x < kFlagSets) st.bad[threadIdx.x] = 0;
@@ -274,7 +301,7 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
     uint32_t n = 0;   // items of earlier parts
     bool ok = true;
     auto wait_all = [&](uint64_t* bar, uint32_t parity) { return __all_sync(0xffffffffu, wait_for(bar, parity, err)); };
-    for (int part = 0; !E4M3 && ok && next_part(); ++part) {
+    for (int part = 0; !CODES && ok && next_part(); ++part) {
       const int32_t* table = a.t.block_table + static_cast<int64_t>(a.seq0 + p.s) * a.t.max_blocks;
       const int pages = (p.q.len + kTreePage - 1) / kTreePage;
       const Items items(p);
@@ -370,7 +397,7 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
         phase ^= 1u << g;
         if (!ok) return;
         uint8_t* tile = base + SM::kSlot0 + slot * SM::kTile;
-        if constexpr (!E4M3) {
+        if constexpr (!CODES) {
           // the last cached chunk's last page: its places beyond the length may hold anything, and a weight of
           // zero would keep a NaN
           const int have = p.q.len - (p.c0 + c) * kChunk;
@@ -415,7 +442,7 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
       if (t == 0) mbar_arrive(bar);
     };
     auto slot_filled = [&](uint64_t* bar) {   // a slot's: with an 8-bit cache each warp goes on by itself
-      if constexpr (E4M3) {
+      if constexpr (CODES) {
         fence_proxy_async_smem();
         __syncwarp();
         if (lane == 0) mbar_arrive(bar);
@@ -423,13 +450,16 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
         filled(bar);
       }
     };
-    // An 8-bit chunk's keys or values: a warp has one page, whose codes it loads an item ahead and converts kTeam rows at
+    // A quantised chunk's keys or values: a warp has one page, whose codes it loads an item ahead and converts kTeam rows at
     // a time; it waits for slots and hands them on by itself.  A row's 8 pieces fill two 64-column parts, whose equal
     // pieces lie in the same banks: lanes 0 to 3 and 4 to 7 take neighbouring rows, which the swizzle puts in different
     // ones.
-    constexpr int kParts = HD / 16, kTeam = 32 / kParts, kSteps = kTreePage / kTeam;   // 16-byte pieces of a row
+    //   A 4-bit piece is a block of 32 elements, whose exponent its lane loads, and fills four pieces of the tile: lanes with the
+    // second part's blocks take them in the order 2 3 0 1, for the same reason.
+    constexpr int kParts = E2M1 ? HD / 32 : HD / 16, kTeam = 32 / kParts, kSteps = kTreePage / kTeam;   // 16-byte pieces of a row
+    constexpr int kRowBytes = E2M1 ? HD / 2 : HD;
     const int my_page = t >> 5, my_piece = lane % kParts;
-    const int my_row = HD == 128 ? (lane >> 4) * 2 + (((lane >> 3) & 1) ^ (my_piece >> 2)) : lane / kParts;   // of a step's
+    const int my_row = HD == 128 && !E2M1 ? (lane >> 4) * 2 + (((lane >> 3) & 1) ^ (my_piece >> 2)) : lane / kParts;   // of a step's
     const uint32_t flip = a.scale_log2 < 0.f ? 0x80008000u : 0u;   // a negative scale turns Q's signs instead
     for (int part = 0; next_part(); ++part) {
       const int rows = p.q.drafts * a.group;
@@ -445,20 +475,26 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
       };
       uint32_t bad = 0;   // items (modulo 4) with a page outside the cache
       uint4 next[kSteps];
-      uint32_t next_e = 0;
+      uint32_t next_e = 0;   // (4-bit: a byte for each step)
       auto load = [&](int item, int32_t page) {
         if (page == -2) bad |= 1u << (item & 3);
         if (page < 0) return;
         int kv;
         items.chunk(item, &kv);
         const int64_t row = ((static_cast<int64_t>(page) * 2 + kv) * a.n_kv + p.g) * kTreePage;
-        const uint8_t* src = a.pages + row * HD + my_row * HD + my_piece * 16;
+        const uint8_t* src = a.pages + row * kRowBytes + my_row * kRowBytes + my_piece * 16;
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) next[k] = ldg_stream(src + k * 512);
-        next_e = __ldg(a.exponents + row + lane % kTreePage);
+        if constexpr (E2M1) {
+          next_e = 0;
+#pragma unroll
+          for (int k = 0; k < kSteps; ++k) next_e |= static_cast<uint32_t>(__ldg(a.exponents + row * kParts + k * 32 + lane)) << (8 * k);
+        } else {
+          next_e = __ldg(a.exponents + row + lane % kTreePage);
+        }
       };
       int32_t page = -1;
-      if constexpr (E4M3) {
+      if constexpr (CODES) {
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) next[k] = make_uint4(0u, 0u, 0u, 0u);
         const int32_t page0 = page_of(0);
@@ -485,7 +521,7 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
 #pragma unroll
         for (int i = 0; i < kRows / kStep; ++i) {
           v[i] = make_uint4(v[i].x ^ flip, v[i].y ^ flip, v[i].z ^ flip, v[i].w ^ flip);
-          *reinterpret_cast<uint4*>(dst + swizzled<HD>(first + i * kStep, piece)) = E4M3 ? paired(v[i]) : v[i];
+          *reinterpret_cast<uint4*>(dst + swizzled<HD>(first + i * kStep, piece)) = E2M1 ? paired4(v[i]) : CODES ? paired(v[i]) : v[i];
         }
       }
       filled(&st.q_full);
@@ -493,10 +529,10 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
         int kv;
         const int c = p.c0 + items.chunk(item, &kv);
         const bool cached = c < p.q.cached_blocks;
-        if (cached && !E4M3) continue;
+        if (cached && !CODES) continue;
         const uint32_t i = n + item, slot = i % SM::kSlots;
         uint8_t* dst = base + SM::kSlot0 + slot * SM::kTile;
-        if constexpr (E4M3) {   // every slot is filled here
+        if constexpr (CODES) {   // every slot is filled here
           if (i >= SM::kSlots) ok = ok && wait_for(&st.slot_empty[slot], (i / SM::kSlots - 1) & 1u, err);
           uint4 codes[kSteps];
 #pragma unroll
@@ -507,6 +543,37 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
           if (cached) {
             if (lane == 0 && (bad >> (item & 3)) & 1u) atomicOr(&st.bad[part % kFlagSets], 1);
             bad &= ~(1u << (item & 3));
+            if constexpr (E2M1) {
+              uint32_t f[kSteps];   // of a block: 2^(e - 127 + 126) as bf16, beyond its range in two; zero past the length
+              bool two = false;
+#pragma unroll
+              for (int k = 0; k < kSteps; ++k) {
+                const uint32_t x = (e >> (8 * k)) & 255u;
+                const bool live = my_page * kTreePage + kTeam * k + my_row < p.q.len - c * kChunk, more = x > 128u && live;
+                f[k] = (more ? 254u : x + 126u) << 7 | (more ? (x == 255u ? 0x7FC0u : (x - 1u) << 7) : 0x3F80u) << 16;
+                if (!live) f[k] = 0x3F800000u;
+                two = two || more;
+              }
+              auto convert = [&](auto plain) {
+#pragma unroll
+                for (int k = 0; k < kSteps; ++k) {
+                  const int row = my_page * kTreePage + k * kTeam + my_row, turn = my_piece & 2;
+                  const uint32_t f1 = __byte_perm(f[k], 0, 0x1010), f2 = __byte_perm(f[k], 0, 0x3232);
+                  const uint32_t w[4] = {turn ? codes[k].z : codes[k].x, turn ? codes[k].w : codes[k].y,
+                                         turn ? codes[k].x : codes[k].z, turn ? codes[k].y : codes[k].w};
+#pragma unroll
+                  for (int i = 0; i < 4; ++i)
+                    *reinterpret_cast<uint4*>(dst + swizzled<HD>(row, 4 * my_piece + (i ^ turn))) =
+                        bf16_of8<decltype(plain)::value>(w[i], f1, f2);
+                }
+              };
+              if (__any_sync(0xffffffffu, two))
+                convert(std::false_type());
+              else
+                convert(std::true_type());
+              slot_filled(&st.slot_full[slot]);
+              continue;
+            }
             // the factor of a row, per lane: 2^(e - 127 + 120) as bf16, beyond its range (or NaN, 255) in two; zero past the
             // length, where the codes may be anything
             const bool live = my_page * kTreePage + lane % kTreePage < p.q.len - c * kChunk, two = e > 134u && live;
@@ -562,7 +629,7 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
               }
             }
           }
-          *reinterpret_cast<uint4*>(dst + swizzled<HD>(row, piece)) = E4M3 ? paired(v) : v;
+          *reinterpret_cast<uint4*>(dst + swizzled<HD>(row, piece)) = E2M1 ? paired4(v) : CODES ? paired(v) : v;
         }
         slot_filled(&st.slot_full[slot]);
       }
@@ -767,7 +834,7 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[i] = ok ? o[i] * f0 + (two_streams ? o1[i] * f1 : 0.f) : 0.f;
-        if (E4M3) in_order(o);
+        in_order<FORMAT>(o);
         if (!live) continue;
         if (whole) {
           uint32_t w[8];
@@ -799,11 +866,11 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
   }
 }
 
-template <int HD, bool E4M3>
+template <int HD, int FORMAT>
 cudaError_t launch(const TreeLaunch& a, const CUtensorMap& map, int ctas, cudaStream_t stream) {
-  using SM = Smem<HD, E4M3>;
+  using SM = Smem<HD, FORMAT != KVPRM_CACHE_BF16>;
   static_assert(SM::kDynamic + sizeof(Static) <= 227 * 1024, "shared memory of a CTA");
-  cudaError_t e = cudaFuncSetAttribute(tree_tc_kernel<HD, E4M3>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  cudaError_t e = cudaFuncSetAttribute(tree_tc_kernel<HD, FORMAT>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        static_cast<int>(SM::kDynamic));
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
@@ -811,7 +878,7 @@ cudaError_t launch(const TreeLaunch& a, const CUtensorMap& map, int ctas, cudaSt
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = SM::kDynamic;
   cfg.stream = stream;
-  return cudaLaunchKernelEx(&cfg, tree_tc_kernel<HD, E4M3>, a, map);
+  return cudaLaunchKernelEx(&cfg, tree_tc_kernel<HD, FORMAT>, a, map);
 }
 
 // Pages [n_pages][2][n_kv][16][hd] as (column of 64, row of 8, 64-column part, half of the page's rows, (2 page + {0: keys,
@@ -831,7 +898,9 @@ CUresult encode_pages(PFN_cuTensorMapEncodeTiled_v12000 encode, CUtensorMap* map
 cudaError_t launch_tree_tc(const TreeLaunch& a, const kvprm_cache& c, int ctas, cudaStream_t stream) {
   CUtensorMap map = {};
   if (c.format == KVPRM_CACHE_E4M3)
-    return c.head_dim == 128 ? launch<128, true>(a, map, ctas, stream) : launch<64, true>(a, map, ctas, stream);
+    return c.head_dim == 128 ? launch<128, KVPRM_CACHE_E4M3>(a, map, ctas, stream) : launch<64, KVPRM_CACHE_E4M3>(a, map, ctas, stream);
+  if (c.format == KVPRM_CACHE_E2M1)
+    return c.head_dim == 128 ? launch<128, KVPRM_CACHE_E2M1>(a, map, ctas, stream) : launch<64, KVPRM_CACHE_E2M1>(a, map, ctas, stream);
   static PFN_cuTensorMapEncodeTiled_v12000 encode = [] {
     void* fn = nullptr;
     cudaDriverEntryPointQueryResult q;
@@ -842,7 +911,7 @@ cudaError_t launch_tree_tc(const TreeLaunch& a, const kvprm_cache& c, int ctas, 
   }();
   if (!encode) return cudaErrorNotSupported;
   if (encode_pages(encode, &map, c) != CUDA_SUCCESS) return cudaErrorInvalidValue;
-  return c.head_dim == 128 ? launch<128, false>(a, map, ctas, stream) : launch<64, false>(a, map, ctas, stream);
+  return c.head_dim == 128 ? launch<128, KVPRM_CACHE_BF16>(a, map, ctas, stream) : launch<64, KVPRM_CACHE_BF16>(a, map, ctas, stream);
 }
 
 }  // namespace kvprm
