@@ -23,7 +23,7 @@ struct TreeLaunch {
   int32_t fill;                        // 1: rows that no sequence writes are written too (tree_fill)
   int32_t weight_full, weight_part;    // places of a block of a pair with all its tiles, or with fewer
   float scale_log2;                    // scores in units of log2
-  int32_t* line;                       // [n_seqs + 1], then the CTAs that took part: for the join
+  int32_t* line;                       // [n_seqs + 1], then the CTAs (or warps) that took part: for the join
   float* part_o;                       // [2 * CTAs][head_dim][rows]
   float2* part_ml;                     // [2 * CTAs][rows]
 };
@@ -246,8 +246,14 @@ using TreeRows = TreeGeometry<16 * TILES, kTreePage, 1, TILES == 1 ? 16 : 20>;
 using TreeTc = TreeGeometry<128, 128, 2, 4>;
 #endif
 cudaError_t launch_tree_rows(const TreeLaunch& a, const kvprm_cache& c, int tiles, int ctas, cudaStream_t stream);
-// tree_e2m1.cu: 4-bit pages, tiles of 8, 16 or 32 query rows (tiles of 8: 1, 2 or 4).
-constexpr int tree_e2m1_per_sm(int tiles) { return tiles == 1 ? 4 : tiles == 2 ? 3 : 2; }
+// tree_e2m1.cu: 4-bit pages, tiles of 8, 16 or 32 query rows (tiles of 8: 1, 2 or 4).  Its shares of the line are warps', and it
+// joins its partial results itself.
+constexpr int kTreeE2m1Warps = 4;   // of a CTA
+#ifdef __CUDACC__
+template <int NT>
+using TreeE2m1 = TreeGeometry<8 * NT, kTreePage, 1, 8>;
+#endif
+constexpr int tree_e2m1_per_sm(int tiles) { return tiles == 1 ? 3 : 2; }
 cudaError_t launch_tree_e2m1(const TreeLaunch& a, const kvprm_cache& c, int tiles, int ctas, cudaStream_t stream);
 // tree_tc.cu: in pairs of tiles of 128, on the tensor cores; one CTA on an SM.  The cache has a page at least.
 cudaError_t launch_tree_tc(const TreeLaunch& a, const kvprm_cache& c, int ctas, cudaStream_t stream);

@@ -20,6 +20,7 @@ struct TreePlan {
   bool tc = false, whole = false;
   int tiles8 = 0;                      // 4-bit pages on registers: tiles of 8 rows
   int ctas = 0, rows = 16, seqs = 0;   // rows: of a partial result; seqs: sequences of a launch
+  int64_t parts() const { return tiles8 ? int64_t{ctas} * kTreeE2m1Warps : ctas; }   // shares of the line
 };
 
 int check(const kvprm_cache* c, const kvprm_tree* t, const char* who) {
@@ -45,6 +46,10 @@ int sm_count(int* sms) {
   return KVPRM_OK;
 }
 
+// 4-bit pages on registers, whose parts are warps': pairs of so many blocks stay whole; a part has so many blocks at least, and
+// a pair so many parts at most.
+constexpr int kWhole4 = 16, kLeast4 = 8, kParts4 = 32;
+
 // More than 32 rows of a kv head go to the tensor cores (us a call, registers / tensor cores: 8 heads with 24 rows over ragged
 // 20,000 bf16 tokens 76 / 78, 8-bit 66 / 89; with 32 over 8 x 32,768 bf16 tokens 187 / 186, 8-bit 155 / 221; 4 heads with 63 over
 // 16 x 9,001 8-bit tokens 97 / 80; 2 heads with 42 over ragged 1,000 bf16 tokens 19 / 21, with 126 22 / 21).  CTAs: as many as
@@ -57,7 +62,7 @@ int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   const bool e2m1 = c.format == KVPRM_CACHE_E2M1;
   p.tc = rows > 32 && c.n_pages > 0;
   p.tiles8 = !e2m1 || p.tc ? 0 : rows > 16 ? 4 : rows > 8 ? 2 : 1;
-  p.rows = p.tc ? 256 : rows > 16 ? 32 : 16;
+  p.rows = p.tc ? 256 : p.tiles8 ? 8 * p.tiles8 : rows > 16 ? 32 : 16;
   const int64_t block = p.tc ? 128 : kTreePage, tiles = ceil_div(rows, p.tc ? 128 : p.rows), lead = 20;
   // the line of a sequence of any length is shorter than this; a launch's stays within 31 bits
   const int64_t depth = ceil_div(int64_t{kTreePage} * t.max_blocks, block) + ceil_div(t.max_drafts, block) + lead;
@@ -68,6 +73,14 @@ int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   const int64_t pairs = int64_t{p.seqs} * c.n_kv_heads * ceil_div(rows, p.rows);
   const int64_t blocks = ceil_div(len, block) + ceil_div(t.max_drafts, block);
   const int64_t most = int64_t{sms} * (p.tc ? 1 : e2m1 ? tree_e2m1_per_sm(p.tiles8) : tree_rows_per_sm(p.rows / 16));
+  if (p.tiles8) {
+    const int64_t warps = most * kTreeE2m1Warps;
+    p.whole = blocks <= kWhole4;
+    const int64_t parts = p.whole ? pairs : std::min(pairs * blocks / kLeast4, pairs * kParts4);
+    p.ctas = static_cast<int>(std::max<int64_t>(1, ceil_div(std::min(warps, parts), kTreeE2m1Warps)));
+    *out = p;
+    return KVPRM_OK;
+  }
   p.whole = blocks <= (pairs <= most ? (p.tc ? 4 : 32) : (p.tc ? 3 : 16));
   p.ctas = static_cast<int>(std::max<int64_t>(1, std::min(most, p.whole ? pairs : pairs * blocks / (p.tc ? 2 : 8))));
   *out = p;
@@ -75,7 +88,7 @@ int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
 }
 
 int64_t workspace_bytes(const kvprm_cache& c, const TreePlan& p) {
-  return kLineBytes + (p.whole ? 0 : int64_t{2} * p.ctas * p.rows * (4 * c.head_dim + 8));
+  return kLineBytes + (p.whole ? 0 : int64_t{2} * p.parts() * p.rows * (4 * c.head_dim + 8));
 }
 
 int attend(const kvprm_cache* cache, const kvprm_tree* t, void* workspace, int64_t workspace_size, void* stream, bool fill,
@@ -117,7 +130,7 @@ int attend(const kvprm_cache* cache, const kvprm_tree* t, void* workspace, int64
   a.weight_part = !p.tc ? 1 : cache->format != KVPRM_CACHE_BF16 ? 4 : 3;
   a.line = static_cast<int32_t*>(workspace);
   a.part_o = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + kLineBytes);
-  a.part_ml = reinterpret_cast<float2*>(a.part_o + int64_t{2} * p.ctas * p.rows * cache->head_dim);
+  a.part_ml = reinterpret_cast<float2*>(a.part_o + int64_t{2} * p.parts() * p.rows * cache->head_dim);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   a.seq0 = 0;
   do {   // (once without sequences, which is to fill only)
@@ -125,7 +138,7 @@ int attend(const kvprm_cache* cache, const kvprm_tree* t, void* workspace, int64
     cudaError_t e = p.tc       ? launch_tree_tc(a, *cache, p.ctas, st)
                     : p.tiles8 ? launch_tree_e2m1(a, *cache, p.tiles8, p.ctas, st)
                                : launch_tree_rows(a, *cache, p.rows / 16, p.ctas, st);
-    if (e == cudaSuccess && !p.whole && seqs) e = launch_tree_join(a, *cache, p.rows, st);
+    if (e == cudaSuccess && !p.whole && seqs && !p.tiles8) e = launch_tree_join(a, *cache, p.rows, st);
     if (e != cudaSuccess) return operator_fail(KVPRM_ECUDA, "%s: %s", who, cudaGetErrorString(e));
     a.seq0 += p.seqs;
   } while (a.seq0 < t->n_seqs);

@@ -34,23 +34,16 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr float kMargin = 3.f;     // a running maximum may be exceeded by so many powers of two
 constexpr float kLift = 12.f;      // weights are times 2^12: 2^(12 + 3) is below 65504
 constexpr int kBelow = 8;          // blocks from 2^-8 of E on, to 2^7, are taken in fp16
+constexpr int kTop = 239;          // E's field at most: 255, NaN, is never in the window
 
-__device__ __forceinline__ uint4 ldg16(const void* p) {
-  uint4 r;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-               : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w)
-               : "l"(p));
-  return r;
+// 16 bytes into shared memory, in the background.
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
-__device__ __forceinline__ uint2 ldg8(const void* p) {
-  uint2 r;
-  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p));
-  return r;
-}
-__device__ __forceinline__ uint32_t ldg4(const void* p) {
-  uint32_t r;
-  asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(r) : "l"(p));
-  return r;
+__device__ __forceinline__ void copies_end() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {   // until all but the last N groups have arrived
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -86,34 +79,54 @@ __device__ __forceinline__ uint32_t bf16_times(uint32_t h, float lo, float hi) {
 // The token of a page that row r of S^T, and index r of P V's sums, stand for: a lane's four values' rows are neighbours.
 __device__ __forceinline__ int token_of(int r) { return 4 * ((r & 7) >> 1) + (r & 1) + ((r >> 3) << 1); }
 
+// A warp's ring of pages: of each a head's keys, values and their exponents.  Rows lie in the order in which the lanes read
+// them, so that an access' 128 bytes are in different banks: key row of lane group gid (+ 2 tokens) at 8 n + gid; value row
+// 4 c + t at 4 t + c, its 16-byte pieces turned by c >> 1 (the rows are 64 bytes with 128 dims).
+template <int HD>
+struct Stage {
+  static constexpr int kRow = HD / 2, kHead = kTreePage * kRow, kExp = kTreePage * HD / 32;
+  static constexpr int kK = 0, kV = kHead, kKe = 2 * kHead, kVe = kKe + kExp, kBytes = kVe + kExp;
+};
+constexpr int kRing = 4;   // pages of a warp
+template <int HD>
+constexpr int ring_bytes() { return kWarps * kRing * Stage<HD>::kBytes; }
+
 // NT: tiles of 8 query rows.
 template <int HD, int NT>
 __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kernel(const __grid_constant__ TreeLaunch a) {
-  using G = TreeRows<NT <= 2 ? 1 : 2>;
+  using G = TreeE2m1<NT>;
   constexpr int KS = HD / 16;            // 16-dim steps of q . k
   constexpr int MT = HD / 16;            // 16-dim tiles of the output
   constexpr int kW = HD / 32;            // a lane's words of a key row, of eight codes
   constexpr int kVW = HD / 64;           // of each of its four value rows
   constexpr int kRowBytes = HD / 2, kBlocks = HD / 32;
+  constexpr int P = NT <= 2 ? 2 : 1;     // pages of a step
+  using S = Stage<HD>;
+  extern __shared__ __align__(16) uint8_t s_ring[];
   __shared__ int32_t s_off[kTreeSeqs + 1];
   __shared__ int32_t s_sum[kWarps];
-  __shared__ union {
-    uint2 q[NT][KS][32];              // the scaled queries' fragments, by lane
-    float o[kWarps][8][HD + 4];       // at a part's end, the warps' outputs
-  } sh;
-  __shared__ float s_m[kWarps][8], s_l[kWarps][8];
+  __shared__ uint2 s_q[kWarps][NT][KS][32];   // the scaled queries' fragments, by lane
   grid_dep_launch();
   tree_line<G, kThreads, HD>(a, s_off, s_sum);
   const int32_t total = s_off[a.n_seqs];
   if (total == 0) return;
-  const TreeShares shares(total, gridDim.x, a.weight_full);
-  const int me = blockIdx.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, c = lane & 3;
+  const TreeShares shares(total, gridDim.x * kWarps, a.weight_full);
+  const int me = blockIdx.x * kWarps + warp;
   tree_leave_line(a, s_off, shares.ctas);
   if (me >= shares.ctas) return;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, c = lane & 3;
   const int64_t head_bytes = kTreePage * kRowBytes, page_bytes = 2 * a.n_kv * head_bytes;
   constexpr int kHeadExp = kTreePage * kBlocks;
   const int64_t page_exp = 2 * static_cast<int64_t>(a.n_kv) * kHeadExp;
+  // where this lane's pieces of a page go
+  uint8_t* const my_ring = s_ring + warp * (kRing * S::kBytes);
+  const uint32_t ring = smem_u32(my_ring);
+  constexpr int kPer = HD / 32;                       // pieces of a row
+  const int row = lane / kPer, piece = lane % kPer;   // (with 128 dims, and 8 rows on)
+  const int k_at = S::kK + (8 * ((row & 3) >> 1) + 2 * (row >> 2) + (row & 1)) * kRowBytes + piece * 16;
+  const int v_at = S::kV + (4 * (row & 3) + (row >> 2)) * kRowBytes + piece * 16;
+  constexpr int k_step = 4 * kRowBytes;
+  const int v_step = 2 * kRowBytes + (piece & 2 ? -32 : 32);
   int32_t u = shares.begin(me);
   const int32_t u_end = shares.begin(me + 1);
   int s_at = tree_find(s_off, a.n_seqs, u);
@@ -122,11 +135,8 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
     const TreeSeq& q = part.q;
     const int g = part.g, row0 = part.tp * G::kSlotRows, rows = q.drafts * a.group;
     const int32_t* table = a.t.block_table + static_cast<int64_t>(a.seq0 + s_at) * a.t.max_blocks;
-    // this lane's bytes of a page: piece c of key row token_of(gid) (the other two rows on), dims of gid of value rows 4 c ..
-    const uint8_t* keys = a.pages + g * head_bytes + token_of(gid) * kRowBytes + c * (kRowBytes / 4);
-    const uint8_t* values = a.pages + (a.n_kv + g) * head_bytes + 4 * c * kRowBytes + gid * (kRowBytes / 8);
-    const uint8_t* key_exp = a.exponents + g * kHeadExp + token_of(gid) * kBlocks + c * kBlocks / 4;
-    const uint8_t* value_exp = a.exponents + (a.n_kv + g) * kHeadExp + 4 * c * kBlocks;
+    const uint8_t* keys = a.pages + g * head_bytes + lane * 16;
+    const uint8_t* exps = a.exponents + g * kHeadExp + (lane < kHeadExp / 16 ? lane * 16 : a.n_kv * kHeadExp + lane * 16 - kHeadExp);
     // the query rows' elements (HD / 4) c .. of row gid of tile nt
     auto query = [&](int nt) -> const uint4* {
       const int r = row0 + 8 * nt + gid;
@@ -136,135 +146,74 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
                                             (g * a.group + r - tok * a.group) * a.t.q_head + c * (HD / 4));
     };
 
-    // ---- the queries, scaled: warp w makes tiles w, w + 4
-    float rs[NT][2];   // of rows 2 c and 2 c + 1: the row's power of two times the scores' scale
-    __syncthreads();   // the last part's have been read
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const uint4* src = query(nt);
-      uint4 v[HD / 32];
-      float most = 0.f;
-#pragma unroll
-      for (int i = 0; i < HD / 32; ++i) {
-        v[i] = src ? __ldg(src + i) : make_uint4(0u, 0u, 0u, 0u);
-        const uint32_t w[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) most = fmaxf(most, fmaxf(fabsf(lo_bf16(w[k])), fabsf(hi_bf16(w[k]))));
-      }
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-      int e = static_cast<int>(__float_as_uint(most) >> 23);   // (infinite or all zero: any scale does)
-      e = e < 1 || e > 253 ? 127 : e;
-      rs[nt][0] = __shfl_sync(0xffffffffu, power_of(e), 8 * c) * a.scale_log2;
-      rs[nt][1] = __shfl_sync(0xffffffffu, power_of(e), 8 * c + 4) * a.scale_log2;
-      if ((nt & (kWarps - 1)) != warp) continue;
-      const float up = power_of(254 - e);
-      auto scaled = [&](uint32_t x) { return pack_f16(lo_bf16(x) * up, hi_bf16(x) * up); };
-#pragma unroll
-      for (int i = 0; i < HD / 32; ++i) {
-        sh.q[nt][2 * i][lane] = make_uint2(scaled(v[i].x), scaled(v[i].y));
-        sh.q[nt][2 * i + 1][lane] = make_uint2(scaled(v[i].z), scaled(v[i].w));
-      }
-    }
-    __syncthreads();
-
-    float o[NT][MT][4], m[NT][2], l[NT][2];   // o: dims gid-rows of a tile, query rows 2 c and 2 c + 1
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-      for (int i = 0; i < MT; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
-      m[nt][0] = m[nt][1] = -INFINITY;
-      l[nt][0] = l[nt][1] = 0.f;
-    }
+    // ---- the pages' numbers, a lane each, 32 at a time; 0 for one outside the cache
+    const int mine = max(0, min(part.c1, q.cached_blocks) - part.c0);
     bool poison = q.bad;        // of all rows of the sequence
-    uint32_t poison_row = 0;    // bit 2 nt + h: of row 2 c + h of tile nt
-    int ek = 127, ev = -64, ev_top = 0;   // exponent bytes that keys' and values' powers are relative to (ev: none yet)
-    auto scale_outputs = [&](float f) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-          for (int k = 0; k < 4; ++k) o[nt][i][k] *= f;
+    auto ids_of = [&](int k0) {
+      const int k = k0 + lane;
+      if (k >= mine) return 0;
+      const int32_t page = __ldg(table + part.c0 + k);
+      const bool in = page >= 0 && page < a.n_pages;
+      poison = poison || !in;
+      return in ? page : 0;
     };
-
-    // One block's softmax step for a tile: scores s in units of log2 (tokens token_of(gid) and two on, rows 2 c and 2 c + 1:
-    // s[0], s[1] and s[2], s[3]) become P^T as an operand, the running maximum, sum and output following.  The maximum moves
-    // only when a score passes it by more than a margin.  The weights are rounded to fp16 or bf16, the values' type: their sum
-    // is not.
-    auto softmax = [&](int nt, const float(&s)[4], uint32_t(&p)[2], bool fp16) {
-      const float mx[2] = {fmaxf(s[0], s[2]), fmaxf(s[1], s[3])};
-      if (__any_sync(0xffffffffu, mx[0] > m[nt][0] + kMargin || mx[1] > m[nt][1] + kMargin)) {
-        float al[2];
+    const int pages = a.n_pages > 0 ? mine : 0;   // (an empty pool: every page is outside it)
+    int32_t ids = ids_of(0), ids_next = ids_of(32);
+    // page k into a place of the ring, if there is one
+    auto fetch = [&](int k, int place) {
+      if (k < pages) {
+        const int64_t page = __shfl_sync(0xffffffffu, ids, k & 31);
+        const uint32_t to = ring + place;
+        const uint8_t* src = keys + page * page_bytes;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          float x = mx[h];
-#pragma unroll
-          for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
-          x = fmaxf(x, m[nt][h]);
-          al[h] = x == m[nt][h] ? 1.f : ex2_ftz(m[nt][h] - x);
-          m[nt][h] = x;
-          l[nt][h] *= al[h];
+        for (int x = 0; x < S::kHead / 512; ++x) {
+          copy16(to + k_at + x * k_step, src + x * 512);
+          copy16(to + v_at + x * v_step, src + a.n_kv * head_bytes + x * 512);
         }
-#pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          o[nt][i][0] *= al[0];
-          o[nt][i][1] *= al[1];
-          o[nt][i][2] *= al[0];
-          o[nt][i][3] *= al[1];
+        if (lane < 2 * S::kExp / 16) copy16(to + S::kKe + lane * 16, exps + page * page_exp);
+        if ((k & 31) == 31) {
+          ids = ids_next;
+          ids_next = ids_of(k + 33);
         }
       }
-      float w[4];
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const float nm = m[nt][h] == -INFINITY ? kLift : kLift - m[nt][h];   // nothing seen yet: every score is -infinity
-        w[h] = ex2_ftz(s[h] + nm);
-        w[2 + h] = ex2_ftz(s[2 + h] + nm);
-        l[nt][h] += w[h] + w[2 + h];
-      }
-      p[0] = transposed(fp16 ? pack_f16(w[0], w[1]) : pack_bf16(w[0], w[1]));
-      p[1] = transposed(fp16 ? pack_f16(w[2], w[3]) : pack_bf16(w[2], w[3]));
     };
-
-    const int c_end = min(part.c1, q.cached_blocks);
-    auto page_of = [&](int b) { return b < c_end ? __ldg(table + b) : 0; };
-    auto in_cache = [&](int32_t page) { return page >= 0 && page < a.n_pages; };
     struct Loaded {
       uint32_t k[2][kW], v[4][kVW];
       uint32_t ke[2], ve[kBlocks];   // ve: the blocks of four tokens' values
     };
-    auto load = [&](int32_t page, Loaded& x) {
-      const int64_t at = in_cache(page) ? page : 0;
-      const uint8_t* k = keys + at * page_bytes;
-      const uint8_t* v = values + at * page_bytes;
-      const uint8_t* ke = key_exp + at * page_exp;
-      const uint8_t* ve = value_exp + at * page_exp;
+    auto read_keys = [&](int place, Loaded& x) {   // and all exponents
+      const uint8_t* at = my_ring + place;
 #pragma unroll
       for (int n = 0; n < 2; ++n) {
+        const uint8_t* row = at + S::kK + (8 * n + gid) * kRowBytes + c * (kRowBytes / 4);
         if constexpr (HD == 128) {
-          const uint4 r = ldg16(k + 2 * n * kRowBytes);
+          const uint4 r = *reinterpret_cast<const uint4*>(row);
           x.k[n][0] = r.x, x.k[n][1] = r.y, x.k[n][2] = r.z, x.k[n][3] = r.w;
         } else {
-          const uint2 r = ldg8(k + 2 * n * kRowBytes);
+          const uint2 r = *reinterpret_cast<const uint2*>(row);
           x.k[n][0] = r.x, x.k[n][1] = r.y;
         }
-        x.ke[n] = __ldg(ke + 2 * n * kBlocks);
+        x.ke[n] = at[S::kKe + (token_of(gid) + 2 * n) * kBlocks + c * kBlocks / 4];
       }
+      const uint8_t* ve = at + S::kVe + 4 * c * kBlocks;
+      if constexpr (HD == 128) {
+        const uint4 r = *reinterpret_cast<const uint4*>(ve);
+        x.ve[0] = r.x, x.ve[1] = r.y, x.ve[2] = r.z, x.ve[3] = r.w;
+      } else {
+        const uint2 r = *reinterpret_cast<const uint2*>(ve);
+        x.ve[0] = r.x, x.ve[1] = r.y;
+      }
+    };
+    auto read_values = [&](int place, Loaded& x) {
+      const uint8_t* at = my_ring + place + S::kV;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         if constexpr (HD == 128) {
-          const uint2 r = ldg8(v + t * kRowBytes);
+          const uint2 r = *reinterpret_cast<const uint2*>(at + (4 * t + c) * kRowBytes + ((gid * 8) ^ ((c >> 1) << 5)));
           x.v[t][0] = r.x, x.v[t][1] = r.y;
         } else {
-          x.v[t][0] = ldg4(v + t * kRowBytes);
+          x.v[t][0] = *reinterpret_cast<const uint32_t*>(at + (4 * t + c) * kRowBytes + gid * 4);
         }
-      }
-      if constexpr (HD == 128) {
-        const uint4 r = __ldg(reinterpret_cast<const uint4*>(ve));
-        x.ve[0] = r.x, x.ve[1] = r.y, x.ve[2] = r.z, x.ve[3] = r.w;
-      } else {
-        const uint2 r = __ldg(reinterpret_cast<const uint2*>(ve));
-        x.ve[0] = r.x, x.ve[1] = r.y;
       }
     };
     // the exponents of this lane's block (of its 16 dims) of its four tokens, a byte each
@@ -277,23 +226,123 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
       }
     };
 
-    // ---- the cache: pages b, b + 4, ..; the next page's bytes are on their way while this one's are used
-    int b = part.c0 + warp;
-    int32_t page = page_of(b), next = page_of(b + kWarps);
-    Loaded now;
-    const bool some = a.n_pages > 0;
-    if (b < c_end && some) load(page, now);
-    for (; b < c_end; b += kWarps) {
-      if (!some) {   // an empty pool: every page is outside it
-        poison = true;
-        continue;
+    // What the part begins with is loaded at once: the pages' numbers, the queries, then the first pages.
+    uint4 qv[NT][HD / 32];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const uint4* src = query(nt);
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i) qv[nt][i] = src ? __ldg(src + i) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int k = 0; k < kRing; ++k) {
+      fetch(k, k * S::kBytes);
+      if (k % P == P - 1) copies_end();
+    }
+
+    // ---- the queries, scaled; a negative scale turns their signs
+    float rs[NT][2];   // of rows 2 c and 2 c + 1: the row's power of two times the scores' scale
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float most = 0.f;
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i) {
+        const uint32_t w[4] = {qv[nt][i].x, qv[nt][i].y, qv[nt][i].z, qv[nt][i].w};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) most = fmaxf(most, fmaxf(fabsf(lo_bf16(w[k])), fabsf(hi_bf16(w[k]))));
       }
-      const int32_t after = page_of(b + 2 * kWarps);
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+      int e = static_cast<int>(__float_as_uint(most) >> 23);   // (infinite or all zero: any scale does)
+      e = e < 1 || e > 253 ? 127 : e;
+      rs[nt][0] = __shfl_sync(0xffffffffu, power_of(e), 8 * c) * fabsf(a.scale_log2);
+      rs[nt][1] = __shfl_sync(0xffffffffu, power_of(e), 8 * c + 4) * fabsf(a.scale_log2);
+      const float up = a.scale_log2 < 0.f ? -power_of(254 - e) : power_of(254 - e);
+      auto scaled = [&](uint32_t w) { return pack_f16(lo_bf16(w) * up, hi_bf16(w) * up); };
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i) {   // (read by this lane alone)
+        s_q[warp][nt][2 * i][lane] = make_uint2(scaled(qv[nt][i].x), scaled(qv[nt][i].y));
+        s_q[warp][nt][2 * i + 1][lane] = make_uint2(scaled(qv[nt][i].z), scaled(qv[nt][i].w));
+      }
+    }
+    auto query_of = [&](int nt, int step) { return s_q[warp][nt][step][lane]; };
+
+    // o: dims gid-rows of a tile, query rows 2 c and 2 c + 1; nm: the lift less the running maximum
+    float o[NT][MT][4], nm[NT][2], l[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int i = 0; i < MT; ++i) o[nt][i][0] = o[nt][i][1] = o[nt][i][2] = o[nt][i][3] = 0.f;
+      nm[nt][0] = nm[nt][1] = INFINITY;
+      l[nt][0] = l[nt][1] = 0.f;
+    }
+    uint32_t poison_row = 0;    // bit 2 nt + h: of row 2 c + h of tile nt
+    int ek = 127, ev = 0, ev_top = 0;   // exponent bytes that keys' and values' powers are relative to (ev: none yet)
+    float kp = 1.f;                      // 2^(ek - 127)
+    auto scale_outputs = [&](float f) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) o[nt][i][k] *= f;
+    };
+
+    // The softmax step of a block or two for a tile: scores f * s in units of log2 (tokens token_of(gid) and two on, rows 2 c and 2 c + 1:
+    // s[.][0], s[.][1] and s[.][2], s[.][3]) become P^T as operands, the running maximum, sum and output following.  The maximum moves
+    // only when a score passes it by more than a margin.  The weights are rounded to fp16 or bf16, the values' type: their sum
+    // is not.  (some: every row sees one of the block's keys, or one before)
+    auto softmax = [&](int nt, const auto& s, float f0, float f1, auto& p, bool fp16, bool some_key) {
+      constexpr int kN = sizeof(s) / 16;   // blocks
+      float mx[2] = {fmaxf(s[0][0], s[0][2]), fmaxf(s[0][1], s[0][3])};
+#pragma unroll
+      for (int x = 1; x < kN; ++x) {
+        mx[0] = fmaxf(mx[0], fmaxf(s[x][0], s[x][2]));
+        mx[1] = fmaxf(mx[1], fmaxf(s[x][1], s[x][3]));
+      }
+      mx[0] *= f0;
+      mx[1] *= f1;
+      if (__any_sync(0xffffffffu, mx[0] + nm[nt][0] > kLift + kMargin || mx[1] + nm[nt][1] > kLift + kMargin)) {
+        float al[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          float x = mx[h];
+#pragma unroll
+          for (int d = 4; d < 32; d <<= 1) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, d));
+          const float to = fminf(nm[nt][h], kLift - x);
+          al[h] = to == nm[nt][h] ? 1.f : ex2_ftz(to - nm[nt][h]);
+          nm[nt][h] = to;
+          l[nt][h] *= al[h];
+        }
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          o[nt][i][0] *= al[0];
+          o[nt][i][1] *= al[1];
+          o[nt][i][2] *= al[0];
+          o[nt][i][3] *= al[1];
+        }
+      }
+      const float n0 = some_key || nm[nt][0] < INFINITY ? nm[nt][0] : 0.f, n1 = some_key || nm[nt][1] < INFINITY ? nm[nt][1] : 0.f;
+#pragma unroll
+      for (int x = 0; x < kN; ++x) {
+        const float w[4] = {ex2_ftz(fmaf(s[x][0], f0, n0)), ex2_ftz(fmaf(s[x][1], f1, n1)), ex2_ftz(fmaf(s[x][2], f0, n0)),
+                            ex2_ftz(fmaf(s[x][3], f1, n1))};
+        l[nt][0] += w[0] + w[2];
+        l[nt][1] += w[1] + w[3];
+        p[x][0] = transposed(fp16 ? pack_f16(w[0], w[1]) : pack_bf16(w[0], w[1]));
+        p[x][1] = transposed(fp16 ? pack_f16(w[2], w[3]) : pack_bf16(w[2], w[3]));
+      }
+    };
+
+    // ---- the cache
+    // A page in the general form: the last one, or one whose powers leave the window.
+    auto general = [&](int at, int place) {
+      Loaded x;
+      read_keys(place, x);
+      read_values(place, x);
+      const int b = part.c0 + at;
+      const uint32_t ve = value_bytes(x);
       const int have = q.len - b * kTreePage;   // tokens of the page: 16 or more where it is full
-      poison = poison || !in_cache(page);
-      Loaded x = now;
-      if (b + kWarps < c_end) load(next, now);
-      uint32_t ve = value_bytes(x);
       uint32_t live = 0x3Fu;   // bits 0, 1: of this lane's key rows, 2 ..: of its value rows
       if (have < kTreePage) {
         live = 0u;
@@ -302,20 +351,9 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
 #pragma unroll
         for (int t = 0; t < 4; ++t) live |= (4 * c + t < have ? 4u : 0u) << t;
       }
-      // Powers relative to Ek and Ev: field - (E - 8) is in 0 .. 15 for all blocks, or the longer form looks what to do.
-      uint32_t kg[2], vg[4];
-#pragma unroll
-      for (int n = 0; n < 2; ++n) kg[n] = x.ke[n] - (ek - kBelow);
-#pragma unroll
-      for (int t = 0; t < 4; ++t) vg[t] = ((ve >> (8 * t)) & 255u) - (ev - kBelow);
       uint32_t kf[2], vf[2];   // factors as fp16 pairs: of a key row, of two tokens' values
-      bool wide = false;
-      if (!__any_sync(0xffffffffu, live != 0x3Fu || ((kg[0] | kg[1] | vg[0] | vg[1] | vg[2] | vg[3]) & ~15u) != 0u)) {
-#pragma unroll
-        for (int n = 0; n < 2; ++n) kf[n] = (kg[n] + 7u) * 0x04000400u;   // 2^(g - 8) in both halves
-#pragma unroll
-        for (int t = 0; t < 2; ++t) vf[t] = (vg[2 * t] + 7u) * 0x0400u + (vg[2 * t + 1] + 7u) * 0x04000000u;
-      } else {
+      bool wide = false;       // bf16 instead
+      {
         // the largest and least powers of rows within the length; blocks of the least power, 2^-127, count as nothing
         int k_most = 0, k_least = 255, v_most = 0, v_least = 255;
         bool nan = false;
@@ -336,10 +374,11 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
         auto fits = [](int most, int least, int e) { return most <= e + 7 && least >= e - kBelow; };
         wide = __any_sync(0xffffffffu, nan);   // (the longer products have a place for it)
         if (k_most > 0 && !fits(k_most, k_least, ek)) {
-          ek = k_least + kBelow;
+          ek = min(k_least + kBelow, kTop);
+          kp = power_of(ek);
           wide = wide || !fits(k_most, k_least, ek);
         }
-        if (v_most > 0 && !fits(v_most, v_least, ev)) {
+        if (v_most > 0 && (ev == 0 || !fits(v_most, v_least, ev))) {
           // Ev goes where they fit, but not further than 2^40 below the highest that it was (the outputs have to stay
           // finite); else to where the largest does
           const int top = max(ev_top, v_most - 7);
@@ -348,9 +387,9 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
             to = max(top, v_most > ev + 7 ? 0 : ev);
             wide = true;
           }
-          to = max(to, 64);   // (2^-63 and less: whatever is there loses nothing that counts)
+          to = min(max(to, 64), kTop);   // (2^-63 and less: whatever is there loses nothing that counts)
           wide = wide || !fits(v_most, v_least, to);
-          if (ev >= 0) scale_outputs(power_of(min(max(127 + ev - to, 0), 254)));
+          if (ev > 0) scale_outputs(power_of(min(max(127 + ev - to, 0), 254)));
           ev = to;
           ev_top = max(ev_top, ev);
         }
@@ -368,9 +407,9 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
         }
       }
       // scores
-      float s[NT][4];
+      float s[NT][1][4];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+      for (int nt = 0; nt < NT; ++nt) s[nt][0][0] = s[nt][0][1] = s[nt][0][2] = s[nt][0][3] = 0.f;
       if (!wide) {
 #pragma unroll
         for (int w = 0; w < kW; ++w) {
@@ -386,15 +425,14 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
           for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-              const uint2 f = sh.q[nt][2 * w + i][lane];
-              mma_f16(s[nt], h0[2 * i], h1[2 * i], h0[2 * i + 1], h1[2 * i + 1], f.x, f.y);
+              const uint2 f = query_of(nt, 2 * w + i);
+              mma_f16(s[nt][0], h0[2 * i], h1[2 * i], h0[2 * i + 1], h1[2 * i + 1], f.x, f.y);
             }
         }
-        const float kp = power_of(min(max(ek, 1), 254));
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) s[nt][i] *= rs[nt][i & 1] * kp;
+          for (int i = 0; i < 4; ++i) s[nt][0][i] *= rs[nt][i & 1] * kp;
       } else {
         const float k0 = row_factor(x.ke[0]), k1 = row_factor(x.ke[1]);
 #pragma unroll 1
@@ -416,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
           for (int i = 0; i < 4; ++i) {
 #pragma unroll
             for (int y = 0; y < NT; ++y)
-              if (y == nt) s[y][i] = t[i] * a.scale_log2;
+              if (y == nt) s[y][0][i] = t[i] * a.scale_log2;
           }
         }
       }
@@ -425,11 +463,11 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (!((live >> (i >> 1)) & 1u)) s[nt][i] = -INFINITY;
+            if (!((live >> (i >> 1)) & 1u)) s[nt][0][i] = -INFINITY;
       }
-      uint32_t p[NT][2];
+      uint32_t p[NT][1][2];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) softmax(nt, s[nt], p[nt], !wide);
+      for (int nt = 0; nt < NT; ++nt) softmax(nt, s[nt], 1.f, 1.f, p[nt], !wide, true);
       // the weights' product with the values: words lo and hi have the even and the odd dims' codes, two tokens' side by side
 #pragma unroll
       for (int w = 0; w < kVW; ++w) {
@@ -446,7 +484,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
             const uint32_t a0 = mul_f16x2(even[0][i], vf[0]), a1 = mul_f16x2(odd[0][i], vf[0]);
             const uint32_t a2 = mul_f16x2(even[1][i], vf[1]), a3 = mul_f16x2(odd[1][i], vf[1]);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][4 * w + i], a0, a1, a2, a3, p[nt][0], p[nt][1]);
+            for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][4 * w + i], a0, a1, a2, a3, p[nt][0][0], p[nt][0][1]);
           }
         } else {
           float f[4];
@@ -460,24 +498,119 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
             const uint32_t a0 = bf16_times(even[0][i], f[0], f[1]), a1 = bf16_times(odd[0][i], f[0], f[1]);
             const uint32_t a2 = bf16_times(even[1][i], f[2], f[3]), a3 = bf16_times(odd[1][i], f[2], f[3]);
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma_bf16_16816(o[nt][4 * w + i], a0, a1, a2, a3, p[nt][0], p[nt][1]);
+            for (int nt = 0; nt < NT; ++nt) mma_bf16_16816(o[nt][4 * w + i], a0, a1, a2, a3, p[nt][0][0], p[nt][0][1]);
           }
         }
       }
-      page = next;
-      next = after;
+    };
+    poison = poison || pages < mine;
+    auto scores = [&](const Loaded(&x)[P], const uint32_t(&kg)[P], float(&s)[P][NT][4]) {
+      uint32_t kf[P][2];   // factors as fp16 pairs, 2^(g - 8): of a key row
+#pragma unroll
+      for (int y = 0; y < P; ++y) {
+        kf[y][0] = __byte_perm(kg[y], 0, 0x0404) * 4u + 0x1C001C00u;
+        kf[y][1] = __byte_perm(kg[y], 0, 0x1414) * 4u + 0x1C001C00u;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) s[y][nt][0] = s[y][nt][1] = s[y][nt][2] = s[y][nt][3] = 0.f;
+      }
+#pragma unroll
+      for (int w = 0; w < kW; ++w) {
+        uint32_t h[P][2][4];
+#pragma unroll
+        for (int y = 0; y < P; ++y)
+#pragma unroll
+          for (int n = 0; n < 2; ++n) {
+            f16_of_e2m1(x[y].k[n][w], h[y][n]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h[y][n][i] = mul_f16x2(h[y][n][i], kf[y][n]);
+          }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            const uint2 f = query_of(nt, 2 * w + i);
+#pragma unroll
+            for (int y = 0; y < P; ++y)
+              mma_f16(s[y][nt], h[y][0][2 * i], h[y][1][2 * i], h[y][0][2 * i + 1], h[y][1][2 * i + 1], f.x, f.y);
+          }
+      }
+    };
+    // The weights' product with the values: words have the even or the odd dims' codes, two tokens' side by side.
+    auto product = [&](int place, const uint32_t(&vg)[P], const uint32_t(&w2)[NT][P][2]) {
+#pragma unroll
+      for (int y = 0; y < P; ++y) {
+        Loaded x;
+        read_values(place + y * S::kBytes, x);
+        const uint32_t vf[2] = {__byte_perm(vg[y], 0, 0x1404) * 4u + 0x1C001C00u, __byte_perm(vg[y], 0, 0x3424) * 4u + 0x1C001C00u};
+#pragma unroll
+        for (int w = 0; w < kVW; ++w) {
+          uint32_t even[2][4], odd[2][4];
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            const uint32_t x0 = x.v[2 * t][w], x1 = x.v[2 * t + 1][w];
+            f16_of_e2m1((x0 & 0x0F0F0F0Fu) | ((x1 << 4) & 0xF0F0F0F0u), even[t]);
+            f16_of_e2m1(((x0 >> 4) & 0x0F0F0F0Fu) | (x1 & 0xF0F0F0F0u), odd[t]);
+          }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t a0 = mul_f16x2(even[0][i], vf[0]), a1 = mul_f16x2(odd[0][i], vf[0]);
+            const uint32_t a2 = mul_f16x2(even[1][i], vf[1]), a3 = mul_f16x2(odd[1][i], vf[1]);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][4 * w + i], a0, a1, a2, a3, w2[nt][y][0], w2[nt][y][1]);
+          }
+        }
+      }
+    };
+    for (int at = 0, place = 0; at < pages; at += P) {
+      copies_wait<kRing / P - 1>();
+      __syncwarp();
+      // powers relative to Ek and Ev, a byte each: field - (E - 8) is in 0 .. 15 for all blocks (one below it borrows)
+      Loaded now[P];
+      uint32_t kg[P], vg[P], out = 0;
+#pragma unroll
+      for (int x = 0; x < P; ++x) {   // (pages that are not there: whatever lies in the ring)
+        read_keys(place + x * S::kBytes, now[x]);
+        kg[x] = (now[x].ke[0] | now[x].ke[1] << 8) - static_cast<uint32_t>(ek - kBelow) * 0x0101u;
+        vg[x] = value_bytes(now[x]) - static_cast<uint32_t>(ev - kBelow) * 0x01010101u;
+        out |= (kg[x] & ~0x0F0Fu) | (vg[x] & 0xF0F0F0F0u);
+      }
+      const bool full = at + P <= pages && q.len - (part.c0 + at + P - 1) * kTreePage >= kTreePage && ev != 0;
+      if (__any_sync(0xffffffffu, out != 0u) || !full) {
+#pragma unroll 1
+        for (int x = 0; x < min(pages - at, P); ++x) general(at + x, place + x * S::kBytes);
+      } else {
+        float s[P][NT][4];
+        scores(now, kg, s);
+        uint32_t p[NT][P][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+          float y[P][4];
+#pragma unroll
+          for (int x = 0; x < P; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[x][i] = s[x][nt][i];
+          softmax(nt, y, rs[nt][0] * kp, rs[nt][1] * kp, p[nt], true, true);
+        }
+        product(place, vg, p);
+      }
+      __syncwarp();   // the places have been read
+#pragma unroll
+      for (int x = 0; x < P; ++x) fetch(at + kRing + x, place + x * S::kBytes);
+      copies_end();
+      place = place == (kRing - P) * S::kBytes ? 0 : place + P * S::kBytes;
     }
+    copies_wait<0>();
 
-    // ---- drafted tokens: bf16 rows of their own tensors, whatever the cache holds (b is the warp's next block after the cache)
-    if (ev < 0) ev = 127;
+    // ---- drafted tokens: bf16 rows of their own tensors, whatever the cache holds
+    if (ev == 0) ev = 127;
     const float rel = power_of(254 - ev);   // what the outputs are kept in, over the values' own
-    for (; b < part.c1; b += kWarps) {
+    for (int b = part.c0 + mine; b < part.c1; ++b) {
       const int j0 = (b - q.cached_blocks) * kTreePage, have = q.drafts - j0;
       const __nv_bfloat16* kd = static_cast<const __nv_bfloat16*>(a.t.k) + (q.start + static_cast<int64_t>(j0)) * a.t.k_token + g * a.t.k_head;
       const __nv_bfloat16* vd = static_cast<const __nv_bfloat16*>(a.t.v) + (q.start + static_cast<int64_t>(j0)) * a.t.v_token + g * a.t.v_head;
-      float s[NT][4];
+      float s[NT][1][4];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+      for (int nt = 0; nt < NT; ++nt) s[nt][0][0] = s[nt][0][1] = s[nt][0][2] = s[nt][0][3] = 0.f;
 #pragma unroll 1
       for (int w = 0; w < HD / 32; ++w) {   // two steps
         uint4 x[2];
@@ -490,8 +623,8 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
         for (int nt = 0; nt < NT; ++nt) {
           const uint4* src = query(nt);
           const uint4 f = src ? __ldg(src + w) : make_uint4(0u, 0u, 0u, 0u);
-          mma_bf16_16816(s[nt], x[0].x, x[1].x, x[0].y, x[1].y, f.x, f.y);
-          mma_bf16_16816(s[nt], x[0].z, x[1].z, x[0].w, x[1].w, f.z, f.w);
+          mma_bf16_16816(s[nt][0], x[0].x, x[1].x, x[0].y, x[1].y, f.x, f.y);
+          mma_bf16_16816(s[nt][0], x[0].z, x[1].z, x[0].w, x[1].w, f.z, f.w);
         }
       }
       constexpr int kD = HD / 64;   // 16-byte pieces of a lane's dims of a value row
@@ -515,7 +648,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
           for (int d = 0; d < kD; ++d) v[t][d] = make_uint4(0u, 0u, 0u, 0u);
         }
       }
-      uint32_t p[NT][2];
+      uint32_t p[NT][1][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -525,9 +658,9 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
           if (sees & bad) poison_row |= 1u << (2 * nt + h);
 #pragma unroll
           for (int n = 0; n < 2; ++n)
-            s[nt][2 * n + h] = (sees >> (token_of(gid) + 2 * n)) & 1u ? s[nt][2 * n + h] * a.scale_log2 : -INFINITY;
+            s[nt][0][2 * n + h] = (sees >> (token_of(gid) + 2 * n)) & 1u ? s[nt][0][2 * n + h] * a.scale_log2 : -INFINITY;
         }
-        softmax(nt, s[nt], p[nt], false);
+        softmax(nt, s[nt], 1.f, 1.f, p[nt], false, false);
       }
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
@@ -542,80 +675,150 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           float t[4] = {0.f, 0.f, 0.f, 0.f};
-          mma_bf16_16816(t, x[0], x[1], x[2], x[3], p[nt][0], p[nt][1]);
+          mma_bf16_16816(t, x[0], x[1], x[2], x[3], p[nt][0][0], p[nt][0][1]);
 #pragma unroll
           for (int k = 0; k < 4; ++k) o[nt][i][k] += t[k] * rel;
         }
       }
     }
 
-    // ---- the part's end: the four warps' states meet, 8 rows at a time
+    // ---- the part's end
     const float down = power_of(ev);   // 1 / rel
+    const bool lost = __any_sync(0xffffffffu, poison);
+    const bool whole = part.whole();
+    // partial results: [row][dim]
+    const int64_t slot = me == shares.owner(part.place(0)) ? 2 * me + 1 : 2 * me;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      if (row0 + 8 * nt >= rows) break;   // (the same for all threads)
-      __syncthreads();   // the queries (or the last 8 rows) have been read
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         float sum = l[nt][h];
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if (poison || (poison_row >> (2 * nt + h)) & 1u) sum = NAN;
-        if (gid == 0) {
-          s_m[warp][2 * c + h] = m[nt][h];
-          s_l[warp][2 * c + h] = sum;
+        if (lost || (poison_row >> (2 * nt + h)) & 1u) sum = NAN;
+        const int slot_row = 8 * nt + 2 * c + h, r = row0 + slot_row;
+        if (r >= rows) continue;
+        float y[2 * MT];   // this lane's HD / 8 dims
+        const float f = whole ? (sum == 0.f ? 0.f : down / sum) : down;   // a row that saw nothing: zeros; NaN stays
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+          y[2 * i] = o[nt][i][h] * f;
+          y[2 * i + 1] = o[nt][i][2 + h] * f;
+        }
+        if (whole) {
+          const int tok = tree_token(a, r);
+          __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.t.out) + (q.start + static_cast<int64_t>(tok)) * a.t.out_token +
+                               (g * a.group + r - tok * a.group) * a.t.out_head + gid * (HD / 8);
+#pragma unroll
+          for (int i = 0; i < 2 * MT; i += 8)
+            *reinterpret_cast<uint4*>(dst + i) = make_uint4(pack_bf16(y[i], y[i + 1]), pack_bf16(y[i + 2], y[i + 3]),
+                                                            pack_bf16(y[i + 4], y[i + 5]), pack_bf16(y[i + 6], y[i + 7]));
+        } else {
+          float* dst = a.part_o + (slot * G::kSlotRows + slot_row) * HD + gid * (HD / 8);
+#pragma unroll
+          for (int i = 0; i < 2 * MT; i += 4) *reinterpret_cast<float4*>(dst + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+          if (gid == 0) a.part_ml[slot * G::kSlotRows + slot_row] = make_float2(-nm[nt][h], sum);
         }
       }
+    }
+    __syncwarp();
+  }
+}
+
+// Joins the partial results of pairs that several warps shared, eight rows and 32 dims of a pair a CTA: launched beside the
+// attention kernel's end, it waits for it; each warp takes every fourth part, in order, and the four states meet in shared
+// memory, so the result does not depend on who was last.  A lane has 8 dims of a row, and four parts' loads in flight.
+constexpr int kJoinAhead = 4, kJoinDims = 32;
+template <int HD, int NT>
+__global__ void __launch_bounds__(kThreads) tree_e2m1_join_kernel(const __grid_constant__ TreeLaunch a, int groups) {
+  using G = TreeE2m1<NT>;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, d0 = blockIdx.y * kJoinDims + (lane & 3) * 8;
+  const int group = blockIdx.x % groups, head = blockIdx.x / groups, g = head % a.n_kv, s = head / a.n_kv;
+  const TreeSeq q = tree_seq<G::ROWS, G::BLOCK>(a, s);
+  const int rows = q.drafts * a.group, row = 8 * group + r, tp = 8 * group / G::kSlotRows, slot_row = row - tp * G::kSlotRows;
+  grid_dep_wait();   // no launch of this kernel ends before the attention kernel
+  if (8 * group >= rows) return;
+  const int32_t off = __ldcg(a.line + s), total = __ldcg(a.line + a.n_seqs), ctas = __ldcg(a.line + a.n_seqs + 1);
+  const TreeShares shares(total, ctas, 1);
+  const int32_t first = off + (q.blocks + G::LEAD) * (g * q.tiles + tp) + G::LEAD;   // (a place is a block: weights of 1)
+  const int i0 = shares.owner(first), i1 = shares.owner(first + q.blocks - 1);
+  if (i0 == i1) return;   // whole: written by its warp
+  __shared__ float s_o[kWarps][32][9];
+  __shared__ float2 s_ml[kWarps][8];
+  float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, best = -INFINITY, sum = 0.f;
+#pragma unroll 1
+  for (int i = i0 + warp; i <= i1; i += kJoinAhead * kWarps) {
+    float4 v[kJoinAhead][2];
+    float2 ml[kJoinAhead];
 #pragma unroll
-      for (int i = 0; i < MT; ++i)   // dims 2 i and 2 i + 1 of this lane's HD / 8
+    for (int x = 0; x < kJoinAhead; ++x) {
+      const int part = min(i + x * kWarps, i1);
+      const int64_t at = (part == i0 ? 2 * i0 + 1 : 2 * part) * static_cast<int64_t>(G::kSlotRows) + slot_row;
+      ml[x] = __ldcg(a.part_ml + at);
+      v[x][0] = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * HD + d0));
+      v[x][1] = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * HD + d0) + 1);
+    }
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-          *reinterpret_cast<float2*>(&sh.o[warp][2 * c + h][gid * (HD / 8) + 2 * i]) = make_float2(o[nt][i][h] * down, o[nt][i][2 + h] * down);
-      __syncthreads();
-      constexpr int kPer = 8 * HD / kThreads;   // outputs of a thread: part of one row
-      const int r = threadIdx.x / 16, d0 = threadIdx.x % 16 * kPer;
-      float top = -INFINITY, sum = 0.f, acc[kPer];
+    for (int x = 0; x < kJoinAhead; ++x) {
+      if (i + x * kWarps > i1) break;
+      const float now = fmaxf(best, ml[x].x);   // -infinity: nothing seen so far (a sum of zero, or NaN)
+      const float f = best == -INFINITY ? 0.f : ex2_ftz(best - now), e = ml[x].x == -INFINITY ? 0.f : ex2_ftz(ml[x].x - now);
+      best = now;
+      sum = sum * f + ml[x].y * e;
+      const float y[8] = {v[x][0].x, v[x][0].y, v[x][0].z, v[x][0].w, v[x][1].x, v[x][1].y, v[x][1].z, v[x][1].w};
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_m[w][r]);
-#pragma unroll
-      for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWarps; ++w) {
-        const float f = s_m[w][r] == -INFINITY ? 0.f : ex2_ftz(s_m[w][r] - top);   // (NaN sums stay NaN)
-        sum += s_l[w][r] * f;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) acc[i] += sh.o[w][r][d0 + i] * f;
-      }
-      const int out_r = row0 + 8 * nt + r;
-      if (!part.whole()) {   // the pair goes on in other CTAs: [dim][row]
-        const int64_t slot = me == shares.owner(part.place(0)) ? 2 * me + 1 : 2 * me;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) a.part_o[(slot * HD + d0 + i) * G::kSlotRows + 8 * nt + r] = acc[i];
-        if (d0 == 0) a.part_ml[slot * G::kSlotRows + 8 * nt + r] = make_float2(top, sum);
-      } else if (out_r < rows) {
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row that saw nothing: zeros; NaN stays
-        const int tok = tree_token(a, out_r);
-        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.t.out) + (q.start + static_cast<int64_t>(tok)) * a.t.out_token +
-                             (g * a.group + out_r - tok * a.group) * a.t.out_head + d0;
-        uint32_t w[kPer / 2];
-#pragma unroll
-        for (int i = 0; i < kPer / 2; ++i) w[i] = pack_bf16(acc[2 * i] * inv, acc[2 * i + 1] * inv);
-        if constexpr (kPer == 8)
-          *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
-        else
-          *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-      }
+      for (int d = 0; d < 8; ++d) o[d] = o[d] * f + y[d] * e;
     }
   }
+#pragma unroll
+  for (int d = 0; d < 8; ++d) s_o[warp][lane][d] = o[d];
+  if ((lane & 3) == 0) s_ml[warp][r] = make_float2(best, sum);
+  __syncthreads();
+  if (warp > 0 || row >= rows) return;
+  float top = -INFINITY, all = 0.f, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_ml[w][r].x);
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) {
+    const float f = s_ml[w][r].x == -INFINITY ? 0.f : ex2_ftz(s_ml[w][r].x - top);   // (NaN sums stay NaN)
+    all += s_ml[w][r].y * f;
+#pragma unroll
+    for (int d = 0; d < 8; ++d) y[d] += s_o[w][lane][d] * f;
+  }
+  const float inv = all == 0.f ? 0.f : 1.f / all;
+  const int tok = tree_token(a, row);
+  __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.t.out) + (q.start + static_cast<int64_t>(tok)) * a.t.out_token +
+                       (g * a.group + row - tok * a.group) * a.t.out_head + d0;
+  *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv),
+                                              pack_bf16(y[4] * inv, y[5] * inv), pack_bf16(y[6] * inv, y[7] * inv));
+}
+
+template <int HD, int NT>
+cudaError_t launch_join(const TreeLaunch& a, cudaStream_t stream) {
+  const int groups = (a.t.max_drafts * a.group + 7) / 8;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(static_cast<int64_t>(a.n_seqs) * a.n_kv * groups), HD / kJoinDims);
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr;
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, tree_e2m1_join_kernel<HD, NT>, a, groups);
 }
 
 template <int HD, int NT>
 cudaError_t launch(const TreeLaunch& a, int ctas, cudaStream_t stream) {
+  cudaError_t e = cudaFuncSetAttribute(tree_e2m1_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes<HD>());
+  if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(ctas));
   cfg.blockDim = dim3(kThreads);
+  cfg.dynamicSmemBytes = ring_bytes<HD>();
   cfg.stream = stream;
-  return cudaLaunchKernelEx(&cfg, tree_e2m1_kernel<HD, NT>, a);
+  e = cudaLaunchKernelEx(&cfg, tree_e2m1_kernel<HD, NT>, a);
+  return e == cudaSuccess && !a.whole && a.n_seqs > 0 ? launch_join<HD, NT>(a, stream) : e;
 }
 
 }  // namespace
