@@ -732,7 +732,7 @@ KVPRM_API int kvprm_tree_attention_filled(const kvprm_cache* cache, const kvprm_
  * n_pages pages of page_bytes consecutive bytes, page p of layer l at base + l * layer_stride + p * page_stride
  * (bytes; all multiples of 16, base 16-byte aligned).  A cache of several layers is one such pool, its exponents are
  * another; layers that were allocated apart are pools of one layer each.  What a page holds does not matter. */
-enum { KVPRM_MAX_POOLS = 96 };
+enum { KVPRM_MAX_POOLS = 96, KVPRM_MAX_SEQS = 8192 };
 typedef struct {
   void* base;
   int64_t layer_stride, page_stride, page_bytes;
@@ -759,7 +759,7 @@ typedef struct {
  * beyond its block table keeps its references, and those that continue it get its length and no pages; an entry
  * outside the pool is taken over as it is.
  *  workspace    as for kvprm_tree_attention, of kvprm_fork_workspace() bytes for the same arguments
- * Errors: KVPRM_EINVAL (also for more than 2^24 sequences, or new tables of 2^30 pages together), KVPRM_ECAPACITY, KVPRM_ECUDA. */
+ * Errors: KVPRM_EINVAL (also for more than KVPRM_MAX_SEQS sequences, or new tables of 2^30 pages together), KVPRM_ECAPACITY, KVPRM_ECUDA. */
 typedef struct {
   const int32_t *refs, *block_table, *lens, *parents, *room;
   int32_t *refs_out, *table_out, *lens_out, *counts;

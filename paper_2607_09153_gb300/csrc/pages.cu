@@ -3,8 +3,8 @@
 //
 // Either is two launches.  The first works out tables, references and who is copied where: one cluster of CTAs, whose
 // barrier separates the steps, because each step needs what all threads found in the one before and the whole is a few
-// thousand to a few hundred thousand numbers.  The second copies pages, warp by warp in pieces of 4 KB, over all layers of
-// all pools; it is launched beside the first one's end and learns there how many there are.  Nothing is decided by who
+// thousand to a few hundred thousand numbers.  The second writes the tables and copies pages, warp by warp in pieces of 4 KB,
+// over all layers of all pools; it is launched beside the first one's end and learns there how many there are.  Nothing is decided by who
 // comes first: counts are sums, of several that want a page the lowest sequence has it, free pages go by their numbers.
 #include <cuda_runtime.h>
 
@@ -18,52 +18,15 @@ namespace kvprm {
 namespace {
 
 constexpr int kThreads = 1024, kCluster = 8;
-constexpr int kCopyCtas = 8;       // of an SM
-constexpr int kMost = 1 << 24;     // sequences, and pages of a block table
+constexpr int kCopyCtas = 4;       // of an SM
+constexpr int kMost = 1 << 24;     // pages of a block table
 constexpr int kPage = 16, kNobody = 0x7FFFFFFF;
 constexpr int kCopyThreads = 256, kCopyUnroll = 8, kPiece = 32 * 16 * kCopyUnroll;   // of a warp: 4 KB
-
-// ---------------------------------------------------------------- copying
-struct CopyLaunch {
-  kvprm_pool pool[KVPRM_MAX_POOLS];
-  int32_t first[KVPRM_MAX_POOLS + 1];   // pieces of a page of the pools before
-  int32_t n_pools;
-  const int32_t* count;                 // of pages to copy
-  const int2* pairs;                    // from, to
-};
-
-__global__ void __launch_bounds__(kCopyThreads) copy_kernel(const __grid_constant__ CopyLaunch a) {
-  grid_dep_wait();
-  const int lane = threadIdx.x & 31;
-  const int per_copy = a.first[a.n_pools];
-  const int64_t items = static_cast<int64_t>(__ldcg(a.count)) * per_copy;
-  const int64_t step = static_cast<int64_t>(gridDim.x) * (kCopyThreads / 32);
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * (kCopyThreads / 32) + (threadIdx.x >> 5); i < items; i += step) {
-    const int64_t j = i / per_copy;
-    int r = static_cast<int>(i - j * per_copy), k = 0;
-    while (r >= a.first[k + 1]) ++k;
-    r -= a.first[k];
-    const kvprm_pool& p = a.pool[k];
-    const int pieces = static_cast<int>((p.page_bytes + kPiece - 1) / kPiece), layer = r / pieces, piece = r - layer * pieces;
-    const int2 pair = __ldcg(a.pairs + j);
-    uint8_t* base = static_cast<uint8_t*>(p.base) + layer * p.layer_stride + static_cast<int64_t>(piece) * kPiece + lane * 16;
-    if (pair.y < 0) continue;   // no page was free
-    const uint8_t* src = base + pair.x * p.page_stride;
-    uint8_t* dst = base + pair.y * p.page_stride;
-    const int64_t left = p.page_bytes - static_cast<int64_t>(piece) * kPiece - lane * 16;   // bytes from this lane's first on
-    uint4 v[kCopyUnroll];
-#pragma unroll
-    for (int x = 0; x < kCopyUnroll; ++x)
-      if (x * 512 < left) v[x] = __ldcs(reinterpret_cast<const uint4*>(src + x * 512));
-#pragma unroll
-    for (int x = 0; x < kCopyUnroll; ++x)
-      if (x * 512 < left) *reinterpret_cast<uint4*>(dst + x * 512) = v[x];
-  }
-}
 
 // ---------------------------------------------------------------- a cluster's steps
 __device__ __forceinline__ int cluster_thread() { return static_cast<int>(cluster_rank()) * kThreads + threadIdx.x; }
 constexpr int kAll = kCluster * kThreads;
+static_assert(kAll == KVPRM_MAX_SEQS, "a thread for each new sequence");
 
 // All threads of the cluster meet, and see what any of them has written.
 __device__ __forceinline__ void step() {
@@ -81,18 +44,6 @@ __device__ __forceinline__ void tell(uint64_t* told, uint64_t value) {   // told
   }
 }
 
-// The sum of a value over the CTA's threads; in all of them.
-__device__ __forceinline__ uint64_t cta_sum(uint64_t v, uint64_t* s_warp) {
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
-  __syncthreads();   // (the last use's sums have been read)
-  if ((threadIdx.x & 31) == 0) s_warp[threadIdx.x >> 5] = v;
-  __syncthreads();
-  uint64_t sum = s_warp[threadIdx.x & 31];
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-  return sum;
-}
 // The sum over the CTA's threads before this one; *total over all.
 __device__ __forceinline__ uint64_t cta_before(uint64_t v, uint64_t* s_warp, uint64_t* total) {
   const int lane = threadIdx.x & 31;
@@ -102,21 +53,22 @@ __device__ __forceinline__ uint64_t cta_before(uint64_t v, uint64_t* s_warp, uin
     const uint64_t up = __shfl_up_sync(0xffffffffu, scan, d);
     if (lane >= d) scan += up;
   }
-  __syncthreads();
+  __syncthreads();   // (the last use's sums have been read)
   if (lane == 31) s_warp[threadIdx.x >> 5] = scan;
   __syncthreads();
-  uint64_t sum = s_warp[lane], before = lane < static_cast<int>(threadIdx.x >> 5) ? sum : 0;
+  uint64_t sum = s_warp[lane];   // one of each of the 32 warps
+  const uint64_t own = sum;
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) {
-    sum += __shfl_xor_sync(0xffffffffu, sum, d);
-    before += __shfl_xor_sync(0xffffffffu, before, d);
+  for (int d = 1; d < 32; d <<= 1) {
+    const uint64_t up = __shfl_up_sync(0xffffffffu, sum, d);
+    if (lane >= d) sum += up;
   }
-  *total = sum;
-  return before + scan - v;
+  const int warp = threadIdx.x >> 5;
+  *total = __shfl_sync(0xffffffffu, sum, 31);
+  return __shfl_sync(0xffffffffu, sum - own, warp) + scan - v;
 }
 
-// Indices 0 .. n - 1 are shared out as one range a CTA.  sum_of tells the cluster what a CTA's range comes to; after its
-// barrier, each_before calls f(index, value, sum of all values before it), and returns the sum of all.
+// Indices 0 .. n - 1 are shared out as one range a CTA.
 struct Range {
   int lo, hi;
   __device__ __forceinline__ explicit Range(int n) {
@@ -124,27 +76,12 @@ struct Range {
     lo = min(n, per * static_cast<int>(cluster_rank()));
     hi = min(n, lo + per);
   }
+  __device__ __forceinline__ int mine() const { return lo + threadIdx.x < hi ? lo + static_cast<int>(threadIdx.x) : -1; }
 };
-template <typename V>
-__device__ __forceinline__ void sum_of(int n, V value, uint64_t* told, uint64_t* s_warp) {
-  const Range r(n);
+__device__ __forceinline__ uint64_t told_before(const uint64_t* told) {
   uint64_t sum = 0;
-  for (int i = r.lo + threadIdx.x; i < r.hi; i += kThreads) sum += value(i);
-  sum = cta_sum(sum, s_warp);
-  if (threadIdx.x == 0) tell(told, sum);
-}
-template <typename V, typename F>
-__device__ __forceinline__ void each_before(int n, V value, F f, const uint64_t* told, uint64_t* s_warp) {
-  const Range r(n);
-  uint64_t carry = 0, total;
-  for (uint32_t i = 0; i < cluster_rank(); ++i) carry += told[i];
-  for (int i0 = r.lo; i0 < r.hi; i0 += kThreads) {
-    const int i = i0 + threadIdx.x;
-    const uint64_t v = i < r.hi ? value(i) : 0;
-    const uint64_t before = cta_before(v, s_warp, &total);
-    if (i < r.hi) f(i, v, carry + before);
-    carry += total;
-  }
+  for (uint32_t i = 0; i < cluster_rank(); ++i) sum += told[i];
+  return sum;
 }
 __device__ __forceinline__ uint64_t sum_told(const uint64_t* told) {
   uint64_t sum = 0;
@@ -152,22 +89,26 @@ __device__ __forceinline__ uint64_t sum_told(const uint64_t* told) {
   return sum;
 }
 
-// Calls f(row, begin, end, lane) for each row of a table in segments of 512 entries, a warp each.
+// Calls f(row, begin, end, lane) for each row of a table in segments of 128 entries, for warp `warp` of `warps`.
 template <typename F>
-__device__ __forceinline__ void each_segment(int rows, int width, F f) {
-  constexpr int kSegment = 512;
+__device__ __forceinline__ void each_segment(int rows, int width, int64_t warp, int64_t warps, F f) {
+  constexpr int kSegment = 128;
   const int per_row = (width + kSegment - 1) / kSegment, lane = threadIdx.x & 31;
-  for (int64_t i = cluster_thread() >> 5; i < static_cast<int64_t>(rows) * per_row; i += kAll / 32) {
+  for (int64_t i = warp; i < static_cast<int64_t>(rows) * per_row; i += warps) {
     const int row = static_cast<int>(i / per_row), begin = static_cast<int>(i - static_cast<int64_t>(row) * per_row) * kSegment;
     f(row, begin, min(width, begin + kSegment), lane);
   }
 }
 
 // ---------------------------------------------------------------- fork
-constexpr int32_t kCopied = 1 << 30;   // beside a sequence's place among the free pages: the first is its copy's
+// A new sequence's row, as the last step writes it: its parent (-1: none), pages taken over, pages in all, its place among the
+// free pages (kCopied: the first of them is its last page's copy).
+constexpr int32_t kCopied = 1 << 30;
 struct ForkLaunch {
   kvprm_fork f;
-  int32_t *children, *first, *free_pages, *at, *count;   // scratch
+  int32_t *first, *free_pages, *count;   // scratch; first: who is the first of the new sequences to end inside a page;
+                                         // count: copies, and pages that are free before any is given away
+  int4* rows;
   int2* pairs;
 };
 
@@ -184,62 +125,65 @@ struct Held {
 
 // What a new sequence takes over and wants.
 struct Heir {
-  int32_t parent, len, pages, full, last, end;   // last: the page that it ends inside, -1: none; end: pages that it is to have
-  int64_t lacking;                               // pages beyond its table's width
+  int32_t parent = -1, len = 0, pages = 0, last = -1, end = 0;   // last: the page that it ends inside; end: pages that it is to have
+  int64_t lacking = 0;                                           // pages beyond its table's width
   __device__ __forceinline__ Heir(const kvprm_fork& f, int i) {
+    if (i < 0) return;
     parent = __ldg(f.parents + i);
+    const int64_t room = f.room ? max(0, __ldg(f.room + i)) : 0;
     if (parent < 0 || parent >= f.n_seqs) parent = -1;
-    len = pages = full = 0;
-    last = -1;
     bool bad = false;
     if (parent >= 0) {
       const Held h(f, parent);
       len = h.len;
       bad = h.pages == 0 && h.len != 0;
       pages = min(h.pages, f.width);
-      full = h.full;
-      if (full < pages) {
-        last = __ldg(f.block_table + static_cast<int64_t>(parent) * f.max_blocks + full);
+      if (h.full < pages) {
+        last = __ldg(f.block_table + static_cast<int64_t>(parent) * f.max_blocks + h.full);
         if (last < 0 || last >= f.n_pages) last = -1;
       }
     }
-    const int64_t room = f.room ? max(0, __ldg(f.room + i)) : 0;
     const int64_t want = bad ? 0 : (len + room + kPage - 1) / kPage;
-    end = static_cast<int32_t>(min(want, static_cast<int64_t>(f.width)));
-    end = max(end, pages);
-    lacking = max(int64_t{0}, want - max(end, 0));
+    end = max(static_cast<int32_t>(min(want, static_cast<int64_t>(f.width))), pages);
+    lacking = max(int64_t{0}, want - end);
   }
 };
 
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 1) fork_kernel(const __grid_constant__ ForkLaunch a) {
   __shared__ uint64_t s_warp[32], s_need[kCluster], s_free[kCluster], s_lacking[kCluster];
+  __shared__ int32_t s_heirs[KVPRM_MAX_SEQS];   // of each sequence: every CTA counts all
   const kvprm_fork& f = a.f;
   const int me = cluster_thread();
   const int n_pages = static_cast<int>(f.n_pages);
   grid_dep_launch();
+  // (what hangs on nothing is loaded first)
+  const int i = Range(f.n_new).mine();   // this thread's new sequence (there are no more of them than threads)
+  const int32_t refs0 = me < n_pages ? __ldg(f.refs + me) : 0, parent0 = static_cast<int>(threadIdx.x) < f.n_new ? __ldg(f.parents + threadIdx.x) : -1;
+  for (int s = threadIdx.x; s < f.n_seqs; s += kThreads) s_heirs[s] = 0;
+  const Heir h(f, i);
+  __syncthreads();
+  if (parent0 >= 0 && parent0 < f.n_seqs) atomicAdd(s_heirs + parent0, 1);
+  for (int j = threadIdx.x + kThreads; j < f.n_new; j += kThreads) {
+    const int parent = __ldg(f.parents + j);
+    if (parent >= 0 && parent < f.n_seqs) atomicAdd(s_heirs + parent, 1);
+  }
   for (int p = me; p < n_pages; p += kAll) {
-    f.refs_out[p] = __ldg(f.refs + p);
+    f.refs_out[p] = p == me ? refs0 : __ldg(f.refs + p);
     a.first[p] = kNobody;
   }
-  for (int s = me; s < f.n_seqs; s += kAll) a.children[s] = 0;
   step();
 
-  // how many continue a sequence, and of those that end inside a page the first
-  for (int i = me; i < f.n_new; i += kAll) {
-    const Heir h(f, i);
-    if (h.parent >= 0) atomicAdd(a.children + h.parent, 1);
-    if (h.last >= 0) atomicMin(a.first + h.last, i);
-  }
-  step();
-
-  // full pages: one reference less, and one more for each that continues the sequence
-  each_segment(f.n_seqs, f.max_blocks, [&](int s, int begin, int end, int lane) {
-    const Held h(f, s);
-    const int heirs = __ldcg(a.children + s);
+  // full pages: one reference less, and one more for each that continues the sequence; of those that end inside a page the first
+  if (h.last >= 0) atomicMin(a.first + h.last, i);
+  each_segment(f.n_seqs, f.max_blocks, (threadIdx.x >> 5) * kCluster + cluster_rank(), kAll / 32, [&](int s, int begin, int end, int lane) {
+    const Held held(f, s);
+    const int heirs = s_heirs[s];
     const int32_t* row = f.block_table + static_cast<int64_t>(s) * f.max_blocks;
-    for (int b = begin + lane; b < min(end, h.pages); b += 32) {
+    const int stop = min(end, held.pages);
+#pragma unroll 4
+    for (int b = begin + lane; b < stop; b += 32) {
       const int32_t page = __ldg(row + b);
-      const int change = (b < h.full && b < f.width ? heirs : 0) - 1;
+      const int change = (b < held.full && b < f.width ? heirs : 0) - 1;
       if (page >= 0 && page < n_pages && change != 0) atomicAdd(f.refs_out + page, change);
     }
   });
@@ -247,88 +191,132 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 1) 
 
   // A page that ends inside is kept by the first who ends in it if nobody else holds it, and copied for the others; what
   // nobody holds or ends in is free.
-  auto copies = [&](int i, const Heir& h) { return h.last >= 0 && !(__ldcg(f.refs_out + h.last) <= 0 && __ldcg(a.first + h.last) == i); };
-  auto need = [&](int i) {   // pages; in the upper half, copies
-    const Heir h(f, i);
-    const bool copy = copies(i, h);
-    return static_cast<uint64_t>(h.end - h.pages + (copy ? 1 : 0)) | static_cast<uint64_t>(copy ? 1 : 0) << 32;
-  };
-  auto is_free = [&](int p) { return static_cast<uint64_t>(__ldcg(f.refs_out + p) <= 0 && __ldcg(a.first + p) == kNobody ? 1 : 0); };
-  sum_of(f.n_new, need, s_need, s_warp);
-  sum_of(n_pages, is_free, s_free, s_warp);
-  sum_of(f.n_new, [&](int i) { return static_cast<uint64_t>(Heir(f, i).lacking); }, s_lacking, s_warp);
+  const bool copied = h.last >= 0 && !(__ldcg(f.refs_out + h.last) <= 0 && __ldcg(a.first + h.last) == i);
+  auto is_free = [&](int p) { return p >= 0 && __ldcg(f.refs_out + p) <= 0 && __ldcg(a.first + p) == kNobody; };
+  const Range pages(n_pages);
+  const int p0 = pages.mine();
+  const bool free0 = is_free(p0);
+  // of a CTA's first 1,024 pages and its new sequences at once: free pages (11 bits), copies (11), pages wanted (31)
+  const uint64_t v = (static_cast<uint64_t>(free0) << 52) | (static_cast<uint64_t>(copied) << 40) |
+                     static_cast<uint64_t>(static_cast<uint32_t>(h.end - h.pages) + (copied ? 1u : 0u));
+  uint64_t total;
+  const uint64_t before = cta_before(v, s_warp, &total);
+  uint64_t frees = total >> 52;
+  for (int q = pages.lo + kThreads; q < pages.hi; q += kThreads) {
+    const int p = q + static_cast<int>(threadIdx.x);
+    frees += __syncthreads_count(is_free(p < pages.hi ? p : -1));
+  }
+  uint64_t lacking = 0;
+  if (__syncthreads_or(h.lacking > 0)) cta_before(h.lacking, s_warp, &lacking);
+  if (threadIdx.x == 0) {
+    tell(s_need, total & ((uint64_t{1} << 52) - 1));
+    tell(s_free, frees);
+    tell(s_lacking, lacking);
+  }
   step();
 
-  const uint64_t needed = sum_told(s_need);
-  const int64_t wanted = static_cast<int64_t>(needed & 0xFFFFFFFFu), have = static_cast<int64_t>(sum_told(s_free));
-  each_before(f.n_new, need, [&](int i, uint64_t v, uint64_t before) {
-    const Heir h(f, i);
-    a.at[i] = static_cast<int32_t>(before & 0xFFFFFFFFu) | (v >> 32 ? kCopied : 0);
-    if (v >> 32) a.pairs[before >> 32] = make_int2(h.last, static_cast<int32_t>(before & 0xFFFFFFFFu));
-    if (h.last >= 0 && (v >> 32) == 0) f.refs_out[h.last] = 1;   // kept
+  const uint64_t needed = sum_told(s_need), mask = (uint64_t{1} << 40) - 1;
+  const int64_t wanted = static_cast<int64_t>(needed & mask), have = static_cast<int64_t>(sum_told(s_free));
+  if (i >= 0) {
+    const uint64_t at = told_before(s_need) + (before & ((uint64_t{1} << 52) - 1));
+    const int32_t place = static_cast<int32_t>(at & mask);
+    a.rows[i] = make_int4(h.parent, h.pages, h.end, place | (copied ? kCopied : 0));
+    if (copied) a.pairs[at >> 40] = make_int2(h.last, place);
+    if (h.last >= 0 && !copied) f.refs_out[h.last] = 1;         // kept
     f.lens_out[i] = h.len;
-  }, s_need, s_warp);
-  each_before(n_pages, is_free, [&](int p, uint64_t v, uint64_t before) {
-    if (!v || static_cast<int64_t>(before) >= wanted) return;
-    a.free_pages[before] = p;
+  }
+  auto give = [&](int p, int64_t rank) {
+    if (rank >= wanted) return;
+    a.free_pages[rank] = p;
     f.refs_out[p] = 1;
-  }, s_free, s_warp);
+  };
+  int64_t rank = static_cast<int64_t>(told_before(s_free));
+  if (free0) give(p0, rank + static_cast<int64_t>(before >> 52));
+  rank += static_cast<int64_t>(total >> 52);
+  for (int q = pages.lo + kThreads; q < pages.hi; q += kThreads) {
+    const int p = q + static_cast<int>(threadIdx.x) < pages.hi ? q + static_cast<int>(threadIdx.x) : -1;
+    const bool free = is_free(p);
+    const int64_t at = rank + static_cast<int64_t>(cta_before(free ? 1 : 0, s_warp, &total));
+    if (free) give(p, at);
+    rank += static_cast<int64_t>(total);
+  }
   if (me == 0) {
     f.counts[0] = static_cast<int32_t>(max(int64_t{0}, have - wanted));
     f.counts[1] = static_cast<int32_t>(min(int64_t{kNobody}, max(int64_t{0}, wanted - have) + static_cast<int64_t>(sum_told(s_lacking))));
+    a.count[0] = static_cast<int>(needed >> 40);
+    a.count[1] = static_cast<int>(have);
   }
-  if (me == 0) *a.count = static_cast<int32_t>(needed >> 32);
-  step();
+}
 
-  auto given = [&](int64_t k) { return k < have ? __ldcg(a.free_pages + k) : -1; };
-  for (int j = me; j < static_cast<int>(needed >> 32); j += kAll) a.pairs[j].y = given(__ldcg(&a.pairs[j].y));
-  each_segment(f.n_new, f.width, [&](int i, int begin, int end, int lane) {
-    const Heir h(f, i);
-    const int32_t at = __ldcg(a.at + i), first = at & (kCopied - 1), more = first + (at & kCopied ? 1 : 0);
-    const int32_t* row = f.block_table + static_cast<int64_t>(h.parent < 0 ? 0 : h.parent) * f.max_blocks;
-    int32_t* out = f.table_out + static_cast<int64_t>(i) * f.width;
+// A new sequence's pages: those that it takes over, and its own.
+__device__ __forceinline__ void fork_tables(const ForkLaunch& a, int64_t warp, int64_t warps) {
+  const kvprm_fork& f = a.f;
+  const int32_t have = __ldcg(a.count + 1);
+  each_segment(f.n_new, f.width, warp, warps, [&](int r, int begin, int end, int lane) {
+    const int4 row = __ldcg(a.rows + r);
+    const int32_t first = row.w & (kCopied - 1), mine = row.y - (row.w & kCopied ? 1 : 0);
+    const int32_t* from = f.block_table + static_cast<int64_t>(max(row.x, 0)) * f.max_blocks;
+    int32_t* out = f.table_out + static_cast<int64_t>(r) * f.width;
+#pragma unroll 4
     for (int b = begin + lane; b < end; b += 32) {
-      int32_t page = -1;
-      if (b < h.pages)
-        page = b == h.full && (at & kCopied) ? given(first) : __ldg(row + b);
-      else if (b < h.end)
-        page = given(more + b - h.pages);
-      out[b] = page;
+      const int32_t k = first + b - mine;
+      out[b] = b < mine ? __ldg(from + b) : b < row.z && k < have ? __ldcg(a.free_pages + k) : -1;
     }
   });
+}
+// Where a copy goes: its place among the free pages; -1: there is none.
+__device__ __forceinline__ int32_t copy_to(const ForkLaunch& a, int32_t place) {
+  return place < __ldcg(a.count + 1) ? __ldcg(a.free_pages + place) : -1;
 }
 
 // ---------------------------------------------------------------- compact
 struct CompactLaunch {
   kvprm_compact f;
-  int32_t *low, *high, *count;   // scratch: free pages before the first `live`, pages in use behind them
+  int32_t *low, *high, *count;   // scratch: free pages before the first `live`, and pages in use by how many are before them
   int2* pairs;
 };
 
 __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 1) compact_kernel(const __grid_constant__ CompactLaunch a) {
-  __shared__ uint64_t s_warp[32], s_live[kCluster], s_below[kCluster];
+  __shared__ uint64_t s_warp[32], s_live[kCluster], s_below;
   const kvprm_compact& f = a.f;
   const int me = cluster_thread(), n_pages = static_cast<int>(f.n_pages);
   grid_dep_launch();
-  auto in_use = [&](int p) { return static_cast<uint64_t>(__ldg(f.refs + p) > 0 ? 1 : 0); };
-  sum_of(n_pages, in_use, s_live, s_warp);
+  const Range pages(n_pages);
+  const int p0 = pages.mine(), refs0 = p0 < 0 ? 0 : __ldg(f.refs + p0);
+  uint64_t total;
+  const uint64_t before = cta_before(refs0 > 0 ? 1 : 0, s_warp, &total);   // of the CTA's first 1,024 pages
+  uint64_t used = total;
+  for (int q = pages.lo + kThreads; q < pages.hi; q += kThreads) {
+    const int p = q + static_cast<int>(threadIdx.x);
+    used += __syncthreads_count(p < pages.hi && __ldg(f.refs + p) > 0);
+  }
+  if (threadIdx.x == 0) tell(s_live, used);
   step();
   const int live = static_cast<int>(sum_told(s_live));
   // of the first `live` pages, those in use: what is free among them are as many as are in use behind
-  sum_of(live, in_use, s_below, s_warp);
-  step();
-  const int below = static_cast<int>(sum_told(s_below)), moves = live - below;
-  each_before(n_pages, in_use, [&](int p, uint64_t used, uint64_t before) {
-    const int rank = static_cast<int>(before);   // pages in use before this one
-    if (p < live && !used) a.low[p - rank] = p;
-    if (p >= live && used) a.high[rank - below] = p;
-    if (p < live && used) f.refs_out[p] = __ldg(f.refs + p);
+  auto sort = [&](int p, int refs, int rank) {   // rank: pages in use before this one
+    if (p == live)
+      for (uint32_t r = 0; r < kCluster; ++r)
+        asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(cluster_addr(&s_below, r)), "l"(static_cast<uint64_t>(rank)) : "memory");
+    if (p < live && refs <= 0) a.low[p - rank] = p;
+    if (p >= live && refs > 0) a.high[rank] = p;
+    if (p < live && refs > 0) f.refs_out[p] = refs;
     if (p >= live) f.refs_out[p] = 0;
-    f.moved[p] = p < live && used ? p : -1;
-  }, s_live, s_warp);
+    f.moved[p] = p < live && refs > 0 ? p : -1;
+  };
+  int rank = static_cast<int>(told_before(s_live));
+  if (p0 >= 0) sort(p0, refs0, rank + static_cast<int>(before));
+  rank += static_cast<int>(total);
+  for (int q = pages.lo + kThreads; q < pages.hi; q += kThreads) {
+    const int p = q + static_cast<int>(threadIdx.x), refs = p < pages.hi ? __ldg(f.refs + p) : 0;
+    const uint64_t at = cta_before(refs > 0 ? 1 : 0, s_warp, &total);
+    if (p < pages.hi) sort(p, refs, rank + static_cast<int>(at));
+    rank += static_cast<int>(total);
+  }
   step();
+  const int below = live < n_pages ? static_cast<int>(s_below) : live, moves = live - below;
   for (int j = me; j < moves; j += kAll) {
-    const int from = __ldcg(a.high + j), to = __ldcg(a.low + j);
+    const int from = __ldcg(a.high + below + j), to = __ldcg(a.low + j);
     a.pairs[j] = make_int2(from, to);
     f.moved[from] = to;
     f.refs_out[to] = __ldg(f.refs + from);
@@ -338,20 +326,74 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 1) 
     f.counts[0] = live;
     f.counts[1] = moves;
   }
-  step();
-  each_segment(f.n_seqs, f.max_blocks, [&](int s, int begin, int end, int lane) {
+}
+
+__device__ __forceinline__ void compact_tables(const CompactLaunch& a, int64_t warp, int64_t warps) {
+  const kvprm_compact& f = a.f;
+  const int n_pages = static_cast<int>(f.n_pages);
+  each_segment(f.n_seqs, f.max_blocks, warp, warps, [&](int s, int begin, int end, int lane) {
     const int32_t len = __ldg(f.lens + s);
-    const int64_t pages = len < 0 || static_cast<int64_t>(len) > static_cast<int64_t>(kPage) * f.max_blocks ? 0 : (len + kPage - 1) / kPage;
+    const int64_t held = len < 0 || static_cast<int64_t>(len) > static_cast<int64_t>(kPage) * f.max_blocks ? 0 : (len + kPage - 1) / kPage;
+    const int64_t row = static_cast<int64_t>(s) * f.max_blocks;
+#pragma unroll 4
     for (int b = begin + lane; b < end; b += 32) {
-      const int64_t at = static_cast<int64_t>(s) * f.max_blocks + b;
       int32_t page = -1;
-      if (b < pages) {
-        page = __ldg(f.block_table + at);
+      if (b < held) {
+        page = __ldg(f.block_table + row + b);
         if (page >= 0 && page < n_pages) page = __ldcg(f.moved + page);
       }
-      f.table_out[at] = page;
+      f.table_out[row + b] = page;
     }
   });
+}
+
+// ---------------------------------------------------------------- copying
+struct CopyLaunch {
+  kvprm_pool pool[KVPRM_MAX_POOLS];
+  int32_t first[KVPRM_MAX_POOLS + 1];   // pieces of a page of the pools before
+  int32_t n_pools;
+};
+
+// T: ForkLaunch or CompactLaunch, whose tables are written first.
+__device__ __forceinline__ void tables(const ForkLaunch& t, int64_t warp, int64_t warps) { fork_tables(t, warp, warps); }
+__device__ __forceinline__ void tables(const CompactLaunch& t, int64_t warp, int64_t warps) { compact_tables(t, warp, warps); }
+__device__ __forceinline__ int32_t copy_to(const CompactLaunch&, int32_t page) { return page; }
+
+// A fork's copies come of few pages, which stay in L2 (256 copies of 64 sequences' pages, 199 MB: 46 us, and 58 with loads that
+// leave L2 first); what a compaction moves is read once.
+__device__ __forceinline__ uint4 load_piece(const ForkLaunch&, const uint8_t* p) { return __ldcg(reinterpret_cast<const uint4*>(p)); }
+__device__ __forceinline__ uint4 load_piece(const CompactLaunch&, const uint8_t* p) { return __ldcs(reinterpret_cast<const uint4*>(p)); }
+
+template <typename T>
+__global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_kernel(const __grid_constant__ CopyLaunch a, const __grid_constant__ T t) {
+  const int lane = threadIdx.x & 31;
+  const int64_t warp = static_cast<int64_t>(threadIdx.x >> 5) * gridDim.x + blockIdx.x, warps = static_cast<int64_t>(gridDim.x) * (kCopyThreads / 32);
+  grid_dep_wait();
+  tables(t, warp, warps);
+  const int per_copy = a.first[a.n_pools];
+  const int64_t items = static_cast<int64_t>(__ldcg(t.count)) * per_copy;
+  for (int64_t i = static_cast<int64_t>(blockIdx.x) * (kCopyThreads / 32) + (threadIdx.x >> 5); i < items; i += warps) {
+    const int64_t j = i / per_copy;
+    int r = static_cast<int>(i - j * per_copy), k = 0;
+    while (r >= a.first[k + 1]) ++k;
+    r -= a.first[k];
+    const kvprm_pool& p = a.pool[k];
+    const int pieces = static_cast<int>((p.page_bytes + kPiece - 1) / kPiece), layer = r / pieces, piece = r - layer * pieces;
+    int2 pair = __ldcg(t.pairs + j);
+    pair.y = copy_to(t, pair.y);
+    uint8_t* base = static_cast<uint8_t*>(p.base) + layer * p.layer_stride + static_cast<int64_t>(piece) * kPiece + lane * 16;
+    if (pair.y < 0) continue;   // no page was free
+    const uint8_t* src = base + pair.x * p.page_stride;
+    uint8_t* dst = base + pair.y * p.page_stride;
+    const int64_t left = p.page_bytes - static_cast<int64_t>(piece) * kPiece - lane * 16;   // bytes from this lane's first on
+    uint4 v[kCopyUnroll];
+#pragma unroll
+    for (int x = 0; x < kCopyUnroll; ++x)
+      if (x * 512 < left) v[x] = load_piece(t, src + x * 512);
+#pragma unroll
+    for (int x = 0; x < kCopyUnroll; ++x)
+      if (x * 512 < left) __stcs(reinterpret_cast<uint4*>(dst + x * 512), v[x]);
+  }
 }
 
 // ---------------------------------------------------------------- host
@@ -388,8 +430,8 @@ int check_sizes(int64_t n_pages, int n_pools, int n_seqs, int max_blocks, int n_
     return operator_fail(KVPRM_EINVAL, "%s: n_pages %lld", who, static_cast<long long>(n_pages));
   if (n_seqs < 0 || max_blocks < 0 || n_new < 0 || width < 0)
     return operator_fail(KVPRM_EINVAL, "%s: n_seqs %d, max_blocks %d, n_new %d, width %d", who, n_seqs, max_blocks, n_new, width);
-  if (n_seqs > kMost || n_new > kMost || max_blocks > kMost || width > kMost)
-    return operator_fail(KVPRM_EINVAL, "%s: more than %d sequences, or block tables of more pages", who, kMost);
+  if (n_seqs > KVPRM_MAX_SEQS || n_new > KVPRM_MAX_SEQS || max_blocks > kMost || width > kMost)
+    return operator_fail(KVPRM_EINVAL, "%s: more than %d sequences, or block tables of more than %d pages", who, KVPRM_MAX_SEQS, kMost);
   if (static_cast<int64_t>(n_new) * width > 0x3FFFFFFF)   // pages that may be wanted: 30 bits, and one for the copy
     return operator_fail(KVPRM_EINVAL, "%s: %d block tables of %d pages", who, n_new, width);
   return KVPRM_OK;
@@ -415,16 +457,17 @@ int check_pools(const kvprm_pool* pools, int n, int64_t n_pages, CopyLaunch* c, 
   return KVPRM_OK;
 }
 
-// `most`: pages that may be copied.
-cudaError_t launch_copy(const CopyLaunch& c, int64_t most, cudaStream_t stream) {
-  const int64_t pieces = c.first[c.n_pools] * most;
-  if (pieces == 0) return cudaSuccess;
+// `most`: pages that may be copied; `entries`: of the tables.
+template <typename T>
+cudaError_t launch_copy(const CopyLaunch& c, const T& t, int64_t most, int64_t entries, cudaStream_t stream) {
+  const int64_t work = std::max(c.first[c.n_pools] * most, (entries + 127) / 128);   // of warps
+  if (work == 0) return cudaSuccess;
   int dev = 0, sms = 0;
   cudaError_t e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(std::min<int64_t>((pieces + kCopyThreads / 32 - 1) / (kCopyThreads / 32), int64_t{sms} * kCopyCtas)));
+  cfg.gridDim = dim3(static_cast<unsigned>(std::min<int64_t>((work + kCopyThreads / 32 - 1) / (kCopyThreads / 32), int64_t{sms} * kCopyCtas)));
   cfg.blockDim = dim3(kCopyThreads);
   cfg.stream = stream;
   cudaLaunchAttribute attr;
@@ -432,7 +475,7 @@ cudaError_t launch_copy(const CopyLaunch& c, int64_t most, cudaStream_t stream) 
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, copy_kernel, c);
+  return cudaLaunchKernelEx(&cfg, copy_kernel<T>, c, t);
 }
 
 template <typename K, typename A>
@@ -445,7 +488,7 @@ cudaError_t launch_cluster(K kernel, const A& a, cudaStream_t stream) {
 }
 
 int64_t fork_bytes(const kvprm_fork& f) {
-  return round_up(4 * int64_t{f.n_seqs}) + 2 * round_up(4 * f.n_pages) + 3 * round_up(4 * int64_t{f.n_new}) + 256;
+  return 256 + 2 * round_up(4 * f.n_pages) + round_up(16 * int64_t{f.n_new}) + round_up(8 * int64_t{f.n_new});
 }
 int64_t compact_bytes(const kvprm_compact& f) { return 4 * round_up(4 * f.n_pages) + 256; }
 
@@ -505,17 +548,14 @@ int kvprm_cache_fork(const kvprm_pool* pools, const kvprm_fork* f, void* workspa
   ForkLaunch a;
   a.f = *f;
   Scratch w{static_cast<uint8_t*>(workspace)};
-  a.count = w.take<int32_t>(1);
-  a.children = w.take<int32_t>(f->n_seqs);
+  a.count = w.take<int32_t>(2);
   a.first = w.take<int32_t>(f->n_pages);
   a.free_pages = w.take<int32_t>(f->n_pages);
-  a.at = w.take<int32_t>(f->n_new);
+  a.rows = w.take<int4>(f->n_new);
   a.pairs = w.take<int2>(f->n_new);
-  c.count = a.count;
-  c.pairs = a.pairs;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = launch_cluster(fork_kernel, a, st);
-  if (e == cudaSuccess) e = launch_copy(c, f->n_new, st);
+  if (e == cudaSuccess) e = launch_copy(c, a, f->n_new, int64_t{f->n_new} * f->width, st);
   return e == cudaSuccess ? KVPRM_OK : operator_fail(KVPRM_ECUDA, "%s: %s", who, cudaGetErrorString(e));
 }
 
@@ -544,11 +584,9 @@ int kvprm_cache_compact(const kvprm_pool* pools, const kvprm_compact* f, void* w
   a.low = w.take<int32_t>(f->n_pages);
   a.high = w.take<int32_t>(f->n_pages);
   a.pairs = w.take<int2>(f->n_pages);
-  c.count = a.count;
-  c.pairs = a.pairs;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e = launch_cluster(compact_kernel, a, st);
-  if (e == cudaSuccess) e = launch_copy(c, f->n_pages / 2, st);
+  if (e == cudaSuccess) e = launch_copy(c, a, f->n_pages / 2, int64_t{f->n_seqs} * f->max_blocks, st);
   return e == cudaSuccess ? KVPRM_OK : operator_fail(KVPRM_ECUDA, "%s: %s", who, cudaGetErrorString(e));
 }
 

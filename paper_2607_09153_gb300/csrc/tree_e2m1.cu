@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
   constexpr int kW = HD / 32;            // a lane's words of a key row, of eight codes
   constexpr int kVW = HD / 64;           // of each of its four value rows
   constexpr int kRowBytes = HD / 2, kBlocks = HD / 32;
-  constexpr int P = NT <= 2 ? 2 : 1;     // pages of a step
+  constexpr int P = 2;                   // pages of a step
   using S = Stage<HD>;
   extern __shared__ __align__(16) uint8_t s_ring[];
   __shared__ int32_t s_off[kTreeSeqs + 1];
@@ -115,9 +115,8 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
   const int me = blockIdx.x * kWarps + warp;
   tree_leave_line(a, s_off, shares.ctas);
   if (me >= shares.ctas) return;
-  const int64_t head_bytes = kTreePage * kRowBytes, page_bytes = 2 * a.n_kv * head_bytes;
-  constexpr int kHeadExp = kTreePage * kBlocks;
-  const int64_t page_exp = 2 * static_cast<int64_t>(a.n_kv) * kHeadExp;
+  constexpr uint32_t head_bytes = kTreePage * kRowBytes, kHeadExp = kTreePage * kBlocks;
+  const uint32_t page_bytes = 2 * a.n_kv * head_bytes, page_exp = 2 * a.n_kv * kHeadExp;   // (of 1,024 heads at most)
   // where this lane's pieces of a page go
   uint8_t* const my_ring = s_ring + warp * (kRing * S::kBytes);
   const uint32_t ring = smem_u32(my_ring);
@@ -136,7 +135,8 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
     const int g = part.g, row0 = part.tp * G::kSlotRows, rows = q.drafts * a.group;
     const int32_t* table = a.t.block_table + static_cast<int64_t>(a.seq0 + s_at) * a.t.max_blocks;
     const uint8_t* keys = a.pages + g * head_bytes + lane * 16;
-    const uint8_t* exps = a.exponents + g * kHeadExp + (lane < kHeadExp / 16 ? lane * 16 : a.n_kv * kHeadExp + lane * 16 - kHeadExp);
+    const uint8_t* values = keys + a.n_kv * head_bytes;
+    const uint8_t* exps = a.exponents + g * kHeadExp + (lane < static_cast<int>(kHeadExp / 16) ? lane * 16 : a.n_kv * kHeadExp + lane * 16 - kHeadExp);
     // the query rows' elements (HD / 4) c .. of row gid of tile nt
     auto query = [&](int nt) -> const uint4* {
       const int r = row0 + 8 * nt + gid;
@@ -159,22 +159,25 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
     };
     const int pages = a.n_pages > 0 ? mine : 0;   // (an empty pool: every page is outside it)
     int32_t ids = ids_of(0), ids_next = ids_of(32);
-    // page k into a place of the ring, if there is one
-    auto fetch = [&](int k, int place) {
-      if (k < pages) {
-        const int64_t page = __shfl_sync(0xffffffffu, ids, k & 31);
-        const uint32_t to = ring + place;
-        const uint8_t* src = keys + page * page_bytes;
+    // pages k .. into a step's places of the ring, as far as there are any (a step's are among the same 32)
+    auto fetch = [&](int k, uint32_t to) {
+#pragma unroll
+      for (int y = 0; y < P; ++y) {
+        if (k + y >= pages) break;
+        const uint32_t page = __shfl_sync(0xffffffffu, ids, (k + y) & 31);
+        const uint8_t* from_k = keys + static_cast<uint64_t>(page) * page_bytes;
+        const uint8_t* from_v = values + static_cast<uint64_t>(page) * page_bytes;
 #pragma unroll
         for (int x = 0; x < S::kHead / 512; ++x) {
-          copy16(to + k_at + x * k_step, src + x * 512);
-          copy16(to + v_at + x * v_step, src + a.n_kv * head_bytes + x * 512);
+          copy16(to + y * S::kBytes + k_at + x * k_step, from_k + x * 512);
+          copy16(to + y * S::kBytes + v_at + x * v_step, from_v + x * 512);
         }
-        if (lane < 2 * S::kExp / 16) copy16(to + S::kKe + lane * 16, exps + page * page_exp);
-        if ((k & 31) == 31) {
-          ids = ids_next;
-          ids_next = ids_of(k + 33);
-        }
+        if (lane < 2 * S::kExp / 16) copy16(to + y * S::kBytes + S::kKe + lane * 16, exps + static_cast<uint64_t>(page) * page_exp);
+      }
+      copies_end();
+      if ((k & 31) == 32 - P) {
+        ids = ids_next;
+        ids_next = ids_of(k + 32 + P);
       }
     };
     struct Loaded {
@@ -235,10 +238,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
       for (int i = 0; i < HD / 32; ++i) qv[nt][i] = src ? __ldg(src + i) : make_uint4(0u, 0u, 0u, 0u);
     }
 #pragma unroll
-    for (int k = 0; k < kRing; ++k) {
-      fetch(k, k * S::kBytes);
-      if (k % P == P - 1) copies_end();
-    }
+    for (int k = 0; k < kRing; k += P) fetch(k, ring + k * S::kBytes);
 
     // ---- the queries, scaled; a negative scale turns their signs
     float rs[NT][2];   // of rows 2 c and 2 c + 1: the row's power of two times the scores' scale
@@ -561,6 +561,8 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
         }
       }
     };
+    const int full = min(pages, q.len / kTreePage - part.c0);   // pages without places beyond the length
+    int plain = 0;                                              // of these, those that the short form may take
     for (int at = 0, place = 0; at < pages; at += P) {
       copies_wait<kRing / P - 1>();
       __syncwarp();
@@ -574,10 +576,10 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
         vg[x] = value_bytes(now[x]) - static_cast<uint32_t>(ev - kBelow) * 0x01010101u;
         out |= (kg[x] & ~0x0F0Fu) | (vg[x] & 0xF0F0F0F0u);
       }
-      const bool full = at + P <= pages && q.len - (part.c0 + at + P - 1) * kTreePage >= kTreePage && ev != 0;
-      if (__any_sync(0xffffffffu, out != 0u) || !full) {
+      if (__any_sync(0xffffffffu, out != 0u) || at + P > plain) {
 #pragma unroll 1
         for (int x = 0; x < min(pages - at, P); ++x) general(at + x, place + x * S::kBytes);
+        plain = ev != 0 ? full : 0;
       } else {
         float s[P][NT][4];
         scores(now, kg, s);
@@ -594,9 +596,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
         product(place, vg, p);
       }
       __syncwarp();   // the places have been read
-#pragma unroll
-      for (int x = 0; x < P; ++x) fetch(at + kRing + x, place + x * S::kBytes);
-      copies_end();
+      fetch(at + kRing, ring + place);
       place = place == (kRing - P) * S::kBytes ? 0 : place + P * S::kBytes;
     }
     copies_wait<0>();
