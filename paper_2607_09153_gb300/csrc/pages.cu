@@ -348,11 +348,14 @@ __device__ __forceinline__ void compact_tables(const CompactLaunch& a, int64_t w
 }
 
 // ---------------------------------------------------------------- copying
+// N: room for pools; a launch with arguments of 4 KB takes the host two microseconds more than one with four pools.
+template <int N>
 struct CopyLaunch {
-  kvprm_pool pool[KVPRM_MAX_POOLS];
-  int32_t first[KVPRM_MAX_POOLS + 1];   // pieces of a page of the pools before
+  kvprm_pool pool[N];
+  int32_t first[N + 1];   // pieces of a page of the pools before
   int32_t n_pools;
 };
+constexpr int kFewPools = 4;
 
 // T: ForkLaunch or CompactLaunch, whose tables are written first.
 __device__ __forceinline__ void tables(const ForkLaunch& t, int64_t warp, int64_t warps) { fork_tables(t, warp, warps); }
@@ -364,8 +367,8 @@ __device__ __forceinline__ int32_t copy_to(const CompactLaunch&, int32_t page) {
 __device__ __forceinline__ uint4 load_piece(const ForkLaunch&, const uint8_t* p) { return __ldcg(reinterpret_cast<const uint4*>(p)); }
 __device__ __forceinline__ uint4 load_piece(const CompactLaunch&, const uint8_t* p) { return __ldcs(reinterpret_cast<const uint4*>(p)); }
 
-template <typename T>
-__global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_kernel(const __grid_constant__ CopyLaunch a, const __grid_constant__ T t) {
+template <int N, typename T>
+__global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_kernel(const __grid_constant__ CopyLaunch<N> a, const __grid_constant__ T t) {
   const int lane = threadIdx.x & 31;
   const int64_t warp = static_cast<int64_t>(threadIdx.x >> 5) * gridDim.x + blockIdx.x, warps = static_cast<int64_t>(gridDim.x) * (kCopyThreads / 32);
   grid_dep_wait();
@@ -437,7 +440,7 @@ int check_sizes(int64_t n_pages, int n_pools, int n_seqs, int max_blocks, int n_
   return KVPRM_OK;
 }
 
-int check_pools(const kvprm_pool* pools, int n, int64_t n_pages, CopyLaunch* c, const char* who) {
+int check_pools(const kvprm_pool* pools, int n, int64_t n_pages, CopyLaunch<KVPRM_MAX_POOLS>* c, const char* who) {
   if (n > 0 && !pools) return operator_fail(KVPRM_EINVAL, "%s: no pools", who);
   int64_t pieces = 0;
   c->n_pools = n;
@@ -459,7 +462,7 @@ int check_pools(const kvprm_pool* pools, int n, int64_t n_pages, CopyLaunch* c, 
 
 // `most`: pages that may be copied; `entries`: of the tables.
 template <typename T>
-cudaError_t launch_copy(const CopyLaunch& c, const T& t, int64_t most, int64_t entries, cudaStream_t stream) {
+cudaError_t launch_copy(const CopyLaunch<KVPRM_MAX_POOLS>& c, const T& t, int64_t most, int64_t entries, cudaStream_t stream) {
   const int64_t work = std::max(c.first[c.n_pools] * most, (entries + 127) / 128);   // of warps
   if (work == 0) return cudaSuccess;
   int dev = 0, sms = 0;
@@ -475,7 +478,12 @@ cudaError_t launch_copy(const CopyLaunch& c, const T& t, int64_t most, int64_t e
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, copy_kernel<T>, c, t);
+  if (c.n_pools > kFewPools) return cudaLaunchKernelEx(&cfg, copy_kernel<KVPRM_MAX_POOLS, T>, c, t);
+  CopyLaunch<kFewPools> few;
+  few.n_pools = c.n_pools;
+  for (int k = 0; k < c.n_pools; ++k) few.pool[k] = c.pool[k];
+  for (int k = 0; k <= c.n_pools; ++k) few.first[k] = c.first[k];
+  return cudaLaunchKernelEx(&cfg, copy_kernel<kFewPools, T>, few, t);
 }
 
 template <typename K, typename A>
@@ -536,7 +544,7 @@ int kvprm_fork_workspace(const kvprm_pool*, const kvprm_fork* f, int64_t* bytes)
 int kvprm_cache_fork(const kvprm_pool* pools, const kvprm_fork* f, void* workspace, int64_t workspace_bytes, void* stream) {
   const char* who = "kvprm_cache_fork";
   if (const int rc = check_fork(f, who)) return rc;
-  CopyLaunch c;
+  CopyLaunch<KVPRM_MAX_POOLS> c;
   if (const int rc = check_pools(pools, f->n_pools, f->n_pages, &c, who)) return rc;
   const int64_t table = 4 * int64_t{f->n_seqs} * f->max_blocks;
   const Part in[] = {{f->refs, 4 * f->n_pages}, {f->block_table, table}, {f->lens, 4 * int64_t{f->n_seqs}},
@@ -570,7 +578,7 @@ int kvprm_compact_workspace(const kvprm_pool*, const kvprm_compact* f, int64_t* 
 int kvprm_cache_compact(const kvprm_pool* pools, const kvprm_compact* f, void* workspace, int64_t workspace_bytes, void* stream) {
   const char* who = "kvprm_cache_compact";
   if (const int rc = check_compact(f, who)) return rc;
-  CopyLaunch c;
+  CopyLaunch<KVPRM_MAX_POOLS> c;
   if (const int rc = check_pools(pools, f->n_pools, f->n_pages, &c, who)) return rc;
   const int64_t table = 4 * int64_t{f->n_seqs} * f->max_blocks;
   const Part in[] = {{f->refs, 4 * f->n_pages}, {f->block_table, table}, {f->lens, 4 * int64_t{f->n_seqs}}};

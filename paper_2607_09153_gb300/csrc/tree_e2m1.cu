@@ -810,7 +810,11 @@ cudaError_t launch_join(const TreeLaunch& a, cudaStream_t stream) {
 
 template <int HD, int NT>
 cudaError_t launch(const TreeLaunch& a, int ctas, cudaStream_t stream) {
-  cudaError_t e = cudaFuncSetAttribute(tree_e2m1_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes<HD>());
+  cudaError_t e = cudaSuccess;
+  // (beyond 48 KB a launch has to ask; a decoding step's are within, and it costs the host a microsecond)
+  constexpr size_t kStatic = 4 * (kTreeSeqs + 1) + 4 * kWarps + sizeof(uint2) * kWarps * NT * (HD / 16) * 32 + 64;
+  if constexpr (kStatic + ring_bytes<HD>() > 48 * 1024)
+    e = cudaFuncSetAttribute(tree_e2m1_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes<HD>());
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(ctas));

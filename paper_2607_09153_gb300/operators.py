@@ -318,9 +318,10 @@ def _cache(T, pages, exponents) -> tuple:
 def _cache4(T, pages, exponents, shape, device) -> tuple:
     """_cache of 4-bit pages [n_pages][2][n_kv_heads][16][head_dim / 2]: uint8 or float4_e2m1fn_x2, with exponents
     [n_pages][2][n_kv_heads][16][head_dim / 32]."""
-    if pages.dtype is not T.bytes[0] and pages.dtype is not getattr(T.torch, "float4_e2m1fn_x2", T.bytes[0]):
-        raise TypeError(f"pages are bfloat16, float8_e4m3fn, or uint8 (float4_e2m1fn_x2) of two codes each, got {pages.dtype}")
-    if exponents is None or exponents.dtype not in T.bytes or exponents.shape != shape[:4] + (shape[4] // 16,) or \
+    dtype, es = pages.dtype, () if exponents is None else exponents.shape
+    if dtype is not T.bytes[0] and dtype is not getattr(T.torch, "float4_e2m1fn_x2", dtype.__class__):
+        raise TypeError(f"pages are bfloat16, float8_e4m3fn, or uint8 (float4_e2m1fn_x2) of two codes each, got {dtype}")
+    if len(es) != 5 or es[:4] != shape[:4] or 16 * es[4] != shape[4] or exponents.dtype not in T.bytes or \
             exponents.get_device() != device or not exponents.is_contiguous():
         raise ValueError("4-bit pages [n_pages][2][n_kv_heads][16][head_dim / 2] need contiguous uint8 or float8_e8m0fnu "
                          "exponents [n_pages][2][n_kv_heads][16][head_dim / 32]")
@@ -519,10 +520,13 @@ def _pools(pools, n_pages: int, device: int) -> bytes:
         if len(shape) < 3 or shape[1] != n_pages or x.get_device() != device:
             raise ValueError(f"a pool is a tensor [layers][{n_pages}]... on CUDA device {device}, got {tuple(shape)} on {x.device}")
         stride, elements = x.stride(), 1
-        for n, st in zip(reversed(shape[2:]), reversed(stride[2:])):
-            if n > 1 and st != elements and x.numel() > 0:
-                raise ValueError(f"the elements of a pool's page are not side by side: shape {tuple(shape)}, strides {stride}")
-            elements *= n
+        if n_pages > 1 and x.numel() > 0 and x.is_contiguous():
+            elements = stride[1]
+        else:
+            for n, st in zip(reversed(shape[2:]), reversed(stride[2:])):
+                if n > 1 and st != elements and x.numel() > 0:
+                    raise ValueError(f"the elements of a pool's page are not side by side: shape {tuple(shape)}, strides {stride}")
+                elements *= n
         # (the stride of a dimension of one is nobody's)
         packed += _POOL.pack(x.data_ptr(), size * stride[0] if shape[0] > 1 else 0, size * stride[1] if shape[1] > 1 else 0,
                              size * elements, shape[0])
