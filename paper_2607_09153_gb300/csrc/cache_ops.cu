@@ -20,6 +20,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <new>
+#include <type_traits>
 
 #include "ptx.cuh"
 #include "rope.h"
@@ -454,6 +455,111 @@ __global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__
   }
 }
 
+// 4-bit pages from keys that are not rotated on the way: eight elements a thread, of U tokens at once, whose slots and rows are
+// all on their way before the first is quantised.
+//
+// bf16 stays in pairs: a block's largest magnitude m as its bits, where NaN and infinity are the largest of all; the exponent
+// byte, ((m + 0x3F) >> 7) - 2, at least 0 -- 6 = 1.5 * 4, and a mantissa above 1.5 (0x40) carries into the exponent --; the
+// scaling by a power of two, which is exact but far below the least code's border.  It costs half the instructions of
+// arithmetic in 32 bits, which bounded the kernel (30,001 tokens of 8 heads: 34 us).
+__device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {   // NaN if either is
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t pairs_to_e2m1(const uint4& v, uint32_t f) {
+  const uint32_t w[4] = {mul_bf16x2(v.x, f), mul_bf16x2(v.y, f), mul_bf16x2(v.z, f), mul_bf16x2(v.w, f)};
+  float x[8];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    x[2 * k] = __uint_as_float(w[k] << 16);
+    x[2 * k + 1] = __uint_as_float(w[k] & 0xFFFF0000u);
+  }
+  return e2m1_of8(x, 1.f);
+}
+
+template <typename T, int HD, int U, bool VEC>
+__global__ void __launch_bounds__(kThreads) write4_kernel(const __grid_constant__ WriteLaunch a, int64_t groups) {
+  constexpr int kRow = HD / 8;                           // threads of a row
+  const int pieces = 2 * a.heads * kRow;                 // of a token
+  const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+  const int64_t group = i / pieces;                      // of tokens group, group + groups ..
+  const int piece = static_cast<int>(i - group * pieces), r = piece / kRow, j = piece % kRow;   // row: its keys' heads, then its values'
+  const bool kv = r >= a.heads;
+  const T* base = (kv ? static_cast<const T*>(a.v) + (r - a.heads) * a.v_head : static_cast<const T*>(a.k) + r * a.k_head) + 8 * j;
+  const int64_t token_step = kv ? a.v_token : a.k_token;
+  int64_t slot[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int64_t t = group + u * groups;
+    slot[u] = group < groups && t < a.n_tokens ? __ldg(a.slots + t) : -1;
+  }
+  auto put = [&](int u, uint32_t codes, uint32_t exponent) {
+    if (slot[u] < 0 || slot[u] >= a.n_slots) return;
+    // (a page's number is below 2^30, and its rows are 2^15 at most)
+    const uint64_t row = static_cast<uint64_t>(static_cast<uint32_t>(slot[u] >> 4)) * (32u * a.heads) + (16u * r + (static_cast<uint32_t>(slot[u]) & 15u));
+    reinterpret_cast<uint32_t*>(a.pages)[row * kRow + j] = codes;
+    if ((j & 3) == 0) a.exponents[row * (HD / 32) + (j >> 2)] = static_cast<uint8_t>(exponent);
+  };
+  if constexpr (VEC && sizeof(T) == 2 && !std::is_same<T, __half>::value) {
+    uint4 v[U];
+    uint32_t m[U], special = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = group + u * groups;
+      v[u] = make_uint4(0u, 0u, 0u, 0u);
+      if (group < groups && t < a.n_tokens) v[u] = *reinterpret_cast<const uint4*>(base + t * token_step);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      constexpr uint32_t kAbs = 0x7FFF7FFFu;
+      uint32_t most = max_bf16x2(max_bf16x2(v[u].x & kAbs, v[u].y & kAbs), max_bf16x2(v[u].z & kAbs, v[u].w & kAbs));
+      most = max_bf16x2(most, __shfl_xor_sync(0xffffffffu, most, 1));
+      most = max_bf16x2(most, __shfl_xor_sync(0xffffffffu, most, 2));
+      m[u] = max(most & 0xFFFFu, most >> 16);   // (bits without a sign: ordered as the values, NaN above all)
+      special = max(special, m[u]);
+    }
+    if (!__any_sync(0xffffffffu, special >= 0x7F80u)) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t e = max((m[u] + 0x3Fu) >> 7, 2u) - 2u;
+        put(u, pairs_to_e2m1(v[u], (254u - e) * 0x00800080u), e);   // 2^(127 - e) in both halves
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
+        float x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
+        uint8_t e;
+        const uint32_t codes = block_of32(x, &e);
+        put(u, codes, e);
+      }
+    }
+  } else {
+    float x[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int64_t t = group + u * groups;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[u][k] = 0.f;
+      if (group < groups && t < a.n_tokens) load_n<T, 8, VEC>(base + t * token_step, x[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      uint8_t e;
+      const uint32_t codes = block_of32(x[u], &e);
+      put(u, codes, e);
+    }
+  }
+}
+
 // ---------------------------------------------------------------- expand
 // Pieces of 8 codes: an 8-byte load, the row's power of two, a 16-byte store, so that a warp's stores are 512 bytes side by
 // side (with 16 codes a thread each store left every other 16 bytes out: 86 % of the copy rate).
@@ -566,7 +672,28 @@ int launch_rope(const RopeLaunch& a, bool vec, unsigned grid, void* stream) {
 }
 
 template <typename T>
-int launch_write(const WriteLaunch& a, int format, bool vec, unsigned grid, void* stream) {
+int launch_write4(const WriteLaunch& a, bool vec, int sms, void* stream) {
+  const int pieces = 2 * a.heads * (a.head_dim >> 3);
+  // several tokens a thread where there are enough for four CTAs an SM all the same
+  const int u = a.n_tokens * pieces >= int64_t{16} * sms * kThreads ? 4 : 1;
+  const int64_t groups = (a.n_tokens + u - 1) / u, grid = (groups * pieces + kThreads - 1) / kThreads;
+  if (grid > 0x7FFFFFFF) return operator_fail(KVPRM_EINVAL, "kvprm_cache_write: n_tokens %lld", static_cast<long long>(a.n_tokens));
+  const bool wide = a.head_dim == 128;
+  auto k = u == 4 ? (wide ? (vec ? write4_kernel<T, 128, 4, true> : write4_kernel<T, 128, 4, false>)
+                          : (vec ? write4_kernel<T, 64, 4, true> : write4_kernel<T, 64, 4, false>))
+                  : (wide ? (vec ? write4_kernel<T, 128, 1, true> : write4_kernel<T, 128, 1, false>)
+                          : (vec ? write4_kernel<T, 64, 1, true> : write4_kernel<T, 64, 1, false>));
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = static_cast<cudaStream_t>(stream);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, k, a, groups);
+  return e == cudaSuccess ? KVPRM_OK : operator_fail(KVPRM_ECUDA, "cache write launch: %s", cudaGetErrorString(e));
+}
+
+template <typename T>
+int launch_write(const WriteLaunch& a, int format, bool vec, unsigned grid, int sms, void* stream) {
+  if (format == KVPRM_CACHE_E2M1 && a.tab.dim == 0) return launch_write4<T>(a, vec, sms, stream);
   const size_t smem = static_cast<size_t>(a.tokens) * a.tab.dim * sizeof(float);
   auto k = format == KVPRM_CACHE_E2M1   ? (vec ? write_kernel<T, KVPRM_CACHE_E2M1, true> : write_kernel<T, KVPRM_CACHE_E2M1, false>)
            : format == KVPRM_CACHE_E4M3 ? (vec ? write_kernel<T, KVPRM_CACHE_E4M3, true> : write_kernel<T, KVPRM_CACHE_E4M3, false>)
@@ -752,9 +879,9 @@ int kvprm_cache_write(const kvprm_cache* cache, int32_t dtype, const void* k, in
   const int64_t grid = (n_tokens + a.tokens - 1) / a.tokens;
   if (grid > 0x7FFFFFFF) return operator_fail(KVPRM_EINVAL, "%s: n_tokens %lld", who, static_cast<long long>(n_tokens));
   const unsigned g = static_cast<unsigned>(grid);
-  if (dtype == KVPRM_F32) return launch_write<float>(a, cache->format, vec, g, stream);
-  if (dtype == KVPRM_BF16) return launch_write<__nv_bfloat16>(a, cache->format, vec, g, stream);
-  return launch_write<__half>(a, cache->format, vec, g, stream);
+  if (dtype == KVPRM_F32) return launch_write<float>(a, cache->format, vec, g, sms, stream);
+  if (dtype == KVPRM_BF16) return launch_write<__nv_bfloat16>(a, cache->format, vec, g, sms, stream);
+  return launch_write<__half>(a, cache->format, vec, g, sms, stream);
 }
 
 int kvprm_cache_expand(const kvprm_cache* cache, const int32_t* src, const int32_t* dst, int64_t n, void* out,

@@ -88,11 +88,13 @@ def test_write_many_heads(n, nkv):
     assert bool(((got - want).abs() <= want.abs().amax(-1, keepdim=True) / 3 * 1.0001).all())
 
 
-def test_write_not_finite():
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("offset", [0, 1])
+def test_write_not_finite(dtype, offset):
     """Infinities become the largest code of the rest's scale; a block with a NaN reads as NaN, the others do not."""
     torch, kp = _kp()
     pool, exps = _pool4(torch, 2, 2, 64)
-    k = torch.ones((3, 2, 64), device="cuda")
+    k = torch.ones(3 * 2 * 64 + 1, device="cuda", dtype=getattr(torch, dtype))[offset:][:3 * 2 * 64].view(3, 2, 64)
     k[0, 0, 3], k[0, 1, 45], k[1, 0, 0], k[1, 1, 32:] = math.inf, -math.inf, math.nan, math.inf
     kp.cache_write(pool, torch.tensor([0, 1, 17], device="cuda"), k, torch.zeros_like(k), exponents=exps)
     out = torch.zeros((2, 2, 2, 16, 64), dtype=torch.bfloat16, device="cuda")
