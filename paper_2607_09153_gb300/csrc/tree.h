@@ -19,7 +19,7 @@ struct TreeLaunch {
   int64_t n_pages;
   int32_t n_kv, group, seq0, n_seqs;   // sequences seq0 .. seq0 + n_seqs - 1
   uint32_t group_m;                    // ceil(2^32 / group), 0 for a group of one (tree_token)
-  int32_t whole;                       // 1: no pair is cut
+  int32_t whole;                       // 1: no pair is cut; 2: CTA i has pair i (4-bit pages)
   int32_t fill;                        // 1: rows that no sequence writes are written too (tree_fill)
   int32_t weight_full, weight_part;    // places of a block of a pair with all its tiles, or with fewer
   float scale_log2;                    // scores in units of log2
@@ -251,7 +251,7 @@ cudaError_t launch_tree_rows(const TreeLaunch& a, const kvprm_cache& c, int tile
 constexpr int kTreeE2m1Warps = 4;   // of a CTA
 #ifdef __CUDACC__
 template <int NT>
-using TreeE2m1 = TreeGeometry<8 * NT, kTreePage, 1, 8>;
+using TreeE2m1 = TreeGeometry<8 * NT, kTreePage, 1, 10>;
 #endif
 constexpr int tree_e2m1_per_sm(int tiles) { return tiles == 1 ? 3 : 2; }
 cudaError_t launch_tree_e2m1(const TreeLaunch& a, const kvprm_cache& c, int tiles, int ctas, cudaStream_t stream);

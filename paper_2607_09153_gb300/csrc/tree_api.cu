@@ -17,7 +17,8 @@ bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) ==
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct TreePlan {
-  bool tc = false, whole = false;
+  bool tc = false;
+  int whole = 0;                       // 1: no pair is cut; 2: CTA i has pair i
   int tiles8 = 0;                      // 4-bit pages on registers: tiles of 8 rows
   int ctas = 0, rows = 16, seqs = 0;   // rows: of a partial result; seqs: sequences of a launch
   int64_t parts() const { return tiles8 ? int64_t{ctas} * kTreeE2m1Warps : ctas; }   // shares of the line
@@ -46,9 +47,11 @@ int sm_count(int* sms) {
   return KVPRM_OK;
 }
 
-// 4-bit pages on registers, whose parts are warps': pairs of so many blocks stay whole; a part has so many blocks at least, and
-// a pair so many parts at most.
-constexpr int kWhole4 = 16, kLeast4 = 8, kParts4 = 32;
+// 4-bit pages on registers (us a call, cut / whole).  Pairs that have a CTA each: 64 x 4 heads over ragged 500 tokens 17 / 12,
+// 1,000 19 / 16, 1,500 21.9 / 20.6, but 4 x 8 heads over 1,500 18 / 20; where CTAs have several: 64 x 8 heads over 300 24 / 22, 500
+// 27 / 29.  A cut pair's parts are warps': of 8 blocks at least (4: the same) and 64 at most (one sequence of 32,768 tokens of 4
+// heads: 16 parts 59, 32 37, 64 27).
+constexpr int kWhole4 = 72, kWholeMany4 = 24, kLeast4 = 8, kParts4 = 64;
 
 // More than 32 rows of a kv head go to the tensor cores (us a call, registers / tensor cores: 8 heads with 24 rows over ragged
 // 20,000 bf16 tokens 76 / 78, 8-bit 66 / 89; with 32 over 8 x 32,768 bf16 tokens 187 / 186, 8-bit 155 / 221; 4 heads with 63 over
@@ -74,10 +77,10 @@ int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   const int64_t blocks = ceil_div(len, block) + ceil_div(t.max_drafts, block);
   const int64_t most = int64_t{sms} * (p.tc ? 1 : e2m1 ? tree_e2m1_per_sm(p.tiles8) : tree_rows_per_sm(p.rows / 16));
   if (p.tiles8) {
-    const int64_t warps = most * kTreeE2m1Warps;
-    p.whole = blocks <= kWhole4;
-    const int64_t parts = p.whole ? pairs : std::min(pairs * blocks / kLeast4, pairs * kParts4);
-    p.ctas = static_cast<int>(std::max<int64_t>(1, ceil_div(std::min(warps, parts), kTreeE2m1Warps)));
+    const bool each = pairs <= most && rows <= p.rows;
+    p.whole = blocks > (each ? kWhole4 : kWholeMany4) ? 0 : each ? 2 : 1;
+    const int64_t parts = std::min(pairs * blocks / kLeast4, pairs * kParts4);
+    p.ctas = static_cast<int>(std::max<int64_t>(1, std::min(most, p.whole ? pairs : ceil_div(parts, kTreeE2m1Warps))));
     *out = p;
     return KVPRM_OK;
   }

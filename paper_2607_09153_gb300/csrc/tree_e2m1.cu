@@ -1,6 +1,5 @@
 // Attention of drafted tokens over 4-bit pages (e2m1 codes, a power of two for each 32 elements): up to 32 query rows (row =
-// drafted token and head of the kv head's group) a tile, by warp-level matrix instructions on fragments that are loaded
-// straight from the pages.
+// drafted token and head of the kv head's group) a tile, by warp-level matrix instructions.
 //
 // The products are the transposed ones, S^T = K Q^T and O^T = V^T P^T: the cache's rows fill the 16 rows of an instruction
 // and the queries its 8 columns, so a plain decoding step (up to 8 query heads on a kv head) takes half the instructions
@@ -16,6 +15,18 @@
 // relative to: blocks from 2^-8 to 2^7 of it are exact.  A page that leaves that window moves Ek or Ev; one whose own
 // blocks are further apart takes its products in bf16 instead, whose range is fp32's.  Weights are kept times 2^12, so
 // that fp16's steps end at 2^-36 of a full weight's.
+//
+// Each warp has a share of the work line (tree.h) of its own, copies its pages into a ring in shared memory by itself, two steps
+// of two pages ahead, and leaves partial results that a second launch joins: nothing waits at a barrier.  Short pairs stay
+// whole instead, a CTA each, whose four warps meet at the end.
+//
+// What bounds it, measured on a GB300, is instructions: a page of a kv head takes some 295 of a warp (64 conversions, 64
+// multiplications by powers, 16 matrix instructions, 16 to put nibbles together, 20 of the softmax, 29 loads and copies), 0.60 of
+// the issue slots with the three warps a scheduler that 163 registers leave (ALU pipe 0.49, DRAM 0.45).  One drafted token
+// over 8 x 32,768 tokens of 8 heads 66 us (4,300 GB/s), four (16 rows) 85, eight (32 rows) 140; 64 ragged sequences up to 9,001
+// of 4 heads 49 us.  Tried: fragments loaded straight into registers, a page ahead (75 us for the first of these: the loads
+// share scoreboards) or in single pages (84); four CTAs an SM (81: spills); the next step's scores beside this one's product
+// (74); CTAs instead of warps as shares (72; the ragged ones 58, for a part then costs 4 us of barriers).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -91,8 +102,8 @@ constexpr int kRing = 4;   // pages of a warp
 template <int HD>
 constexpr int ring_bytes() { return kWarps * kRing * Stage<HD>::kBytes; }
 
-// NT: tiles of 8 query rows.
-template <int HD, int NT>
+// NT: tiles of 8 query rows.  WHOLE: no pair is cut.
+template <int HD, int NT, bool WHOLE>
 __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kernel(const __grid_constant__ TreeLaunch a) {
   using G = TreeE2m1<NT>;
   constexpr int KS = HD / 16;            // 16-dim steps of q . k
@@ -106,15 +117,19 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
   __shared__ int32_t s_off[kTreeSeqs + 1];
   __shared__ int32_t s_sum[kWarps];
   __shared__ uint2 s_q[kWarps][NT][KS][32];   // the scaled queries' fragments, by lane
+  __shared__ float2 s_ml[kWarps][8];
   grid_dep_launch();
   tree_line<G, kThreads, HD>(a, s_off, s_sum);
   const int32_t total = s_off[a.n_seqs];
   if (total == 0) return;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, gid = lane >> 2, c = lane & 3;
-  const TreeShares shares(total, gridDim.x * kWarps, a.weight_full);
-  const int me = blockIdx.x * kWarps + warp;
+  // Whole pairs are a CTA's, whose warps take a quarter of the blocks each -- where there is a CTA for each, by its number, for
+  // an equal share of the line may hold several short pairs --; else a share is a warp's.
+  const TreeShares shares(total, WHOLE ? gridDim.x : gridDim.x * kWarps, a.weight_full);
+  const int me = WHOLE ? blockIdx.x : blockIdx.x * kWarps + warp;
   tree_leave_line(a, s_off, shares.ctas);
-  if (me >= shares.ctas) return;
+  const bool direct = WHOLE && a.whole == 2;
+  if (!direct && me >= shares.ctas) return;
   constexpr uint32_t head_bytes = kTreePage * kRowBytes, kHeadExp = kTreePage * kBlocks;
   const uint32_t page_bytes = 2 * a.n_kv * head_bytes, page_exp = 2 * a.n_kv * kHeadExp;   // (of 1,024 heads at most)
   // where this lane's pieces of a page go
@@ -126,11 +141,22 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
   const int v_at = S::kV + (4 * (row & 3) + (row >> 2)) * kRowBytes + piece * 16;
   constexpr int k_step = 4 * kRowBytes;
   const int v_step = 2 * kRowBytes + (piece & 2 ? -32 : 32);
-  int32_t u = shares.begin(me);
-  const int32_t u_end = shares.begin(me + 1);
-  int s_at = tree_find(s_off, a.n_seqs, u);
+  int32_t u = direct ? 0 : shares.begin(me);
+  const int32_t u_end = direct ? 1 : shares.begin(me + 1);
+  int s_at = direct ? blockIdx.x / a.n_kv : tree_find(s_off, a.n_seqs, u);
   TreePart part;
-  while (tree_next<G>(a, s_off, u, u_end, s_at, part)) {
+  auto next_part = [&]() {
+    if (!direct) return tree_next<G>(a, s_off, u, u_end, s_at, part);
+    if (u++ > 0 || s_at >= a.n_seqs) return false;
+    part.q = tree_seq<G::ROWS, G::BLOCK>(a, s_at);
+    part.g = blockIdx.x - s_at * a.n_kv;
+    part.s = s_at;
+    part.tp = part.first = part.c0 = 0;
+    part.tiles = part.weight = 1;
+    part.c1 = part.q.drafts > 0 ? part.q.blocks : 0;
+    return part.c1 > 0;
+  };
+  while (next_part()) {
     const TreeSeq& q = part.q;
     const int g = part.g, row0 = part.tp * G::kSlotRows, rows = q.drafts * a.group;
     const int32_t* table = a.t.block_table + static_cast<int64_t>(a.seq0 + s_at) * a.t.max_blocks;
@@ -147,12 +173,14 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
     };
 
     // ---- the pages' numbers, a lane each, 32 at a time; 0 for one outside the cache
-    const int mine = max(0, min(part.c1, q.cached_blocks) - part.c0);
+    const int n_blocks = part.c1 - part.c0;
+    const int c0 = WHOLE ? part.c0 + n_blocks * warp / kWarps : part.c0, c1 = WHOLE ? part.c0 + n_blocks * (warp + 1) / kWarps : part.c1;
+    const int mine = max(0, min(c1, q.cached_blocks) - c0);
     bool poison = q.bad;        // of all rows of the sequence
     auto ids_of = [&](int k0) {
       const int k = k0 + lane;
       if (k >= mine) return 0;
-      const int32_t page = __ldg(table + part.c0 + k);
+      const int32_t page = __ldg(table + c0 + k);
       const bool in = page >= 0 && page < a.n_pages;
       poison = poison || !in;
       return in ? page : 0;
@@ -340,7 +368,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
       Loaded x;
       read_keys(place, x);
       read_values(place, x);
-      const int b = part.c0 + at;
+      const int b = c0 + at;
       const uint32_t ve = value_bytes(x);
       const int have = q.len - b * kTreePage;   // tokens of the page: 16 or more where it is full
       uint32_t live = 0x3Fu;   // bits 0, 1: of this lane's key rows, 2 ..: of its value rows
@@ -561,7 +589,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
         }
       }
     };
-    const int full = min(pages, q.len / kTreePage - part.c0);   // pages without places beyond the length
+    const int full = min(pages, q.len / kTreePage - c0);   // pages without places beyond the length
     int plain = 0;                                              // of these, those that the short form may take
     for (int at = 0, place = 0; at < pages; at += P) {
       copies_wait<kRing / P - 1>();
@@ -604,7 +632,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
     // ---- drafted tokens: bf16 rows of their own tensors, whatever the cache holds
     if (ev == 0) ev = 127;
     const float rel = power_of(254 - ev);   // what the outputs are kept in, over the values' own
-    for (int b = part.c0 + mine; b < part.c1; ++b) {
+    for (int b = c0 + mine; b < c1; ++b) {
       const int j0 = (b - q.cached_blocks) * kTreePage, have = q.drafts - j0;
       const __nv_bfloat16* kd = static_cast<const __nv_bfloat16*>(a.t.k) + (q.start + static_cast<int64_t>(j0)) * a.t.k_token + g * a.t.k_head;
       const __nv_bfloat16* vd = static_cast<const __nv_bfloat16*>(a.t.v) + (q.start + static_cast<int64_t>(j0)) * a.t.v_token + g * a.t.v_head;
@@ -685,39 +713,90 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
     // ---- the part's end
     const float down = power_of(ev);   // 1 / rel
     const bool lost = __any_sync(0xffffffffu, poison);
-    const bool whole = part.whole();
-    // partial results: [row][dim]
-    const int64_t slot = me == shares.owner(part.place(0)) ? 2 * me + 1 : 2 * me;
+    auto sum_of = [&](int nt, int h) {
+      float sum = l[nt][h];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
+      for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+      return lost || (poison_row >> (2 * nt + h)) & 1u ? NAN : sum;
+    };
+    if constexpr (WHOLE) {   // the warps' states meet, 8 rows at a time, in their rings
+      constexpr int kOutRow = HD + 4, kPer = 8 * HD / kThreads;   // kPer: outputs of a thread, part of one row
+      auto out_of = [&](int w) { return reinterpret_cast<float*>(s_ring + w * (kRing * S::kBytes)); };
+      static_assert(8 * kOutRow * 4 <= kRing * S::kBytes, "a warp's rows fit its ring");
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float sum = l[nt][h];
+      for (int nt = 0; nt < NT; ++nt) {
+        if (row0 + 8 * nt >= rows) break;   // (the same for all threads)
+        if (nt > 0) __syncthreads();        // the last 8 rows have been read
 #pragma unroll
-        for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-        if (lost || (poison_row >> (2 * nt + h)) & 1u) sum = NAN;
-        const int slot_row = 8 * nt + 2 * c + h, r = row0 + slot_row;
-        if (r >= rows) continue;
-        float y[2 * MT];   // this lane's HD / 8 dims
-        const float f = whole ? (sum == 0.f ? 0.f : down / sum) : down;   // a row that saw nothing: zeros; NaN stays
+        for (int h = 0; h < 2; ++h) {
+          const float sum = sum_of(nt, h);
+          if (gid == 0) s_ml[warp][2 * c + h] = make_float2(-nm[nt][h], sum);
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-          y[2 * i] = o[nt][i][h] * f;
-          y[2 * i + 1] = o[nt][i][2 + h] * f;
+          for (int i = 0; i < MT; ++i)   // dims 2 i and 2 i + 1 of this lane's HD / 8
+            *reinterpret_cast<float2*>(out_of(warp) + (2 * c + h) * kOutRow + gid * (HD / 8) + 2 * i) = make_float2(o[nt][i][h] * down, o[nt][i][2 + h] * down);
         }
-        if (whole) {
-          const int tok = tree_token(a, r);
-          __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.t.out) + (q.start + static_cast<int64_t>(tok)) * a.t.out_token +
-                               (g * a.group + r - tok * a.group) * a.t.out_head + gid * (HD / 8);
+        __syncthreads();
+        const int r = threadIdx.x / 16, d0 = threadIdx.x % 16 * kPer, out_r = row0 + 8 * nt + r;
+        float top = -INFINITY, sum = 0.f, acc[kPer];
 #pragma unroll
-          for (int i = 0; i < 2 * MT; i += 8)
-            *reinterpret_cast<uint4*>(dst + i) = make_uint4(pack_bf16(y[i], y[i + 1]), pack_bf16(y[i + 2], y[i + 3]),
-                                                            pack_bf16(y[i + 4], y[i + 5]), pack_bf16(y[i + 6], y[i + 7]));
-        } else {
-          float* dst = a.part_o + (slot * G::kSlotRows + slot_row) * HD + gid * (HD / 8);
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_ml[w][r].x);
 #pragma unroll
-          for (int i = 0; i < 2 * MT; i += 4) *reinterpret_cast<float4*>(dst + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
-          if (gid == 0) a.part_ml[slot * G::kSlotRows + slot_row] = make_float2(-nm[nt][h], sum);
+        for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const float f = s_ml[w][r].x == -INFINITY ? 0.f : ex2_ftz(s_ml[w][r].x - top);   // (NaN sums stay NaN)
+          sum += s_ml[w][r].y * f;
+#pragma unroll
+          for (int i = 0; i < kPer; ++i) acc[i] += out_of(w)[r * kOutRow + d0 + i] * f;
+        }
+        if (out_r >= rows) continue;
+        const float inv = sum == 0.f ? 0.f : 1.f / sum;   // a row that saw nothing: zeros; NaN stays
+        const int tok = tree_token(a, out_r);
+        __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.t.out) + (q.start + static_cast<int64_t>(tok)) * a.t.out_token +
+                             (g * a.group + out_r - tok * a.group) * a.t.out_head + d0;
+        uint32_t w[kPer / 2];
+#pragma unroll
+        for (int i = 0; i < kPer / 2; ++i) w[i] = pack_bf16(acc[2 * i] * inv, acc[2 * i + 1] * inv);
+        if constexpr (kPer == 8)
+          *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+        else
+          *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+      }
+      __syncthreads();   // the rings are free for the next part
+      continue;
+    }
+    if constexpr (!WHOLE) {
+      const bool whole = part.whole();
+      // partial results: [row][dim]
+      const int64_t slot = me == shares.owner(part.place(0)) ? 2 * me + 1 : 2 * me;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float sum = sum_of(nt, h);
+          const int slot_row = 8 * nt + 2 * c + h, r = row0 + slot_row;
+          if (r >= rows) continue;
+          float y[2 * MT];   // this lane's HD / 8 dims
+          const float f = whole ? (sum == 0.f ? 0.f : down / sum) : down;   // a row that saw nothing: zeros; NaN stays
+#pragma unroll
+          for (int i = 0; i < MT; ++i) {
+            y[2 * i] = o[nt][i][h] * f;
+            y[2 * i + 1] = o[nt][i][2 + h] * f;
+          }
+          if (whole) {
+            const int tok = tree_token(a, r);
+            __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.t.out) + (q.start + static_cast<int64_t>(tok)) * a.t.out_token +
+                                 (g * a.group + r - tok * a.group) * a.t.out_head + gid * (HD / 8);
+#pragma unroll
+            for (int i = 0; i < 2 * MT; i += 8)
+              *reinterpret_cast<uint4*>(dst + i) = make_uint4(pack_bf16(y[i], y[i + 1]), pack_bf16(y[i + 2], y[i + 3]),
+                                                              pack_bf16(y[i + 4], y[i + 5]), pack_bf16(y[i + 6], y[i + 7]));
+          } else {
+            float* dst = a.part_o + (slot * G::kSlotRows + slot_row) * HD + gid * (HD / 8);
+#pragma unroll
+            for (int i = 0; i < 2 * MT; i += 4) *reinterpret_cast<float4*>(dst + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+            if (gid == 0) a.part_ml[slot * G::kSlotRows + slot_row] = make_float2(-nm[nt][h], sum);
+          }
         }
       }
     }
@@ -808,21 +887,25 @@ cudaError_t launch_join(const TreeLaunch& a, cudaStream_t stream) {
   return cudaLaunchKernelEx(&cfg, tree_e2m1_join_kernel<HD, NT>, a, groups);
 }
 
-template <int HD, int NT>
+template <int HD, int NT, bool WHOLE>
 cudaError_t launch(const TreeLaunch& a, int ctas, cudaStream_t stream) {
   cudaError_t e = cudaSuccess;
   // (beyond 48 KB a launch has to ask; a decoding step's are within, and it costs the host a microsecond)
-  constexpr size_t kStatic = 4 * (kTreeSeqs + 1) + 4 * kWarps + sizeof(uint2) * kWarps * NT * (HD / 16) * 32 + 64;
+  constexpr size_t kStatic = 4 * (kTreeSeqs + 1) + 4 * kWarps + sizeof(uint2) * kWarps * (NT * (HD / 16) * 32 + 8) + 64;
   if constexpr (kStatic + ring_bytes<HD>() > 48 * 1024)
-    e = cudaFuncSetAttribute(tree_e2m1_kernel<HD, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes<HD>());
+    e = cudaFuncSetAttribute(tree_e2m1_kernel<HD, NT, WHOLE>, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes<HD>());
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(ctas));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = ring_bytes<HD>();
   cfg.stream = stream;
-  e = cudaLaunchKernelEx(&cfg, tree_e2m1_kernel<HD, NT>, a);
-  return e == cudaSuccess && !a.whole && a.n_seqs > 0 ? launch_join<HD, NT>(a, stream) : e;
+  e = cudaLaunchKernelEx(&cfg, tree_e2m1_kernel<HD, NT, WHOLE>, a);
+  return e == cudaSuccess && !WHOLE && a.n_seqs > 0 ? launch_join<HD, NT>(a, stream) : e;
+}
+template <int HD, int NT>
+cudaError_t launch(const TreeLaunch& a, int ctas, cudaStream_t stream) {
+  return a.whole ? launch<HD, NT, true>(a, ctas, stream) : launch<HD, NT, false>(a, ctas, stream);
 }
 
 }  // namespace
