@@ -484,36 +484,44 @@ __device__ __forceinline__ uint32_t pairs_to_e2m1(const uint4& v, uint32_t f) {
 }
 
 template <typename T, int HD, int U, bool VEC>
-__global__ void __launch_bounds__(kThreads) write4_kernel(const __grid_constant__ WriteLaunch a, int64_t groups) {
+__global__ void __launch_bounds__(kThreads) write4_kernel(const __grid_constant__ WriteLaunch a, int32_t n_tokens, int32_t groups,
+                                                          int32_t at_once, FastDiv by_pieces) {
   constexpr int kRow = HD / 8;                           // threads of a row
-  const int pieces = 2 * a.heads * kRow;                 // of a token
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  const int64_t group = i / pieces;                      // of tokens group, group + groups ..
-  const int piece = static_cast<int>(i - group * pieces), r = piece / kRow, j = piece % kRow;   // row: its keys' heads, then its values'
+  const int pieces = 2 * a.heads * kRow;                 // of a token; a CTA has at_once tokens', or 256 of one's
+  const int side = at_once > 1 ? static_cast<int>(by_pieces.div(threadIdx.x)) : 0;
+  const int group = blockIdx.x * at_once + side;         // of tokens group, group + groups ..
+  const int piece = threadIdx.x - side * pieces + blockIdx.y * kThreads;
+  const int r = piece / kRow, j = piece % kRow;          // row: its keys' heads, then its values'
+  const int tokens = group < groups && side < at_once && piece < pieces ? n_tokens : 0;
   const bool kv = r >= a.heads;
   const T* base = (kv ? static_cast<const T*>(a.v) + (r - a.heads) * a.v_head : static_cast<const T*>(a.k) + r * a.k_head) + 8 * j;
   const int64_t token_step = kv ? a.v_token : a.k_token;
   int64_t slot[U];
 #pragma unroll
   for (int u = 0; u < U; ++u) {
-    const int64_t t = group + u * groups;
-    slot[u] = group < groups && t < a.n_tokens ? __ldg(a.slots + t) : -1;
+    const int t = group + u * groups;
+    slot[u] = t < tokens ? __ldg(a.slots + t) : -1;
   }
+  // where a row's codes and exponents are: of page 0's place 0, and how far a page is
+  uint32_t* const codes0 = reinterpret_cast<uint32_t*>(a.pages) + (16 * r * kRow + j);
+  uint8_t* const exponents0 = a.exponents + (16 * r * (HD / 32) + (j >> 2));
+  const uint32_t page_rows = 32u * a.heads;   // (2^15 at most, and a page's number is below 2^30)
   auto put = [&](int u, uint32_t codes, uint32_t exponent) {
-    if (slot[u] < 0 || slot[u] >= a.n_slots) return;
-    // (a page's number is below 2^30, and its rows are 2^15 at most)
-    const uint64_t row = static_cast<uint64_t>(static_cast<uint32_t>(slot[u] >> 4)) * (32u * a.heads) + (16u * r + (static_cast<uint32_t>(slot[u]) & 15u));
-    reinterpret_cast<uint32_t*>(a.pages)[row * kRow + j] = codes;
-    if ((j & 3) == 0) a.exponents[row * (HD / 32) + (j >> 2)] = static_cast<uint8_t>(exponent);
+    if (static_cast<uint64_t>(slot[u]) >= static_cast<uint64_t>(a.n_slots)) return;
+    const uint32_t page = static_cast<uint32_t>(slot[u] >> 4), place = static_cast<uint32_t>(slot[u]) & 15u;
+    codes0[static_cast<uint64_t>(page) * (page_rows * kRow) + place * kRow] = codes;
+    if ((j & 3) == 0) exponents0[static_cast<uint64_t>(page) * (page_rows * (HD / 32)) + place * (HD / 32)] = static_cast<uint8_t>(exponent);
   };
+  base += static_cast<int64_t>(group) * token_step;
+  const int64_t next = static_cast<int64_t>(groups) * token_step;
   if constexpr (VEC && sizeof(T) == 2 && !std::is_same<T, __half>::value) {
     uint4 v[U];
     uint32_t m[U], special = 0;
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t t = group + u * groups;
+      const int t = group + u * groups;
       v[u] = make_uint4(0u, 0u, 0u, 0u);
-      if (group < groups && t < a.n_tokens) v[u] = *reinterpret_cast<const uint4*>(base + t * token_step);
+      if (t < tokens) v[u] = *reinterpret_cast<const uint4*>(base + u * next);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -546,10 +554,10 @@ __global__ void __launch_bounds__(kThreads) write4_kernel(const __grid_constant_
     float x[U][8];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      const int64_t t = group + u * groups;
+      const int t = group + u * groups;
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[u][k] = 0.f;
-      if (group < groups && t < a.n_tokens) load_n<T, 8, VEC>(base + t * token_step, x[u]);
+      if (t < tokens) load_n<T, 8, VEC>(base + u * next, x[u]);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -676,24 +684,23 @@ int launch_write4(const WriteLaunch& a, bool vec, int sms, void* stream) {
   const int pieces = 2 * a.heads * (a.head_dim >> 3);
   // several tokens a thread where there are enough for four CTAs an SM all the same
   const int u = a.n_tokens * pieces >= int64_t{16} * sms * kThreads ? 4 : 1;
-  const int64_t groups = (a.n_tokens + u - 1) / u, grid = (groups * pieces + kThreads - 1) / kThreads;
-  if (grid > 0x7FFFFFFF) return operator_fail(KVPRM_EINVAL, "kvprm_cache_write: n_tokens %lld", static_cast<long long>(a.n_tokens));
+  const int groups = static_cast<int>((a.n_tokens + u - 1) / u), at_once = pieces < kThreads ? kThreads / pieces : 1;
   const bool wide = a.head_dim == 128;
   auto k = u == 4 ? (wide ? (vec ? write4_kernel<T, 128, 4, true> : write4_kernel<T, 128, 4, false>)
                           : (vec ? write4_kernel<T, 64, 4, true> : write4_kernel<T, 64, 4, false>))
                   : (wide ? (vec ? write4_kernel<T, 128, 1, true> : write4_kernel<T, 128, 1, false>)
                           : (vec ? write4_kernel<T, 64, 1, true> : write4_kernel<T, 64, 1, false>));
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(static_cast<unsigned>(grid));
+  cfg.gridDim = dim3(static_cast<unsigned>((groups + at_once - 1) / at_once), static_cast<unsigned>((pieces + kThreads - 1) / kThreads));
   cfg.blockDim = dim3(kThreads);
   cfg.stream = static_cast<cudaStream_t>(stream);
-  const cudaError_t e = cudaLaunchKernelEx(&cfg, k, a, groups);
+  const cudaError_t e = cudaLaunchKernelEx(&cfg, k, a, static_cast<int32_t>(a.n_tokens), groups, at_once, FastDiv(static_cast<uint32_t>(pieces)));
   return e == cudaSuccess ? KVPRM_OK : operator_fail(KVPRM_ECUDA, "cache write launch: %s", cudaGetErrorString(e));
 }
 
 template <typename T>
 int launch_write(const WriteLaunch& a, int format, bool vec, unsigned grid, int sms, void* stream) {
-  if (format == KVPRM_CACHE_E2M1 && a.tab.dim == 0) return launch_write4<T>(a, vec, sms, stream);
+  if (format == KVPRM_CACHE_E2M1 && a.tab.dim == 0 && a.n_tokens <= (1 << 28)) return launch_write4<T>(a, vec, sms, stream);
   const size_t smem = static_cast<size_t>(a.tokens) * a.tab.dim * sizeof(float);
   auto k = format == KVPRM_CACHE_E2M1   ? (vec ? write_kernel<T, KVPRM_CACHE_E2M1, true> : write_kernel<T, KVPRM_CACHE_E2M1, false>)
            : format == KVPRM_CACHE_E4M3 ? (vec ? write_kernel<T, KVPRM_CACHE_E4M3, true> : write_kernel<T, KVPRM_CACHE_E4M3, false>)
