@@ -455,13 +455,14 @@ __global__ void __launch_bounds__(kThreads) write_kernel(const __grid_constant__
   }
 }
 
-// 4-bit pages from keys that are not rotated on the way: eight elements a thread, of U tokens at once, whose slots and rows are
-// all on their way before the first is quantised.
+// 4-bit pages from keys that are not rotated on the way: a few elements a thread, of U tokens at once, whose slots and rows are all
+// on their way before the first is quantised.
 //
 // bf16 stays in pairs: a block's largest magnitude m as its bits, where NaN and infinity are the largest of all; the exponent
 // byte, ((m + 0x3F) >> 7) - 2, at least 0 -- 6 = 1.5 * 4, and a mantissa above 1.5 (0x40) carries into the exponent --; the
-// scaling by a power of two, which is exact but far below the least code's border.  It costs half the instructions of
-// arithmetic in 32 bits, which bounded the kernel (30,001 tokens of 8 heads: 34 us).
+// scaling by a power of two, which is exact but far below the least code's border.  What bounds it is memory beside the ALU pipe: 30,001
+// tokens of 8 heads (154 MB) take 27 us; in 32 bits, a token after the other as above, 34, in pairs with eight elements a
+// thread 29 (ALU pipe 0.70, and half of its instructions were a thread's indices).
 __device__ __forceinline__ uint32_t max_bf16x2(uint32_t a, uint32_t b) {   // NaN if either is
   uint32_t r;
   asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
@@ -483,10 +484,11 @@ __device__ __forceinline__ uint32_t pairs_to_e2m1(const uint4& v, uint32_t f) {
   return e2m1_of8(x, 1.f);
 }
 
-template <typename T, int HD, int U, bool VEC>
-__global__ void __launch_bounds__(kThreads) write4_kernel(const __grid_constant__ WriteLaunch a, int32_t n_tokens, int32_t groups,
-                                                          int32_t at_once, FastDiv by_pieces) {
-  constexpr int kRow = HD / 8;                           // threads of a row
+// bf16, 16-byte aligned rows: 16 elements a thread (a block is two neighbouring lanes').
+template <int HD, int U>
+__global__ void __launch_bounds__(kThreads) write4_pairs_kernel(const __grid_constant__ WriteLaunch a, int32_t n_tokens, int32_t groups,
+                                                                int32_t at_once, FastDiv by_pieces) {
+  constexpr int kRow = HD / 16;                          // threads of a row
   const int pieces = 2 * a.heads * kRow;                 // of a token; a CTA has at_once tokens', or 256 of one's
   const int side = at_once > 1 ? static_cast<int>(by_pieces.div(threadIdx.x)) : 0;
   const int group = blockIdx.x * at_once + side;         // of tokens group, group + groups ..
@@ -494,7 +496,8 @@ __global__ void __launch_bounds__(kThreads) write4_kernel(const __grid_constant_
   const int r = piece / kRow, j = piece % kRow;          // row: its keys' heads, then its values'
   const int tokens = group < groups && side < at_once && piece < pieces ? n_tokens : 0;
   const bool kv = r >= a.heads;
-  const T* base = (kv ? static_cast<const T*>(a.v) + (r - a.heads) * a.v_head : static_cast<const T*>(a.k) + r * a.k_head) + 8 * j;
+  const __nv_bfloat16* base = (kv ? static_cast<const __nv_bfloat16*>(a.v) + (r - a.heads) * a.v_head
+                                  : static_cast<const __nv_bfloat16*>(a.k) + r * a.k_head) + 16 * j;
   const int64_t token_step = kv ? a.v_token : a.k_token;
   int64_t slot[U];
 #pragma unroll
@@ -502,69 +505,101 @@ __global__ void __launch_bounds__(kThreads) write4_kernel(const __grid_constant_
     const int t = group + u * groups;
     slot[u] = t < tokens ? __ldg(a.slots + t) : -1;
   }
-  // where a row's codes and exponents are: of page 0's place 0, and how far a page is
-  uint32_t* const codes0 = reinterpret_cast<uint32_t*>(a.pages) + (16 * r * kRow + j);
-  uint8_t* const exponents0 = a.exponents + (16 * r * (HD / 32) + (j >> 2));
-  const uint32_t page_rows = 32u * a.heads;   // (2^15 at most, and a page's number is below 2^30)
-  auto put = [&](int u, uint32_t codes, uint32_t exponent) {
-    if (static_cast<uint64_t>(slot[u]) >= static_cast<uint64_t>(a.n_slots)) return;
-    const uint32_t page = static_cast<uint32_t>(slot[u] >> 4), place = static_cast<uint32_t>(slot[u]) & 15u;
-    codes0[static_cast<uint64_t>(page) * (page_rows * kRow) + place * kRow] = codes;
-    if ((j & 3) == 0) exponents0[static_cast<uint64_t>(page) * (page_rows * (HD / 32)) + place * (HD / 32)] = static_cast<uint8_t>(exponent);
-  };
   base += static_cast<int64_t>(group) * token_step;
   const int64_t next = static_cast<int64_t>(groups) * token_step;
-  if constexpr (VEC && sizeof(T) == 2 && !std::is_same<T, __half>::value) {
-    uint4 v[U];
-    uint32_t m[U], special = 0;
+  uint4 v[U][2];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int t = group + u * groups;
-      v[u] = make_uint4(0u, 0u, 0u, 0u);
-      if (t < tokens) v[u] = *reinterpret_cast<const uint4*>(base + u * next);
+  for (int u = 0; u < U; ++u) {
+    v[u][0] = v[u][1] = make_uint4(0u, 0u, 0u, 0u);
+    if (group + u * groups < tokens) {
+      v[u][0] = reinterpret_cast<const uint4*>(base + u * next)[0];
+      v[u][1] = reinterpret_cast<const uint4*>(base + u * next)[1];
     }
+  }
+  uint32_t m[U], special = 0;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      constexpr uint32_t kAbs = 0x7FFF7FFFu;
-      uint32_t most = max_bf16x2(max_bf16x2(v[u].x & kAbs, v[u].y & kAbs), max_bf16x2(v[u].z & kAbs, v[u].w & kAbs));
-      most = max_bf16x2(most, __shfl_xor_sync(0xffffffffu, most, 1));
-      most = max_bf16x2(most, __shfl_xor_sync(0xffffffffu, most, 2));
-      m[u] = max(most & 0xFFFFu, most >> 16);   // (bits without a sign: ordered as the values, NaN above all)
-      special = max(special, m[u]);
-    }
-    if (!__any_sync(0xffffffffu, special >= 0x7F80u)) {
+  for (int u = 0; u < U; ++u) {
+    constexpr uint32_t kAbs = 0x7FFF7FFFu;
+    uint32_t most = 0;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const uint32_t e = max((m[u] + 0x3Fu) >> 7, 2u) - 2u;
-        put(u, pairs_to_e2m1(v[u], (254u - e) * 0x00800080u), e);   // 2^(127 - e) in both halves
+    for (int h = 0; h < 2; ++h)
+      most = max_bf16x2(most, max_bf16x2(max_bf16x2(v[u][h].x & kAbs, v[u][h].y & kAbs), max_bf16x2(v[u][h].z & kAbs, v[u][h].w & kAbs)));
+    most = max_bf16x2(most, __shfl_xor_sync(0xffffffffu, most, 1));
+    m[u] = max(most & 0xFFFFu, most >> 16);   // (bits without a sign: ordered as the values, NaN above all)
+    special = max(special, m[u]);
+  }
+  // where a row's codes and exponents are: of page 0's place 0, and how far a page is
+  uint2* const codes0 = reinterpret_cast<uint2*>(a.pages) + (16 * r * kRow + j);
+  uint8_t* const exponents0 = a.exponents + (16 * r * (HD / 32) + (j >> 1));
+  const uint32_t page_rows = 32u * a.heads;   // (2^15 at most, and a page's number is below 2^30)
+  const bool odd = __any_sync(0xffffffffu, special >= 0x7F80u);
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    uint32_t e = max((m[u] + 0x3Fu) >> 7, 2u) - 2u;
+    uint2 codes;
+    if (!odd) {
+      const uint32_t f = (254u - e) * 0x00800080u;   // 2^(127 - e) in both halves
+      codes = make_uint2(pairs_to_e2m1(v[u][0], f), pairs_to_e2m1(v[u][1], f));
+    } else {   // something is not finite: the largest magnitude that is
+      float x[2][8], most = 0.f;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        const uint4& q = v[u][k / 8];
+        const uint32_t w = k % 8 / 2 == 0 ? q.x : k % 8 / 2 == 1 ? q.y : k % 8 / 2 == 2 ? q.z : q.w;
+        x[k / 8][k % 8] = __uint_as_float(k & 1 ? w & 0xFFFF0000u : w << 16);
+        if (fabsf(x[k / 8][k % 8]) < INFINITY) most = fmaxf(most, fabsf(x[k / 8][k % 8]));
       }
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-        float x[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = __uint_as_float(k & 1 ? w[k / 2] & 0xFFFF0000u : w[k / 2] << 16);
-        uint8_t e;
-        const uint32_t codes = block_of32(x, &e);
-        put(u, codes, e);
-      }
+      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+      const bool nan = m[u] > 0x7F80u;
+      const int power = nan ? 0 : block_exponent(most);
+      const float f = __uint_as_float(static_cast<uint32_t>(127 - power) << 23);
+      codes = make_uint2(e2m1_of8(x[0], f), e2m1_of8(x[1], f));
+      e = nan ? 255u : static_cast<uint32_t>(power + 127);
     }
-  } else {
-    float x[U][8];
+    if (static_cast<uint64_t>(slot[u]) >= static_cast<uint64_t>(a.n_slots)) continue;
+    const uint32_t page = static_cast<uint32_t>(slot[u] >> 4), place = static_cast<uint32_t>(slot[u]) & 15u;
+    codes0[static_cast<uint64_t>(page) * (page_rows * kRow) + place * kRow] = codes;
+    if ((j & 1) == 0) exponents0[static_cast<uint64_t>(page) * (page_rows * (HD / 32)) + place * (HD / 32)] = static_cast<uint8_t>(e);
+  }
+}
+
+// Other types and alignments: eight elements a thread (a block is four neighbouring lanes'), in 32 bits.
+template <typename T, int HD, int U, bool VEC>
+__global__ void __launch_bounds__(kThreads) write4_kernel(const __grid_constant__ WriteLaunch a, int32_t n_tokens, int32_t groups,
+                                                          int32_t at_once, FastDiv by_pieces) {
+  constexpr int kRow = HD / 8;
+  const int pieces = 2 * a.heads * kRow;
+  const int side = at_once > 1 ? static_cast<int>(by_pieces.div(threadIdx.x)) : 0;
+  const int group = blockIdx.x * at_once + side;
+  const int piece = threadIdx.x - side * pieces + blockIdx.y * kThreads;
+  const int r = piece / kRow, j = piece % kRow;
+  const int tokens = group < groups && side < at_once && piece < pieces ? n_tokens : 0;
+  const bool kv = r >= a.heads;
+  const T* base = (kv ? static_cast<const T*>(a.v) + (r - a.heads) * a.v_head : static_cast<const T*>(a.k) + r * a.k_head) + 8 * j;
+  const int64_t token_step = kv ? a.v_token : a.k_token;
+  base += static_cast<int64_t>(group) * token_step;
+  const int64_t next = static_cast<int64_t>(groups) * token_step;
+  int64_t slot[U];
+  float x[U][8];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int t = group + u * groups;
+  for (int u = 0; u < U; ++u) {
+    const int t = group + u * groups;
+    slot[u] = t < tokens ? __ldg(a.slots + t) : -1;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) x[u][k] = 0.f;
-      if (t < tokens) load_n<T, 8, VEC>(base + u * next, x[u]);
-    }
+    for (int k = 0; k < 8; ++k) x[u][k] = 0.f;
+    if (t < tokens) load_n<T, 8, VEC>(base + u * next, x[u]);
+  }
+  uint32_t* const codes0 = reinterpret_cast<uint32_t*>(a.pages) + (16 * r * kRow + j);
+  uint8_t* const exponents0 = a.exponents + (16 * r * (HD / 32) + (j >> 2));
+  const uint32_t page_rows = 32u * a.heads;
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      uint8_t e;
-      const uint32_t codes = block_of32(x[u], &e);
-      put(u, codes, e);
-    }
+  for (int u = 0; u < U; ++u) {
+    uint8_t e;
+    const uint32_t codes = block_of32(x[u], &e);
+    if (static_cast<uint64_t>(slot[u]) >= static_cast<uint64_t>(a.n_slots)) continue;
+    const uint32_t page = static_cast<uint32_t>(slot[u] >> 4), place = static_cast<uint32_t>(slot[u]) & 15u;
+    codes0[static_cast<uint64_t>(page) * (page_rows * kRow) + place * kRow] = codes;
+    if ((j & 3) == 0) exponents0[static_cast<uint64_t>(page) * (page_rows * (HD / 32)) + place * (HD / 32)] = e;
   }
 }
 
@@ -681,15 +716,19 @@ int launch_rope(const RopeLaunch& a, bool vec, unsigned grid, void* stream) {
 
 template <typename T>
 int launch_write4(const WriteLaunch& a, bool vec, int sms, void* stream) {
-  const int pieces = 2 * a.heads * (a.head_dim >> 3);
+  const bool in_pairs = vec && std::is_same<T, __nv_bfloat16>::value, wide = a.head_dim == 128;
+  const int pieces = 2 * a.heads * (a.head_dim / (in_pairs ? 16 : 8));
   // several tokens a thread where there are enough for four CTAs an SM all the same
-  const int u = a.n_tokens * pieces >= int64_t{16} * sms * kThreads ? 4 : 1;
+  constexpr int most = 2;
+  const int u = a.n_tokens * pieces >= int64_t{4} * most * sms * kThreads ? most : 1;
   const int groups = static_cast<int>((a.n_tokens + u - 1) / u), at_once = pieces < kThreads ? kThreads / pieces : 1;
-  const bool wide = a.head_dim == 128;
-  auto k = u == 4 ? (wide ? (vec ? write4_kernel<T, 128, 4, true> : write4_kernel<T, 128, 4, false>)
-                          : (vec ? write4_kernel<T, 64, 4, true> : write4_kernel<T, 64, 4, false>))
-                  : (wide ? (vec ? write4_kernel<T, 128, 1, true> : write4_kernel<T, 128, 1, false>)
-                          : (vec ? write4_kernel<T, 64, 1, true> : write4_kernel<T, 64, 1, false>));
+  auto k = wide ? (u == 1 ? (vec ? write4_kernel<T, 128, 1, true> : write4_kernel<T, 128, 1, false>)
+                          : (vec ? write4_kernel<T, 128, most, true> : write4_kernel<T, 128, most, false>))
+                : (u == 1 ? (vec ? write4_kernel<T, 64, 1, true> : write4_kernel<T, 64, 1, false>)
+                          : (vec ? write4_kernel<T, 64, most, true> : write4_kernel<T, 64, most, false>));
+  if (in_pairs)
+    k = wide ? (u == 1 ? write4_pairs_kernel<128, 1> : write4_pairs_kernel<128, most>)
+             : (u == 1 ? write4_pairs_kernel<64, 1> : write4_pairs_kernel<64, most>);
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>((groups + at_once - 1) / at_once), static_cast<unsigned>((pieces + kThreads - 1) / kThreads));
   cfg.blockDim = dim3(kThreads);

@@ -1,11 +1,17 @@
 // The pages' bookkeeping between two steps of a search: kvprm_cache_fork (sequences dropped, doubled and given room) and
 // kvprm_cache_compact (pages in use moved to the pool's beginning).
 //
-// Either is two launches.  The first works out tables, references and who is copied where: one cluster of CTAs, whose
-// barrier separates the steps, because each step needs what all threads found in the one before and the whole is a few
-// thousand to a few hundred thousand numbers.  The second writes the tables and copies pages, warp by warp in pieces of 4 KB,
-// over all layers of all pools; it is launched beside the first one's end and learns there how many there are.  Nothing is decided by who
-// comes first: counts are sums, of several that want a page the lowest sequence has it, free pages go by their numbers.
+// Either is two launches.  The first works out references and who is copied where: one cluster of CTAs, whose barrier
+// separates the steps, because each step needs what all threads found in the one before and the whole is a few thousand to a few
+// hundred thousand numbers.  The second writes the tables and copies pages, warp by warp in pieces of 4 KB, over all layers of all
+// pools; it is launched beside the first one's end and learns there how many there are.  (Few of both are the cluster's too.)
+// Nothing is decided by who comes first: counts are sums, of several that want a page the lowest sequence has it, free pages go
+// by their numbers.
+//
+// What bounds them, measured on a GB300: memory, once copies are many (462 pages of 0.46 MB compacted in 76 us, 67 of them the
+// copies', 6,400 GB/s; 217 pages of 0.92 MB copied in a fork of 64 sequences into 256 in 54 us, 43 of them 199 MB written from
+// pages that L2 keeps); the steps' latencies before that, 7 to 10 us of a fork and 5 of a compaction (four and three cluster barriers,
+// each behind loads or atomics of the step).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -20,6 +26,7 @@ namespace {
 constexpr int kThreads = 1024, kCluster = 8;
 constexpr int kCopyCtas = 4;       // of an SM
 constexpr int kMost = 1 << 24;     // pages of a block table
+constexpr int kSmall = 1024;       // pieces, or segments of tables, that the cluster alone sees to
 constexpr int kPage = 16, kNobody = 0x7FFFFFFF;
 constexpr int kCopyThreads = 256, kCopyUnroll = 8, kPiece = 32 * 16 * kCopyUnroll;   // of a warp: 4 KB
 
@@ -149,13 +156,13 @@ struct Heir {
   }
 };
 
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 1) fork_kernel(const __grid_constant__ ForkLaunch a) {
+// Everything but the tables and the copies.
+__device__ __forceinline__ void plan(const ForkLaunch& a) {
   __shared__ uint64_t s_warp[32], s_need[kCluster], s_free[kCluster], s_lacking[kCluster];
   __shared__ int32_t s_heirs[KVPRM_MAX_SEQS];   // of each sequence: every CTA counts all
   const kvprm_fork& f = a.f;
   const int me = cluster_thread();
   const int n_pages = static_cast<int>(f.n_pages);
-  grid_dep_launch();
   // (what hangs on nothing is loaded first)
   const int i = Range(f.n_new).mine();   // this thread's new sequence (there are no more of them than threads)
   const int32_t refs0 = me < n_pages ? __ldg(f.refs + me) : 0, parent0 = static_cast<int>(threadIdx.x) < f.n_new ? __ldg(f.parents + threadIdx.x) : -1;
@@ -276,11 +283,10 @@ struct CompactLaunch {
   int2* pairs;
 };
 
-__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 1) compact_kernel(const __grid_constant__ CompactLaunch a) {
+__device__ __forceinline__ void plan(const CompactLaunch& a) {
   __shared__ uint64_t s_warp[32], s_live[kCluster], s_below;
   const kvprm_compact& f = a.f;
   const int me = cluster_thread(), n_pages = static_cast<int>(f.n_pages);
-  grid_dep_launch();
   const Range pages(n_pages);
   const int p0 = pages.mine(), refs0 = p0 < 0 ? 0 : __ldg(f.refs + p0);
   uint64_t total;
@@ -367,15 +373,12 @@ __device__ __forceinline__ int32_t copy_to(const CompactLaunch&, int32_t page) {
 __device__ __forceinline__ uint4 load_piece(const ForkLaunch&, const uint8_t* p) { return __ldcg(reinterpret_cast<const uint4*>(p)); }
 __device__ __forceinline__ uint4 load_piece(const CompactLaunch&, const uint8_t* p) { return __ldcs(reinterpret_cast<const uint4*>(p)); }
 
+// The copies, for warp `first` of `warps`.
 template <int N, typename T>
-__global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_kernel(const __grid_constant__ CopyLaunch<N> a, const __grid_constant__ T t) {
-  const int lane = threadIdx.x & 31;
-  const int64_t warp = static_cast<int64_t>(threadIdx.x >> 5) * gridDim.x + blockIdx.x, warps = static_cast<int64_t>(gridDim.x) * (kCopyThreads / 32);
-  grid_dep_wait();
-  tables(t, warp, warps);
-  const int per_copy = a.first[a.n_pools];
+__device__ __forceinline__ void copies(const CopyLaunch<N>& a, const T& t, int64_t first, int64_t warps) {
+  const int lane = threadIdx.x & 31, per_copy = a.first[a.n_pools];
   const int64_t items = static_cast<int64_t>(__ldcg(t.count)) * per_copy;
-  for (int64_t i = static_cast<int64_t>(blockIdx.x) * (kCopyThreads / 32) + (threadIdx.x >> 5); i < items; i += warps) {
+  for (int64_t i = first; i < items; i += warps) {
     const int64_t j = i / per_copy;
     int r = static_cast<int>(i - j * per_copy), k = 0;
     while (r >= a.first[k + 1]) ++k;
@@ -397,6 +400,30 @@ __global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_kernel(const __g
     for (int x = 0; x < kCopyUnroll; ++x)
       if (x * 512 < left) __stcs(reinterpret_cast<uint4*>(dst + x * 512), v[x]);
   }
+}
+
+template <typename T>
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 1) plan_kernel(const __grid_constant__ T t) {
+  grid_dep_launch();
+  plan(t);
+}
+template <int N, typename T>
+__global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_kernel(const __grid_constant__ CopyLaunch<N> a, const __grid_constant__ T t) {
+  const int warp = threadIdx.x >> 5;
+  const int64_t warps = static_cast<int64_t>(gridDim.x) * (kCopyThreads / 32);
+  grid_dep_wait();
+  tables(t, static_cast<int64_t>(warp) * gridDim.x + blockIdx.x, warps);
+  copies(a, t, static_cast<int64_t>(blockIdx.x) * (kCopyThreads / 32) + warp, warps);
+}
+// All of a small call by the cluster alone.
+template <typename T>
+__global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 1)
+    small_kernel(const __grid_constant__ CopyLaunch<kFewPools> a, const __grid_constant__ T t) {
+  plan(t);
+  step();
+  const int64_t warp = static_cast<int64_t>(threadIdx.x >> 5) * kCluster + cluster_rank();
+  tables(t, warp, kAll / 32);
+  copies(a, t, warp, kAll / 32);
 }
 
 // ---------------------------------------------------------------- host
@@ -460,39 +487,34 @@ int check_pools(const kvprm_pool* pools, int n, int64_t n_pages, CopyLaunch<KVPR
   return KVPRM_OK;
 }
 
-// `most`: pages that may be copied; `entries`: of the tables.
+// `most`: pages that may be copied; `entries`: of the tables.  One launch where both are few: a launch among others takes 8 us of a
+// stream's time, so a step of 16 sequences 9 instead of 16, while the cluster copies 4 MB in 8.
 template <typename T>
-cudaError_t launch_copy(const CopyLaunch<KVPRM_MAX_POOLS>& c, const T& t, int64_t most, int64_t entries, cudaStream_t stream) {
-  const int64_t work = std::max(c.first[c.n_pools] * most, (entries + 127) / 128);   // of warps
-  if (work == 0) return cudaSuccess;
+cudaError_t launch(const CopyLaunch<KVPRM_MAX_POOLS>& c, const T& t, int64_t most, int64_t entries, cudaStream_t stream) {
+  const int64_t pieces = c.first[c.n_pools] * most, work = std::max(pieces, (entries + 127) / 128);   // of warps
+  CopyLaunch<kFewPools> few;
+  few.n_pools = std::min(c.n_pools, kFewPools);
+  for (int k = 0; k < few.n_pools; ++k) few.pool[k] = c.pool[k];
+  for (int k = 0; k <= few.n_pools; ++k) few.first[k] = c.first[k];
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(kCluster);   // (the kernel's own cluster size)
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = stream;
+  if (c.n_pools <= kFewPools && work <= kSmall) return cudaLaunchKernelEx(&cfg, small_kernel<T>, few, t);
+  cudaError_t e = cudaLaunchKernelEx(&cfg, plan_kernel<T>, t);
   int dev = 0, sms = 0;
-  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
   if (e != cudaSuccess) return e;
-  cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(std::min<int64_t>((work + kCopyThreads / 32 - 1) / (kCopyThreads / 32), int64_t{sms} * kCopyCtas)));
   cfg.blockDim = dim3(kCopyThreads);
-  cfg.stream = stream;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  if (c.n_pools > kFewPools) return cudaLaunchKernelEx(&cfg, copy_kernel<KVPRM_MAX_POOLS, T>, c, t);
-  CopyLaunch<kFewPools> few;
-  few.n_pools = c.n_pools;
-  for (int k = 0; k < c.n_pools; ++k) few.pool[k] = c.pool[k];
-  for (int k = 0; k <= c.n_pools; ++k) few.first[k] = c.first[k];
-  return cudaLaunchKernelEx(&cfg, copy_kernel<kFewPools, T>, few, t);
-}
-
-template <typename K, typename A>
-cudaError_t launch_cluster(K kernel, const A& a, cudaStream_t stream) {
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3(kCluster);   // (the kernel's own cluster size)
-  cfg.blockDim = dim3(kThreads);
-  cfg.stream = stream;
-  return cudaLaunchKernelEx(&cfg, kernel, a);
+  return c.n_pools <= kFewPools ? cudaLaunchKernelEx(&cfg, copy_kernel<kFewPools, T>, few, t)
+                                : cudaLaunchKernelEx(&cfg, copy_kernel<KVPRM_MAX_POOLS, T>, c, t);
 }
 
 int64_t fork_bytes(const kvprm_fork& f) {
@@ -562,8 +584,7 @@ int kvprm_cache_fork(const kvprm_pool* pools, const kvprm_fork* f, void* workspa
   a.rows = w.take<int4>(f->n_new);
   a.pairs = w.take<int2>(f->n_new);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = launch_cluster(fork_kernel, a, st);
-  if (e == cudaSuccess) e = launch_copy(c, a, f->n_new, int64_t{f->n_new} * f->width, st);
+  const cudaError_t e = launch(c, a, f->n_new, int64_t{f->n_new} * f->width, st);
   return e == cudaSuccess ? KVPRM_OK : operator_fail(KVPRM_ECUDA, "%s: %s", who, cudaGetErrorString(e));
 }
 
@@ -593,8 +614,7 @@ int kvprm_cache_compact(const kvprm_pool* pools, const kvprm_compact* f, void* w
   a.high = w.take<int32_t>(f->n_pages);
   a.pairs = w.take<int2>(f->n_pages);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  cudaError_t e = launch_cluster(compact_kernel, a, st);
-  if (e == cudaSuccess) e = launch_copy(c, a, f->n_pages / 2, int64_t{f->n_seqs} * f->max_blocks, st);
+  const cudaError_t e = launch(c, a, f->n_pages / 2, int64_t{f->n_seqs} * f->max_blocks, st);
   return e == cudaSuccess ? KVPRM_OK : operator_fail(KVPRM_ECUDA, "%s: %s", who, cudaGetErrorString(e));
 }
 
