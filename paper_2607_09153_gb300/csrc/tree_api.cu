@@ -50,8 +50,10 @@ int sm_count(int* sms) {
 // 4-bit pages on registers (us a call, cut / whole).  Pairs that have a CTA each: 64 x 4 heads over ragged 500 tokens 17 / 12,
 // 1,000 19 / 16, 1,500 21.9 / 20.6, but 4 x 8 heads over 1,500 18 / 20; where CTAs have several: 64 x 8 heads over 300 24 / 22, 500
 // 27 / 29.  A cut pair's parts are warps': of 8 blocks at least (4: the same) and 64 at most (one sequence of 32,768 tokens of 4
-// heads: 16 parts 59, 32 37, 64 27).
-constexpr int kWhole4 = 72, kWholeMany4 = 24, kLeast4 = 8, kParts4 = 64;
+// heads: 16 parts 59, 32 37, 64 27).  More than 32 rows go to the tensor cores, but for caches so short that the latter's beginning
+// counts, where each tile of 32 rows has a CTA (tensor cores / registers: 4 x 2 heads with 144 rows over ragged 40 tokens 16.9 /
+// 10.3, 300 17.0 / 13.1, 1,000 19.9 / 23.2; 16 x 4 heads with 84 rows over 300 21.3 / 18.2, 1,000 24.8 / 27.2).
+constexpr int kShort4 = 28, kWhole4 = 72, kWholeMany4 = 24, kLeast4 = 8, kParts4 = 64;
 
 // More than 32 rows of a kv head go to the tensor cores (us a call, registers / tensor cores: 8 heads with 24 rows over ragged
 // 20,000 bf16 tokens 76 / 78, 8-bit 66 / 89; with 32 over 8 x 32,768 bf16 tokens 187 / 186, 8-bit 155 / 221; 4 heads with 63 over
@@ -64,6 +66,9 @@ int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   const int64_t rows = int64_t{t.max_drafts} * (t.n_q_heads / c.n_kv_heads);
   const bool e2m1 = c.format == KVPRM_CACHE_E2M1;
   p.tc = rows > 32 && c.n_pages > 0;
+  const int64_t len = std::min<int64_t>(t.max_len, int64_t{kTreePage} * t.max_blocks);
+  if (e2m1 && p.tc && ceil_div(len, kTreePage) + ceil_div(t.max_drafts, kTreePage) <= kShort4)
+    p.tc = int64_t{t.n_seqs} * c.n_kv_heads * ceil_div(rows, 32) > int64_t{sms} * tree_e2m1_per_sm(4);
   p.tiles8 = !e2m1 || p.tc ? 0 : rows > 16 ? 4 : rows > 8 ? 2 : 1;
   p.rows = p.tc ? 256 : p.tiles8 ? 8 * p.tiles8 : rows > 16 ? 32 : 16;
   const int64_t block = p.tc ? 128 : kTreePage, tiles = ceil_div(rows, p.tc ? 128 : p.rows), lead = 20;
@@ -72,12 +77,11 @@ int plan(const kvprm_cache& c, const kvprm_tree& t, int sms, TreePlan* out) {
   const int64_t line = depth * (p.tc ? 4 * ceil_div(tiles, 2) : tiles) * c.n_kv_heads;
   if (line > 0x7FFFFFFF) return operator_fail(KVPRM_ECAPACITY, "kvprm_tree: block tables of %d pages", t.max_blocks);
   p.seqs = static_cast<int>(std::min<int64_t>({t.n_seqs, kTreeSeqs, 0x7FFFFFFF / line}));
-  const int64_t len = std::min<int64_t>(t.max_len, int64_t{kTreePage} * t.max_blocks);
   const int64_t pairs = int64_t{p.seqs} * c.n_kv_heads * ceil_div(rows, p.rows);
   const int64_t blocks = ceil_div(len, block) + ceil_div(t.max_drafts, block);
   const int64_t most = int64_t{sms} * (p.tc ? 1 : e2m1 ? tree_e2m1_per_sm(p.tiles8) : tree_rows_per_sm(p.rows / 16));
   if (p.tiles8) {
-    const bool each = pairs <= most && rows <= p.rows;
+    const bool each = pairs <= most;
     p.whole = blocks > (each ? kWhole4 : kWholeMany4) ? 0 : each ? 2 : 1;
     const int64_t parts = std::min(pairs * blocks / kLeast4, pairs * kParts4);
     p.ctas = static_cast<int>(std::max<int64_t>(1, std::min(most, p.whole ? pairs : ceil_div(parts, kTreeE2m1Warps))));

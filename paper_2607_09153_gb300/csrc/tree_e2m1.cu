@@ -143,17 +143,20 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
   const int v_step = 2 * kRowBytes + (piece & 2 ? -32 : 32);
   int32_t u = direct ? 0 : shares.begin(me);
   const int32_t u_end = direct ? 1 : shares.begin(me + 1);
-  int s_at = direct ? blockIdx.x / a.n_kv : tree_find(s_off, a.n_seqs, u);
+  const int head_tiles = (a.t.max_drafts * a.group + G::ROWS - 1) / G::ROWS;   // (direct) CTAs of a kv head
+  int s_at = direct ? blockIdx.x / (a.n_kv * head_tiles) : tree_find(s_off, a.n_seqs, u);
   TreePart part;
   auto next_part = [&]() {
     if (!direct) return tree_next<G>(a, s_off, u, u_end, s_at, part);
     if (u++ > 0 || s_at >= a.n_seqs) return false;
     part.q = tree_seq<G::ROWS, G::BLOCK>(a, s_at);
-    part.g = blockIdx.x - s_at * a.n_kv;
+    const int rest = blockIdx.x - s_at * a.n_kv * head_tiles;
+    part.g = rest / head_tiles;
+    part.tp = rest - part.g * head_tiles;
     part.s = s_at;
-    part.tp = part.first = part.c0 = 0;
+    part.first = part.c0 = 0;
     part.tiles = part.weight = 1;
-    part.c1 = part.q.drafts > 0 ? part.q.blocks : 0;
+    part.c1 = part.tp < part.q.tiles ? part.q.blocks : 0;
     return part.c1 > 0;
   };
   while (next_part()) {

@@ -164,11 +164,14 @@ def test_refusals():
 
 # ---------------------------------------------------------------- attention
 @pytest.mark.parametrize("nq,nkv,hd", HEADS)
-def test_tree_small(nq, nkv, hd):
-    """Lengths about a page's and a block's ends, one token to a few."""
+@pytest.mark.parametrize("width", [None, 100])
+def test_tree_small(nq, nkv, hd, width):
+    """Lengths about a page's and a block's ends, one token to a few, on the kernels for short calls and on those for long ones."""
     torch, _ = _kp()
-    t = Tree4(torch, nq, nkv, hd, [0, 1, 15, 16, 17, 64, 65, 200], [1, 3, 2, 1, 17, 1, 5, 4], seed=nq + hd)
+    t = Tree4(torch, nq, nkv, hd, [0, 1, 15, 16, 17, 64, 65, 200], [1, 3, 2, 1, 17, 1, 5, 4], seed=nq + hd, max_blocks=width)
     t.check(t.run())
+    if width:
+        return
     t = Tree4(torch, nq, nkv, hd, [0, 1, 15, 16, 17, 64, 65, 200], [1] * 8, seed=nq + hd + 1)
     t.check(t.run())
 
@@ -239,11 +242,12 @@ def test_tree_powers_apart(apart, hd, drafts):
 
 
 @pytest.mark.parametrize("exponent", [100, 60, 8, -8, -40, -100, -126])
-@pytest.mark.parametrize("drafts", [1, 20])
-def test_tree_scales(exponent, drafts):
-    """A whole cache at one far power: values anywhere in the range, keys where queries make up for it."""
+@pytest.mark.parametrize("drafts,width", [(1, None), (20, None), (20, 100)])
+def test_tree_scales(exponent, drafts, width):
+    """A whole cache at one far power: values anywhere in the range, keys where queries make up for it.  (With a wide table many rows
+    go to the tensor cores.)"""
     torch, _ = _kp()
-    t = Tree4(torch, 2, 1, 128, [64, 17], [drafts, 1], seed=3, q_std=2.0 ** -max(-30, min(exponent, 100)))
+    t = Tree4(torch, 2, 1, 128, [64, 17], [drafts, 1], seed=3, q_std=2.0 ** -max(-30, min(exponent, 100)), max_blocks=width)
     t.exps[:, 0] = 127 + max(-30, exponent)
     t.exps[:, 1] = 127 + exponent
     t.remake()
@@ -253,11 +257,11 @@ def test_tree_scales(exponent, drafts):
     t.check(t.run())
 
 
-@pytest.mark.parametrize("drafts", [1, 2, 4, 20])
-def test_tree_zero_blocks(drafts):
+@pytest.mark.parametrize("drafts,width", [(1, None), (2, None), (4, None), (20, None), (20, 100)])
+def test_tree_zero_blocks(drafts, width):
     """Rows of zeros (exponent 0), whole pages of them, and the first page."""
     torch, _ = _kp()
-    t = Tree4(torch, 4, 2, 128, [200, 30, 16], [drafts] * 3, seed=21)
+    t = Tree4(torch, 4, 2, 128, [200, 30, 16], [drafts] * 3, seed=21, max_blocks=width)
     for b, j in ((0, 0), (0, 4), (1, 1), (2, 0)):
         p = int(t.table[b, j])
         t.pages[p], t.exps[p] = 0, 0
@@ -267,12 +271,12 @@ def test_tree_zero_blocks(drafts):
     t.check(t.run())
 
 
-@pytest.mark.parametrize("drafts", [1, 3, 6, 20])
-def test_tree_not_finite(drafts):
+@pytest.mark.parametrize("drafts,width", [(1, None), (3, None), (6, None), (20, None), (20, 100)])
+def test_tree_not_finite(drafts, width):
     """Drafts that are not finite reach the rows that see them and no others; a NaN in the cache reaches its sequence: a key's all
     of it, a value's the 32 dimensions of its block."""
     torch, _ = _kp()
-    t = Tree4(torch, 4, 2, 64, [50, 0, 33], [drafts, 40, 2], seed=6)
+    t = Tree4(torch, 4, 2, 64, [50, 0, 33], [drafts, 40, 2], seed=6, max_blocks=width)
     want, bound = t.want()
     hurt = torch.zeros(t.q.shape[0], dtype=torch.bool, device="cuda")
     for s, j, x, i in ((0, drafts // 2, t.v, math.nan), (0, drafts - 1, t.v, math.inf), (1, 35, t.k, math.nan), (1, 20, t.v, -math.inf)):
@@ -291,11 +295,12 @@ def test_tree_not_finite(drafts):
     assert bool(out[s2:, 2:].isnan().all()) and bool(((out.double() - want).abs() <= bound)[s2:, :2, :32].all())
 
 
-def test_tree_bad_tables():
+@pytest.mark.parametrize("width", [None, 100])
+def test_tree_bad_tables(width):
     """What the host cannot see: NaN for a sequence with a bad page or length, others untouched; bad drafts left out."""
     torch, _ = _kp()
     for drafts in ([3, 4, 5, 40], [1, 1, 2, 1]):
-        t = Tree4(torch, 4, 2, 64, [50, 40, 33, 300], drafts, seed=8)
+        t = Tree4(torch, 4, 2, 64, [50, 40, 33, 300], drafts, seed=8, max_blocks=width)
         want, bound = t.want()
         i32 = lambda x: torch.tensor(x, dtype=torch.int32).cuda()  # noqa: E731
         fine = lambda o, s: bool(((o.double() - want).abs() <= bound)[t.start[s]:t.start[s + 1]].all())  # noqa: E731
