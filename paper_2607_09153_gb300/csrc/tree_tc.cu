@@ -475,7 +475,7 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
       };
       uint32_t bad = 0;   // items (modulo 4) with a page outside the cache
       uint4 next[kSteps];
-      uint32_t next_e = 0;   // (4-bit: a byte for each step)
+      uint32_t next_e[E2M1 ? kSteps : 1] = {};   // (as loaded: to put a 4-bit cache's two together is to wait for them)
       auto load = [&](int item, int32_t page) {
         if (page == -2) bad |= 1u << (item & 3);
         if (page < 0) return;
@@ -486,11 +486,10 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
 #pragma unroll
         for (int k = 0; k < kSteps; ++k) next[k] = ldg_stream(src + k * 512);
         if constexpr (E2M1) {
-          next_e = 0;
 #pragma unroll
-          for (int k = 0; k < kSteps; ++k) next_e |= static_cast<uint32_t>(__ldg(a.exponents + row * kParts + k * 32 + lane)) << (8 * k);
+          for (int k = 0; k < kSteps; ++k) next_e[k] = __ldg(a.exponents + row * kParts + k * 32 + lane);
         } else {
-          next_e = __ldg(a.exponents + row + lane % kTreePage);
+          next_e[0] = __ldg(a.exponents + row + lane % kTreePage);
         }
       };
       int32_t page = -1;
@@ -537,7 +536,10 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
           uint4 codes[kSteps];
 #pragma unroll
           for (int k = 0; k < kSteps; ++k) codes[k] = next[k];
-          const uint32_t e = next_e;
+          uint32_t es[E2M1 ? kSteps : 1];
+#pragma unroll
+          for (int k = 0; k < (E2M1 ? kSteps : 1); ++k) es[k] = next_e[k];
+          const uint32_t e = es[0];
           load(item + 1, page);
           page = page_of(item + 2);
           if (cached) {
@@ -548,7 +550,7 @@ __global__ void __launch_bounds__(640, 1) tree_tc_kernel(const __grid_constant__
               bool two = false;
 #pragma unroll
               for (int k = 0; k < kSteps; ++k) {
-                const uint32_t x = (e >> (8 * k)) & 255u;
+                const uint32_t x = es[k];
                 const bool live = my_page * kTreePage + kTeam * k + my_row < p.q.len - c * kChunk, more = x > 128u && live;
                 f[k] = (more ? 254u : x + 126u) << 7 | (more ? (x == 255u ? 0x7FC0u : (x - 1u) << 7) : 0x3F80u) << 16;
                 if (!live) f[k] = 0x3F800000u;
