@@ -286,6 +286,7 @@ struct CompactLaunch {
 __device__ __forceinline__ void plan(const CompactLaunch& a) {
   __shared__ uint64_t s_warp[32], s_live[kCluster], s_below;
   const kvprm_compact& f = a.f;
+  cluster_arrive();   // (the CTAs tell each other something only when all have begun)
   const int me = cluster_thread(), n_pages = static_cast<int>(f.n_pages);
   const Range pages(n_pages);
   const int p0 = pages.mine(), refs0 = p0 < 0 ? 0 : __ldg(f.refs + p0);
@@ -296,6 +297,8 @@ __device__ __forceinline__ void plan(const CompactLaunch& a) {
     const int p = q + static_cast<int>(threadIdx.x);
     used += __syncthreads_count(p < pages.hi && __ldg(f.refs + p) > 0);
   }
+  __syncwarp();
+  cluster_wait();
   if (threadIdx.x == 0) tell(s_live, used);
   step();
   const int live = static_cast<int>(sum_told(s_live));
