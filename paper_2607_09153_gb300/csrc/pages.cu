@@ -508,7 +508,7 @@ cudaError_t launch(const CopyLaunch<KVPRM_MAX_POOLS>& c, const T& t, int64_t mos
   int dev = 0, sms = 0;
   if (e == cudaSuccess) e = cudaGetDevice(&dev);
   if (e == cudaSuccess) e = cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
-  if (e != cudaSuccess) return e;
+  if (e != cudaSuccess || work == 0) return e;   // (no tables, no copies)
   cfg.gridDim = dim3(static_cast<unsigned>(std::min<int64_t>((work + kCopyThreads / 32 - 1) / (kCopyThreads / 32), int64_t{sms} * kCopyCtas)));
   cfg.blockDim = dim3(kCopyThreads);
   cudaLaunchAttribute attr;

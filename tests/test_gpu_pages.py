@@ -190,6 +190,17 @@ def test_fork_of_a_large_pool():
     assert out[0].tolist() == [[n - 2], [n - 1]] and bool((pool[0, n - 1] == 3.0).all())
 
 
+def test_nothing_to_do_in_many_pools():
+    """Every sequence dropped, and none to begin with, with layers that were allocated apart."""
+    torch, kp = _kp()
+    s = Search(torch, [40, 20], seed=8, layers=7)
+    s.pools = [p[i:i + 1] for p in s.pools for i in range(7)]
+    _fork(s, [])
+    e = torch.empty((0, 4), dtype=torch.int32, device="cuda")
+    out = kp.cache_compact([p[:, :1] for p in s.pools], s.i32([2]), e, e[:, 0].contiguous())
+    assert [x.tolist() for x in out] == [[], [2], [0], [1, 0]]
+
+
 @pytest.mark.parametrize("seed", range(8))
 @pytest.mark.parametrize("fmt", ["4", "16"])
 def test_compact(seed, fmt):
