@@ -284,8 +284,8 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
       }
       most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
       most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-      int e = static_cast<int>(__float_as_uint(most) >> 23);   // (infinite or all zero: any scale does)
-      e = e < 1 || e > 253 ? 127 : e;
+      // (2^(127 - e) has to be a normal number; all zero or infinite: any scale does)
+      const int e = min(max(static_cast<int>(__float_as_uint(most) >> 23), 1), 253);
       rs[nt][0] = __shfl_sync(0xffffffffu, power_of(e), 8 * c) * fabsf(a.scale_log2);
       rs[nt][1] = __shfl_sync(0xffffffffu, power_of(e), 8 * c + 4) * fabsf(a.scale_log2);
       const float up = a.scale_log2 < 0.f ? -power_of(254 - e) : power_of(254 - e);

@@ -257,6 +257,21 @@ def test_tree_scales(exponent, drafts, width):
     t.check(t.run())
 
 
+@pytest.mark.parametrize("drafts,width", [(1, None), (4, None), (20, None), (20, 100)])
+@pytest.mark.parametrize("up", [True, False])
+def test_tree_far_queries(up, drafts, width):
+    """Queries at the ends of bf16's range, whole ones beyond 2^127 or below 2^-126, with keys that make up for it."""
+    torch, _ = _kp()
+    t = Tree4(torch, 4, 2, 128, [300, 17, 0], [drafts, 1, 2], seed=31, max_blocks=width)
+    power = 125 if up else -130
+    t.q = (t.q.double() * 2.0 ** power).clamp(-3e38, 3e38).bfloat16()
+    t.exps[:, 0] = t.exps[:, 0].int().add(-120 if up else 120).to(torch.uint8)
+    t.k.mul_(2.0 ** (-120 if up else 120))
+    t.remake()
+    scale = 2.0 ** (-5 if up else 10) * 128 ** -0.5
+    t.check(t.run(scale=scale), scale)
+
+
 @pytest.mark.parametrize("drafts,width", [(1, None), (2, None), (4, None), (20, None), (20, 100)])
 def test_tree_zero_blocks(drafts, width):
     """Rows of zeros (exponent 0), whole pages of them, and the first page."""
