@@ -633,7 +633,10 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
     copies_wait<0>();
 
     // ---- drafted tokens: bf16 rows of their own tensors, whatever the cache holds
-    if (ev == 0) ev = 127;
+    if (ev < 127) {   // (drafted values times a larger power might not be finite)
+      if (ev > 0) scale_outputs(power_of(ev));
+      ev = 127;
+    }
     const float rel = power_of(254 - ev);   // what the outputs are kept in, over the values' own
     for (int b = c0 + mine; b < c1; ++b) {
       const int j0 = (b - q.cached_blocks) * kTreePage, have = q.drafts - j0;

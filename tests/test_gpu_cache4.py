@@ -272,6 +272,18 @@ def test_tree_far_queries(up, drafts, width):
     t.check(t.run(scale=scale), scale)
 
 
+@pytest.mark.parametrize("drafts,width", [(1, None), (4, None), (20, None), (20, 100)])
+@pytest.mark.parametrize("mask", ["tree", "none"])
+def test_tree_drafts_beyond_the_cache(mask, drafts, width):
+    """Drafted values 2^160 of the cached ones, seen and not seen."""
+    torch, _ = _kp()
+    t = Tree4(torch, 4, 2, 128, [300, 17, 40], [drafts, 1, 2], mask=mask, seed=32, max_blocks=width)
+    t.exps[:, 1] -= 60
+    t.remake()
+    t.v.mul_(2.0 ** 100)
+    t.check(t.run())
+
+
 @pytest.mark.parametrize("drafts,width", [(1, None), (2, None), (4, None), (20, None), (20, 100)])
 def test_tree_zero_blocks(drafts, width):
     """Rows of zeros (exponent 0), whole pages of them, and the first page."""
