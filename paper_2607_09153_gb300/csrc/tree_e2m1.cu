@@ -26,7 +26,8 @@
 // over 8 x 32,768 tokens of 8 heads 66 us (4,300 GB/s), four (16 rows) 85, eight (32 rows) 140; 64 ragged sequences up to 9,001
 // of 4 heads 49 us.  Tried: fragments loaded straight into registers, a page ahead (75 us for the first of these: the loads
 // share scoreboards) or in single pages (84); four CTAs an SM (81: spills); the next step's scores beside this one's product
-// (74); CTAs instead of warps as shares (72; the ragged ones 58, for a part then costs 4 us of barriers).
+// (74); CTAs instead of warps as shares (72; the ragged ones 58, for a part then costs 4 us of barriers); two CTAs of six
+// or seven warps (65.6, and 76: spills); a page's scores in two chains of products (the same).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>

@@ -18,8 +18,9 @@
 // shared memory's bandwidth), softmax (1,500) and O (500), 3,400 cycles a chunk for both groups: 8 kv heads, 64
 // tokens of 4 heads each over 4 x 16,384 bf16 tokens in 80 us, 860 TFLOP/s.  An 8-bit chunk: its conversion, some
 // 1,800 cycles of the eight producer warps for a tile of 128 x 128, which beside two tiles' products takes
-// 2,800: 16 sequences of 4 heads with 126 rows over 9,001 tokens in 86 us (bf16: 70).  Short calls: what a part
-// begins and ends with, 5 and 2 us, and the join.
+// 2,800: 16 sequences of 4 heads with 126 rows over 9,001 tokens in 86 us (bf16: 70).  A 4-bit one costs as
+// much: 16 ragged sequences up to 16,384 of 4 heads with 448 rows in 159 us (8 bits 160; 141 with the
+// conversion taken out).  Short calls: what a part begins and ends with, 5 and 2 us, and the join.
 #include <cuda.h>
 #include <cudaTypedefs.h>
 #include <cuda_bf16.h>
