@@ -49,11 +49,11 @@ int sm_count(int* sms) {
 
 // 4-bit pages on registers (us a call, cut / whole).  Pairs that have a CTA each: 64 x 4 heads over ragged 500 tokens 17 / 12,
 // 1,000 19 / 16, 1,500 21.9 / 20.6, but 4 x 8 heads over 1,500 18 / 20; where CTAs have several: 64 x 8 heads over 300 24 / 22, 500
-// 27 / 29.  A cut pair's parts are warps': of 8 blocks at least (4: the same) and 64 at most (one sequence of 32,768 tokens of 4
-// heads: 16 parts 59, 32 37, 64 27).  More than 32 rows go to the tensor cores, but for caches so short that the latter's beginning
+// 27 / 29.  A cut pair's parts are warps': of 8 blocks at least (5: the same) and 128 at most (one sequence of 32,768 tokens of 4
+// heads: 32 parts 34, 64 24, 128 21, 256 24; of 120,000 64 57, 128 38, 256 36).  More than 32 rows go to the tensor cores, but for caches so short that the latter's beginning
 // counts, where each tile of 32 rows has a CTA (tensor cores / registers: 4 x 2 heads with 144 rows over ragged 40 tokens 16.9 /
 // 10.3, 300 17.0 / 13.1, 1,000 19.9 / 23.2; 16 x 4 heads with 84 rows over 300 21.3 / 18.2, 1,000 24.8 / 27.2).
-constexpr int kShort4 = 28, kWhole4 = 72, kWholeMany4 = 24, kLeast4 = 8, kParts4 = 64;
+constexpr int kShort4 = 28, kWhole4 = 72, kWholeMany4 = 24, kLeast4 = 8, kParts4 = 128;
 
 // More than 32 rows of a kv head go to the tensor cores (us a call, registers / tensor cores: 8 heads with 24 rows over ragged
 // 20,000 bf16 tokens 76 / 78, 8-bit 66 / 89; with 32 over 8 x 32,768 bf16 tokens 187 / 186, 8-bit 155 / 221; 4 heads with 63 over

@@ -23,8 +23,8 @@
 // What bounds it, measured on a GB300, is instructions: a page of a kv head takes some 295 of a warp (64 conversions, 64
 // multiplications by powers, 16 matrix instructions, 16 to put nibbles together, 20 of the softmax, 29 loads and copies), 0.60 of
 // the issue slots with the three warps a scheduler that 163 registers leave (ALU pipe 0.49, DRAM 0.45).  One drafted token
-// over 8 x 32,768 tokens of 8 heads 66 us (4,300 GB/s), four (16 rows) 85, eight (32 rows) 140; 64 ragged sequences up to 9,001
-// of 4 heads 49 us.  Tried: fragments loaded straight into registers, a page ahead (75 us for the first of these: the loads
+// over 8 x 32,768 tokens of 8 heads 64 us (4,490 GB/s), four (16 rows) 84, eight (32 rows) 139; 64 ragged sequences up to 9,001
+// of 4 heads 48 us; one sequence of 32,768 of 4 heads 21.  Tried: fragments loaded straight into registers, a page ahead (75 us for the first of these: the loads
 // share scoreboards) or in single pages (84); four CTAs an SM (81: spills); the next step's scores beside this one's product
 // (74); CTAs instead of warps as shares (72; the ragged ones 58, for a part then costs 4 us of barriers); two CTAs of six
 // or seven warps (65.6, and 76: spills); a page's scores in two chains of products (the same).
@@ -811,72 +811,70 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
   }
 }
 
-// Joins the partial results of pairs that several warps shared, eight rows and 32 dims of a pair a CTA: launched beside the
-// attention kernel's end, it waits for it; each warp takes every fourth part, in order, and the four states meet in shared
-// memory, so the result does not depend on who was last.  A lane has 8 dims of a row, and four parts' loads in flight.
-constexpr int kJoinAhead = 4, kJoinDims = 32;
-template <int HD, int NT>
-__global__ void __launch_bounds__(kThreads) tree_e2m1_join_kernel(const __grid_constant__ TreeLaunch a, int groups) {
+// Joins the partial results of pairs that several warps shared, eight rows and 64 dims of a pair a CTA: launched beside the
+// attention kernel's end, it waits for it; each of W warps takes every W-th part, in order, and their states meet in shared
+// memory, so the result does not depend on who was last.  A lane has four times four dims of a row, 16 apart.
+//
+// What it costs is latencies: 5 us of the 48 of 64 ragged sequences of 4 heads (256 pairs of some eight parts), of which 1.4 are a
+// launch's and 2 the line's.  Eight warps, or sixteen where so few CTAs leave SMs idle (that call / one sequence of 32,768 tokens with 64
+// parts a pair: eight 47.7 / 26.2, sixteen 50.5 / 24.4; four with 32 dims and four parts ahead 48.6 / 27.4; eight with 128 dims 48.2 / 29.5).
+constexpr int kJoinDims = 64, kJoinFew = 128;
+template <int HD, int NT, int W>
+__global__ void __launch_bounds__(32 * W) tree_e2m1_join_kernel(const __grid_constant__ TreeLaunch a, int groups) {
   using G = TreeE2m1<NT>;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, d0 = blockIdx.y * kJoinDims + (lane & 3) * 8;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, d0 = blockIdx.y * kJoinDims + (lane & 3) * 4;
   const int group = blockIdx.x % groups, head = blockIdx.x / groups, g = head % a.n_kv, s = head / a.n_kv;
   const TreeSeq q = tree_seq<G::ROWS, G::BLOCK>(a, s);
   const int rows = q.drafts * a.group, row = 8 * group + r, tp = 8 * group / G::kSlotRows, slot_row = row - tp * G::kSlotRows;
   grid_dep_wait();   // no launch of this kernel ends before the attention kernel
-  if (8 * group >= rows) return;
   const int32_t off = __ldcg(a.line + s), total = __ldcg(a.line + a.n_seqs), ctas = __ldcg(a.line + a.n_seqs + 1);
+  if (8 * group >= rows) return;
   const TreeShares shares(total, ctas, 1);
   const int32_t first = off + (q.blocks + G::LEAD) * (g * q.tiles + tp) + G::LEAD;   // (a place is a block: weights of 1)
   const int i0 = shares.owner(first), i1 = shares.owner(first + q.blocks - 1);
   if (i0 == i1) return;   // whole: written by its warp
-  __shared__ float s_o[kWarps][32][9];
-  __shared__ float2 s_ml[kWarps][8];
-  float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, best = -INFINITY, sum = 0.f;
+  __shared__ float s_o[W][32][17];
+  __shared__ float2 s_ml[W][8];
+  float o[16] = {}, best = -INFINITY, sum = 0.f;
 #pragma unroll 1
-  for (int i = i0 + warp; i <= i1; i += kJoinAhead * kWarps) {
-    float4 v[kJoinAhead][2];
-    float2 ml[kJoinAhead];
+  for (int part = i0 + warp; part <= i1; part += W) {
+    const int64_t at = (part == i0 ? 2 * i0 + 1 : 2 * part) * static_cast<int64_t>(G::kSlotRows) + slot_row;
+    const float2 ml = __ldcg(a.part_ml + at);
+    float4 v[4];
 #pragma unroll
-    for (int x = 0; x < kJoinAhead; ++x) {
-      const int part = min(i + x * kWarps, i1);
-      const int64_t at = (part == i0 ? 2 * i0 + 1 : 2 * part) * static_cast<int64_t>(G::kSlotRows) + slot_row;
-      ml[x] = __ldcg(a.part_ml + at);
-      v[x][0] = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * HD + d0));
-      v[x][1] = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * HD + d0) + 1);
-    }
+    for (int d = 0; d < 4; ++d) v[d] = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * HD + d0 + 16 * d));
+    const float now = fmaxf(best, ml.x);   // -infinity: nothing seen so far (a sum of zero, or NaN)
+    const float f = best == -INFINITY ? 0.f : ex2_ftz(best - now), e = ml.x == -INFINITY ? 0.f : ex2_ftz(ml.x - now);
+    best = now;
+    sum = sum * f + ml.y * e;
 #pragma unroll
-    for (int x = 0; x < kJoinAhead; ++x) {
-      if (i + x * kWarps > i1) break;
-      const float now = fmaxf(best, ml[x].x);   // -infinity: nothing seen so far (a sum of zero, or NaN)
-      const float f = best == -INFINITY ? 0.f : ex2_ftz(best - now), e = ml[x].x == -INFINITY ? 0.f : ex2_ftz(ml[x].x - now);
-      best = now;
-      sum = sum * f + ml[x].y * e;
-      const float y[8] = {v[x][0].x, v[x][0].y, v[x][0].z, v[x][0].w, v[x][1].x, v[x][1].y, v[x][1].z, v[x][1].w};
-#pragma unroll
-      for (int d = 0; d < 8; ++d) o[d] = o[d] * f + y[d] * e;
+    for (int d = 0; d < 4; ++d) {
+      o[4 * d] = o[4 * d] * f + v[d].x * e;
+      o[4 * d + 1] = o[4 * d + 1] * f + v[d].y * e;
+      o[4 * d + 2] = o[4 * d + 2] * f + v[d].z * e;
+      o[4 * d + 3] = o[4 * d + 3] * f + v[d].w * e;
     }
   }
 #pragma unroll
-  for (int d = 0; d < 8; ++d) s_o[warp][lane][d] = o[d];
+  for (int d = 0; d < 16; ++d) s_o[warp][lane][d] = o[d];
   if ((lane & 3) == 0) s_ml[warp][r] = make_float2(best, sum);
   __syncthreads();
-  if (warp > 0 || row >= rows) return;
-  float top = -INFINITY, all = 0.f, y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (warp >= 4 || row >= rows) return;   // a warp for each of the lanes' fours
+  float top = -INFINITY, all = 0.f, y[4] = {};
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_ml[w][r].x);
+  for (int w = 0; w < W; ++w) top = fmaxf(top, s_ml[w][r].x);
 #pragma unroll
-  for (int w = 0; w < kWarps; ++w) {
+  for (int w = 0; w < W; ++w) {
     const float f = s_ml[w][r].x == -INFINITY ? 0.f : ex2_ftz(s_ml[w][r].x - top);   // (NaN sums stay NaN)
     all += s_ml[w][r].y * f;
 #pragma unroll
-    for (int d = 0; d < 8; ++d) y[d] += s_o[w][lane][d] * f;
+    for (int d = 0; d < 4; ++d) y[d] += s_o[w][lane][4 * warp + d] * f;
   }
   const float inv = all == 0.f ? 0.f : 1.f / all;
   const int tok = tree_token(a, row);
   __nv_bfloat16* dst = static_cast<__nv_bfloat16*>(a.t.out) + (q.start + static_cast<int64_t>(tok)) * a.t.out_token +
-                       (g * a.group + row - tok * a.group) * a.t.out_head + d0;
-  *reinterpret_cast<uint4*>(dst) = make_uint4(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv),
-                                              pack_bf16(y[4] * inv, y[5] * inv), pack_bf16(y[6] * inv, y[7] * inv));
+                       (g * a.group + row - tok * a.group) * a.t.out_head + d0 + 16 * warp;
+  *reinterpret_cast<uint2*>(dst) = make_uint2(pack_bf16(y[0] * inv, y[1] * inv), pack_bf16(y[2] * inv, y[3] * inv));
 }
 
 template <int HD, int NT>
@@ -884,14 +882,15 @@ cudaError_t launch_join(const TreeLaunch& a, cudaStream_t stream) {
   const int groups = (a.t.max_drafts * a.group + 7) / 8;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(static_cast<int64_t>(a.n_seqs) * a.n_kv * groups), HD / kJoinDims);
-  cfg.blockDim = dim3(kThreads);
+  const bool few = int64_t{cfg.gridDim.x} * cfg.gridDim.y <= kJoinFew;
+  cfg.blockDim = dim3(few ? 512 : 256);
   cfg.stream = stream;
   cudaLaunchAttribute attr;
   attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
   attr.val.programmaticStreamSerializationAllowed = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, tree_e2m1_join_kernel<HD, NT>, a, groups);
+  return cudaLaunchKernelEx(&cfg, few ? tree_e2m1_join_kernel<HD, NT, 16> : tree_e2m1_join_kernel<HD, NT, 8>, a, groups);
 }
 
 template <int HD, int NT, bool WHOLE>
