@@ -201,6 +201,26 @@ def test_nothing_to_do_in_many_pools():
     assert [x.tolist() for x in out] == [[], [2], [0], [1, 0]]
 
 
+@pytest.mark.parametrize("m,width", [(3, 5), (1, 1), (0, 7)])
+def test_results_are_tensors_like_others(m, width):
+    """Results of odd sizes, written in place, and handed to the next calls."""
+    torch, kp = _kp()
+    s = Search(torch, [10, 0], seed=2, spare=5, width=3)
+    refs, table, lens = s.tensors()
+    room = s.i32([16] * m)
+    table, lens, refs, counts = kp.cache_fork(s.pools, refs, table, lens, s.i32([0] * m), room, width=width)
+    lens.add_(6)
+    refs[s.n - 1] = 1
+    counts.zero_()
+    table[:, -1:] = -1
+    assert table.is_contiguous() and tuple(table.shape) == (m, width) and lens.tolist() == [16] * m and counts.tolist() == [0, 0]
+    now = Pool(refs.tolist(), table.tolist(), lens.tolist())
+    out = kp.cache_compact(s.pools, refs, table, lens)
+    assert [x.tolist() for x in out] == [list(x) for x in now.compact()[:4]]
+    want = now.fork([-1] * m, [17] * m, width)
+    assert [x.tolist() for x in kp.cache_fork(s.pools, refs, table, lens, s.i32([-1] * m), s.i32([17] * m))] == list(want[:4])
+
+
 @pytest.mark.parametrize("seed", range(8))
 @pytest.mark.parametrize("fmt", ["4", "16"])
 def test_compact(seed, fmt):
