@@ -96,16 +96,19 @@ __device__ __forceinline__ uint64_t sum_told(const uint64_t* told) {
   return sum;
 }
 
-// Calls f(row, begin, end, lane) for each row of a table in segments of 128 entries, for warp `warp` of `warps`.
+// Calls f(row, begin, end, lane) for each row of a table in segments of 128 entries (2^30 at most), for warp `warp` of `warps`.
+constexpr int kSegment = 128;
+static_assert(int64_t{KVPRM_MAX_SEQS} * (kMost / kSegment) <= 1 << 30, "segments");
 template <typename F>
-__device__ __forceinline__ void each_segment(int rows, int width, int64_t warp, int64_t warps, F f) {
-  constexpr int kSegment = 128;
-  const int per_row = (width + kSegment - 1) / kSegment, lane = threadIdx.x & 31;
-  for (int64_t i = warp; i < static_cast<int64_t>(rows) * per_row; i += warps) {
-    const int row = static_cast<int>(i / per_row), begin = static_cast<int>(i - static_cast<int64_t>(row) * per_row) * kSegment;
-    f(row, begin, min(width, begin + kSegment), lane);
+__device__ __forceinline__ void each_segment(int rows, int width, uint32_t warp, uint32_t warps, F f) {
+  const uint32_t per_row = (width + kSegment - 1) / kSegment, lane = threadIdx.x & 31;
+  for (uint32_t i = warp; i < rows * per_row; i += warps) {
+    const uint32_t row = i / per_row;
+    const int begin = static_cast<int>(i - row * per_row) * kSegment;
+    f(static_cast<int>(row), begin, min(width, begin + kSegment), static_cast<int>(lane));
   }
 }
+constexpr uint32_t kOnce = 1u << 31;   // `warps` for a warp's first segment alone
 
 // ---------------------------------------------------------------- fork
 // A new sequence's row, as the last step writes it: its parent (-1: none), pages taken over, pages in all, its place among the
@@ -178,21 +181,40 @@ __device__ __forceinline__ void plan(const ForkLaunch& a) {
     f.refs_out[p] = p == me ? refs0 : __ldg(f.refs + p);
     a.first[p] = kNobody;
   }
+  // (the warp's first segment of the old tables is on its way over the barrier)
+  const uint32_t warp = (threadIdx.x >> 5) * kCluster + cluster_rank();
+  constexpr int kFirst = kSegment / 32;
+  int32_t ahead[kFirst];
+  each_segment(f.n_seqs, f.max_blocks, warp, kOnce, [&](int s, int begin, int end, int lane) {
+    const int stop = min(end, Held(f, s).pages);
+#pragma unroll
+    for (int x = 0; x < kFirst; ++x) {
+      const int b = begin + lane + 32 * x;
+      ahead[x] = b < stop ? __ldg(f.block_table + static_cast<int64_t>(s) * f.max_blocks + b) : -1;
+    }
+  });
   step();
 
   // full pages: one reference less, and one more for each that continues the sequence; of those that end inside a page the first
   if (h.last >= 0) atomicMin(a.first + h.last, i);
-  each_segment(f.n_seqs, f.max_blocks, (threadIdx.x >> 5) * kCluster + cluster_rank(), kAll / 32, [&](int s, int begin, int end, int lane) {
+  bool first = true;
+  auto change = [&](const Held& held, int heirs, int b, int32_t page) {
+    const int by = (b < held.full && b < f.width ? heirs : 0) - 1;
+    if (page >= 0 && page < n_pages && by != 0) atomicAdd(f.refs_out + page, by);
+  };
+  each_segment(f.n_seqs, f.max_blocks, warp, kAll / 32, [&](int s, int begin, int end, int lane) {
     const Held held(f, s);
     const int heirs = s_heirs[s];
+    if (first) {
+      first = false;
+#pragma unroll
+      for (int x = 0; x < kFirst; ++x) change(held, heirs, begin + lane + 32 * x, ahead[x]);
+      return;
+    }
     const int32_t* row = f.block_table + static_cast<int64_t>(s) * f.max_blocks;
     const int stop = min(end, held.pages);
 #pragma unroll 4
-    for (int b = begin + lane; b < stop; b += 32) {
-      const int32_t page = __ldg(row + b);
-      const int change = (b < held.full && b < f.width ? heirs : 0) - 1;
-      if (page >= 0 && page < n_pages && change != 0) atomicAdd(f.refs_out + page, change);
-    }
+    for (int b = begin + lane; b < stop; b += 32) change(held, heirs, b, __ldg(row + b));
   });
   step();
 
@@ -256,7 +278,7 @@ __device__ __forceinline__ void plan(const ForkLaunch& a) {
 }
 
 // A new sequence's pages: those that it takes over, and its own.
-__device__ __forceinline__ void fork_tables(const ForkLaunch& a, int64_t warp, int64_t warps) {
+__device__ __forceinline__ void fork_tables(const ForkLaunch& a, uint32_t warp, uint32_t warps) {
   const kvprm_fork& f = a.f;
   const int32_t have = __ldcg(a.count + 1);
   each_segment(f.n_new, f.width, warp, warps, [&](int r, int begin, int end, int lane) {
@@ -337,7 +359,7 @@ __device__ __forceinline__ void plan(const CompactLaunch& a) {
   }
 }
 
-__device__ __forceinline__ void compact_tables(const CompactLaunch& a, int64_t warp, int64_t warps) {
+__device__ __forceinline__ void compact_tables(const CompactLaunch& a, uint32_t warp, uint32_t warps) {
   const kvprm_compact& f = a.f;
   const int n_pages = static_cast<int>(f.n_pages);
   each_segment(f.n_seqs, f.max_blocks, warp, warps, [&](int s, int begin, int end, int lane) {
@@ -367,8 +389,8 @@ struct CopyLaunch {
 constexpr int kFewPools = 4;
 
 // T: ForkLaunch or CompactLaunch, whose tables are written first.
-__device__ __forceinline__ void tables(const ForkLaunch& t, int64_t warp, int64_t warps) { fork_tables(t, warp, warps); }
-__device__ __forceinline__ void tables(const CompactLaunch& t, int64_t warp, int64_t warps) { compact_tables(t, warp, warps); }
+__device__ __forceinline__ void tables(const ForkLaunch& t, uint32_t warp, uint32_t warps) { fork_tables(t, warp, warps); }
+__device__ __forceinline__ void tables(const CompactLaunch& t, uint32_t warp, uint32_t warps) { compact_tables(t, warp, warps); }
 __device__ __forceinline__ int32_t copy_to(const CompactLaunch&, int32_t page) { return page; }
 
 // A fork's copies come of few pages, which stay in L2 (256 copies of 64 sequences' pages, 199 MB: 46 us, and 58 with loads that
@@ -413,9 +435,9 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 1) 
 template <int N, typename T>
 __global__ void __launch_bounds__(kCopyThreads, kCopyCtas) copy_kernel(const __grid_constant__ CopyLaunch<N> a, const __grid_constant__ T t) {
   const int warp = threadIdx.x >> 5;
-  const int64_t warps = static_cast<int64_t>(gridDim.x) * (kCopyThreads / 32);
+  const uint32_t warps = gridDim.x * (kCopyThreads / 32);
   grid_dep_wait();
-  tables(t, static_cast<int64_t>(warp) * gridDim.x + blockIdx.x, warps);
+  tables(t, warp * gridDim.x + blockIdx.x, warps);
   copies(a, t, static_cast<int64_t>(blockIdx.x) * (kCopyThreads / 32) + warp, warps);
 }
 // All of a small call by the cluster alone.
@@ -424,7 +446,7 @@ __global__ void __cluster_dims__(kCluster, 1, 1) __launch_bounds__(kThreads, 1)
     small_kernel(const __grid_constant__ CopyLaunch<kFewPools> a, const __grid_constant__ T t) {
   plan(t);
   step();
-  const int64_t warp = static_cast<int64_t>(threadIdx.x >> 5) * kCluster + cluster_rank();
+  const uint32_t warp = (threadIdx.x >> 5) * kCluster + cluster_rank();
   tables(t, warp, kAll / 32);
   copies(a, t, warp, kAll / 32);
 }
