@@ -10,7 +10,7 @@
 //
 // What bounds them, measured on a GB300: memory, once copies are many (462 pages of 0.46 MB compacted in 76 us, 67 of them the
 // copies', 6,400 GB/s; 217 pages of 0.92 MB copied in a fork of 64 sequences into 256 in 54 us, 43 of them 199 MB written from
-// pages that L2 keeps); the steps' latencies before that, 7 to 10 us of a fork and 5 of a compaction (four and three cluster barriers,
+// pages that L2 keeps); the steps' latencies before that, 7 to 9 us of a fork and 5 of a compaction (four and three cluster barriers,
 // each behind loads or atomics of the step).
 #include <cuda_runtime.h>
 
