@@ -700,6 +700,9 @@ KVPRM_API int kvprm_cache_expand(const kvprm_cache* cache, const int32_t* src, c
  * values are rounded to bf16 (an 8-bit cache with up to 32 query rows of a kv
  * head: fp16, near the sequence's largest power of two; a 4-bit one likewise, weights
  * below 2^-26 of the largest in steps of 2^-36 of it), as the output is to bf16.
+ * The sums of weights times values stay finite where the output is only in a 4-bit cache's kernel for
+ * up to 32 query rows; elsewhere a row whose values are beyond 2^112 over its number of keys
+ * may come out infinite.
  * What the host cannot see: a sequence whose length is negative or beyond its
  * block table, or that has a page outside the cache, gets NaN in every output; one whose
  * drafted tokens are not within [0, n_tokens), or more than max_drafts, is left

@@ -80,8 +80,13 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 __device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ float power_of(int field) { return __uint_as_float(static_cast<uint32_t>(field) << 23); }
-__device__ __forceinline__ bool not_finite2(uint32_t w) {
-  return (w & 0x7F80u) == 0x7F80u || (w & 0x7F800000u) == 0x7F800000u;
+// The larger magnitudes of eight bf16 numbers, as bits, in two halves, and whether either of these is 2^k or more (field: k + 127;
+// 255: not finite).
+__device__ __forceinline__ uint32_t magnitude2(const uint4& v) {
+  return __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+}
+__device__ __forceinline__ bool from(uint32_t magnitude, uint32_t field) {
+  return max(magnitude & 0xFFFFu, magnitude >> 16) >= field << 7;
 }
 // Two codes' fp16 times factors, as bf16 (the longer form).
 __device__ __forceinline__ uint32_t bf16_times(uint32_t h, float lo, float hi) {
@@ -90,6 +95,16 @@ __device__ __forceinline__ uint32_t bf16_times(uint32_t h, float lo, float hi) {
 }
 // The token of a page that row r of S^T, and index r of P V's sums, stand for: a lane's four values' rows are neighbours.
 __device__ __forceinline__ int token_of(int r) { return 4 * ((r & 7) >> 1) + (r & 1) + ((r >> 3) << 1); }
+
+// Parts are joined with the weights of their means: a part's sum times 2^(its maximum - top), where top is so far above the
+// maximum (by the sum's power, and 2^12 for the number of parts) that all parts' weights together are 1 at most, and the joined sums
+// of weights times means finite.  ml: a part's maximum (-infinity: it saw nothing) and sum (0 then; NaN stays NaN).
+__device__ __forceinline__ float part_top(const float2& ml) {
+  return ml.x + static_cast<float>(static_cast<int>(__float_as_uint(ml.y) >> 23) - 127 + 12);
+}
+__device__ __forceinline__ float part_weight(const float2& ml, float top) {
+  return ml.y * (ml.x == -INFINITY ? 0.f : ex2_ftz(ml.x - top));
+}
 
 // A warp's ring of pages: of each a head's keys, values and their exponents.  Rows lie in the order in which the lanes read
 // them, so that an access' 128 bytes are in different banks: key row of lane group gid (+ 2 tokens) at 8 n + gid; value row
@@ -323,8 +338,8 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
     // The softmax step of a block or two for a tile: scores f * s in units of log2 (tokens token_of(gid) and two on, rows 2 c and 2 c + 1:
     // s[.][0], s[.][1] and s[.][2], s[.][3]) become P^T as operands, the running maximum, sum and output following.  The maximum moves
     // only when a score passes it by more than a margin.  The weights are rounded to fp16 or bf16, the values' type: their sum
-    // is not.  (some: every row sees one of the block's keys, or one before)
-    auto softmax = [&](int nt, const auto& s, float f0, float f1, auto& p, bool fp16, bool some_key) {
+    // is not.  (some_key: every row sees one of the block's keys, or one before; unit: what bf16 weights are taken times)
+    auto softmax = [&](int nt, const auto& s, float f0, float f1, auto& p, bool fp16, bool some_key, float unit) {
       constexpr int kN = sizeof(s) / 16;   // blocks
       float mx[2] = {fmaxf(s[0][0], s[0][2]), fmaxf(s[0][1], s[0][3])};
 #pragma unroll
@@ -361,8 +376,8 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
                             ex2_ftz(fmaf(s[x][3], f1, n1))};
         l[nt][0] += w[0] + w[2];
         l[nt][1] += w[1] + w[3];
-        p[x][0] = transposed(fp16 ? pack_f16(w[0], w[1]) : pack_bf16(w[0], w[1]));
-        p[x][1] = transposed(fp16 ? pack_f16(w[2], w[3]) : pack_bf16(w[2], w[3]));
+        p[x][0] = transposed(fp16 ? pack_f16(w[0], w[1]) : pack_bf16(w[0] * unit, w[1] * unit));
+        p[x][1] = transposed(fp16 ? pack_f16(w[2], w[3]) : pack_bf16(w[2] * unit, w[3] * unit));
       }
     };
 
@@ -499,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
       }
       uint32_t p[NT][1][2];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) softmax(nt, s[nt], 1.f, 1.f, p[nt], !wide, true);
+      for (int nt = 0; nt < NT; ++nt) softmax(nt, s[nt], 1.f, 1.f, p[nt], !wide, true, 1.f);
       // the weights' product with the values: words lo and hi have the even and the odd dims' codes, two tokens' side by side
 #pragma unroll
       for (int w = 0; w < kVW; ++w) {
@@ -623,7 +638,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
           for (int x = 0; x < P; ++x)
 #pragma unroll
             for (int i = 0; i < 4; ++i) y[x][i] = s[x][nt][i];
-          softmax(nt, y, rs[nt][0] * kp, rs[nt][1] * kp, p[nt], true, true);
+          softmax(nt, y, rs[nt][0] * kp, rs[nt][1] * kp, p[nt], true, true, 1.f);
         }
         product(place, vg, p);
       }
@@ -634,11 +649,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
     copies_wait<0>();
 
     // ---- drafted tokens: bf16 rows of their own tensors, whatever the cache holds
-    if (ev < 127) {   // (drafted values times a larger power might not be finite)
-      if (ev > 0) scale_outputs(power_of(ev));
-      ev = 127;
-    }
-    const float rel = power_of(254 - ev);   // what the outputs are kept in, over the values' own
+    if (ev == 0) ev = 127;   // (nothing so far)
     for (int b = c0 + mine; b < c1; ++b) {
       const int j0 = (b - q.cached_blocks) * kTreePage, have = q.drafts - j0;
       const __nv_bfloat16* kd = static_cast<const __nv_bfloat16*>(a.t.k) + (q.start + static_cast<int64_t>(j0)) * a.t.k_token + g * a.t.k_head;
@@ -665,24 +676,37 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
       constexpr int kD = HD / 64;   // 16-byte pieces of a lane's dims of a value row
       uint4 v[4][kD];
       uint32_t bad = 0;   // tokens whose value row is not finite
+      uint32_t most = 0;  // the others' largest magnitudes
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const int tok = 4 * c + t;
-        bool off = false;
+        uint32_t magnitude = 0;
 #pragma unroll
         for (int d = 0; d < kD; ++d) {
           v[t][d] = tok < have ? __ldg(reinterpret_cast<const uint4*>(vd + tok * a.t.v_token + gid * (HD / 8)) + d) : make_uint4(0u, 0u, 0u, 0u);
-          off = off || not_finite2(v[t][d].x) || not_finite2(v[t][d].y) || not_finite2(v[t][d].z) || not_finite2(v[t][d].w);
+          magnitude = __vmaxu2(magnitude, magnitude2(v[t][d]));
         }
-        const uint32_t who = __ballot_sync(0xffffffffu, off);
+        const uint32_t who = __ballot_sync(0xffffffffu, from(magnitude, 255));
 #pragma unroll
         for (int x = 0; x < 4; ++x)
           if (who & (0x11111111u << x)) bad |= 1u << (4 * x + t);
         if ((bad >> tok) & 1u) {   // a weight of zero must leave no trace of it: rows that see it are marked instead
 #pragma unroll
           for (int d = 0; d < kD; ++d) v[t][d] = make_uint4(0u, 0u, 0u, 0u);
+          magnitude = 0;
         }
+        most = __vmaxu2(most, magnitude);
       }
+      // Outputs are kept in units of 1 at least, for drafted values times a larger power might not be finite.  Weights are 2^15 at
+      // most and may be many: beside values of 2^88 and more the units are 2^40 at least, so that the sums stay finite (an output
+      // below 2^-98 loses bits beside such values).  Up to 2^40 of a unit goes to the weights, whose least that counts is
+      // far above bf16's least, the rest to the products.
+      const int least = __any_sync(0xffffffffu, from(most, 127 + 88)) ? 127 + 40 : 127;
+      if (ev < least) {
+        scale_outputs(power_of(127 + ev - least));
+        ev = least;
+      }
+      const float unit = power_of(max(254 - ev, 127 - 40)), rest = power_of(min(254 - ev + 40, 127));
       uint32_t p[NT][1][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
@@ -695,7 +719,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
           for (int n = 0; n < 2; ++n)
             s[nt][0][2 * n + h] = (sees >> (token_of(gid) + 2 * n)) & 1u ? s[nt][0][2 * n + h] * a.scale_log2 : -INFINITY;
         }
-        softmax(nt, s[nt], 1.f, 1.f, p[nt], false, false);
+        softmax(nt, s[nt], 1.f, 1.f, p[nt], false, false, unit);
       }
 #pragma unroll
       for (int i = 0; i < MT; ++i) {
@@ -712,20 +736,27 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
           float t[4] = {0.f, 0.f, 0.f, 0.f};
           mma_bf16_16816(t, x[0], x[1], x[2], x[3], p[nt][0][0], p[nt][0][1]);
 #pragma unroll
-          for (int k = 0; k < 4; ++k) o[nt][i][k] += t[k] * rel;
+          for (int k = 0; k < 4; ++k) o[nt][i][k] += t[k] * rest;
         }
       }
     }
 
     // ---- the part's end
-    const float down = power_of(ev);   // 1 / rel
+    // What a part leaves is its own mean, in the values' own scale, with the sum of its weights beside it: the sum of weights
+    // times values may be beyond fp32 where the mean is not.
     const bool lost = __any_sync(0xffffffffu, poison);
-    auto sum_of = [&](int nt, int h) {
-      float sum = l[nt][h];
+    float mean[NT][2];   // what makes a mean of an output
 #pragma unroll
-      for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-      return lost || (poison_row >> (2 * nt + h)) & 1u ? NAN : sum;
-    };
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float sum = l[nt][h];
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+        if (lost || (poison_row >> (2 * nt + h)) & 1u) sum = NAN;
+        l[nt][h] = sum;
+        mean[nt][h] = sum == 0.f ? 0.f : __fdividef(power_of(ev), sum);   // a row that saw nothing: zeros; NaN stays
+      }
     if constexpr (WHOLE) {   // the warps' states meet, 8 rows at a time, in their rings
       constexpr int kOutRow = HD + 4, kPer = 8 * HD / kThreads;   // kPer: outputs of a thread, part of one row
       auto out_of = [&](int w) { return reinterpret_cast<float*>(s_ring + w * (kRing * S::kBytes)); };
@@ -736,23 +767,23 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
         if (nt > 0) __syncthreads();        // the last 8 rows have been read
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float sum = sum_of(nt, h);
-          if (gid == 0) s_ml[warp][2 * c + h] = make_float2(-nm[nt][h], sum);
+          const float f = mean[nt][h];
+          if (gid == 0) s_ml[warp][2 * c + h] = make_float2(-nm[nt][h], l[nt][h]);
 #pragma unroll
           for (int i = 0; i < MT; ++i)   // dims 2 i and 2 i + 1 of this lane's HD / 8
-            *reinterpret_cast<float2*>(out_of(warp) + (2 * c + h) * kOutRow + gid * (HD / 8) + 2 * i) = make_float2(o[nt][i][h] * down, o[nt][i][2 + h] * down);
+            *reinterpret_cast<float2*>(out_of(warp) + (2 * c + h) * kOutRow + gid * (HD / 8) + 2 * i) = make_float2(o[nt][i][h] * f, o[nt][i][2 + h] * f);
         }
         __syncthreads();
         const int r = threadIdx.x / 16, d0 = threadIdx.x % 16 * kPer, out_r = row0 + 8 * nt + r;
         float top = -INFINITY, sum = 0.f, acc[kPer];
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, s_ml[w][r].x);
+        for (int w = 0; w < kWarps; ++w) top = fmaxf(top, part_top(s_ml[w][r]));
 #pragma unroll
         for (int i = 0; i < kPer; ++i) acc[i] = 0.f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-          const float f = s_ml[w][r].x == -INFINITY ? 0.f : ex2_ftz(s_ml[w][r].x - top);   // (NaN sums stay NaN)
-          sum += s_ml[w][r].y * f;
+          const float f = part_weight(s_ml[w][r], top);
+          sum += f;
 #pragma unroll
           for (int i = 0; i < kPer; ++i) acc[i] += out_of(w)[r * kOutRow + d0 + i] * f;
         }
@@ -780,11 +811,10 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
       for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const float sum = sum_of(nt, h);
           const int slot_row = 8 * nt + 2 * c + h, r = row0 + slot_row;
           if (r >= rows) continue;
           float y[2 * MT];   // this lane's HD / 8 dims
-          const float f = whole ? (sum == 0.f ? 0.f : down / sum) : down;   // a row that saw nothing: zeros; NaN stays
+          const float f = mean[nt][h];
 #pragma unroll
           for (int i = 0; i < MT; ++i) {
             y[2 * i] = o[nt][i][h] * f;
@@ -802,7 +832,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
             float* dst = a.part_o + (slot * G::kSlotRows + slot_row) * HD + gid * (HD / 8);
 #pragma unroll
             for (int i = 0; i < 2 * MT; i += 4) *reinterpret_cast<float4*>(dst + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
-            if (gid == 0) a.part_ml[slot * G::kSlotRows + slot_row] = make_float2(-nm[nt][h], sum);
+            if (gid == 0) a.part_ml[slot * G::kSlotRows + slot_row] = make_float2(-nm[nt][h], l[nt][h]);
           }
         }
       }
@@ -843,10 +873,10 @@ __global__ void __launch_bounds__(32 * W) tree_e2m1_join_kernel(const __grid_con
     float4 v[4];
 #pragma unroll
     for (int d = 0; d < 4; ++d) v[d] = __ldcg(reinterpret_cast<const float4*>(a.part_o + at * HD + d0 + 16 * d));
-    const float now = fmaxf(best, ml.x);   // -infinity: nothing seen so far (a sum of zero, or NaN)
-    const float f = best == -INFINITY ? 0.f : ex2_ftz(best - now), e = ml.x == -INFINITY ? 0.f : ex2_ftz(ml.x - now);
+    const float now = fmaxf(best, part_top(ml));   // -infinity: nothing seen so far (a sum of zero, or NaN)
+    const float f = best == -INFINITY ? 0.f : ex2_ftz(best - now), e = part_weight(ml, now);
     best = now;
-    sum = sum * f + ml.y * e;
+    sum = sum * f + e;
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
       o[4 * d] = o[4 * d] * f + v[d].x * e;

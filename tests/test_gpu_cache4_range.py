@@ -1,0 +1,40 @@
+"""Attention over 4-bit pages at the ends of what its rows can hold, up to 32 query rows of a kv head: against the definition in 64
+bits, as tests/test_gpu_cache4.py, on calls whose pairs are whole (a CTA each, or several) and cut (parts that are joined)."""
+import pytest
+
+from tests.cache4_util import Tree4
+from tests.test_gpu_operators import _kp
+
+pytestmark = pytest.mark.gpu
+# (lens, drafts, kv heads): whole pairs, a CTA each; several of a CTA; parts of long ones, beside short ones that one warp has
+CALLS = {"whole": ([64, 17, 300], [1, 3, 2], 2), "many": ([40 + i for i in range(150)], [1] * 150, 4),
+         "cut": ([5000, 17, 3000], [1, 2, 3], 2), "cut_rows": ([5000, 17], [8, 5], 2)}
+
+
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("q_std", [2.0, 0.0])
+def test_large_cached_values(call, q_std):
+    """Values up to 2^120, whose sum over the keys no fp32 number holds, though bf16 holds their mean; equal weights among them."""
+    torch, _ = _kp()
+    lens, drafts, nkv = CALLS[call]
+    t = Tree4(torch, 2 * nkv, nkv, 128, lens, drafts, seed=41, q_std=q_std)
+    t.exps[:, 1] += 117                      # 123 .. 126 (and, where nobody looks, 255)
+    t.remake()
+    out = t.run()
+    assert bool(out.isfinite().all())
+    t.check(out)
+
+
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("far", [0, 60, -60])
+def test_large_drafted_values(call, far):
+    """Drafted values up to 2^120 beside cached ones of about one, 2^60 and 2^-60."""
+    torch, _ = _kp()
+    lens, drafts, nkv = CALLS[call]
+    t = Tree4(torch, 2 * nkv, nkv, 64, lens, drafts, seed=42)
+    t.exps[:, 1] = (t.exps[:, 1].int() + far).clamp(max=255).to(torch.uint8)
+    t.remake()
+    t.v.mul_(2.0 ** 118)
+    out = t.run()
+    assert bool(out.isfinite().all())
+    t.check(out)
