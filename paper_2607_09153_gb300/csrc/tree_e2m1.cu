@@ -9,8 +9,8 @@
 // nibbles of two tokens are put side by side, so that one conversion gives an operand's pair.  S^T's columns become P^T's
 // by one 8 x 8 transposition in registers.
 //
-// What fp16 lacks in range is kept beside it as powers of two.  A query row is scaled to a largest magnitude of 1 to 2 (exact
-// but for elements 2^-14 of that and smaller, which lose what is below 2^-25 of it).  A page's key blocks are taken
+// What fp16 lacks in range is kept beside it as powers of two.  A query row is scaled to a largest magnitude of 2^15 to 2^16
+// (exact for elements down to 2^-32 of that; rows with smaller ones take their products in bf16, as they are).  A page's key blocks are taken
 // relative to a power Ek that its scores are multiplied by in fp32, the values' relative to a power Ev that the outputs are kept
 // relative to: blocks from 2^-8 to 2^7 of it are exact.  A page that leaves that window moves Ek or Ev; one whose own
 // blocks are further apart takes its products in bf16 instead, whose range is fp32's.  Weights are kept times 2^12, so
@@ -80,13 +80,28 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 __device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ float power_of(int field) { return __uint_as_float(static_cast<uint32_t>(field) << 23); }
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t min_s16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("min.s16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
 // The larger magnitudes of eight bf16 numbers, as bits, in two halves, and whether either of these is 2^k or more (field: k + 127;
 // 255: not finite).
 __device__ __forceinline__ uint32_t magnitude2(const uint4& v) {
-  return __vmaxu2(__vmaxu2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), __vmaxu2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+  return max_u16x2(max_u16x2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), max_u16x2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
 }
 __device__ __forceinline__ bool from(uint32_t magnitude, uint32_t field) {
   return max(magnitude & 0xFFFFu, magnitude >> 16) >= field << 7;
+}
+// The least magnitude of eight that is not zero, plus 0x7FFF, in two halves with a sign: a zero, 0x7FFF, is above all others.
+__device__ __forceinline__ uint32_t least2(const uint4& v) {
+  auto lifted = [](uint32_t w) { return (w & 0x7FFF7FFFu) + 0x7FFF7FFFu; };
+  return min_s16x2(min_s16x2(lifted(v.x), lifted(v.y)), min_s16x2(lifted(v.z), lifted(v.w)));
 }
 // Two codes' fp16 times factors, as bf16 (the longer form).
 __device__ __forceinline__ uint32_t bf16_times(uint32_t h, float lo, float hi) {
@@ -289,22 +304,26 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
 
     // ---- the queries, scaled; a negative scale turns their signs
     float rs[NT][2];   // of rows 2 c and 2 c + 1: the row's power of two times the scores' scale
+    bool far = false;  // a row that fp16 does not hold
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-      float most = 0.f;
+      uint32_t most = 0, least = 0x7FFF7FFFu;
 #pragma unroll
       for (int i = 0; i < HD / 32; ++i) {
-        const uint32_t w[4] = {qv[nt][i].x, qv[nt][i].y, qv[nt][i].z, qv[nt][i].w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) most = fmaxf(most, fmaxf(fabsf(lo_bf16(w[k])), fabsf(hi_bf16(w[k]))));
+        most = max_u16x2(most, magnitude2(qv[nt][i]));
+        least = min_s16x2(least, least2(qv[nt][i]));
       }
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-      most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-      // (2^(127 - e) has to be a normal number; all zero or infinite: any scale does)
-      const int e = min(max(static_cast<int>(__float_as_uint(most) >> 23), 1), 253);
-      rs[nt][0] = __shfl_sync(0xffffffffu, power_of(e), 8 * c) * fabsf(a.scale_log2);
-      rs[nt][1] = __shfl_sync(0xffffffffu, power_of(e), 8 * c + 4) * fabsf(a.scale_log2);
-      const float up = a.scale_log2 < 0.f ? -power_of(254 - e) : power_of(254 - e);
+      most = max(most & 0xFFFFu, most >> 16);   // (bits without a sign: ordered as the values)
+      most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
+      most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
+      // 2^(142 - e) has to be a normal number; all zero or not finite: any scale does.  An element's last bit is 2^-7 of its power,
+      // and 2^-24 is fp16's.
+      const int e = min(max(static_cast<int>(most >> 7), 15), 254);
+      least ^= 0x80008000u;   // a magnitude less one
+      far = far || static_cast<int>((min(least & 0xFFFFu, least >> 16) + 1u) >> 7) < e - 32;
+      rs[nt][0] = __shfl_sync(0xffffffffu, power_of(e), 8 * c) * (0x1p-15f * fabsf(a.scale_log2));
+      rs[nt][1] = __shfl_sync(0xffffffffu, power_of(e), 8 * c + 4) * (0x1p-15f * fabsf(a.scale_log2));
+      const float up = a.scale_log2 < 0.f ? -power_of(269 - e) : power_of(269 - e);
       auto scaled = [&](uint32_t w) { return pack_f16(lo_bf16(w) * up, hi_bf16(w) * up); };
 #pragma unroll
       for (int i = 0; i < HD / 32; ++i) {   // (read by this lane alone)
@@ -312,6 +331,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
         s_q[warp][nt][2 * i + 1][lane] = make_uint2(scaled(qv[nt][i].z), scaled(qv[nt][i].w));
       }
     }
+    far = __any_sync(0xffffffffu, far);
     auto query_of = [&](int nt, int step) { return s_q[warp][nt][step][lane]; };
 
     // o: dims gid-rows of a tile, query rows 2 c and 2 c + 1; nm: the lift less the running maximum
@@ -419,7 +439,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
         v_most = __reduce_max_sync(0xffffffffu, v_most);
         v_least = __reduce_min_sync(0xffffffffu, v_least);
         auto fits = [](int most, int least, int e) { return most <= e + 7 && least >= e - kBelow; };
-        wide = __any_sync(0xffffffffu, nan);   // (the longer products have a place for it)
+        wide = far || __any_sync(0xffffffffu, nan);   // (the longer products have a place for it)
         if (k_most > 0 && !fits(k_most, k_least, ek)) {
           ek = min(k_least + kBelow, kTop);
           kp = power_of(ek);
@@ -626,7 +646,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
       if (__any_sync(0xffffffffu, out != 0u) || at + P > plain) {
 #pragma unroll 1
         for (int x = 0; x < min(pages - at, P); ++x) general(at + x, place + x * S::kBytes);
-        plain = ev != 0 ? full : 0;
+        plain = ev != 0 && !far ? full : 0;
       } else {
         float s[P][NT][4];
         scores(now, kg, s);
@@ -684,7 +704,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
 #pragma unroll
         for (int d = 0; d < kD; ++d) {
           v[t][d] = tok < have ? __ldg(reinterpret_cast<const uint4*>(vd + tok * a.t.v_token + gid * (HD / 8)) + d) : make_uint4(0u, 0u, 0u, 0u);
-          magnitude = __vmaxu2(magnitude, magnitude2(v[t][d]));
+          magnitude = max_u16x2(magnitude, magnitude2(v[t][d]));
         }
         const uint32_t who = __ballot_sync(0xffffffffu, from(magnitude, 255));
 #pragma unroll
@@ -695,7 +715,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
           for (int d = 0; d < kD; ++d) v[t][d] = make_uint4(0u, 0u, 0u, 0u);
           magnitude = 0;
         }
-        most = __vmaxu2(most, magnitude);
+        most = max_u16x2(most, magnitude);
       }
       // Outputs are kept in units of 1 at least, for drafted values times a larger power might not be finite.  Weights are 2^15 at
       // most and may be many: beside values of 2^88 and more the units are 2^40 at least, so that the sums stay finite (an output

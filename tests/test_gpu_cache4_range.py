@@ -38,3 +38,26 @@ def test_large_drafted_values(call, far):
     out = t.run()
     assert bool(out.isfinite().all())
     t.check(out)
+
+
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("apart", [17, 20, 31, 45])
+@pytest.mark.parametrize("some", [False, True])
+def test_queries_far_apart(call, apart, some):
+    """Query rows (all, or a sequence's first drafted token's alone) with one element 2^apart of the others, where all keys are zero: the
+    scores are made of the small ones, with keys that make up for it."""
+    torch, _ = _kp()
+    lens, drafts, nkv = CALLS[call]
+    t = Tree4(torch, 2 * nkv, nkv, 128, lens, drafts, seed=43)
+    rows = t.start[:-1] if some else slice(None)
+    t.q[rows] *= 2.0 ** -apart
+    t.q[rows, :, 5] = 1.5
+    t.pages[:, 0, :, :, 2] &= 0x0F           # dimension 5
+    t.k[:, :, 5] = 0
+    if some:                                 # (the other rows' scores: keys are as large for them)
+        others = [i for i in range(t.q.shape[0]) if i not in rows]
+        t.q[others] *= 2.0 ** -apart
+    t.exps[:, 0] = (t.exps[:, 0].int() + apart).clamp(max=254).to(torch.uint8)
+    t.k.mul_(2.0 ** apart)
+    t.remake()
+    t.check(t.run())
