@@ -421,25 +421,38 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
       uint32_t kf[2], vf[2];   // factors as fp16 pairs: of a key row, of two tokens' values
       bool wide = false;       // bf16 instead
       {
-        // the largest and least powers of rows within the length; blocks of the least power, 2^-127, count as nothing
+        // the largest and least powers of rows within the length; blocks of the least power, 2^-127, count as nothing where their codes
+        // are zeros, and are beyond any window else
         int k_most = 0, k_least = 255, v_most = 0, v_least = 255;
-        bool nan = false;
-        auto take = [&](bool in, uint32_t field, int& most, int& least) {
-          nan = nan || (in && field == 255u);
+        bool beyond = false;   // NaN, or something in the least power: the longer products have a place for it
+        auto take = [&](bool in, uint32_t field, uint32_t codes, int& most, int& least) {
+          const bool something = field == 0u && (codes & 0x77777777u) != 0u;
+          beyond = beyond || (in && (field == 255u || something));
+          if (something) field = 1u;
           if (!in || field == 0u || field == 255u) return;
           most = max(most, static_cast<int>(field));
           least = min(least, static_cast<int>(field));
         };
 #pragma unroll
-        for (int n = 0; n < 2; ++n) take((live >> n) & 1u, x.ke[n], k_most, k_least);
+        for (int n = 0; n < 2; ++n) {
+          uint32_t codes = 0;
 #pragma unroll
-        for (int t = 0; t < 4; ++t) take((live >> (2 + t)) & 1u, (ve >> (8 * t)) & 255u, v_most, v_least);
+          for (int w = 0; w < kW; ++w) codes |= x.k[n][w];
+          take((live >> n) & 1u, x.ke[n], codes, k_most, k_least);
+        }
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          uint32_t codes = 0;
+#pragma unroll
+          for (int w = 0; w < kVW; ++w) codes |= x.v[t][w];
+          take((live >> (2 + t)) & 1u, (ve >> (8 * t)) & 255u, codes, v_most, v_least);
+        }
         k_most = __reduce_max_sync(0xffffffffu, k_most);
         k_least = __reduce_min_sync(0xffffffffu, k_least);
         v_most = __reduce_max_sync(0xffffffffu, v_most);
         v_least = __reduce_min_sync(0xffffffffu, v_least);
         auto fits = [](int most, int least, int e) { return most <= e + 7 && least >= e - kBelow; };
-        wide = far || __any_sync(0xffffffffu, nan);   // (the longer products have a place for it)
+        wide = far || __any_sync(0xffffffffu, beyond);
         if (k_most > 0 && !fits(k_most, k_least, ek)) {
           ek = min(k_least + kBelow, kTop);
           kp = power_of(ek);
@@ -558,7 +571,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
 #pragma unroll
           for (int t = 0; t < 4; ++t) {
             const int e = static_cast<int>((ve >> (8 * t)) & 255u);
-            f[t] = !((live >> (2 + t)) & 1u) ? 0.f : e == 255 ? NAN : power_of(min(max(e == 0 ? 0 : 127 + e - ev, 0), 254));
+            f[t] = !((live >> (2 + t)) & 1u) ? 0.f : e == 255 ? NAN : power_of(min(max(127 + e - ev, 0), 254));
           }
 #pragma unroll
           for (int i = 0; i < 4; ++i) {

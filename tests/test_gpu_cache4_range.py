@@ -61,3 +61,32 @@ def test_queries_far_apart(call, apart, some):
     t.k.mul_(2.0 ** apart)
     t.remake()
     t.check(t.run())
+
+
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("mixed", [False, True])
+def test_keys_of_the_least_power(call, mixed):
+    """Key blocks with the least exponent byte, 0, whose codes are not zero, with queries of 2^124; others' beside them."""
+    torch, _ = _kp()
+    lens, drafts, nkv = CALLS[call]
+    t = Tree4(torch, 2 * nkv, nkv, 64, lens, drafts, seed=44)
+    least = torch.rand(t.exps[:, 0].shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)) < (0.4 if mixed else 2)
+    t.exps[:, 0] = torch.where(least, 0, t.exps[:, 0] - 121)   # 0, and 2 .. 5
+    t.q.mul_(2.0 ** 124)
+    t.k.mul_(2.0 ** -125)
+    t.remake()
+    t.check(t.run())
+
+
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("mixed", [False, True])
+def test_values_of_the_least_power(call, mixed):
+    """Value blocks with the least exponent byte: outputs among the least that bf16 holds, in steps of 2^-133."""
+    torch, _ = _kp()
+    lens, drafts, nkv = CALLS[call]
+    t = Tree4(torch, 2 * nkv, nkv, 64, lens, drafts, mask="none", seed=45)
+    least = torch.rand(t.exps[:, 1].shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)) < (0.4 if mixed else 2)
+    t.exps[:, 1] = torch.where(least, 0, t.exps[:, 1] - 121)
+    t.remake()
+    want, bound = t.want()
+    assert bool(((t.run().double() - want).abs() <= bound - 1e-30 + 2.0 ** -133).all())
