@@ -734,7 +734,8 @@ KVPRM_API int kvprm_tree_attention_filled(const kvprm_cache* cache, const kvprm_
 /* Pages between two steps of a search.  A pool is what a block table's page numbers index: `layers` times
  * n_pages pages of page_bytes consecutive bytes, page p of layer l at base + l * layer_stride + p * page_stride
  * (bytes; all multiples of 16, base 16-byte aligned).  A cache of several layers is one such pool, its exponents are
- * another; layers that were allocated apart are pools of one layer each.  What a page holds does not matter. */
+ * another; layers that were allocated apart are pools of one layer each.  What a page holds does not matter.  No two
+ * pages may overlap, of one pool or of several (pools may lie between each other's pages, with the same page_stride). */
 enum { KVPRM_MAX_POOLS = 96, KVPRM_MAX_SEQS = 8192 };
 typedef struct {
   void* base;
@@ -748,7 +749,7 @@ typedef struct {
  *  block_table  int32 [n_seqs][max_blocks], lens int32 [n_seqs]: the first ceil(lens[s] / 16) entries of a row are its pages
  *  parents      int32 [n_new]: the sequence that is continued; any other number begins an empty one
  *  room         int32 [n_new] (may be NULL): tokens that a new sequence is to have pages for beyond its cached ones
- * Written (none may overlap another or an input):
+ * Written (none may overlap another, an input, a page or the workspace):
  *  table_out    int32 [n_new][width]: the pages, -1 behind them
  *  lens_out     int32 [n_new]: the cached tokens, lens[parents[i]] or 0
  *  refs_out     int32 [n_pages]: refs without the old tables' references and with the new ones'

@@ -15,6 +15,7 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <utility>
 
 #include "ptx.cuh"
 #include "rope.h"
@@ -464,6 +465,63 @@ bool meet(const Part& a, const Part& b) {
   return a.bytes > 0 && b.bytes > 0 && x < y + b.bytes && y < x + a.bytes;
 }
 
+// Pages in memory: `layers` times `n` of `bytes`, with strides that are not negative (0 where there is one).
+using Wide = __int128;   // (sums of strides of any size)
+struct Box {
+  Wide at, layer_stride, stride;
+  int64_t layers, n, bytes;
+  Box() {}
+  explicit Box(const Part& a) : at(reinterpret_cast<uintptr_t>(a.p)), layer_stride(0), stride(0), layers(1), n(1), bytes(a.bytes) {}
+  Box(const kvprm_pool& p, int64_t n_pages)
+      : at(reinterpret_cast<uintptr_t>(p.base)), layer_stride(p.layers > 1 ? p.layer_stride : 0), stride(n_pages > 1 ? p.page_stride : 0),
+        layers(p.layers), n(n_pages), bytes(p.page_bytes) {
+    if (layer_stride < 0) at += layer_stride * (layers - 1), layer_stride = -layer_stride;
+    if (stride < 0) at += stride * (n - 1), stride = -stride;
+  }
+  bool empty() const { return layers <= 0 || n <= 0 || bytes <= 0; }
+  Wide row() const { return stride * (n - 1) + bytes; }   // from a layer's first page to its end
+  Wide end() const { return at + layer_stride * (layers - 1) + row(); }
+};
+Wide floor_div(Wide a, Wide b) { return a / b - (a % b < 0 ? 1 : 0); }   // b > 0
+
+// Whether pages of a layer of a and of one of b, which begins `by` behind it, meet.
+bool rows_meet(const Box& a, const Box& b, Wide by) {
+  if (by >= a.row() || -by >= b.row()) return false;
+  if (a.n > 1 && b.n > 1 && a.stride != b.stride) return true;   // (not looked into)
+  const Wide stride = a.n > 1 ? a.stride : b.stride;
+  if (stride == 0) return true;
+  // some page j of b and i of a with -b.bytes < by + (j - i) stride < a.bytes
+  const Wide lo = floor_div(-by - b.bytes, stride) + 1, hi = -floor_div(by - a.bytes, stride) - 1;
+  return std::max<Wide>(lo, 1 - a.n) <= std::min<Wide>(hi, b.n - 1);
+}
+
+bool meet(const Box& a, const Box& b) {
+  if (a.empty() || b.empty() || a.at >= b.end() || b.at >= a.end()) return false;
+  if (a.layers == 1 || b.layers == 1 || a.layer_stride == b.layer_stride) {
+    const Wide stride = a.layers > 1 ? a.layer_stride : b.layer_stride;
+    for (int64_t d = 1 - a.layers; d < b.layers; ++d)
+      if (rows_meet(a, b, b.at - a.at + d * stride)) return true;
+    return false;
+  }
+  if (a.layers * b.layers > 1 << 22) return true;   // (not looked into)
+  for (int64_t i = 0; i < a.layers; ++i)
+    for (int64_t j = 0; j < b.layers; ++j)
+      if (rows_meet(a, b, b.at + j * b.layer_stride - a.at - i * a.layer_stride)) return true;
+  return false;
+}
+
+// Whether two pages of one pool meet.
+bool meets_itself(Box a) {
+  if (a.empty()) return false;
+  if ((a.n > 1 && a.stride < a.bytes) || (a.layers > 1 && a.layer_stride < a.bytes)) return true;
+  if (a.layers == 1 || a.n == 1 || a.layer_stride >= a.row() || a.stride >= a.layer_stride * (a.layers - 1) + a.bytes) return false;
+  if (Wide{a.layers} * a.n * a.bytes > a.end() - a.at) return true;
+  if (a.n < a.layers) std::swap(a.n, a.layers), std::swap(a.stride, a.layer_stride);
+  for (int64_t d = 1; d < a.layers; ++d)
+    if (rows_meet(a, a, d * a.layer_stride)) return true;
+  return false;
+}
+
 // Whether the arrays that a call writes are apart from each other and from what it reads.
 int check_apart(const Part* in, int n_in, const Part* out, int n_out, const char* who) {
   for (int i = 0; i < n_out; ++i) {
@@ -509,6 +567,43 @@ int check_pools(const kvprm_pool* pools, int n, int64_t n_pages, CopyLaunch<KVPR
     if (pieces > 0x7FFFFFFF) return operator_fail(KVPRM_EINVAL, "%s: pages of all layers are too large", who);
   }
   c->first[n] = static_cast<int32_t>(pieces);
+  return KVPRM_OK;
+}
+
+// Whether the pages that a call copies are apart from each other, from its arrays and from its workspace, and that from the arrays.
+int check_pages_apart(const kvprm_pool* pools, int n, int64_t n_pages, const Part* in, int n_in, const Part* out, int n_out, const Part& workspace,
+                      const char* who) {
+  struct Place {
+    Box box;
+    int k;   // pool, or -1
+  };
+  Place places[KVPRM_MAX_POOLS + 16];
+  int count = 0;
+  for (int k = 0; k < n; ++k) {
+    const Box box(pools[k], n_pages);
+    if (meets_itself(box)) return operator_fail(KVPRM_EINVAL, "%s: pages of pool %d overlap", who, k);
+    if (!box.empty()) places[count++] = {box, k};
+  }
+  auto add = [&](const Part& p) {
+    if (p.bytes > 0) places[count++] = {Box(p), -1};
+  };
+  for (int i = 0; i < n_in; ++i) {
+    if (meet(workspace, in[i])) return operator_fail(KVPRM_EINVAL, "%s: the workspace overlaps an input", who);
+    add(in[i]);
+  }
+  for (int i = 0; i < n_out; ++i) {
+    if (meet(workspace, out[i])) return operator_fail(KVPRM_EINVAL, "%s: the workspace overlaps an output", who);
+    add(out[i]);
+  }
+  add(workspace);
+  std::sort(places, places + count, [](const Place& a, const Place& b) { return a.box.at < b.box.at; });
+  for (int i = 0; i < count; ++i)
+    for (int j = i + 1; j < count && places[j].box.at < places[i].box.end(); ++j) {
+      const Place &a = places[i], &b = places[j];
+      if ((a.k < 0 && b.k < 0) || !meet(a.box, b.box)) continue;
+      if (a.k < 0 || b.k < 0) return operator_fail(KVPRM_EINVAL, "%s: pool %d overlaps another argument", who, std::max(a.k, b.k));
+      return operator_fail(KVPRM_EINVAL, "%s: pools %d and %d overlap", who, std::min(a.k, b.k), std::max(a.k, b.k));
+    }
   return KVPRM_OK;
 }
 
@@ -600,6 +695,7 @@ int kvprm_cache_fork(const kvprm_pool* pools, const kvprm_fork* f, void* workspa
                       {f->lens_out, 4 * int64_t{f->n_new}}, {f->counts, 8}};
   if (const int rc = check_apart(in, 5, out, 4, who)) return rc;
   if (const int rc = check_workspace(workspace, workspace_bytes, fork_bytes(*f), who)) return rc;
+  if (const int rc = check_pages_apart(pools, f->n_pools, f->n_pages, in, 5, out, 4, {workspace, fork_bytes(*f)}, who)) return rc;
   ForkLaunch a;
   a.f = *f;
   Scratch w{static_cast<uint8_t*>(workspace)};
@@ -631,6 +727,7 @@ int kvprm_cache_compact(const kvprm_pool* pools, const kvprm_compact* f, void* w
   const Part out[] = {{f->refs_out, 4 * f->n_pages}, {f->table_out, table}, {f->moved, 4 * f->n_pages}, {f->counts, 8}};
   if (const int rc = check_apart(in, 3, out, 4, who)) return rc;
   if (const int rc = check_workspace(workspace, workspace_bytes, compact_bytes(*f), who)) return rc;
+  if (const int rc = check_pages_apart(pools, f->n_pools, f->n_pages, in, 3, out, 4, {workspace, compact_bytes(*f)}, who)) return rc;
   CompactLaunch a;
   a.f = *f;
   Scratch w{static_cast<uint8_t*>(workspace)};
