@@ -759,7 +759,12 @@ typedef struct {
  * new pages are taken from the free ones, those that the dropped sequences held among them, the lowest first,
  * sequence by sequence (a copy before the pages to come).  Where none is left, the entry is -1 and a copy is left out:
  * such a table makes NaN in kvprm_tree_attention, and its slots are not written by kvprm_cache_write.  Pages for which
- * a row of `width` has no place count as wanted.  What the host cannot see: a sequence whose length is negative or
+ * a row of `width` has no place count as wanted.  Any call, one that runs short among them, may write copies over pages
+ * that only sequences without descendants held (or behind `width`): from the old tables it can be run again only with parents
+ * that continue none of these.  A step that may run short is planned first, with n_pools 0: that copies nothing, and the
+ * tables and counts are the same.
+ * Pages that were given as room and that a sequence has not reached when the next step begins (they are behind
+ * ceil(lens / 16) entries of its row) keep their reference: whoever leaves some unused takes it off refs.  What the host cannot see: a sequence whose length is negative or
  * beyond its block table keeps its references, and those that continue it get its length and no pages; an entry
  * outside the pool is taken over as it is.
  *  workspace    as for kvprm_tree_attention, of kvprm_fork_workspace() bytes for the same arguments

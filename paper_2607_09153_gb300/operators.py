@@ -565,7 +565,8 @@ def cache_fork(pools, refs, block_table, lens, parents, room=None, width: int | 
     pools: tensors [layers][n_pages]... that block_table's numbers index -- pages and exponents, of any type; a single layer's
     as x[None].  refs (int32 [n_pages]): how many hold a page; 0: it is free.  Returns (block_table [n_new][width], -1 behind a
     row's pages; lens; refs; counts: pages that are free now, and pages that were wanted and not to be had, which are -1 in
-    the table).  width: default that of `out`, else of block_table, which has to have places for the pages to come.  out: a
+    the table).  Copies may go over pages of sequences that nobody continues, also where the call runs short: with no pools ([])
+    it copies nothing and its results are the same, so a step can be planned before it is made.  width: default that of `out`, else of block_table, which has to have places for the pages to come.  out: a
     tuple of four tensors to write instead of new ones; none may share memory with the inputs."""
     T = _t or _torch()
     dev, n_pages, n, blocks, *at = _page_table(T, refs, block_table, lens)
