@@ -9,8 +9,8 @@
 //
 // 8-bit codes become fp16 in registers (one instruction for two; to bf16 it takes nine for four: 8 x 32,768 tokens of 8 kv
 // heads 129 us, so 113), once for both tiles of 32 rows.  What fp16 lacks in range is kept beside it as powers of two: a query row is
-// scaled to a largest magnitude of 1 to 2 (exact but for elements 2^-14 of that and smaller, which lose what is below
-// 2^-25 of it), a key row's power multiplies the scores in fp32, and a value row's multiplies the weights, relative to the
+// scaled to a largest magnitude of 2^15 to 2^16 (exact for elements down to 2^-32 of that; with a row that has smaller ones, the
+// scores' products are bf16's), a key row's power multiplies the scores in fp32, and a value row's multiplies the weights, relative to the
 // largest one met, E: a weight p becomes p 2^(e - E + 10), whose fp16 steps end at 2^-34 of a full weight's.  A page with a
 // power below 2^-10 of E takes its values' product in bf16 instead, whose range is fp32's: its weights would lose what E,
 // which may stand for a row that is not looked at, leaves out.
@@ -111,7 +111,7 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(TILES))
   auto& s_q = sh.q.bf16;
   auto& s_qh = sh.q.fp16;
   auto& s_o = sh.o;
-  __shared__ float s_most[TILES][16][HD / 32];      // largest magnitude of 32 dims of a query row
+  __shared__ uint2 s_most[TILES][16][HD / 32];      // largest and least magnitudes of 32 dims of a query row
   __shared__ float s_m[kWarps][16], s_l[kWarps][16];
   grid_dep_launch();
   tree_line<G, kThreads, HD>(a, s_off, s_sum);
@@ -139,6 +139,7 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(TILES))
     // ---- query fragments: rows gid and gid + 8 of a tile; warp w dims 32 w .. (two steps)
     __syncthreads();   // the last part's have been read
     float rs[TILES][2];   // what a row's scores are to be multiplied by
+    bool far = false;     // a row that fp16 does not hold: the scaled queries are bf16
     {
       uint4 f[TILES][2];
 #pragma unroll
@@ -161,15 +162,13 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(TILES))
           (h ? f[ti][1].y : f[ti][1].x) = v.z;
           (h ? f[ti][1].w : f[ti][1].z) = v.w;
           if (E4M3) {
-            float most = 0.f;
+            uint32_t most = magnitude2(v), least = least2(v);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t x = word(v, k);
-              most = fmaxf(most, fmaxf(fabsf(__uint_as_float(x << 16)), fabsf(__uint_as_float(x & 0xFFFF0000u))));
+            for (int d = 1; d <= 2; d <<= 1) {
+              most = max_u16x2(most, __shfl_xor_sync(0xffffffffu, most, d));
+              least = min_s16x2(least, __shfl_xor_sync(0xffffffffu, least, d));
             }
-            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
-            most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
-            if (c == 0) s_most[ti][gid + 8 * h][warp] = most;
+            if (c == 0) s_most[ti][gid + 8 * h][warp] = make_uint2(most, least);
           }
         }
         s_q[ti][2 * warp][lane] = f[ti][0];
@@ -177,27 +176,36 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(TILES))
       }
       __syncthreads();
       if constexpr (E4M3) {
+        float up[TILES][2];
 #pragma unroll
-        for (int ti = 0; ti < TILES; ++ti) {
-          float up[2];
+        for (int ti = 0; ti < TILES; ++ti)
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
-            float most = 0.f;
+            uint2 m = s_most[ti][gid + 8 * h][0];
 #pragma unroll
-            for (int k = 0; k < HD / 32; ++k) most = fmaxf(most, s_most[ti][gid + 8 * h][k]);
-            int e = static_cast<int>(__float_as_uint(most) >> 23);   // (infinite or all zero: any scale does)
-            e = e < 1 || e > 253 ? 127 : e;
-            rs[ti][h] = power_of(e);
-            up[h] = power_of(254 - e);
+            for (int k = 1; k < HD / 32; ++k) {
+              const uint2 x = s_most[ti][gid + 8 * h][k];
+              m = make_uint2(max_u16x2(m.x, x.x), min_s16x2(m.y, x.y));
+            }
+            const uint32_t most = max(m.x & 0xFFFFu, m.x >> 16);
+            // (both powers have to be normal numbers; all zero or not finite: any scale does)
+            const int e = min(max(static_cast<int>(most >> 7), 16), 254);
+            far = far || beyond_f16(most, m.y, e);
+            rs[ti][h] = power_of(e - 15);
+            up[ti][h] = power_of(269 - e);
           }
+        far = __any_sync(0xffffffffu, far);   // (the warps have all rows each)
+#pragma unroll
+        for (int ti = 0; ti < TILES; ++ti) {
           if (warp < HD / 32) {
             auto scaled = [&](uint32_t x, float by) {
-              return pack_f16(__uint_as_float(x << 16) * by, __uint_as_float(x & 0xFFFF0000u) * by);
+              const float lo = __uint_as_float(x << 16) * by, hi = __uint_as_float(x & 0xFFFF0000u) * by;
+              return far ? pack_bf16(lo, hi) : pack_f16(lo, hi);
             };
 #pragma unroll
             for (int k = 0; k < 2; ++k)
-              s_qh[ti][2 * warp + k][lane] = make_uint4(scaled(f[ti][k].x, up[0]), scaled(f[ti][k].y, up[1]),
-                                                        scaled(f[ti][k].z, up[0]), scaled(f[ti][k].w, up[1]));
+              s_qh[ti][2 * warp + k][lane] = make_uint4(scaled(f[ti][k].x, up[ti][0]), scaled(f[ti][k].y, up[ti][1]),
+                                                        scaled(f[ti][k].z, up[ti][0]), scaled(f[ti][k].w, up[ti][1]));
           }
         }
         __syncthreads();
@@ -317,29 +325,47 @@ __global__ void __launch_bounds__(kThreads, tree_rows_per_sm(TILES))
       for (int ti = 0; ti < TILES; ++ti)
 #pragma unroll
         for (int n = 0; n < 2; ++n) s[ti][n][0] = s[ti][n][1] = s[ti][n][2] = s[ti][n][3] = 0.f;
+      if (!E4M3 || !far) {
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        uint32_t b0[2], b1[2];
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-          if constexpr (E4M3) {
-            const uint32_t x = word(kr[n][k / 4], k % 4);
-            b0[n] = codes_lo(x);
-            b1[n] = codes_hi(x);
-          } else {
-            b0[n] = word(kr[n][k / 2], 2 * (k % 2));
-            b1[n] = word(kr[n][k / 2], 2 * (k % 2) + 1);
-          }
-        }
-#pragma unroll
-        for (int ti = 0; ti < TILES; ++ti) {
-          const uint4 f = E4M3 ? s_qh[E4M3 ? ti : 0][E4M3 ? k : 0][lane] : s_q[ti][k][lane];
+        for (int k = 0; k < KS; ++k) {
+          uint32_t b0[2], b1[2];
 #pragma unroll
           for (int n = 0; n < 2; ++n) {
-            if constexpr (E4M3)
-              mma_f16_16816(s[ti][n], f.x, f.y, f.z, f.w, b0[n], b1[n]);
-            else
-              mma_bf16_16816(s[ti][n], f.x, f.y, f.z, f.w, b0[n], b1[n]);
+            if constexpr (E4M3) {
+              const uint32_t x = word(kr[n][k / 4], k % 4);
+              b0[n] = codes_lo(x);
+              b1[n] = codes_hi(x);
+            } else {
+              b0[n] = word(kr[n][k / 2], 2 * (k % 2));
+              b1[n] = word(kr[n][k / 2], 2 * (k % 2) + 1);
+            }
+          }
+#pragma unroll
+          for (int ti = 0; ti < TILES; ++ti) {
+            const uint4 f = E4M3 ? s_qh[E4M3 ? ti : 0][E4M3 ? k : 0][lane] : s_q[ti][k][lane];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+              if constexpr (E4M3)
+                mma_f16_16816(s[ti][n], f.x, f.y, f.z, f.w, b0[n], b1[n]);
+              else
+                mma_bf16_16816(s[ti][n], f.x, f.y, f.z, f.w, b0[n], b1[n]);
+            }
+          }
+        }
+      } else if constexpr (E4M3) {   // a step at a time, its codes loaded again: the registers are the other form's
+        const uint8_t* base = keys + at * head_bytes + gid * HD + 16 * c;
+#pragma unroll 1
+        for (int k = 0; k < KS; ++k) {
+          uint32_t x[2];
+#pragma unroll
+          for (int n = 0; n < 2; ++n)
+            x[n] = a.n_pages > 0 ? __ldg(reinterpret_cast<const uint32_t*>(base + 8 * n * HD + 64 * (k >> 2) + 4 * (k & 3))) : 0u;
+#pragma unroll
+          for (int ti = 0; ti < TILES; ++ti) {
+            const uint4 f = s_qh[ti][k][lane];
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+              mma_bf16_16816(s[ti][n], f.x, f.y, f.z, f.w, bf16_of_f16(codes_lo(x[n])), bf16_of_f16(codes_hi(x[n])));
           }
         }
       }

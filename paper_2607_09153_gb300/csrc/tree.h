@@ -231,6 +231,33 @@ __device__ __forceinline__ uint32_t tree_sees16(const TreeLaunch& a, const TreeS
   return have >= 16 ? bits : bits & ((1u << have) - 1u);
 }
 
+// Magnitudes of bf16 numbers as their bits without a sign, which are ordered as the values.
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t min_s16x2(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("min.s16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+// The larger magnitudes of eight bf16 numbers, as bits, in two halves.
+__device__ __forceinline__ uint32_t magnitude2(const uint4& v) {
+  return max_u16x2(max_u16x2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), max_u16x2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
+}
+// The least magnitude of eight that is not zero, plus 0x7FFF, in two halves with a sign: a zero, 0x7FFF, is above all others.
+__device__ __forceinline__ uint32_t least2(const uint4& v) {
+  auto lifted = [](uint32_t w) { return (w & 0x7FFF7FFFu) + 0x7FFF7FFFu; };
+  return min_s16x2(min_s16x2(lifted(v.x), lifted(v.y)), min_s16x2(lifted(v.z), lifted(v.w)));
+}
+// Whether a row with the largest magnitude `most` and the least one of `least` loses something as fp16 times 2^(142 - e): an element's
+// last bit is 2^-7 of its power, and 2^-24 is fp16's.  (One that is not finite has nothing to lose.)
+__device__ __forceinline__ bool beyond_f16(uint32_t most, uint32_t least, int e) {
+  least ^= 0x80008000u;   // less one
+  return most < 0x7F80u && static_cast<int>((min(least & 0xFFFFu, least >> 16) + 1u) >> 7) < e - 32;
+}
+
 #endif  // __CUDACC__
 
 // tree.cu: query rows in tiles of 16 (tiles 1) or 32 (tiles 2); CTAs of four warps that run at once on an SM, by the

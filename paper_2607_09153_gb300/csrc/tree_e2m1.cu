@@ -80,28 +80,9 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
 __device__ __forceinline__ float lo_bf16(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float hi_bf16(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
 __device__ __forceinline__ float power_of(int field) { return __uint_as_float(static_cast<uint32_t>(field) << 23); }
-__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("max.u16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-__device__ __forceinline__ uint32_t min_s16x2(uint32_t a, uint32_t b) {
-  uint32_t r;
-  asm("min.s16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
-  return r;
-}
-// The larger magnitudes of eight bf16 numbers, as bits, in two halves, and whether either of these is 2^k or more (field: k + 127;
-// 255: not finite).
-__device__ __forceinline__ uint32_t magnitude2(const uint4& v) {
-  return max_u16x2(max_u16x2(v.x & 0x7FFF7FFFu, v.y & 0x7FFF7FFFu), max_u16x2(v.z & 0x7FFF7FFFu, v.w & 0x7FFF7FFFu));
-}
+// Whether one of two magnitudes is 2^k or more (field: k + 127; 255: not finite).
 __device__ __forceinline__ bool from(uint32_t magnitude, uint32_t field) {
   return max(magnitude & 0xFFFFu, magnitude >> 16) >= field << 7;
-}
-// The least magnitude of eight that is not zero, plus 0x7FFF, in two halves with a sign: a zero, 0x7FFF, is above all others.
-__device__ __forceinline__ uint32_t least2(const uint4& v) {
-  auto lifted = [](uint32_t w) { return (w & 0x7FFF7FFFu) + 0x7FFF7FFFu; };
-  return min_s16x2(min_s16x2(lifted(v.x), lifted(v.y)), min_s16x2(lifted(v.z), lifted(v.w)));
 }
 // Two codes' fp16 times factors, as bf16 (the longer form).
 __device__ __forceinline__ uint32_t bf16_times(uint32_t h, float lo, float hi) {
@@ -316,11 +297,9 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
       most = max(most & 0xFFFFu, most >> 16);   // (bits without a sign: ordered as the values)
       most = max(most, __shfl_xor_sync(0xffffffffu, most, 1));
       most = max(most, __shfl_xor_sync(0xffffffffu, most, 2));
-      // 2^(142 - e) has to be a normal number; all zero or not finite: any scale does.  An element's last bit is 2^-7 of its power,
-      // and 2^-24 is fp16's.
+      // (2^(142 - e) has to be a normal number; all zero or not finite: any scale does)
       const int e = min(max(static_cast<int>(most >> 7), 15), 254);
-      least ^= 0x80008000u;   // a magnitude less one
-      far = far || static_cast<int>((min(least & 0xFFFFu, least >> 16) + 1u) >> 7) < e - 32;
+      far = far || beyond_f16(most, least, e);
       rs[nt][0] = __shfl_sync(0xffffffffu, power_of(e), 8 * c) * (0x1p-15f * fabsf(a.scale_log2));
       rs[nt][1] = __shfl_sync(0xffffffffu, power_of(e), 8 * c + 4) * (0x1p-15f * fabsf(a.scale_log2));
       const float up = a.scale_log2 < 0.f ? -power_of(269 - e) : power_of(269 - e);
