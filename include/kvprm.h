@@ -695,11 +695,15 @@ KVPRM_API int kvprm_cache_expand(const kvprm_cache* cache, const int32_t* src, c
  *               sees itself and those before it (a chain)
  *  max_drafts   no sequence has more drafted tokens, 1 .. 1024
  *  max_len      about the longest cached length; it sizes the launch, and results
- *               do not depend on it beyond the order of sums
+ *               do not depend on it beyond the order of sums -- and, over a 4-bit
+ *               cache with more than 32 query rows of a kv head, the rounding of the
+ *               weights, which may be that of up to 32 rows where max_len is short
+ *               (28 pages, the drafted tokens among them)
  * Scores, weights' sums and accumulators are fp32; the weights that multiply the
  * values are rounded to bf16 (an 8-bit cache with up to 32 query rows of a kv
  * head: fp16, near the sequence's largest power of two; a 4-bit one likewise, weights
  * below 2^-26 of the largest in steps of 2^-36 of it), as the output is to bf16.
+ * Queries, keys and values enter the products as they are.
  * The sums of weights times values stay finite where the output is only in a 4-bit cache's kernel for
  * up to 32 query rows; elsewhere a row whose values are beyond 2^112 over its number of keys
  * may come out infinite.

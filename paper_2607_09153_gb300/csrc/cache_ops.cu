@@ -11,8 +11,9 @@
 // rotated and written as e4m3 in 47 us (3,930 GB/s: a chain of slot, row, shuffles and store for each
 // token of a thread, whose loads stall it most, with 0.62 of the issue slots in use; not rotated 39 us,
 // from fp32 55, into bf16 pages 49).  Steps of 16 to 64 tokens take 2 to 2.5 us of the GPU's time.  In 4
-// bits: 30,001 tokens of 8 heads written, not rotated, in 27 us (5,700 GB/s, and the ALU pipe at 0.63), 4,099
-// pages of 8 heads expanded in 56 us (6,070 GB/s).
+// bits: 30,001 tokens of 8 heads written, not rotated, in 24 to 27 us (slots in order or not; 5,700 GB/s of these, and the
+// ALU pipe at 0.63), from fp16 31, from fp32 41, from rows that are not 16-byte aligned 40 (fp32 60); rotated on the way 45
+// (fp32 56: the kernel of 8 bits, a token after the other); 4,099 pages of 8 heads expanded in 56 us (6,070 GB/s).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>

@@ -8,10 +8,10 @@
 // Nothing is decided by who comes first: counts are sums, of several that want a page the lowest sequence has it, free pages go
 // by their numbers.
 //
-// What bounds them, measured on a GB300: memory, once copies are many (462 pages of 0.46 MB compacted in 76 us, 67 of them the
-// copies', 6,400 GB/s; 217 pages of 0.92 MB copied in a fork of 64 sequences into 256 in 54 us, 43 of them 199 MB written from
-// pages that L2 keeps); the steps' latencies before that, 7 to 9 us of a fork and 5 of a compaction (four and three cluster barriers,
-// each behind loads or atomics of the step).
+// What bounds them, measured on a GB300: memory, once copies are many (462 pages of 0.46 MB compacted in 77 us, 67 of them the
+// copies', 6,400 GB/s; 217 pages of 0.92 MB copied in a fork of 64 sequences into 256 in 55 us, 44 of them 199 MB written from
+// pages that L2 keeps); the steps' latencies before that, 7 to 10 us of a fork and 5 of a compaction (three cluster barriers each, each
+// behind loads or atomics of the step, and a fourth where the cluster writes tables and copies itself).
 #include <cuda_runtime.h>
 
 #include <algorithm>
@@ -394,7 +394,7 @@ __device__ __forceinline__ void tables(const ForkLaunch& t, uint32_t warp, uint3
 __device__ __forceinline__ void tables(const CompactLaunch& t, uint32_t warp, uint32_t warps) { compact_tables(t, warp, warps); }
 __device__ __forceinline__ int32_t copy_to(const CompactLaunch&, int32_t page) { return page; }
 
-// A fork's copies come of few pages, which stay in L2 (256 copies of 64 sequences' pages, 199 MB: 46 us, and 58 with loads that
+// A fork's copies come of few pages, which stay in L2 (217 copies of 64 sequences' pages, 199 MB: 46 us, and 58 with loads that
 // leave L2 first); what a compaction moves is read once.
 __device__ __forceinline__ uint4 load_piece(const ForkLaunch&, const uint8_t* p) { return __ldcg(reinterpret_cast<const uint4*>(p)); }
 __device__ __forceinline__ uint4 load_piece(const CompactLaunch&, const uint8_t* p) { return __ldcs(reinterpret_cast<const uint4*>(p)); }

@@ -17,7 +17,7 @@
 //
 // What bounds it, measured on a GB300, a drafted token per sequence: a bf16 cache memory (8 kv heads of 128, 4 query heads
 // each, 8 x 32,768 tokens in 168 us, 6,390 GB/s), an 8-bit one a page's instructions and its values' latency (the same in 107
-// us, 5,040 GB/s; with 7 query heads each over 64 ragged sequences 75 us, 4,500 GB/s).  Loads two pages ahead did not help,
+// us, 5,040 GB/s; with 7 query heads each over 64 ragged sequences 73 us, 4,610 GB/s).  Loads two pages ahead did not help,
 // in registers (100: they share scoreboards) or by asynchronous copies (79), nor did a fourth CTA.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>

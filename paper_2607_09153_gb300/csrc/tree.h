@@ -23,9 +23,9 @@ struct TreeLaunch {
   int32_t fill;                        // 1: rows that no sequence writes are written too (tree_fill)
   int32_t weight_full, weight_part;    // places of a block of a pair with all its tiles, or with fewer
   float scale_log2;                    // scores in units of log2
-  int32_t* line;                       // [n_seqs + 1], then the CTAs (or warps) that took part: for the join
-  float* part_o;                       // [2 * CTAs][head_dim][rows]
-  float2* part_ml;                     // [2 * CTAs][rows]
+  int32_t* line;                       // [n_seqs + 1], then the CTAs (4-bit pages on registers: the warps) that took part: for the join
+  float* part_o;                       // [2 * CTAs][head_dim][rows] (4-bit pages on registers: means, [2 * warps][rows][head_dim])
+  float2* part_ml;                     // [2 * CTAs][rows], or [2 * warps][rows]: maxima and sums
 };
 
 #ifdef __CUDACC__

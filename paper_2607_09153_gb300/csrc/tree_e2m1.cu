@@ -22,9 +22,11 @@
 //
 // What bounds it, measured on a GB300, is instructions: a page of a kv head takes some 295 of a warp (64 conversions, 64
 // multiplications by powers, 16 matrix instructions, 16 to put nibbles together, 20 of the softmax, 29 loads and copies), 0.60 of
-// the issue slots with the three warps a scheduler that 163 registers leave (ALU pipe 0.49, DRAM 0.45).  One drafted token
-// over 8 x 32,768 tokens of 8 heads 64 us (4,490 GB/s), four (16 rows) 84, eight (32 rows) 139; 64 ragged sequences up to 9,001
-// of 4 heads 48 us; one sequence of 32,768 of 4 heads 21.  Tried: fragments loaded straight into registers, a page ahead (75 us for the first of these: the loads
+// the issue slots with the three warps a scheduler that 167 registers leave (ALU pipe 0.47, DRAM 0.53).  One drafted token
+// over 8 x 32,768 tokens of 8 heads 63 us (4,530 GB/s), four (16 rows) 83, eight (32 rows) 139; 64 ragged sequences up to 9,001
+// of 4 heads 48 us; one sequence of 32,768 of 4 heads 20.  Pages in the general form cost more (the ragged ones / four drafts): a zero
+// block in 1,000 56 / 102 us, in 100 72 / 132, blocks 2^26 apart in every page 109 / 252, a query row that fp16 does not hold 103 /
+// 237.  Tried: fragments loaded straight into registers, a page ahead (75 us for the first of these: the loads
 // share scoreboards) or in single pages (84); four CTAs an SM (81: spills); the next step's scores beside this one's product
 // (74); CTAs instead of warps as shares (72; the ragged ones 58, for a part then costs 4 us of barriers); two CTAs of six
 // or seven warps (65.6, and 76: spills); a page's scores in two chains of products (the same).
@@ -860,6 +862,7 @@ __global__ void __launch_bounds__(kThreads, tree_e2m1_per_sm(NT)) tree_e2m1_kern
 // What it costs is latencies: 5 us of the 48 of 64 ragged sequences of 4 heads (256 pairs of some eight parts), of which 1.4 are a
 // launch's and 2 the line's.  Eight warps, or sixteen where so few CTAs leave SMs idle (that call / one sequence of 32,768 tokens with 64
 // parts a pair: eight 47.7 / 26.2, sixteen 50.5 / 24.4; four with 32 dims and four parts ahead 48.6 / 27.4; eight with 128 dims 48.2 / 29.5).
+// Weighing means instead of sums by their own reciprocals, part after part, 0.5 more than by powers of two (part_top).
 constexpr int kJoinDims = 64, kJoinFew = 128;
 template <int HD, int NT, int W>
 __global__ void __launch_bounds__(32 * W) tree_e2m1_join_kernel(const __grid_constant__ TreeLaunch a, int groups) {
