@@ -64,7 +64,8 @@ def test_layouts_that_are_fine(call):
     for pools in ([pool()], [pool(layer_stride=page, page_stride=28 * page)],
                   [pool(page_bytes=page // 2), pool(base=BASE + page // 2, page_bytes=page // 2)],
                   [pool(base=BASE + 16 * page * i, layers=1, layer_stride=0) for i in range(96)],
-                  [pool(layers=14, layer_stride=32 * page), pool(base=BASE + 16 * page)][:1],
+                  [pool(layer_stride=20 * page), pool(base=BASE + 16 * page, layer_stride=20 * page, page_stride=page // 4, page_bytes=page // 4)],
+                  [pool(layers=14, layer_stride=32 * page), pool(base=BASE + 16 * page, layers=14, layer_stride=32 * page)],
                   [pool(page_bytes=48), pool(base=BASE + 48, layers=14, layer_stride=32 * page, page_bytes=16), pool(base=BASE + 64, layers=1, page_bytes=64)],
                   [pool(layers=1 << 20, page_bytes=0)], [pool(layers=0, page_stride=0)]):
         rc = call(x, pools)
